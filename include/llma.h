@@ -223,6 +223,84 @@ int llma_generate_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs,
                         int32_t *out_tokens, int32_t *n_out,
                         llma_step_rec *trace, int32_t *n_steps);
 
+/* --- serving on pages: stateless calls ------------------------------------------------- */
+/* Calls for programs that keep the sequences' cache in pages of 8-bit values (and that sample).  As
+ * llma_find_trigger_static: inputs, outputs and workspace are DEVICE memory of the caller, everything is enqueued
+ * on hip_stream (NULL = default stream) of the current device, nothing is allocated, copied to the host or waited for, and
+ * HIP graphs may capture the calls.  Calls that use different workspaces and outputs may run at the same time; two that
+ * share one must be ordered by the caller (two graphs that were captured with one workspace: not at the same time).
+ * What the host can see is checked before anything is enqueued (INVAL, RANGE); numbers that lie in device memory are
+ * checked where they are used, and none of them makes a kernel leave the buffers described here. */
+#define LLMA_PAGE 64             /* positions per page */
+#define LLMA_DTYPE_F16 2         /* rows of these calls only: fp16 (a context is F32 or BF16) */
+#define LLMA_PAGED_MAX_SEQS 4096 /* sequences of one llma_attend_paged */
+#define LLMA_SAMPLED_MAX_K 63    /* drafts per sequence of one llma_verify_sampled */
+
+/* A layer's cache.  k [n_pages][n_kv_heads][64][head_dim] and v [n_pages][n_kv_heads][head_dim][64] (transposed) hold
+ * OCP fp8 e4m3 codes, k_scale and v_scale [n_pages][n_kv_heads] powers of two, one for each page and head; a cached value is
+ * code * scale.  head_dim 64 or 128; k and v 16-byte aligned. */
+typedef struct {
+    void *k, *v;
+    float *k_scale, *v_scale;
+    int32_t n_pages, n_kv_heads, head_dim;
+} llma_paged_cache;
+
+/* Pages and slots of a step, from the sequences' lengths on the device.  Per slot (one of n_slots places a sequence can have;
+ * slots int32[n_seqs] names them, distinct; NULL = 0 .. n_seqs-1): lens[slot] positions already cached, owned[slot] pages it has,
+ * table[slot][max_blocks] their numbers (owned[slot] of them, the rest -1).  Per sequence of the call: rows[b] new positions.
+ * free_pages [n_pages] is a stack of unused pages, *n_free its height.
+ * Sequence b needs ceil((lens + rows) / 64) pages (0: none).  What it owns beyond that goes back on the stack, in the reverse order of
+ * granting, so that a grant taken back leaves the stack as it was; then what sequences lack comes off its top, sequence by sequence.
+ * A finished sequence gives everything back with lens = rows = 0.
+ * Outputs: row_offsets[n_seqs+1] (sums of rows), lens_after[n_seqs] = lens + rows; for row i of sequence b, at row_offsets[b] + i:
+ * row_pos = lens + i and slot_map = 64 * page + position in the page; entries behind the last row up to max_rows: 0 and -1.
+ * slot_map and row_pos may be NULL with max_rows = 0.  *status: 0; the number of pages that were missing; or a negative LLMA_E_*
+ * (INVAL: a negative length, a slot listed twice, counts that do not fit the table or the stack; RANGE: a slot outside [0, n_slots),
+ * more than max_blocks pages or max_rows rows).  Unless it is 0, table, owned and the stack stay as they were and
+ * the call describes a step without rows.  lens_after may not be lens.  n_slots <= 65536. */
+int llma_map_pages(const int32_t *lens, const int32_t *rows, const int32_t *slots, int32_t n_seqs, int32_t n_slots,
+                   int32_t *table, int32_t max_blocks, int32_t *owned, int32_t *free_pages, int32_t *n_free, int32_t n_pages,
+                   int32_t *row_offsets, int32_t *lens_after, int32_t *slot_map, int32_t *row_pos, int32_t max_rows,
+                   int32_t *status, void *hip_stream);
+
+/* Writes rows into the cache.  k, v: n_rows x n_kv_heads x head_dim values of dtype (LLMA_DTYPE_*), strides in elements
+ * (features contiguous; pointers and strides multiples of 16 bytes); row i goes to slot_map[i], rows whose slot is negative or
+ * no page's nowhere.  A run is a stretch of rows with consecutive slots inside one page; a call may have one run per page.  The
+ * run's scale, per head, for K and for V: the smallest power of two (from 2^-64 to 2^120) s with max |x| / s <= 448 over its finite values; a run that
+ * starts behind its page's first position keeps the page's scale where that is larger, and where s is larger the codes before
+ * the run are rounded again to s.  Codes are x / s rounded to nearest even; +-inf become +-448, NaN stays NaN.  Codes
+ * behind the run stay as they are. */
+int llma_append_paged(const llma_paged_cache *cache, const void *k, const void *v, int32_t dtype, int64_t k_row_stride,
+                      int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot_map, int32_t n_rows,
+                      void *hip_stream);
+
+/* Causal attention of a step's rows over the cache.  Rows row_offsets[b] .. row_offsets[b+1]-1 of q are sequence b's; row j of
+ * m sees positions 0 .. lens[b] - m + j of the pages table[slots[b]] (lens counts the step's own rows, which
+ * llma_append_paged has written).  out = softmax(scale * q K^T) V per head; query head h reads key head h / (n_heads /
+ * n_kv_heads).  q, out: n_rows x n_heads x head_dim of dtype, strides in elements, pointers and strides multiples of 16 bytes; out may not overlap q.
+ * max_rows: at least the rows of every sequence (further rows are not written); rows behind the last sequence's stay as they are.
+ * A row that sees nothing becomes 0.  Positions whose page number is outside [0, n_pages) are not seen.
+ * work: llma_attend_paged_workspace(...) bytes, 16-byte aligned. */
+int64_t llma_attend_paged_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);
+int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtype, int32_t n_heads, int64_t q_row_stride,
+                      int64_t q_head_stride, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,
+                      const int32_t *lens, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, int32_t max_rows, float scale,
+                      void *out, int64_t out_row_stride, int64_t out_head_stride, void *work, int64_t work_bytes, void *hip_stream);
+
+/* Verification of drafted tokens against the target's probabilities, from given random numbers.  logits: n_seqs * (k + 1) rows of
+ * vocab values of dtype, row_stride elements apart; row (b, j) follows drafts[b][0 .. j).  p = softmax(logits / temperature[b]).
+ * Draft j of n_draft[b] (NULL: k everywhere) is accepted while u_accept[b][j] * q(draft) < p(draft), q = draft_probs[b][j] [vocab]
+ * (NULL: a copied token, q = 1).  The next token is drawn from max(p - q, 0) at the first rejection (copied token: p without it; p itself
+ * where nothing is left), from p of row n_draft when all were accepted: the smallest v whose cumulative weight passes u_sample[b] times
+ * the sum.  u in [0, 1).  temperature NULL: 1; not above 0: the arg max, lowest id on ties, as llma_verify_step has it.
+ * NaN logits count as minus infinity; drafts outside [0, vocab) are rejected.
+ * Outputs: n_accepted[b] = a, next_token[b] (-1: a row without a logit above minus infinity), emitted[b][0 .. k]: the accepted drafts, the next token, then -1. */
+int64_t llma_verify_sampled_workspace(int32_t n_seqs, int32_t k, int32_t vocab);
+int llma_verify_sampled(const void *logits, int32_t dtype, int64_t row_stride, int32_t vocab, int32_t n_seqs, int32_t k,
+                        const int32_t *drafts, const int32_t *n_draft, const float *draft_probs, const float *temperature,
+                        const float *u_accept, const float *u_sample, int32_t *n_accepted, int32_t *next_token, int32_t *emitted,
+                        void *work, int64_t work_bytes, void *hip_stream);
+
 /* --- inspection / measurement --------------------------------------------------------- */
 /* When dev_buf != NULL every later forward also writes its rows' logits, fp32
  * [rows, vocab] row-major, to this DEVICE buffer (capacity_rows >= rows of the largest

@@ -25,9 +25,12 @@ EXPORTS = [
     "llma_set_pending", "llma_kv_import", "llma_find_trigger", "llma_verify_step",
     "llma_verify_step_batch", "llma_generate", "llma_generate_batch", "llma_set_logits_dump", "llma_set_option",
     "llma_get_kernel_timing", "llma_time_ffn_gemm", "llma_time_step_gemm", "llma_device_bytes", "llma_find_trigger_static", "llma_truncate",
-    "llma_describe",
+    "llma_describe", "llma_map_pages", "llma_append_paged", "llma_attend_paged", "llma_attend_paged_workspace",
+    "llma_verify_sampled", "llma_verify_sampled_workspace",
 ]
 LLMA_TRIGGER_STATIC_MAX_REF = 1 << 20
+LLMA_DTYPE_F16 = 2
+LLMA_PAGE, LLMA_PAGED_MAX_SEQS, LLMA_SAMPLED_MAX_K = 64, 4096, 63
 
 
 class LlmaError(RuntimeError):
@@ -46,6 +49,11 @@ class WeightsC(ctypes.Structure):
     _fields_ = [("embed", c_void_p), ("lm_head", c_void_p), ("final_norm", c_void_p),
                 ("wqkv", POINTER(c_void_p)), ("wo", POINTER(c_void_p)), ("wgu", POINTER(c_void_p)),
                 ("wdown", POINTER(c_void_p)), ("norm1", POINTER(c_void_p)), ("norm2", POINTER(c_void_p))]
+
+
+class PagedCacheC(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("n_pages", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32)]
 
 
 class StepRec(ctypes.Structure):
@@ -88,6 +96,15 @@ def load_library() -> ctypes.CDLL:
     lib.llma_get_kernel_timing.argtypes = [vp, POINTER(c_int64), POINTER(c_double)]
     lib.llma_time_ffn_gemm.argtypes = [vp, c_int32, c_int32, POINTER(c_double)]
     lib.llma_time_step_gemm.argtypes = [vp, c_int32, c_int32, c_int32, POINTER(c_double)]
+    lib.llma_map_pages.argtypes = [vp, vp, vp, c_int32, c_int32, vp, c_int32, vp, vp, vp, c_int32, vp, vp, vp, vp, c_int32, vp, vp]
+    lib.llma_append_paged.argtypes = [POINTER(PagedCacheC), vp, vp, c_int32, c_int64, c_int64, c_int64, c_int64, vp, c_int32, vp]
+    lib.llma_attend_paged_workspace.argtypes = [c_int32] * 6
+    lib.llma_attend_paged_workspace.restype = c_int64
+    lib.llma_attend_paged.argtypes = [POINTER(PagedCacheC), vp, c_int32, c_int32, c_int64, c_int64, vp, vp, c_int32, c_int32, vp, vp,
+                                      c_int32, c_int32, c_int32, c_float, vp, c_int64, c_int64, vp, c_int64, vp]
+    lib.llma_verify_sampled_workspace.argtypes = [c_int32] * 3
+    lib.llma_verify_sampled_workspace.restype = c_int64
+    lib.llma_verify_sampled.argtypes = [vp, c_int32, c_int64, c_int32, c_int32, c_int32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, c_int64, vp]
     lib.llma_describe.argtypes = [vp, c_char_p, c_int32]
     lib.llma_device_bytes.argtypes = [vp]
     lib.llma_device_bytes.restype = c_int64
@@ -133,6 +150,187 @@ def llma_find_trigger_static(y_dev, ref_dev, doc_offsets_dev, n: int, result_dev
     _check(lib.llma_find_trigger_static(c_void_p(y_dev.data_ptr()), int(y_dev.numel()), c_void_p(ref_dev.data_ptr()),
                                         int(ref_dev.numel()), c_void_p(doc_offsets_dev.data_ptr()), n_docs, n,
                                         c_void_p(result_dev.data_ptr()), st))
+
+
+# ---- serving on pages: device tensors, a stream, no wait (see llma.h) --------------------------------------------------
+class PagedCache:
+    """A layer's cache: uint8 tensors k [n_pages, n_kv_heads, 64, head_dim] and v [n_pages, n_kv_heads, head_dim, 64], fp32
+    k_scale and v_scale [n_pages, n_kv_heads]."""
+    __slots__ = ("k", "v", "k_scale", "v_scale")
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
+        import torch
+        return cls(torch.empty((n_pages, n_kv_heads, LLMA_PAGE, head_dim), dtype=torch.uint8, device=device),
+                   torch.empty((n_pages, n_kv_heads, head_dim, LLMA_PAGE), dtype=torch.uint8, device=device),
+                   torch.empty((n_pages, n_kv_heads), dtype=torch.float32, device=device),
+                   torch.empty((n_pages, n_kv_heads), dtype=torch.float32, device=device))
+
+
+class PageTable:
+    """Who has which page: int32 tensors table [n_slots, max_blocks], owned [n_slots], free_pages [n_pages], n_free [1]."""
+    __slots__ = ("table", "owned", "free_pages", "n_free")
+
+    def __init__(self, table, owned, free_pages, n_free):
+        self.table, self.owned, self.free_pages, self.n_free = table, owned, free_pages, n_free
+
+    @classmethod
+    def empty(cls, n_slots: int, max_blocks: int, n_pages: int, device="cuda"):
+        """All pages free; page 0 is granted first."""
+        import torch
+        return cls(torch.full((n_slots, max_blocks), -1, dtype=torch.int32, device=device), torch.zeros(n_slots, dtype=torch.int32, device=device),
+                   torch.arange(n_pages - 1, -1, -1, dtype=torch.int32, device=device), torch.full((1,), n_pages, dtype=torch.int32, device=device))
+
+
+def _refuse(msg: str):
+    raise LlmaError(LLMA_E_INVAL, msg)
+
+
+class _Call:
+    """Checks a call's tensors -- all on one device, of the type and shape they should have -- and names its stream."""
+
+    def __init__(self, who: str, first, stream):
+        import torch
+        self.torch, self.who = torch, who
+        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+            _refuse(f"{who}: device tensors are wanted")
+        self.device = first.device
+        if stream is not None and getattr(stream, "device", self.device) != self.device:
+            _refuse(f"{who}: the stream is not on the tensors' device")
+        self.given = stream
+        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+
+    def ptr(self, name, t, dtype, shape):
+        """a contiguous tensor's address; shape: sizes, None where any will do"""
+        if t.dtype is not dtype or t.device != self.device or not t.is_contiguous() or t.dim() != len(shape):
+            _refuse(f"{self.who}: {name} has to be a contiguous {dtype} tensor of {len(shape)} dimensions on {self.device}")
+        for have, want in zip(t.shape, shape):
+            if want is not None and have != want:
+                _refuse(f"{self.who}: {name} has shape {tuple(t.shape)}, wanted {shape}")
+        return t.data_ptr()
+
+    def rows(self, name, t, shape):
+        """(address, dtype code) of rows whose features lie together, any other strides"""
+        codes = {self.torch.bfloat16: LLMA_DTYPE_BF16, self.torch.float16: LLMA_DTYPE_F16, self.torch.float32: LLMA_DTYPE_F32}
+        if t.dtype not in codes or t.device != self.device or t.dim() != len(shape) or (t.numel() and t.stride(-1) != 1):
+            _refuse(f"{self.who}: {name} has to be a bf16, fp16 or fp32 tensor of {len(shape)} dimensions on {self.device} whose features lie together")
+        for have, want in zip(t.shape, shape):
+            if want is not None and have != want:
+                _refuse(f"{self.who}: {name} has shape {tuple(t.shape)}, wanted {shape}")
+        return t.data_ptr(), codes[t.dtype]
+
+    def cache(self, c):
+        t = self.torch
+        if c.k.dim() != 4 or c.k.shape[2] != LLMA_PAGE:
+            _refuse(f"{self.who}: cache.k has to be [n_pages, n_kv_heads, {LLMA_PAGE}, head_dim]")
+        P, H, _, D = c.k.shape
+        return PagedCacheC(self.ptr("cache.k", c.k, t.uint8, (P, H, LLMA_PAGE, D)), self.ptr("cache.v", c.v, t.uint8, (P, H, D, LLMA_PAGE)),
+                           self.ptr("cache.k_scale", c.k_scale, t.float32, (P, H)), self.ptr("cache.v_scale", c.v_scale, t.float32, (P, H)), P, H, D)
+
+    def workspace(self, given, size: int):
+        """a workspace of the caller's, or one that lives until the stream has used it (the allocator orders its reuse on the stream)"""
+        _check(size)
+        if given is not None:
+            if not given.is_cuda or given.device != self.device or not given.is_contiguous():
+                _refuse(f"{self.who}: workspace has to be a contiguous tensor on {self.device}")
+            return given, given.numel() * given.element_size()
+        if self.given is None:
+            return self.torch.empty(size, dtype=self.torch.uint8, device=self.device), size
+        with self.torch.cuda.stream(self.given):
+            return self.torch.empty(size, dtype=self.torch.uint8, device=self.device), size
+
+    def run(self, fn, *args):
+        if self.device.index == self.torch.cuda.current_device():
+            _check(fn(*args, c_void_p(self.stream.cuda_stream)))
+        else:
+            with self.torch.cuda.device(self.device):
+                _check(fn(*args, c_void_p(self.stream.cuda_stream)))
+
+
+def llma_map_pages(pages, lens, rows, row_offsets, lens_after, slot_map, row_pos, status, slots=None, stream=None):
+    """Pages and slots of a step from the sequences' lengths (see llma.h).  pages: a PageTable; int32 tensors lens [n_slots],
+    rows [n_seqs], slots [n_seqs] or None; written: row_offsets [n_seqs + 1], lens_after [n_seqs], slot_map and row_pos [max_rows] (or both None), status [1].
+    Enqueues on `stream` (None: torch's current stream of the tensors' device) and returns without synchronising."""
+    c = _Call("llma_map_pages", lens, stream)
+    i32, p = c.torch.int32, c.ptr
+    table = p("pages.table", pages.table, i32, (None, None))
+    S, blocks = pages.table.shape
+    B, P = rows.numel(), pages.free_pages.numel()
+    if (slot_map is None) != (row_pos is None):
+        _refuse("llma_map_pages: slot_map and row_pos come together")
+    n = 0 if slot_map is None else slot_map.numel()
+    c.run(load_library().llma_map_pages, p("lens", lens, i32, (S,)), p("rows", rows, i32, (B,)), None if slots is None else p("slots", slots, i32, (B,)), B, S, table, blocks,
+          p("pages.owned", pages.owned, i32, (S,)), p("pages.free_pages", pages.free_pages, i32, (P,)), p("pages.n_free", pages.n_free, i32, (1,)), P,
+          p("row_offsets", row_offsets, i32, (B + 1,)), p("lens_after", lens_after, i32, (B,)), None if n == 0 else p("slot_map", slot_map, i32, (n,)),
+          None if n == 0 else p("row_pos", row_pos, i32, (n,)), n, p("status", status, i32, (1,)))
+
+
+def llma_append_paged(cache, k, v, slot_map, stream=None):
+    """Writes rows k, v [n_rows, n_kv_heads, head_dim] (bf16, fp16 or fp32; features together, other strides as they are) into the paged
+    cache at slot_map (int32 [n_rows], negative: nowhere); see llma.h.  Enqueues and returns without synchronising."""
+    c = _Call("llma_append_paged", k, stream)
+    d = c.cache(cache)
+    shape = (k.shape[0], d.n_kv_heads, d.head_dim)
+    kp, kt = c.rows("k", k, shape)
+    vp, vt = c.rows("v", v, shape)
+    if kt != vt:
+        _refuse("llma_append_paged: k and v have different types")
+    c.run(load_library().llma_append_paged, byref(d), kp, vp, kt, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+          c.ptr("slot_map", slot_map, c.torch.int32, (shape[0],)), shape[0])
+
+
+def llma_attend_paged(cache, q, table, lens, row_offsets, max_rows: int, scale: float, out, slots=None, workspace=None, stream=None):
+    """Causal attention of rows q [n_rows, n_heads, head_dim] over the paged cache into out (see llma.h).  int32 tensors table
+    [n_slots, max_blocks], lens [n_seqs] (the step's rows included), row_offsets [n_seqs + 1], slots [n_seqs] or None; max_rows: no sequence has more
+    rows.  workspace: at least llma_attend_paged_workspace() bytes of device memory, None: allocated for the call.  Enqueues
+    and returns without synchronising.  Returns out."""
+    c = _Call("llma_attend_paged", q, stream)
+    i32, d = c.torch.int32, c.cache(cache)
+    qp, qt = c.rows("q", q, (None, None, d.head_dim))
+    n, heads = q.shape[0], q.shape[1]
+    op, ot = c.rows("out", out, (n, heads, d.head_dim))
+    if qt != ot:
+        _refuse("llma_attend_paged: out and q have different types")
+    B = lens.numel()
+    tp = c.ptr("table", table, i32, (None, None))
+    lib = load_library()
+    ws, size = c.workspace(workspace, lib.llma_attend_paged_workspace(B, table.shape[1], heads, d.n_kv_heads, d.head_dim, max_rows))
+    c.run(lib.llma_attend_paged, byref(d), qp, qt, heads, q.stride(0), q.stride(1), tp, None if slots is None else c.ptr("slots", slots, i32, (B,)),
+          table.shape[0], table.shape[1], c.ptr("lens", lens, i32, (B,)), c.ptr("row_offsets", row_offsets, i32, (B + 1,)), B, n, max_rows, scale,
+          op, out.stride(0), out.stride(1), ws.data_ptr(), size)
+    return out
+
+
+def llma_attend_paged_workspace(n_seqs: int, max_blocks: int, n_heads: int, n_kv_heads: int, head_dim: int, max_rows: int) -> int:
+    return _check(load_library().llma_attend_paged_workspace(n_seqs, max_blocks, n_heads, n_kv_heads, head_dim, max_rows))
+
+
+def llma_verify_sampled(logits, drafts, u_accept, u_sample, n_accepted, next_token, emitted, n_draft=None, draft_probs=None, temperature=None,
+                        workspace=None, stream=None):
+    """Verifies drafts against the target's probabilities with given random numbers (see llma.h).  logits [n_seqs, k + 1, vocab] (bf16, fp16 or fp32, rows any
+    stride apart), drafts int32 [n_seqs, k], u_accept fp32 [n_seqs, k], u_sample fp32 [n_seqs], n_draft int32 [n_seqs], draft_probs fp32
+    [n_seqs, k, vocab], temperature fp32 [n_seqs]; written, int32: n_accepted, next_token [n_seqs], emitted [n_seqs, k + 1].  workspace: at least
+    llma_verify_sampled_workspace() bytes of device memory, None: allocated for the call.  Enqueues and returns without synchronising."""
+    c = _Call("llma_verify_sampled", logits, stream)
+    i32, f32 = c.torch.int32, c.torch.float32
+    lp, lt = c.rows("logits", logits, (None, None, None))
+    B, k, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    if k < 0 or (B > 1 and logits.stride(0) != (k + 1) * logits.stride(1)):
+        _refuse("llma_verify_sampled: logits has to be [n_seqs, k + 1, vocab] with all rows the same stride apart")
+    row = logits.stride(1) if k > 0 else logits.stride(0)
+    lib = load_library()
+    ws, size = c.workspace(workspace, lib.llma_verify_sampled_workspace(B, k, V))
+    c.run(lib.llma_verify_sampled, lp, lt, row if B * (k + 1) > 1 else max(row, V), V, B, k, c.ptr("drafts", drafts, i32, (B, k)),
+          None if n_draft is None else c.ptr("n_draft", n_draft, i32, (B,)), None if draft_probs is None else c.ptr("draft_probs", draft_probs, f32, (B, k, V)),
+          None if temperature is None else c.ptr("temperature", temperature, f32, (B,)), c.ptr("u_accept", u_accept, f32, (B, k)), c.ptr("u_sample", u_sample, f32, (B,)),
+          c.ptr("n_accepted", n_accepted, i32, (B,)), c.ptr("next_token", next_token, i32, (B,)), c.ptr("emitted", emitted, i32, (B, k + 1)), ws.data_ptr(), size)
+
+
+def llma_verify_sampled_workspace(n_seqs: int, k: int, vocab: int) -> int:
+    return _check(load_library().llma_verify_sampled_workspace(n_seqs, k, vocab))
 
 
 class Context:

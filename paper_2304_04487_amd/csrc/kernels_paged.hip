@@ -1,0 +1,839 @@
+// The paged 8-bit cache: pages and slots of a step, the write into the cache, attention of a step's rows over it.
+#include "../../include/llma.h"
+#include "paged.h"
+
+// ---------------------------------------------------------------------------------------------
+// sums over a workgroup
+// ---------------------------------------------------------------------------------------------
+__device__ __forceinline__ int wave_scan(int v) {              // inclusive
+    const int lane = threadIdx.x & 63;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const int o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    return v;
+}
+// exclusive prefix sum of v over the workgroup's NW waves, *total the sum; part: LDS of at least NW words, free again after the next barrier
+template <int NW>
+__device__ __forceinline__ int block_scan(int v, int *part, int *total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const int in = wave_scan(v);
+    __syncthreads();
+    if (lane == 63) part[wave] = in;
+    __syncthreads();
+    int before = 0, sum = 0;
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const int p = part[w];
+        before += w < wave ? p : 0;
+        sum += p;
+    }
+    *total = sum;
+    return before + in - v;
+}
+// number of entries of the ascending list p[0 .. n) that are <= v
+template <typename P>
+__device__ __forceinline__ int count_le(const P *p, int n, int v) {
+    int lo = 0, hi = n;
+    while (lo < hi) {
+        const int mid = (lo + hi) >> 1;
+        if (p[mid] <= v) lo = mid + 1; else hi = mid;
+    }
+    return lo;
+}
+
+// ---------------------------------------------------------------------------------------------
+// pages and slots of a step
+// ---------------------------------------------------------------------------------------------
+// need_b = ceil((len_b + rows_b) / 64) pages.  What a sequence owns beyond that goes back on the stack of free pages, in the reverse
+// order of granting (a grant taken back leaves the stack as it was); what it lacks comes off the stack's top, sequence by sequence.
+// Places are prefix sums, so the result does not depend on the order of execution.  One workgroup, a thread per sequence
+// and then a thread per page and per row: all of it is a chain of dependent reads, a few microseconds however little there is to do.
+#define MAP_THREADS 1024
+#define MAP_ROWS_HERE 8192       // rows whose slots the same workgroup writes; more take a launch of many
+#define MAP_MAX_SLOTS 65536      // (bits of LDS that find a slot listed twice)
+
+struct MapSeq { int slot, len, rows, own, need; };
+__device__ __forceinline__ MapSeq map_seq(const MapArgs &a, int b, bool ok) {
+    MapSeq s{0, 0, 0, 0, 0};
+    if (b >= a.n_seqs || !ok) return s;
+    s.slot = a.slots ? a.slots[b] : b;
+    s.len = a.lens[s.slot];
+    s.rows = a.rows[b];
+    s.own = a.owned[s.slot];
+    s.need = (int)(((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS);
+    return s;
+}
+
+__device__ __forceinline__ void map_row(const MapArgs &a, int i, int total, const int *offsets) {
+    if (i >= total) {
+        a.slot_map[i] = -1;
+        a.row_pos[i] = 0;
+        return;
+    }
+    const int b = count_le(offsets + 1, a.n_seqs, i);
+    const int slot = a.slots ? a.slots[b] : b;
+    const int pos = a.lens[slot] + i - offsets[b];
+    const int page = a.table[(size_t)slot * a.max_blocks + pos / PAGE_POS];
+    a.slot_map[i] = (unsigned)page < (unsigned)a.n_pages ? page * PAGE_POS + pos % PAGE_POS : -1;      // (a free list that holds no page's number)
+    a.row_pos[i] = pos;
+}
+
+__global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
+    constexpr int NW = MAP_THREADS / 64;
+    __shared__ int part[NW];
+    __shared__ unsigned listed[MAP_MAX_SLOTS / 32];
+    __shared__ int first[MAP_THREADS + 1];
+    __shared__ int bad;
+    __shared__ unsigned long long sums[3];                       // pages back, pages granted, rows
+    const int t = threadIdx.x;
+    if (t == 0) { bad = 0; sums[0] = sums[1] = sums[2] = 0; }
+    if (a.slots)
+        for (int w = t; w < (a.n_slots + 31) / 32; w += MAP_THREADS) listed[w] = 0;
+    __syncthreads();
+    // ---- what the lists ask for, and whether they make sense
+    for (int b = t; b < a.n_seqs; b += MAP_THREADS) {
+        const int slot = a.slots ? a.slots[b] : b;
+        if ((unsigned)slot >= (unsigned)a.n_slots) { atomicMin(&bad, LLMA_E_RANGE); continue; }
+        if (a.slots && (atomicOr(&listed[slot / 32], 1u << (slot % 32)) >> (slot % 32) & 1)) { atomicMin(&bad, LLMA_E_INVAL); continue; }
+        const int len = a.lens[slot], rows = a.rows[b], own = a.owned[slot];
+        if (len < 0 || rows < 0 || own < 0 || own > a.max_blocks) { atomicMin(&bad, LLMA_E_INVAL); continue; }
+        const long long need = ((long long)len + rows + PAGE_POS - 1) / PAGE_POS;
+        if (need > a.max_blocks) { atomicMin(&bad, LLMA_E_RANGE); continue; }
+        if (own > need) atomicAdd(&sums[0], (unsigned long long)(own - need));
+        if (need > own) atomicAdd(&sums[1], (unsigned long long)(need - own));
+        atomicAdd(&sums[2], (unsigned long long)rows);
+    }
+    __syncthreads();
+    const int top = *a.n_free;
+    int status = bad;
+    if (status == 0 && (top < 0 || sums[0] > (unsigned long long)a.n_pages || top > a.n_pages - (int)sums[0])) status = LLMA_E_INVAL;
+    // (without a slot map only the tables and offsets are wanted: any number of rows)
+    if (status == 0 && (sums[2] > 0x7fffffffull || (a.max_rows > 0 && sums[2] > (unsigned long long)a.max_rows))) status = LLMA_E_RANGE;
+    const int stack = top + (status == 0 ? (int)sums[0] : 0);    // its height once everything is back
+    if (status == 0 && sums[1] > (unsigned long long)stack) status = (int)(sums[1] - (unsigned long long)stack);
+    const bool ok = status == 0;
+    const int total = ok ? (int)sums[2] : 0;
+    if (t == 0) *a.status = status;
+    if (ok) {
+        // ---- pages that go back: the j-th of them in granting order lies j below the stack's new top
+        int before = 0;
+        for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
+            const MapSeq s = map_seq(a, b0 + t, true);
+            int sum;
+            const int at = block_scan<NW>(s.own > s.need ? s.own - s.need : 0, part, &sum);
+            first[t] = at;
+            if (t == 0) first[MAP_THREADS] = sum;
+            __syncthreads();
+            for (int i = t; i < sum; i += MAP_THREADS) {
+                const int q = count_le(first, MAP_THREADS, i) - 1;
+                const MapSeq o = map_seq(a, b0 + q, true);
+                int *entry = a.table + (size_t)o.slot * a.max_blocks + o.need + (i - first[q]);
+                a.free_pages[stack - 1 - (before + i)] = *entry;
+                *entry = -1;
+            }
+            before += sum;
+            __syncthreads();
+        }
+        __syncthreads();
+        // ---- pages that are granted
+        before = 0;
+        for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
+            const MapSeq s = map_seq(a, b0 + t, true);
+            int sum;
+            const int at = block_scan<NW>(s.need > s.own ? s.need - s.own : 0, part, &sum);
+            first[t] = at;
+            if (t == 0) first[MAP_THREADS] = sum;
+            __syncthreads();
+            for (int i = t; i < sum; i += MAP_THREADS) {
+                const int q = count_le(first, MAP_THREADS, i) - 1;
+                const MapSeq o = map_seq(a, b0 + q, true);
+                a.table[(size_t)o.slot * a.max_blocks + o.own + (i - first[q])] = a.free_pages[stack - 1 - (before + i)];
+            }
+            before += sum;
+            __syncthreads();                                     // (everyone has read owned)
+            if (b0 + t < a.n_seqs) a.owned[s.slot] = s.need;
+        }
+        if (t == 0) *a.n_free = stack - before;
+    }
+    // ---- rows
+    int before = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
+        const int b = b0 + t;
+        int len = 0, rows = 0;
+        if (b < a.n_seqs) {
+            const int slot = a.slots ? a.slots[b] : b;
+            if ((unsigned)slot < (unsigned)a.n_slots) len = a.lens[slot];
+            if (ok) rows = a.rows[b];
+        }
+        int sum;
+        const int at = block_scan<NW>(rows, part, &sum);
+        if (b < a.n_seqs) {
+            a.row_offsets[b] = before + at;
+            a.lens_after[b] = len + rows;
+        }
+        before += sum;
+    }
+    if (t == 0) a.row_offsets[a.n_seqs] = before;
+    __syncthreads();
+    if (a.max_rows > MAP_ROWS_HERE) return;
+    for (int i = t; i < a.max_rows; i += MAP_THREADS) map_row(a, i, total, a.row_offsets);
+}
+__global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
+    const int total = a.row_offsets[a.n_seqs];
+    for (int i = blockIdx.x * 1024 + threadIdx.x; i < a.max_rows && i < (int)(blockIdx.x + 1) * 1024; i += 256) map_row(a, i, total, a.row_offsets);
+}
+void launch_map_pages(const MapArgs &a, hipStream_t st) {
+    hipLaunchKernelGGL(map_pages_kernel, dim3(1), dim3(MAP_THREADS), 0, st, a);
+    if (a.max_rows > MAP_ROWS_HERE) hipLaunchKernelGGL(map_rows_kernel, dim3((a.max_rows + 1023) / 1024), dim3(256), 0, st, a);
+}
+
+// ---------------------------------------------------------------------------------------------
+// rows of a call: eight neighbouring features as fp32
+// ---------------------------------------------------------------------------------------------
+typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+template <int TYPE>
+__device__ __forceinline__ void row8(const void *p, int64_t at, float v[8]) {
+    if constexpr (TYPE == ROWS_F32) {
+        const f32x4 a = *(const f32x4 *)((const float *)p + at), b = *(const f32x4 *)((const float *)p + at + 4);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[e] = a[e]; v[4 + e] = b[e]; }
+    } else if constexpr (TYPE == ROWS_F16) {
+        const f16x8 a = *(const f16x8 *)((const _Float16 *)p + at);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)a[e];
+    } else {
+        const u32x4 a = *(const u32x4 *)((const bf16_t *)p + at);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(a[e] << 16); v[2 * e + 1] = __uint_as_float(a[e] & 0xffff0000u); }
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// write into the cache
+// ---------------------------------------------------------------------------------------------
+// A run = rows with consecutive slots inside one page.  Per run and head: the smallest power of two s with max |x| / s <= 448 (over finite
+// values); a run that starts inside its page keeps the page's scale where that is larger, and where s is larger the
+// codes before it are rounded again to the new scale.  code = x / s rounded to nearest even: the division is exact, so the one rounding
+// to four significant bits is the format's.  +-inf become +-448, NaN stays NaN.
+// A wave per run and head holds the run in registers: 16 (8) lanes share a row's 128 (64) features, eight each, and a lane
+// has four neighbouring positions in turn, so that a dim's four codes leave as one word of the transposed V.
+__device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
+// exponent of the scale: -64 .. 120
+__device__ __forceinline__ int scale_exponent(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 127 - 8 + ((b & 0x7fffffu) > 0x600000u);      // 448 = 1.75 * 2^8
+    return e < -64 ? -64 : e > 120 ? 120 : e;
+}
+__device__ __forceinline__ float code_input(float x) { return x != x ? x : fminf(fmaxf(x, -448.f), 448.f); }
+__device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
+    uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_input(a), code_input(b), 0, false);
+    return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_input(c), code_input(d), (int)w, true);
+}
+__device__ __forceinline__ float code_value(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
+
+template <int DH, int TYPE, bool KEYS>
+__device__ __forceinline__ void append_run(const AppendArgs &a, int head, int row0, int n, int page, int off) {
+    constexpr int LPR = DH / 8;                     // lanes per row
+    constexpr int QUADS = 64 / LPR;                 // groups of four positions a wave has at once
+    constexpr int ROUNDS = PAGE_POS / (4 * QUADS);
+    const int lane = threadIdx.x & 63, d0 = lane % LPR * 8, quad = lane / LPR;
+    const size_t block = (size_t)page * a.c.heads + head;
+    uint8_t *const codes = (KEYS ? a.c.k : a.c.v) + block * (PAGE_POS * DH);
+    float *const scale = (KEYS ? a.c.k_scale : a.c.v_scale) + block;
+    const float old = off > 0 ? *scale : 0.f;
+    const void *const src = KEYS ? a.k : a.v;
+    const int64_t rs = KEYS ? a.k_row : a.v_row, hs = KEYS ? a.k_head : a.v_head;
+    float x[ROUNDS][4][8];
+    float amax = 0.f;
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int i = 4 * (quad + r * QUADS) + j - off;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) x[r][j][e] = 0.f;
+            if (i < 0 || i >= n) continue;
+            if constexpr (TYPE == ROWS_TILED) {
+                const bf16_t *p = (const bf16_t *)src + head * hs;
+                if constexpr (KEYS) {
+                    row8<ROWS_BF16>(p, (int64_t)kcache_off(row0 + i, d0, DH), x[r][j]);
+                } else {
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) x[r][j][e] = bf16_to_f32(p[vcache_off(row0 + i, d0 + e, DH)]);
+                }
+            } else {
+                row8<TYPE>(src, (int64_t)(row0 + i) * rs + head * hs + d0, x[r][j]);
+            }
+        }
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const float m = fabsf(x[r][j][e]);
+                amax = m < __builtin_huge_valf() ? fmaxf(amax, m) : amax;          // (false for NaN)
+            }
+    butterfly<32>([&](auto o) { amax = fmaxf(amax, lane_xor<o.value>(amax)); });
+    float s = pow2(scale_exponent(amax));
+    if (off > 0) {
+        if (s > old) {
+            // the codes before the run, byte by byte: those of its own positions are not touched
+            const float by = old / s;
+            for (int i = lane; i < off * DH; i += 64) {
+                uint8_t *const c = KEYS ? codes + i : codes + (size_t)(i / off) * PAGE_POS + i % off;
+                *c = (uint8_t)codes4(code_value(*c) * by, 0.f, 0.f, 0.f);
+            }
+        } else {
+            s = old;
+        }
+    }
+    if (lane == 0) *scale = s;
+    const float inv = 1.f / s;                      // (exact)
+#pragma unroll
+    for (int r = 0; r < ROUNDS; ++r) {
+        const int p0 = 4 * (quad + r * QUADS);      // the lane's positions in the page
+        if (p0 + 3 < off || p0 >= off + n) continue;
+        uint32_t w[4][2];                           // [position]: eight dims' codes
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const float *v = x[r][j];
+            w[j][0] = codes4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
+            w[j][1] = codes4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
+        }
+        if constexpr (KEYS) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                if (p0 + j >= off && p0 + j < off + n) *(u32x2 *)(codes + (p0 + j) * DH + d0) = (u32x2){w[j][0], w[j][1]};
+        } else {
+            const bool whole = p0 >= off && p0 + 3 < off + n;
+#pragma unroll
+            for (int e = 0; e < 8; ++e) {
+                const int sh = e % 4 * 8;
+                uint8_t *const to = codes + (d0 + e) * PAGE_POS + p0;
+                if (whole) {
+                    *(uint32_t *)to = (w[0][e / 4] >> sh & 255) | (w[1][e / 4] >> sh & 255) << 8 | (w[2][e / 4] >> sh & 255) << 16 | (w[3][e / 4] >> sh) << 24;
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        if (p0 + j >= off && p0 + j < off + n) to[j] = (uint8_t)(w[j][e / 4] >> sh);
+                }
+            }
+        }
+    }
+}
+
+// a wave per (window of rows, head, K or V): the runs that begin in the window, one after the other
+template <int DH, int TYPE>
+__global__ __launch_bounds__(256) void append_paged_kernel(AppendArgs a, int window, int n_windows) {
+    const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63;
+    const int win = unit / (2 * a.c.heads), head = unit % (2 * a.c.heads) / 2;
+    if (win >= n_windows) return;
+    const int r0 = win * window, r1 = r0 + window < a.n_rows ? r0 + window : a.n_rows;
+    const int i = r0 + lane;
+    int slot = -1, prev = -1;
+    if (i < r1) {
+        slot = a.slot_map[i];
+        prev = i > 0 ? a.slot_map[i - 1] : -1;
+    }
+    const bool live = slot >= 0 && slot / PAGE_POS < a.c.n_pages;
+    unsigned long long begins = __ballot(live && (prev < 0 || slot != prev + 1 || slot % PAGE_POS == 0));
+    while (begins) {
+        const int at = __builtin_ctzll(begins);
+        begins &= begins - 1;
+        const int first = __builtin_amdgcn_readlane(slot, at), off = first % PAGE_POS;
+        // its length: rows that follow with the slots that follow, to the page's end
+        const int left = PAGE_POS - off, j = r0 + at + lane;
+        const bool follows = lane < left && j < a.n_rows && a.slot_map[j < a.n_rows ? j : 0] == first + lane;
+        const unsigned long long same = __ballot(follows);
+        const int n = ~same == 0 ? 64 : __builtin_ctzll(~same);
+        if (unit & 1) append_run<DH, TYPE, false>(a, head, r0 + at, n, first / PAGE_POS, off);
+        else append_run<DH, TYPE, true>(a, head, r0 + at, n, first / PAGE_POS, off);
+    }
+}
+
+void launch_append_paged(const AppendArgs &a, hipStream_t st) {
+    if (a.n_rows < 1) return;
+    // a wave takes up to 64 rows' runs (a prompt's page); fewer while the chip has room for more waves (a step's runs are short)
+    int window = 64;
+    while (window > 1 && (int64_t)((a.n_rows + window - 1) / window) * 2 * a.c.heads < 4096) window /= 2;
+    const int n_windows = (a.n_rows + window - 1) / window;
+    const dim3 grid((unsigned)(((int64_t)n_windows * 2 * a.c.heads + 3) / 4));
+    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, window, n_windows); };
+    auto of = [&](auto dh) {
+        constexpr int DH = decltype(dh)::value;
+        if (a.type == ROWS_BF16) go(append_paged_kernel<DH, ROWS_BF16>);
+        else if (a.type == ROWS_F16) go(append_paged_kernel<DH, ROWS_F16>);
+        else if (a.type == ROWS_F32) go(append_paged_kernel<DH, ROWS_F32>);
+        else go(append_paged_kernel<DH, ROWS_TILED>);
+    };
+    if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
+    else of(std::integral_constant<int, 64>{});
+}
+
+// ---------------------------------------------------------------------------------------------
+// attention over the pages
+// ---------------------------------------------------------------------------------------------
+// Row j of sequence b sees positions 0 .. len - rows + j.  A key head's query rows (rows x query heads per key head) are the columns
+// of both products: S^T = K Q^T, O^T = V^T P^T, 16 rows a tile, NT tiles a wave.  Row i of score tile g is position 16 (i/4) + 4 g + i%4 of the page,
+// so that a lane's 16 probabilities are those of 16 neighbouring positions -- the ones its V bytes hold.
+// One pass with the running maximum and sum of the softmax in fp32; scores in powers of two.
+// The pages of all sequences, end to end, are cut into equal shares, one per workgroup and key head: ragged lengths load the chip
+// evenly, and a share's four waves take its pages in turn and meet in LDS at a sequence's end.  A sequence that lies in one share
+// is finished there; the others' parts are joined by attend_join_kernel.
+#define ATTEND_SHARES 512        // workgroups wanted: two per compute unit
+#define ATTEND_MIN_PAGES 4       // of a share: a page per wave
+
+struct AttendPlan { int nt, tiles, shares; };
+static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows) {
+    const int64_t r = (int64_t)max_rows * (n_heads / kv_heads);
+    AttendPlan p;
+    p.nt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
+    p.tiles = (int)((r + 16 * p.nt - 1) / (16 * p.nt));
+    const int64_t pages = (int64_t)n_seqs * max_blocks, most = (pages + ATTEND_MIN_PAGES - 1) / ATTEND_MIN_PAGES;
+    int64_t shares = ATTEND_SHARES / ((int64_t)kv_heads * p.tiles);
+    if (shares > most) shares = most;
+    p.shares = shares < 1 ? 1 : (int)shares;
+    return p;
+}
+// work: [pages before every sequence, n_seqs + 1 ints, rounded up to 64][parts' O][parts' m][parts' l]
+__host__ __device__ static inline int64_t attend_parts(const AttendPlan &p, int kv_heads) { return p.shares > 1 ? (int64_t)p.shares * 2 * kv_heads * p.tiles : 0; }
+int64_t attend_paged_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
+    const AttendPlan p = attend_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows);
+    return ((int64_t)(n_seqs + 1 + 63) / 64 * 64 + attend_parts(p, kv_heads) * 16 * p.nt * (dh + 2)) * 4;
+}
+
+struct AttendSeq { int slot, len, rows, row0; };
+// a sequence as the kernels take it: whatever the lists hold, nothing outside the buffers is reached
+__device__ __forceinline__ AttendSeq attend_seq(const AttendArgs &a, int b) {
+    AttendSeq s;
+    s.row0 = a.row_offsets[b];
+    s.rows = a.row_offsets[b + 1] - s.row0;
+    s.rows = s.rows > a.max_rows ? a.max_rows : s.rows;
+    if (s.row0 < 0 || s.row0 > a.n_rows) s.rows = 0;
+    else if (s.rows > a.n_rows - s.row0) s.rows = a.n_rows - s.row0;
+    s.slot = a.slots ? a.slots[b] : b;
+    s.len = a.lens[b];
+    const int64_t most = (int64_t)a.max_blocks * PAGE_POS;
+    if (s.len > most) s.len = (int)most;
+    if (s.len < 0 || (unsigned)s.slot >= (unsigned)a.n_slots) s.len = 0;
+    return s;
+}
+__device__ __forceinline__ int attend_pages(const AttendSeq &s) {      // a sequence without positions still has rows to write
+    if (s.rows <= 0) return 0;
+    return s.len < 1 ? 1 : (s.len + PAGE_POS - 1) / PAGE_POS;
+}
+
+// q: 16-byte operand pieces in LDS, [plane][tile][64-dim group][half][lane]
+template <int DH, int NT, int NQ, int TYPE>
+__device__ __forceinline__ void attend_take_q(const AttendArgs &a, const AttendSeq &s, int head, int group, int r0, u32x4 *q) {
+    constexpr int PIECES = NT * (DH / 64) * 2 * 64;
+    for (int i = threadIdx.x; i < PIECES; i += 256) {
+        const int lane = i & 63, half = i >> 6 & 1, t = (i >> 7) % (DH / 64), nt = (i >> 7) / (DH / 64);
+        const int r = r0 + nt * 16 + (lane & 15), d = 64 * t + 16 * (lane >> 4) + 8 * half;
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = 0.f;
+        u32x4 p[3] = {(u32x4){0, 0, 0, 0}, (u32x4){0, 0, 0, 0}, (u32x4){0, 0, 0, 0}};
+        if (r < s.rows * group) {
+            const int row = s.row0 + r / group, h = head * group + r % group;
+            if constexpr (TYPE == ROWS_TILED) {
+                const size_t at = xtile_off(row, h * DH + d, a.tile_ksp, a.quads);
+                p[0] = *(const u32x4 *)((const bf16_t *)a.q + at);
+                p[1] = *(const u32x4 *)((const bf16_t *)a.q_lo + at);
+            } else {
+                row8<TYPE>(a.q, (int64_t)row * a.q_row + h * a.q_head + d, v);
+            }
+        }
+        if constexpr (TYPE != ROWS_TILED) {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                float x = v[2 * w], y = v[2 * w + 1];
+#pragma unroll
+                for (int n = 0; n < NQ; ++n) {
+                    p[n][w] = bf16_pair(x, y);
+                    if (n + 1 < NQ) { x -= __uint_as_float(p[n][w] << 16); y -= __uint_as_float(p[n][w] & 0xffff0000u); }
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NQ; ++n) q[n * PIECES + i] = p[n];
+    }
+}
+// 16 codes as two operands of eight bf16, times a power of two
+__device__ __forceinline__ void widen16(u32x4 c, float scale, u32x4 &lo, u32x4 &hi) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        lo[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[w], scale, false));
+        lo[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[w], scale, true));
+        hi[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 + w], scale, false));
+        hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 + w], scale, true));
+    }
+}
+// ones where one of 16 codes is NaN, as bf16 operands; *any: whether there is one.  The codes themselves become zero there
+__device__ __forceinline__ void take_nans(u32x4 &c, u32x4 &lo, u32x4 &hi, bool &any) {
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        uint32_t m = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+            if ((c[w] >> (8 * e) & 0x7f) == 0x7f) m |= 0xffu << (8 * e);
+        c[w] &= ~m;
+        any |= m != 0;
+        const uint32_t a = (m & 1 ? 0x3f80u : 0) | (m & 0x100 ? 0x3f800000u : 0), b = (m & 0x10000 ? 0x3f80u : 0) | (m & 0x1000000 ? 0x3f800000u : 0);
+        if (w < 2) { lo[2 * w] = a; lo[2 * w + 1] = b; }
+        else { hi[2 * w - 4] = a; hi[2 * w - 3] = b; }
+    }
+}
+
+template <int TYPE>
+__device__ __forceinline__ void attend_store(const AttendArgs &a, int row, int h, int d, f32x4 v) {      // four neighbouring features
+    if constexpr (TYPE == ROWS_TILED) {
+        const size_t at = xtile_off(row, h * a.c.dh + d, a.tile_out_ksp, a.quads);
+        const float f[4] = {v[0], v[1], v[2], v[3]};
+        u32x2 hi, lo;
+        split4(f, hi, lo);
+        *(u32x2 *)((bf16_t *)a.out + at) = hi;
+        *(u32x2 *)((bf16_t *)a.out_lo + at) = lo;
+    } else {
+        const int64_t at = (int64_t)row * a.out_row + h * a.out_head + d;
+        if constexpr (TYPE == ROWS_F32) {
+            *(f32x4 *)((float *)a.out + at) = v;
+        } else if constexpr (TYPE == ROWS_F16) {
+            typedef __attribute__((ext_vector_type(4))) _Float16 f16x4;
+            *(f16x4 *)((_Float16 *)a.out + at) = (f16x4){(_Float16)v[0], (_Float16)v[1], (_Float16)v[2], (_Float16)v[3]};
+        } else {
+            *(u32x2 *)((bf16_t *)a.out + at) = (u32x2){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3])};
+        }
+    }
+}
+
+// Planes of bf16 that hold a row type's q exactly (fp32: 24 bits) and a probability to the output's precision: one bf16 probability is off by at most
+// 2^-8 of itself, as a bf16 output is, two by 2^-16 (fp16: 2^-11), three by 2^-24.
+template <int TYPE> constexpr int attend_nq = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
+template <int TYPE> constexpr int attend_np = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
+
+template <int DH, int NT, int TYPE>
+__global__ __launch_bounds__(256) void attend_paged_kernel(AttendArgs a, AttendPlan plan) {
+    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE>;
+    constexpr int TD = DH / 64, DT = DH / 16, PIECES = NT * TD * 2 * 64;
+    constexpr int JOIN = 2 * NT * DT * 64;                       // two waves' sums, in 16-byte pieces
+    extern __shared__ u32x4 lds[];
+    constexpr int BIG = NQ * PIECES > JOIN ? NQ * PIECES : JOIN;
+    u32x4 *const q = lds;
+    f32x4 *const osum = (f32x4 *)lds;                            // (the queries' place, once they are used)
+    __shared__ float ml[2][2][NT * 16];
+    __shared__ int part[4];
+    int *const starts = (int *)(lds + BIG);                      // [n_seqs + 1]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int share = blockIdx.x % plan.shares, head = blockIdx.x / plan.shares % a.c.heads, tile = blockIdx.x / plan.shares / a.c.heads;
+    const int group = a.n_heads / a.c.heads, r0 = tile * NT * 16;
+    // ---- where the sequences' pages begin
+    int total = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += 256) {
+        const int b = b0 + threadIdx.x;
+        int sum;
+        const int at = block_scan<4>(b < a.n_seqs ? attend_pages(attend_seq(a, b)) : 0, part, &sum);
+        if (b < a.n_seqs) starts[b] = total + at;
+        total += sum;
+    }
+    if (threadIdx.x == 0) starts[a.n_seqs] = total;
+    __syncthreads();
+    if (plan.shares > 1 && blockIdx.x == 0)        // (for attend_join_kernel)
+        for (int b = threadIdx.x; b <= a.n_seqs; b += 256) ((int *)a.work)[b] = starts[b];
+    int per = (total + plan.shares - 1) / plan.shares;
+    per = per < ATTEND_MIN_PAGES ? ATTEND_MIN_PAGES : per;
+    const int64_t from = (int64_t)share * per;
+    if (from >= total) return;
+    const int p0 = (int)from, p1 = p0 + per < total ? p0 + per : total;
+    const float to_log2 = a.scale * 1.44269504088896340736f;
+    const int kb = lane >> 4, col = lane & 15;
+    const int k_off = (16 * (col >> 2) + (col & 3)) * DH + 16 * kb, v_off = col * PAGE_POS + 16 * kb;
+
+    for (int b = count_le(starts, a.n_seqs + 1, p0) - 1; b < a.n_seqs && starts[b] < p1; ++b) {
+        const int first = p0 > starts[b] ? p0 - starts[b] : 0, pages = starts[b + 1] - starts[b];
+        const int last = (p1 < starts[b + 1] ? p1 : starts[b + 1]) - starts[b];
+        const AttendSeq s = attend_seq(a, b);
+        if (first >= last || r0 >= s.rows * group) continue;     // (uniform)
+        __syncthreads();
+        attend_take_q<DH, NT, NQ, TYPE>(a, s, head, group, r0, q);
+        __syncthreads();
+        // the last position that every column sees, and each lane's columns' own
+        const int seen = s.len - s.rows;
+        int limit[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = r0 + 16 * n + col;
+            limit[n] = r < s.rows * group ? seen + r / group : -1;
+        }
+        f32x4 o[NT][DT];
+        float m[NT], l[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            m[n] = LLMA_NEG_INF;
+            l[n] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[n][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        for (int i0 = first + wave; i0 < last; i0 += 256) {      // 64 pages of this wave: their numbers and scales
+            int id = -1;
+            float ks = 0.f, vs = 0.f;
+            if (i0 + 4 * lane < last && (i0 + 4 * lane) * PAGE_POS < s.len) {
+                id = a.table[(size_t)s.slot * a.max_blocks + i0 + 4 * lane];
+                if ((unsigned)id >= (unsigned)a.c.n_pages) id = -1;
+            }
+            if (id >= 0) {
+                ks = a.c.k_scale[(size_t)id * a.c.heads + head];
+                vs = a.c.v_scale[(size_t)id * a.c.heads + head];
+            }
+            const int n_here = (last - i0 + 3) / 4 < 64 ? (last - i0 + 3) / 4 : 64;
+            for (int it = 0; it < n_here; ++it) {
+                const int page = __builtin_amdgcn_readlane(id, it), base = (i0 + 4 * it) * PAGE_POS;
+                if (page < 0) continue;                          // no such page: its positions are not seen
+                const float pks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), it)), pvs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), it));
+                const size_t block = ((size_t)page * a.c.heads + head) * (PAGE_POS * DH);
+                u32x4 kc[4][TD], vc[DT];
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int t = 0; t < TD; ++t) kc[g][t] = *(const u32x4 *)(a.c.k + block + k_off + 4 * g * DH + 64 * t);
+#pragma unroll
+                for (int d = 0; d < DT; ++d) vc[d] = *(const u32x4 *)(a.c.v + block + v_off + 16 * d * PAGE_POS);
+                f32x4 sc[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) sc[n][g] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                for (int t = 0; t < TD; ++t)
+#pragma unroll
+                    for (int g = 0; g < 4; ++g) {
+                        u32x4 lo, hi;
+                        widen16(kc[g][t], 1.f, lo, hi);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int pl = NQ - 1; pl >= 0; --pl) {
+                                sc[n][g] = mfma16x16x32(lo, q[pl * PIECES + ((n * TD + t) * 2) * 64 + lane], sc[n][g]);
+                                sc[n][g] = mfma16x16x32(hi, q[pl * PIECES + ((n * TD + t) * 2 + 1) * 64 + lane], sc[n][g]);
+                            }
+                    }
+                const float by = to_log2 * pks;
+                const bool masked = base + PAGE_POS - 1 > seen;
+                bool nans = false;
+                if (masked) {
+                    const int there = s.len - base - 16 * kb;    // of the lane's 16 positions of V
+#pragma unroll
+                    for (int d = 0; d < DT; ++d)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int n = there - 4 * w;
+                            vc[d][w] &= n >= 4 ? ~0u : n <= 0 ? 0u : ~(~0u << (8 * n));
+                            // a NaN that only later rows see must not reach the others through 0 * NaN
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) nans |= (vc[d][w] >> (8 * e) & 0x7f) == 0x7f;
+                        }
+                }
+                u32x4 pb[NT][NP][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float x[16], top = LLMA_NEG_INF;
+#pragma unroll
+                    for (int g = 0; g < 4; ++g)
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            float v = sc[n][g][r] * by;
+                            if (masked && base + 16 * kb + 4 * g + r > limit[n]) v = LLMA_NEG_INF;
+                            x[4 * g + r] = v;
+                            top = fmaxf(top, v);
+                        }
+                    top = fmaxf(top, lane_xor<16>(top));
+                    top = fmaxf(top, lane_xor<32>(top));
+                    const float mn = fmaxf(m[n], top), ref = mn == LLMA_NEG_INF ? 0.f : mn;
+                    const float keep = __builtin_amdgcn_exp2f(m[n] - ref);
+                    m[n] = mn;
+                    l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
+                        l[n] += x[e];
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            float y = x[8 * u + 2 * w], z = x[8 * u + 2 * w + 1];
+#pragma unroll
+                            for (int pl = 0; pl < NP; ++pl) {
+                                pb[n][pl][u][w] = bf16_pair(y, z);
+                                if (pl + 1 < NP) { y -= __uint_as_float(pb[n][pl][u][w] << 16); z -= __uint_as_float(pb[n][pl][u][w] & 0xffff0000u); }
+                            }
+                        }
+                }
+                if (masked && __ballot(nans) != 0) {             // rare: rows that see a NaN get it, the others do not
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) {
+                        u32x4 lo, hi;
+                        bool any = false;
+                        take_nans(vc[d], lo, hi, any);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            u32x4 vis[2];
+#pragma unroll
+                            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                                for (int w = 0; w < 4; ++w) {
+                                    const int p = base + 16 * kb + 8 * u + 2 * w;
+                                    vis[u][w] = (p <= limit[n] ? 0x3f80u : 0) | (p + 1 <= limit[n] ? 0x3f800000u : 0);
+                                }
+                            f32x4 hit = (f32x4){0.f, 0.f, 0.f, 0.f};
+                            hit = mfma16x16x32(lo, vis[0], hit);
+                            hit = mfma16x16x32(hi, vis[1], hit);
+#pragma unroll
+                            for (int r = 0; r < 4; ++r)
+                                if (hit[r] > 0.f) o[n][d][r] = __builtin_nanf("");
+                        }
+                    }
+                }
+#pragma unroll
+                for (int d = 0; d < DT; ++d) {
+                    u32x4 lo, hi;
+                    widen16(vc[d], pvs, lo, hi);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int pl = NP - 1; pl >= 0; --pl) {
+                            o[n][d] = mfma16x16x32(lo, pb[n][pl][0], o[n][d]);
+                            o[n][d] = mfma16x16x32(hi, pb[n][pl][1], o[n][d]);
+                        }
+                }
+            }
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            l[n] += lane_xor<16>(l[n]);
+            l[n] += lane_xor<32>(l[n]);
+        }
+        // ---- the waves' sums meet: 2 and 3 with 0 and 1, then 1 with 0
+#pragma unroll
+        for (int step = 2; step >= 1; step /= 2) {
+            __syncthreads();
+            if (wave >= step && wave < 2 * step) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) osum[((wave - step) * NT * DT + n * DT + d) * 64 + lane] = o[n][d];
+                    if (kb == 0) { ml[wave - step][0][n * 16 + col] = m[n]; ml[wave - step][1][n * 16 + col] = l[n]; }
+                }
+            }
+            __syncthreads();
+            if (wave < step) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const float om = ml[wave][0][n * 16 + col], ol = ml[wave][1][n * 16 + col];
+                    const float mn = fmaxf(m[n], om), ref = mn == LLMA_NEG_INF ? 0.f : mn;
+                    const float f0 = __builtin_amdgcn_exp2f(m[n] - ref), f1 = __builtin_amdgcn_exp2f(om - ref);
+                    m[n] = mn;
+                    l[n] = l[n] * f0 + ol * f1;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] = o[n][d] * f0 + osum[(wave * NT * DT + n * DT + d) * 64 + lane] * f1;
+                }
+            }
+        }
+        if (wave == 0) {
+            const bool whole = first == 0 && last == pages;
+            // the part's place: a share has at most one sequence that began before it (0) and one that goes on behind it (1)
+            const int64_t at = (((int64_t)share * 2 + (first == 0)) * a.c.heads + head) * plan.tiles + tile;
+            float *const po = (float *)a.work + (a.n_seqs + 1 + 63) / 64 * 64;
+            float *const pm = po + attend_parts(plan, a.c.heads) * 16 * NT * DH, *const pl = pm + attend_parts(plan, a.c.heads) * 16 * NT;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int r = r0 + 16 * n + col;
+                if (r >= s.rows * group) continue;
+                if (whole) {
+                    const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 16 * d + 4 * kb, o[n][d] * inv);
+                } else {
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) *(f32x4 *)(po + (at * 16 * NT + 16 * n + col) * DH + 16 * d + 4 * kb) = o[n][d];
+                    if (kb == 0) { pm[at * 16 * NT + 16 * n + col] = m[n]; pl[at * 16 * NT + 16 * n + col] = l[n]; }
+                }
+            }
+        }
+    }
+}
+
+// a wave per row of a sequence that lies in several shares
+template <int DH, int TYPE>
+__global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, AttendPlan plan) {
+    const int lane = threadIdx.x & 63, group = a.n_heads / a.c.heads;
+    const int b = blockIdx.z, head = blockIdx.y, r = blockIdx.x * 4 + (threadIdx.x >> 6);
+    const int *const starts = (const int *)a.work;
+    const int total = starts[a.n_seqs], p0 = starts[b], p1 = starts[b + 1];
+    const AttendSeq s = attend_seq(a, b);
+    if (r >= s.rows * group || p0 >= p1) return;
+    int per = (total + plan.shares - 1) / plan.shares;
+    per = per < ATTEND_MIN_PAGES ? ATTEND_MIN_PAGES : per;
+    const int s0 = p0 / per, s1 = (p1 - 1) / per;
+    if (s0 == s1) return;
+    const int nt16 = 16 * plan.nt, tile = r / nt16, at16 = r % nt16;
+    const int64_t parts = attend_parts(plan, a.c.heads);
+    const float *const po = (const float *)a.work + (a.n_seqs + 1 + 63) / 64 * 64, *const pm = po + parts * nt16 * DH, *const pl = pm + parts * nt16;
+    const auto place = [&](int sh) { return ((((int64_t)sh * 2 + (sh == s0)) * a.c.heads + head) * plan.tiles + tile) * nt16 + at16; };
+    float m = LLMA_NEG_INF;
+    for (int sh = s0 + lane; sh <= s1; sh += 64) m = fmaxf(m, pm[place(sh)]);
+    butterfly<32>([&](auto o) { m = fmaxf(m, lane_xor<o.value>(m)); });
+    const float ref = m == LLMA_NEG_INF ? 0.f : m;
+    const int d = lane % (DH / 4) * 4, g0 = lane / (DH / 4);     // four features a lane; the wave's groups take parts in turn
+    constexpr int GROUPS = 256 / DH;
+    float l = 0.f;
+    f32x4 o = (f32x4){0.f, 0.f, 0.f, 0.f};
+    for (int sh = s0 + g0; sh <= s1; sh += GROUPS) {
+        const int64_t at = place(sh);
+        const float f = __builtin_amdgcn_exp2f(pm[at] - ref);
+        l += pl[at] * f;
+        o += *(const f32x4 *)(po + at * DH + d) * f;
+    }
+    const auto add = [&](auto off) {
+        l += lane_xor<off.value>(l);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] += lane_xor<off.value>(o[e]);
+    };
+    add(std::integral_constant<int, 32>{});
+    if constexpr (DH == 64) add(std::integral_constant<int, 16>{});
+    if (g0 == 0) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, d, o * (l == 0.f ? 0.f : 1.f / l));
+}
+
+template <int DH, int NT, int TYPE>
+static void launch_attend_nt(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
+    constexpr int NQ = attend_nq<TYPE>, PIECES = NT * (DH / 64) * 2 * 64, JOIN = 2 * NT * (DH / 16) * 64;
+    const size_t bytes = (size_t)(NQ * PIECES > JOIN ? NQ * PIECES : JOIN) * 16 + (size_t)(a.n_seqs + 1) * 4;
+    hipLaunchKernelGGL((attend_paged_kernel<DH, NT, TYPE>), dim3(p.shares * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
+}
+template <int DH, int TYPE>
+static void launch_attend_type(const AttendArgs &a, hipStream_t st) {
+    const AttendPlan p = attend_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows);
+    if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
+    else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
+    else launch_attend_nt<DH, 4, TYPE>(a, p, st);
+    if (p.shares > 1)
+        hipLaunchKernelGGL((attend_join_kernel<DH, TYPE>), dim3((a.max_rows * (a.n_heads / a.c.heads) + 3) / 4, a.c.heads, a.n_seqs), dim3(256), 0, st, a, p);
+}
+void launch_attend_paged(const AttendArgs &a, hipStream_t st) {
+    if (a.n_seqs < 1 || a.n_rows < 1 || a.max_rows < 1) return;
+    auto of = [&](auto dh) {
+        constexpr int DH = decltype(dh)::value;
+        if (a.type == ROWS_BF16) launch_attend_type<DH, ROWS_BF16>(a, st);
+        else if (a.type == ROWS_F16) launch_attend_type<DH, ROWS_F16>(a, st);
+        else if (a.type == ROWS_F32) launch_attend_type<DH, ROWS_F32>(a, st);
+        else launch_attend_type<DH, ROWS_TILED>(a, st);
+    };
+    if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
+    else of(std::integral_constant<int, 64>{});
+}

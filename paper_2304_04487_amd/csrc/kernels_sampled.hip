@@ -1,0 +1,420 @@
+// Verification of drafted tokens against the target's probabilities, from given random numbers (speculative sampling).
+//   p_j = softmax(logits_j / T), q_j the draft's distribution (one-hot where it is a copied token).  Draft j is accepted while u_j q_j(x_j) < p_j(x_j);
+//   at the first rejection the token comes from max(p_j - q_j, 0), after all were accepted from p_k: the smallest v with
+//   sum_{i <= v} w_i > r * sum w.  T <= 0: the arg max (lowest id), as the greedy step has it.
+// Bound by one read of the logits.  That pass keeps maxima and fp32 sums of 2^x, which decide all but about one test in 10^4; a test too near its border
+// for them is decided again with the row's sum in 64 bits.  The one row that is sampled is read again in 64 bits throughout, so that
+// a token does not depend on how the sums were cut: exponentials off by 1e-7 would move one sample in some hundreds.
+#include "../../include/llma.h"
+#include "paged.h"
+
+#define ROW_THREADS 256
+#define PICK_BLOCKS 512          // 16-byte pieces of a row per workgroup when it is sampled (two a thread)
+
+template <int TYPE> constexpr int sampled_epb = TYPE == ROWS_F32 ? 4 : 8;        // logits of a 16-byte piece
+
+// Rows begin anywhere: a row is read in the aligned 16-byte pieces that hold it, and what of the first and last is not its own is masked
+// (both pieces hold a byte of the row, so they lie in its allocation).
+struct RowView { const u32x4 *base; int skip; };                // pieces from the one with the row's first logit; logits before it in there
+template <int TYPE>
+__device__ __forceinline__ RowView row_view(const SampledArgs &a, int64_t row) {
+    constexpr int SIZE = TYPE == ROWS_F32 ? 4 : 2;
+    const uintptr_t at = (uintptr_t)a.logits + (uintptr_t)(row * a.row_stride) * SIZE;
+    return RowView{(const u32x4 *)(at & ~(uintptr_t)15), (int)(at & 15) / SIZE};
+}
+template <int TYPE>
+__device__ __forceinline__ void piece_values(u32x4 p, float v[sampled_epb<TYPE>]) {
+    if constexpr (TYPE == ROWS_F32) {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(p[e]);
+    } else if constexpr (TYPE == ROWS_F16) {
+        typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
+        const f16x8 h = __builtin_bit_cast(f16x8, p);
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+    } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(p[e] << 16); v[2 * e + 1] = __uint_as_float(p[e] & 0xffff0000u); }
+    }
+}
+__device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
+    const int n = a.n_draft ? a.n_draft[b] : a.k;
+    return n < 0 ? 0 : n > a.k ? a.k : n;
+}
+__device__ __forceinline__ float logit_of(float x) { return x != x ? LLMA_NEG_INF : x; }           // NaN: a token that cannot be
+// e^((x - top) / T) in 64 bits; the top itself (also +inf) counts 1, minus infinity 0
+__device__ __forceinline__ double weight64(float x, float top, double inv_t) {
+    return x == top ? (x == LLMA_NEG_INF ? 0.0 : 1.0) : x == LLMA_NEG_INF ? 0.0 : exp(((double)x - (double)top) * inv_t);
+}
+
+struct RowPart { float top, sum; int where; };                   // of a chunk: maximum, sum of 2^((x - top) log2(e) / T), first index of the maximum
+
+// work: RowPart[rows][chunks] | per sequence: Choice | double weight sums [n_seqs][picks] (and, with draft probabilities, exponentials' sums before them)
+struct Choice { int accepted, row, token, residual; float top; int greedy; double sum; };
+
+struct SampledPlan { int chunk_blocks, chunks, picks; int64_t at_choice, at_sums, bytes; };
+static SampledPlan sampled_plan(int n_seqs, int k, int vocab, int epb) {
+    SampledPlan p;
+    const int64_t blocks = ((int64_t)vocab + epb - 1) / epb + 1, rows = (int64_t)n_seqs * (k + 1);       // (+ 1: a row that begins inside a piece)
+    // eight pieces a thread where that leaves enough workgroups for the chip, two where it does not
+    p.chunk_blocks = rows * ((blocks + 2047) / 2048) >= 1024 ? 2048 : 512;
+    p.chunks = (int)((blocks + p.chunk_blocks - 1) / p.chunk_blocks);
+    p.picks = (int)((blocks + PICK_BLOCKS - 1) / PICK_BLOCKS);
+    p.at_choice = (rows * p.chunks * (int64_t)sizeof(RowPart) + 63) / 64 * 64;
+    p.at_sums = p.at_choice + (n_seqs * (int64_t)sizeof(Choice) + 63) / 64 * 64;
+    p.bytes = p.at_sums + 2 * (int64_t)n_seqs * p.picks * 8;
+    return p;
+}
+int64_t verify_sampled_bytes(int n_seqs, int k, int vocab) {
+    const SampledPlan a = sampled_plan(n_seqs, k, vocab, 4), b = sampled_plan(n_seqs, k, vocab, 8);
+    return a.bytes > b.bytes ? a.bytes : b.bytes;
+}
+
+template <int NB, int TYPE>
+__global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a, SampledPlan plan) {
+    constexpr int EPB = sampled_epb<TYPE>;
+    __shared__ RowPart parts[4];
+    const int row = blockIdx.x, b = row / (a.k + 1), j = row % (a.k + 1), t = threadIdx.x, lane = t & 63;
+    if (j > drafts_of(a, b)) return;                             // (a row that no draft leads to)
+    const float temp = a.temperature ? a.temperature[b] : 1.f;
+    const bool greedy = !(temp > 0.f);
+    const RowView v = row_view<TYPE>(a, row);
+    const int blocks = (v.skip + a.vocab + EPB - 1) / EPB, first = blockIdx.y * plan.chunk_blocks;
+    float x[NB][EPB];
+    float top = LLMA_NEG_INF;
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int blk = first + i * ROW_THREADS + t;
+        piece_values<TYPE>(v.base[blk < blocks ? blk : 0], x[i]);
+    }
+#pragma unroll
+    for (int i = 0; i < NB; ++i) {
+        const int id0 = (first + i * ROW_THREADS + t) * EPB - v.skip;
+#pragma unroll
+        for (int e = 0; e < EPB; ++e) {
+            x[i][e] = id0 + e >= 0 && id0 + e < a.vocab ? logit_of(x[i][e]) : LLMA_NEG_INF;
+            top = fmaxf(top, x[i][e]);
+        }
+    }
+    butterfly<32>([&](auto o) { top = fmaxf(top, lane_xor<o.value>(top)); });
+    if (lane == 0) parts[t >> 6].top = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(parts[0].top, parts[1].top), fmaxf(parts[2].top, parts[3].top));
+    float sum = 0.f;
+    int where = 0x7fffffff;
+    if (greedy) {
+#pragma unroll
+        for (int i = NB - 1; i >= 0; --i)
+#pragma unroll
+            for (int e = EPB - 1; e >= 0; --e)
+                if (x[i][e] == top && top != LLMA_NEG_INF) where = (first + i * ROW_THREADS + t) * EPB - v.skip + e;
+        butterfly<32>([&](auto o) { const int w = lane_xor<o.value>(where); where = w < where ? w : where; });
+    } else {
+        const float by = 1.44269504088896340736f / temp;
+#pragma unroll
+        for (int i = 0; i < NB; ++i)
+#pragma unroll
+            for (int e = 0; e < EPB; ++e) {
+                const float w = x[i][e] == top ? 1.f : __builtin_amdgcn_exp2f((x[i][e] - top) * by);
+                sum += x[i][e] == LLMA_NEG_INF ? 0.f : w;
+            }
+        butterfly<32>([&](auto o) { sum += lane_xor<o.value>(sum); });
+    }
+    if (lane == 0) { parts[t >> 6].sum = sum; parts[t >> 6].where = where; }
+    __syncthreads();
+    if (t == 0) {
+        RowPart p{top, 0.f, 0x7fffffff};
+        for (int w = 0; w < 4; ++w) { p.sum += parts[w].sum; p.where = parts[w].where < p.where ? parts[w].where : p.where; }
+        ((RowPart *)a.work)[(int64_t)row * plan.chunks + blockIdx.y] = p;
+    }
+}
+
+__device__ __forceinline__ double block_sum(double v, double *part) {       // over 256 threads; part: LDS of four words
+#pragma unroll
+    for (int d = 32; d >= 1; d /= 2) v += __shfl_xor(v, d);
+    __syncthreads();
+    if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
+    __syncthreads();
+    return part[0] + part[1] + part[2] + part[3];
+}
+// inclusive prefix sum over 256 threads, *total the sum
+__device__ __forceinline__ double scan64(double v, double *part, double *total) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+        const double o = __shfl_up(v, d);
+        if (lane >= d) v += o;
+    }
+    __syncthreads();
+    if (lane == 63) part[wave] = v;
+    __syncthreads();
+    double before = 0.0, sum = 0.0;
+#pragma unroll
+    for (int w = 0; w < 4; ++w) {
+        before += w < wave ? part[w] : 0.0;
+        sum += part[w];
+    }
+    *total = sum;
+    return before + v;
+}
+template <int TYPE>
+__device__ double row_sum64(const SampledArgs &a, int64_t row, float top, double inv_t, double *part) {
+    constexpr int EPB = sampled_epb<TYPE>;
+    const RowView v = row_view<TYPE>(a, row);
+    const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
+    double s = 0.0;
+    for (int blk = threadIdx.x; blk < blocks; blk += 256) {
+        float x[EPB];
+        piece_values<TYPE>(v.base[blk], x);
+#pragma unroll
+        for (int e = 0; e < EPB; ++e) {
+            const int id = blk * EPB - v.skip + e;
+            if (id >= 0 && id < a.vocab) s += weight64(logit_of(x[e]), top, inv_t);
+        }
+    }
+    return block_sum(s, part);
+}
+template <int TYPE>
+__device__ __forceinline__ float logit_at(const SampledArgs &a, int64_t row, int id) {
+    const int64_t at = row * a.row_stride + id;
+    if constexpr (TYPE == ROWS_F32) return logit_of(((const float *)a.logits)[at]);
+    else if constexpr (TYPE == ROWS_F16) return logit_of((float)((const _Float16 *)a.logits)[at]);
+    else return logit_of(bf16_to_f32(((const bf16_t *)a.logits)[at]));
+}
+
+// How many drafts of sequence b hold, and which row its token comes from.  All threads of a workgroup call it and get the same; lane j looks at
+// row j.  The sums of the rows' chunks are fp32: a test whose sides are nearer than 2^-15 of each other is decided
+// again with the row's sum in 64 bits (the sums are off by 4e-6 at most: 2e-7 of the exponent, which has 17 bits where weights still matter).
+template <int TYPE>
+__device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, double *part) {
+    const int lane = threadIdx.x & 63;
+    const int n_draft = drafts_of(a, b);
+    const float temp = a.temperature ? a.temperature[b] : 1.f;
+    const bool greedy = !(temp > 0.f);
+    const double inv_t = greedy ? 0.0 : 1.0 / (double)temp;
+    float top = LLMA_NEG_INF;
+    double sum = 0.0;
+    int where = 0x7fffffff, draft = -1;
+    const int64_t row = (int64_t)b * (a.k + 1) + lane;
+    if (lane <= n_draft) {
+        const RowPart *p = (const RowPart *)a.work + row * plan.chunks;
+        for (int c = 0; c < plan.chunks; ++c) top = fmaxf(top, p[c].top);
+        for (int c = 0; c < plan.chunks; ++c) {
+            if (p[c].top == top && p[c].where < where) where = p[c].where;
+            if (!greedy && p[c].top > LLMA_NEG_INF)
+                sum += (double)p[c].sum * (p[c].top == top ? 1.0 : exp(((double)p[c].top - (double)top) * inv_t));
+        }
+    }
+    double left = 0.0, right = 0.0;                              // u q sum < e
+    bool ok = false, near = false;
+    float q = 1.f, u = 0.f;
+    if (lane < n_draft) {
+        draft = a.drafts[(int64_t)b * a.draft_stride + lane];
+        if ((unsigned)draft < (unsigned)a.vocab && top > LLMA_NEG_INF) {
+            if (greedy) {
+                ok = draft == where;
+            } else {
+                u = a.u_accept[(int64_t)b * a.k + lane];
+                if (a.probs) q = a.probs[((int64_t)b * a.k + lane) * a.vocab + draft];
+                right = weight64(logit_at<TYPE>(a, row, draft), top, inv_t);
+                left = (double)u * (double)q * sum;
+                ok = left < right;
+                near = right > 0.0 && fabs(left - right) <= 3e-5 * right;
+            }
+        }
+    }
+    unsigned long long yes = __ballot(ok), unsure = __ballot(near);
+    // (the first rejection ends it: only tests before it matter)
+    while (true) {
+        const unsigned long long no = ~yes;
+        const int stop = __builtin_ctzll(no);                    // lane n_draft <= 63 is never ok
+        const unsigned long long look = unsure & ((2ull << stop) - 1);
+        if (look == 0) break;
+        const int j = __builtin_ctzll(look);
+        unsure &= ~(1ull << j);
+        const float tj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), j));
+        const double s = row_sum64<TYPE>(a, (int64_t)b * (a.k + 1) + j, tj, inv_t, part);
+        const unsigned long long again = __ballot(lane == j && (double)u * (double)q * s < right);
+        yes = (yes & ~(1ull << j)) | again;
+    }
+    const int n = __builtin_ctzll(~yes);
+    Choice c;
+    c.accepted = n;
+    c.row = (int)((int64_t)b * (a.k + 1) + n);
+    c.residual = n < n_draft;
+    c.greedy = greedy;
+    c.top = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), n));
+    c.token = c.residual ? __builtin_amdgcn_readlane(draft, n) : -1;       // the rejected draft
+    if (greedy) c.token = __builtin_amdgcn_readlane(where, n);             // (0x7fffffff: nothing to choose)
+    c.sum = 0.0;
+    return c;
+}
+
+// the weights of a piece of the sampled row: e, or what is left of p once q is taken off
+template <int TYPE>
+__device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice &c, const RowView &v, int blocks, int blk, double inv_t, bool minus, const float *q, double w[sampled_epb<TYPE>]) {
+    constexpr int EPB = sampled_epb<TYPE>;
+    float x[EPB];
+    piece_values<TYPE>(v.base[blk < blocks ? blk : 0], x);
+#pragma unroll
+    for (int e = 0; e < EPB; ++e) {
+        const int id = blk * EPB - v.skip + e;
+        double y = 0.0;
+        if (blk < blocks && id >= 0 && id < a.vocab) {
+            y = weight64(logit_of(x[e]), c.top, inv_t);
+            if (minus) {
+                if (q) y = fmax(y / c.sum - (double)q[id], 0.0);
+                else if (id == c.token) y = 0.0;
+            }
+        }
+        w[e] = y;
+    }
+}
+
+// a workgroup per (piece range of the sampled row, sequence): sums of its weights.  PASS 0 decides and sums the exponentials (without draft probabilities:
+// the weights themselves); PASS 1, with draft probabilities, sums max(p - q, 0)
+template <int TYPE, int PASS>
+__global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, SampledPlan plan) {
+    constexpr int EPB = sampled_epb<TYPE>;
+    __shared__ double part[4];
+    const int b = blockIdx.x;
+    Choice *const choice = (Choice *)((char *)a.work + plan.at_choice) + b;
+    double *const sums = (double *)((char *)a.work + plan.at_sums) + (int64_t)b * 2 * plan.picks;
+    Choice c;
+    if constexpr (PASS == 0) {
+        c = decide<TYPE>(a, plan, b, part);
+        if (blockIdx.y == 0 && threadIdx.x == 0) *choice = c;
+    } else {
+        c = *choice;
+        if (!c.residual) return;
+        double s = 0.0;
+        for (int i = threadIdx.x; i < plan.picks; i += 256) s += sums[i];
+        c.sum = block_sum(s, part);
+        if (blockIdx.y == 0 && threadIdx.x == 0) choice->sum = c.sum;       // (the other fields are read by all, this one by the next kernel)
+    }
+    if (c.greedy) return;
+    const double inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
+    const RowView v = row_view<TYPE>(a, c.row);
+    const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
+    const bool minus = PASS == 1 || (a.probs == nullptr && c.residual);
+    const float *const q = PASS == 1 ? a.probs + ((int64_t)b * a.k + c.accepted) * a.vocab : nullptr;
+    double s = 0.0;
+#pragma unroll
+    for (int i = 0; i < PICK_BLOCKS / 256; ++i) {
+        double w[EPB];
+        piece_weights<TYPE>(a, c, v, blocks, blockIdx.y * PICK_BLOCKS + i * 256 + threadIdx.x, inv_t, minus, q, w);
+#pragma unroll
+        for (int e = 0; e < EPB; ++e) s += w[e];
+    }
+    s = block_sum(s, part);
+    if (threadIdx.x == 0) sums[PASS * plan.picks + blockIdx.y] = s;
+}
+
+// a workgroup per sequence: the range the random number falls into, then the token in it
+template <int TYPE>
+__global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, SampledPlan plan) {
+    constexpr int EPB = sampled_epb<TYPE>, PER = PICK_BLOCKS / 256;
+    __shared__ double part[4];
+    __shared__ double s_range_before;
+    __shared__ int s_range, s_token, s_last;
+    const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
+    Choice c = ((const Choice *)((const char *)a.work + plan.at_choice))[b];
+    const double *const base = (const double *)((const char *)a.work + plan.at_sums) + (int64_t)b * 2 * plan.picks;
+    int token = -1;
+    if (c.greedy) {
+        token = c.token == 0x7fffffff ? -1 : c.token;
+    } else {
+        const bool with_q = c.residual && a.probs != nullptr;
+        bool minus = c.residual;
+        const double *sums = with_q ? base + plan.picks : base;
+        double s = 0.0;
+        for (int i = t; i < plan.picks; i += 256) s += sums[i];
+        double total = block_sum(s, part);
+        if (c.residual && !(total > 0.0)) {                      // p nowhere above q: p itself
+            minus = false;
+            if (with_q) {
+                sums = base;
+                total = c.sum;
+            } else if (c.top > LLMA_NEG_INF) {
+                token = c.token;                                 // (the rejected token is the only one there is)
+            }
+        }
+        if (total > 0.0) {
+            const double target = (double)a.u_sample[b] * total;
+            if (t == 0) { s_range = 0x7fffffff; s_last = -1; s_token = 0x7fffffff; }
+            // the first range whose cumulative sum passes the target, else the last with a weight: 256 ranges at a time
+            double before = 0.0, mine_before = 0.0;
+            int mine = -1;                                       // the thread's first range that passes, else its last with a weight; what lies before it
+            bool passed = false;
+            for (int i0 = 0; i0 < plan.picks; i0 += 256) {
+                const double w = i0 + t < plan.picks ? sums[i0 + t] : 0.0, up_to = before + scan64(w, part, &s);
+                before += s;
+                if (w > 0.0 && !passed) { mine = i0 + t; mine_before = up_to - w; passed = up_to > target; }
+                if (w > 0.0 && up_to > target) atomicMin(&s_range, i0 + t);
+                if (w > 0.0) atomicMax(&s_last, i0 + t);
+            }
+            __syncthreads();
+            const int range = s_range != 0x7fffffff ? s_range : s_last;
+            if (mine == range) s_range_before = mine_before;
+            __syncthreads();
+            if (t == 0) s_last = -1;
+            __syncthreads();
+            const double inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
+            const RowView v = row_view<TYPE>(a, c.row);
+            const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
+            const float *const q = with_q && minus ? a.probs + ((int64_t)b * a.k + c.accepted) * a.vocab : nullptr;
+            // a thread's pieces are neighbours, so that cumulative sums run along the threads
+            double w[PER][EPB], own = 0.0;
+            const int blk0 = range * PICK_BLOCKS + t * PER;
+#pragma unroll
+            for (int i = 0; i < PER; ++i) {
+                piece_weights<TYPE>(a, c, v, blocks, blk0 + i, inv_t, minus, q, w[i]);
+#pragma unroll
+                for (int e = 0; e < EPB; ++e) own += w[i][e];
+            }
+            double run = s_range_before + scan64(own, part, &s) - own;
+            int found = 0x7fffffff, last = -1;
+#pragma unroll
+            for (int i = 0; i < PER; ++i)
+#pragma unroll
+                for (int e = 0; e < EPB; ++e) {
+                    const int id = (blk0 + i) * EPB - v.skip + e;
+                    run += w[i][e];
+                    if (w[i][e] > 0.0) {
+                        last = id;
+                        if (run > target && found == 0x7fffffff) found = id;
+                    }
+                }
+            atomicMin(&s_token, found);
+            atomicMax(&s_last, last);
+            __syncthreads();
+            token = s_token != 0x7fffffff ? s_token : s_last;
+        }
+    }
+    if (t <= a.k) {
+        int e = -1;
+        if (t < c.accepted) e = a.drafts[(int64_t)b * a.draft_stride + t];
+        else if (t == c.accepted) e = token;
+        a.emitted[(int64_t)b * a.emit_stride + t] = e;
+    }
+    if (t == 0) {
+        a.n_accepted[b] = c.accepted;
+        a.next[b] = token;
+    }
+}
+
+template <int TYPE>
+static void launch_sampled(const SampledArgs &a, hipStream_t st) {
+    const SampledPlan p = sampled_plan(a.n_seqs, a.k, a.vocab, sampled_epb<TYPE>);
+    const dim3 rows(a.n_seqs * (a.k + 1), p.chunks), picks(a.n_seqs, p.picks);
+    if (p.chunk_blocks == 2048) hipLaunchKernelGGL((sampled_rows_kernel<8, TYPE>), rows, dim3(ROW_THREADS), 0, st, a, p);
+    else hipLaunchKernelGGL((sampled_rows_kernel<2, TYPE>), rows, dim3(ROW_THREADS), 0, st, a, p);
+    hipLaunchKernelGGL((sampled_pick_kernel<TYPE, 0>), picks, dim3(256), 0, st, a, p);
+    if (a.probs) hipLaunchKernelGGL((sampled_pick_kernel<TYPE, 1>), picks, dim3(256), 0, st, a, p);
+    hipLaunchKernelGGL((sampled_finish_kernel<TYPE>), dim3(a.n_seqs), dim3(256), 0, st, a, p);
+}
+void launch_verify_sampled(const SampledArgs &a, hipStream_t st) {
+    if (a.type == ROWS_BF16) launch_sampled<ROWS_BF16>(a, st);
+    else if (a.type == ROWS_F16) launch_sampled<ROWS_F16>(a, st);
+    else launch_sampled<ROWS_F32>(a, st);
+}
