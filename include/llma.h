@@ -41,6 +41,13 @@ extern "C" {
 #define LLMA_DTYPE_BF16 1    /* bf16 weights and KV cache, bf16 MFMA with fp32 accumulation,
                                 fp32 residual stream / softmax / logits */
 
+#define LLMA_KV_PAGED 2      /* kv_split: K and V as e4m3 codes in pages of 64 positions with a scale per page and head, kept
+                                and read by the kernels of llma_map_pages, llma_append_paged and llma_attend_paged: a third of the
+                                bytes of kv_split = 1, half of one bf16 plane.  Values are rounded to four significant bits, so
+                                logits are those of another, rounded cache (not within the tolerance of the two planes), and a
+                                rejected draft may have raised its page's scale, which rounds values below e4m3's normal range
+                                again: the tokens of k > 0 and k = 0 agree except at near-ties. */
+
 typedef struct llma_ctx llma_ctx;           /* opaque; owns re-tiled weights, KV cache, scratch */
 
 typedef struct {
@@ -51,7 +58,8 @@ typedef struct {
     int32_t dtype;         /* LLMA_DTYPE_*                                                  */
     int32_t kv_split;      /* bf16 only: 1 = keep K and V as a bf16 hi plane plus an 8-bit lo plane
                               (the residual x - hi as fp8 e4m3 of 256 times it: 1.5 x the cache
-                              bytes, 12 significand bits), 0 = one bf16 plane.  Ignored for fp32 */
+                              bytes, 12 significand bits), 0 = one bf16 plane, LLMA_KV_PAGED = pages of 8-bit
+                              values (below).  Ignored for fp32 */
     float   rms_eps;       /* RMSNorm(x; g) = g * x / sqrt(mean(x^2) + rms_eps)              */
     float   rope_theta;    /* rotary base: feature i pairs with i + head_dim/2, angle
                               pos * rope_theta^(-2i/head_dim)                               */
@@ -116,7 +124,8 @@ int llma_set_pending(llma_ctx *ctx, int32_t seq, int32_t token);
  * the verify-step microbenchmark from a given cache without running a prefill.  With
  * kv_split the imported values fill the hi planes exactly and the lo planes with zeros;
  * when all layers of a slot have been imported with one len (and nothing was computed on
- * the slot in between), batched steps do not read the lo planes below that position. */
+ * the slot in between), batched steps do not read the lo planes below that position.  A paged cache rounds the
+ * imported values as llma_append_paged does (k and v 16-byte aligned). */
 int llma_kv_import(llma_ctx *ctx, int32_t seq, int32_t layer, const void *k, const void *v, int32_t len);
 
 /* --- the three calls of the method ---------------------------------------------------- */
@@ -177,6 +186,16 @@ int llma_verify_step(llma_ctx *ctx, int32_t seq, const int32_t *draft, int32_t k
 int llma_verify_step_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs,
                            const int32_t *drafts, int32_t k,
                            int32_t *n_accepted, int32_t *next_token, int32_t *emitted);
+
+/* The step with sampling in place of the arg max: the same forward, then llma_verify_sampled on its logits with the drafts as copied
+ * tokens (accepted with probability p(draft) / 1, else a token from p without it), so that emitted tokens are distributed as the model's
+ * own at that temperature.  temperature, u_sample: HOST float[n_seqs]; u_accept: HOST float[n_seqs*k]; u in [0, 1), temperature >= 0 (0: the
+ * greedy step's tokens), finite, else RANGE.  Everything else as above.  The first call allocates device memory for the logits (grown when a
+ * step has more rows; with a logits dump set they are written there). */
+int llma_verify_step_sampled(llma_ctx *ctx, int32_t seq, const int32_t *draft, int32_t k, float temperature, const float *u_accept, float u_sample,
+                             int32_t *n_accepted, int32_t *next_token, int32_t *emitted);
+int llma_verify_step_sampled_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs, const int32_t *drafts, int32_t k, const float *temperature,
+                                   const float *u_accept, const float *u_sample, int32_t *n_accepted, int32_t *next_token, int32_t *emitted);
 
 /* LLMA decoding (paper: Algorithm 1) of exactly max_new tokens for slot `seq`: reset,
  * prefill, then steps; each step runs the trigger on the device against the reference

@@ -26,10 +26,10 @@ EXPORTS = [
     "llma_verify_step_batch", "llma_generate", "llma_generate_batch", "llma_set_logits_dump", "llma_set_option",
     "llma_get_kernel_timing", "llma_time_ffn_gemm", "llma_time_step_gemm", "llma_device_bytes", "llma_find_trigger_static", "llma_truncate",
     "llma_describe", "llma_map_pages", "llma_append_paged", "llma_attend_paged", "llma_attend_paged_workspace",
-    "llma_verify_sampled", "llma_verify_sampled_workspace",
+    "llma_verify_sampled", "llma_verify_sampled_workspace", "llma_verify_step_sampled", "llma_verify_step_sampled_batch",
 ]
 LLMA_TRIGGER_STATIC_MAX_REF = 1 << 20
-LLMA_DTYPE_F16 = 2
+LLMA_DTYPE_F16, LLMA_KV_PAGED = 2, 2
 LLMA_PAGE, LLMA_PAGED_MAX_SEQS, LLMA_SAMPLED_MAX_K = 64, 4096, 63
 
 
@@ -87,6 +87,8 @@ def load_library() -> ctypes.CDLL:
     lib.llma_find_trigger_static.argtypes = [vp, c_int32, vp, c_int32, vp, c_int32, c_int32, vp, vp]
     lib.llma_verify_step.argtypes = [vp, c_int32, i32p, c_int32, i32p, i32p, i32p]
     lib.llma_verify_step_batch.argtypes = [vp, c_int32, i32p, i32p, c_int32, i32p, i32p, i32p]
+    lib.llma_verify_step_sampled.argtypes = [vp, c_int32, i32p, c_int32, c_float, POINTER(c_float), c_float, i32p, i32p, i32p]
+    lib.llma_verify_step_sampled_batch.argtypes = [vp, c_int32, i32p, i32p, c_int32, POINTER(c_float), POINTER(c_float), POINTER(c_float), i32p, i32p, i32p]
     lib.llma_generate.argtypes = [vp, c_int32, i32p, c_int32, i32p, i32p, c_int32, c_int32, c_int32, c_int32,
                                   i32p, i32p, POINTER(StepRec), i32p]
     lib.llma_generate_batch.argtypes = [vp, c_int32, i32p, i32p, i32p, i32p, i32p, i32p, c_int32, c_int32, c_int32,
@@ -336,10 +338,11 @@ def llma_verify_sampled_workspace(n_seqs: int, k: int, vocab: int) -> int:
 class Context:
     """Owns one llma_ctx.  `cfg` is any object with n_layers, d_model, n_heads, head_dim, d_ffn,
     vocab, dtype ("fp32" | "bf16"), rms_eps, rope_theta; `weights` the dict of numpy arrays
-    (bf16 as uint16 bit patterns) laid out as llma.h describes."""
+    (bf16 as uint16 bit patterns) laid out as llma.h describes.  kv_paged: the cache as 8-bit pages (bf16 models) in place of
+    the planes that kv_split names."""
 
     def __init__(self, cfg, weights: dict, max_seq: int, max_batch: int = 1, max_k: int = 16, device="cuda:0",
-                 kv_split: bool = True):
+                 kv_split: bool = True, kv_paged: bool = False):
         import torch
         self._torch = torch
         self.lib = load_library()
@@ -351,7 +354,7 @@ class Context:
         stream = torch.cuda.current_stream(self.device)
         L = len(weights["layers"])
         c = ModelCfgC(L, cfg.d_model, cfg.n_heads, cfg.head_dim, cfg.d_ffn, cfg.vocab, max_seq, max_batch, max_k,
-                      LLMA_DTYPE_BF16 if cfg.dtype == "bf16" else LLMA_DTYPE_F32, int(bool(kv_split)),
+                      LLMA_DTYPE_BF16 if cfg.dtype == "bf16" else LLMA_DTYPE_F32, LLMA_KV_PAGED if kv_paged else int(bool(kv_split)),
                       cfg.rms_eps, cfg.rope_theta)
 
         def dev(a):
@@ -427,6 +430,30 @@ class Context:
         na, nt = np.zeros(len(s), np.int32), np.zeros(len(s), np.int32)
         em = np.zeros(len(s) * (k + 1), np.int32)
         self._ck(self.lib.llma_verify_step_batch(self._h, len(s), _ptr(s), _ptr(d), k, _ptr(na), _ptr(nt), _ptr(em)))
+        em = em.reshape(len(s), k + 1)
+        return na, nt, [em[b, :na[b] + 1].tolist() for b in range(len(s))]
+
+    def verify_step_sampled(self, draft, temperature: float, u_accept, u_sample: float, seq: int = 0):
+        """The step with sampling: u_accept [k] and u_sample in [0, 1).  Returns (n_accepted, next_token, emitted list)."""
+        na, nt, em = self.verify_step_sampled_batch([seq], [list(draft)], [temperature], [list(u_accept)], [u_sample])
+        return int(na[0]), int(nt[0]), em[0]
+
+    def verify_step_sampled_batch(self, seqs, drafts, temperature, u_accept, u_sample):
+        """drafts, u_accept: [n_seqs, k]; temperature, u_sample: [n_seqs].  Returns (n_accepted[n_seqs], next_token[n_seqs], emitted[n_seqs][...])."""
+        def f32(a, n, name):
+            a = np.ascontiguousarray(np.asarray(a, dtype=np.float32).reshape(-1))
+            if len(a) != n:
+                _refuse(f"verify_step_sampled: {name} has {len(a)} entries, wanted {n}")
+            return a
+        s = _i32(seqs)
+        d = np.asarray(drafts, dtype=np.int32).reshape(len(s), -1)
+        k = d.shape[1]
+        d = _i32(d)
+        t, ua, us = f32(temperature, len(s), "temperature"), f32(u_accept, len(s) * k, "u_accept"), f32(u_sample, len(s), "u_sample")
+        na, nt = np.zeros(len(s), np.int32), np.zeros(len(s), np.int32)
+        em = np.zeros(len(s) * (k + 1), np.int32)
+        fp = lambda a: a.ctypes.data_as(POINTER(c_float))
+        self._ck(self.lib.llma_verify_step_sampled_batch(self._h, len(s), _ptr(s), _ptr(d), k, fp(t), fp(ua), fp(us), _ptr(na), _ptr(nt), _ptr(em)))
         em = em.reshape(len(s), k + 1)
         return na, nt, [em[b, :na[b] + 1].tolist() for b in range(len(s))]
 

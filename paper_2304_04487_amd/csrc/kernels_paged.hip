@@ -189,6 +189,16 @@ void launch_map_pages(const MapArgs &a, hipStream_t st) {
     if (a.max_rows > MAP_ROWS_HERE) hipLaunchKernelGGL(map_rows_kernel, dim3((a.max_rows + 1023) / 1024), dim3(256), 0, st, a);
 }
 
+__global__ __launch_bounds__(256) void pass_rows_kernel(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots) {
+    for (int b = threadIdx.x; b < n_seqs; b += 256) {
+        rows[b] = segs ? segs[b].rows : m;
+        slots[b] = segs ? segs[b].slot : batch_slots[b];
+    }
+}
+void launch_pass_rows(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots, hipStream_t st) {
+    hipLaunchKernelGGL(pass_rows_kernel, dim3(1), dim3(256), 0, st, segs, batch_slots, n_seqs, m, rows, slots);
+}
+
 // ---------------------------------------------------------------------------------------------
 // rows of a call: eight neighbouring features as fp32
 // ---------------------------------------------------------------------------------------------

@@ -418,3 +418,27 @@ void launch_verify_sampled(const SampledArgs &a, hipStream_t st) {
     else if (a.type == ROWS_F16) launch_sampled<ROWS_F16>(a, st);
     else launch_sampled<ROWS_F32>(a, st);
 }
+
+// ---------------------------------------------------------------------------------------------
+// a context's sampled step
+// ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void take_words_kernel(const int *pinned, int *dev, int words) {
+    for (int i = threadIdx.x; i < words; i += 256) dev[i] = pinned[i];
+}
+void launch_take_words(const int *pinned, int *dev, int words, hipStream_t st) { hipLaunchKernelGGL(take_words_kernel, dim3(1), dim3(256), 0, st, pinned, dev, words); }
+
+// The accepted rows stay in the cache (T += a + 1), the new token becomes the pending one.  A row without a token leaves its sequence as it was: the
+// host sees the -1 and reports it.
+__global__ __launch_bounds__(256) void commit_sampled_kernel(CommitArgs c) {
+    for (int b = threadIdx.x; b < c.n_seqs; b += 256) {
+        const int n = c.n_accepted[b], next = c.next[b], slot = c.batch_slots[b];
+        for (int j = 0; j <= n; ++j)
+            __hip_atomic_store(c.io_emit + (size_t)b * c.io_stride + j, c.emitted[(size_t)b * c.emit_stride + j], __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        __hip_atomic_store(c.io_nacc + b, n, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        __hip_atomic_store(c.io_next + b, next, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_SYSTEM);
+        if (next < 0) continue;
+        c.T[slot] += n + 1;
+        c.pending[slot] = next;
+    }
+}
+void launch_commit_sampled(const CommitArgs &c, hipStream_t st) { hipLaunchKernelGGL(commit_sampled_kernel, dim3(1), dim3(256), 0, st, c); }

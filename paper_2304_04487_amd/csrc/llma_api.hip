@@ -18,6 +18,7 @@
 #include "../../include/llma.h"
 #include "common.h"
 #include "kernels.h"
+#include "paged.h"
 
 static thread_local std::string g_err;      // errors of calls that have no context
 void llma_set_error_text(const char *text) { g_err = text ? text : ""; }   // for the library's other source files
@@ -27,7 +28,7 @@ void llma_set_error_text(const char *text) { g_err = text ? text : ""; }   // fo
 
 struct EventPair { hipEvent_t a, b; };
 
-enum StepKind { STEP_PREFILL = 0, STEP_VERIFY = 1, STEP_GEN = 2, STEP_PROMPTS = 3 /* a prompt pass over several sequences */ };
+enum StepKind { STEP_PREFILL = 0, STEP_VERIFY = 1, STEP_GEN = 2, STEP_PROMPTS = 3 /* a prompt pass over several sequences */, STEP_SAMPLED = 4 };
 
 // what a captured step graph was recorded for: (kind, sequences, rows per sequence, attention chunks, slot, trigger spans)
 typedef std::array<int, 6> GraphKey;
@@ -62,6 +63,15 @@ struct llma_ctx {
     std::vector<void *> kc, vc, kc_lo, vc_lo;
     float *cs_table = nullptr;
     bool kv_split = false;
+    // kv_split = 2: the cache in pages of 8-bit values instead, enough of them for every slot at its full length.  The QKV GEMM leaves a pass's
+    // K and V in fresh_k / fresh_v (the cache layout above, one slot, position = row of the pass), from where they go into the pages.
+    bool paged = false;
+    int blocks = 0;                    // pages of a slot at its full length
+    std::vector<PagedCache> pages;     // per layer; all layers share the lists
+    int *pg_table = nullptr, *pg_owned = nullptr, *pg_free = nullptr, *pg_n_free = nullptr, *pg_rows = nullptr, *pg_slots = nullptr, *pg_offsets = nullptr;
+    int *pg_after = nullptr, *pg_slot_map = nullptr, *pg_row_pos = nullptr, *pg_status = nullptr, *pg_iota = nullptr, *pg_zeros = nullptr;
+    void *fresh_k = nullptr, *fresh_v = nullptr, *attend_work = nullptr;
+    int fresh_cap = 0, pg_seqs = 0, pg_max_rows = 0;     // the last two: the pass being enqueued
 
     // scratch for up to Rmax rows.  bf16: x/q/att/act are tiled hi/lo planes; fp32: row-major in *_hi
     int Rmax = 0;
@@ -109,6 +119,11 @@ struct llma_ctx {
     int dump_rows = 0;
     int opt_split = 1, opt_timing = 0, opt_graph = 1;
     std::vector<EventPair> events;
+    // sampled steps (allocated by the first): logits where there is no dump, [temperature | u_sample | u_accept] and results on the device, the workspace,
+    // and pinned memory that the inputs come from
+    int *sample_logits = nullptr, *sample_dev = nullptr, *sample_work = nullptr, *pin_sample = nullptr, *pin_sample_dev = nullptr;
+    size_t cap_sample_logits = 0, cap_sample_work = 0;
+    float *logits_out = nullptr;       // where the LM head of the pass being enqueued writes logits, or null
 };
 
 static int fail(llma_ctx *c, int code, const char *fmt, ...) {
@@ -172,6 +187,12 @@ static int check_cfg(const llma_model_cfg *g) {
     } else {
         return fail(nullptr, LLMA_E_INVAL, "unknown dtype %d", g->dtype);
     }
+    if (g->dtype == LLMA_DTYPE_BF16 && g->kv_split == LLMA_KV_PAGED) {
+        const int64_t blocks = ((int64_t)g->max_seq + PAGE_POS - 1) / PAGE_POS;
+        if (g->max_batch > LLMA_PAGED_MAX_SEQS || g->n_heads > 1024 || blocks * g->max_batch > 0x7fffffff / PAGE_POS)
+            return fail(nullptr, LLMA_E_INVAL, "a paged cache needs max_batch <= %d, n_heads <= 1024 and max_batch * max_seq < 2^31", LLMA_PAGED_MAX_SEQS);
+        if (!launch_map_pages || !launch_append_paged || !launch_attend_paged) return fail(nullptr, LLMA_E_INVAL, "built without the paged cache");
+    }
     if (!(g->rms_eps >= 0.f) || !(g->rope_theta > 0.f)) return fail(nullptr, LLMA_E_INVAL, "bad rms_eps / rope_theta");
     return LLMA_OK;
 }
@@ -186,6 +207,42 @@ static int take_matrix(llma_ctx *c, void **dst, const void *src, int N, int K, i
         ALLOC(c, *dst, bytes);
         HIP_TRY(c, hipMemcpyAsync(*dst, src, bytes, hipMemcpyDeviceToDevice, c->st));
     }
+    return LLMA_OK;
+}
+
+// the paged cache of a context: pages for every slot at its full length, all of them free, and what a pass needs beside them
+static int create_pages(llma_ctx *c, size_t Rp) {
+    const llma_model_cfg &g = c->cfg;
+    const int H = g.n_heads, dh = g.head_dim, n_pages = c->blocks * g.max_batch;
+    for (int l = 0; l < g.n_layers; ++l) {
+        PagedCache p{nullptr, nullptr, nullptr, nullptr, n_pages, H, dh};
+        ALLOC(c, p.k, (size_t)n_pages * H * PAGE_POS * dh);
+        ALLOC(c, p.v, (size_t)n_pages * H * PAGE_POS * dh);
+        ALLOC(c, p.k_scale, (size_t)n_pages * H * 4);
+        ALLOC(c, p.v_scale, (size_t)n_pages * H * 4);
+        c->pages.push_back(p);
+    }
+    const size_t B = g.max_batch, rows = Rp > (size_t)g.max_seq ? Rp : (size_t)g.max_seq;
+    std::vector<int> table(B * c->blocks, -1), free_pages(n_pages), iota(rows);
+    for (int i = 0; i < n_pages; ++i) free_pages[i] = n_pages - 1 - i;
+    for (size_t i = 0; i < rows; ++i) iota[i] = (int)i;
+    const std::vector<int> zeros(rows > B ? rows : B, 0);
+    struct { int **p; size_t words; const int *from; } lists[] = {
+        {&c->pg_table, table.size(), table.data()}, {&c->pg_free, free_pages.size(), free_pages.data()}, {&c->pg_n_free, 1, &n_pages}, {&c->pg_owned, B, zeros.data()},
+        {&c->pg_rows, B, nullptr}, {&c->pg_slots, B, nullptr}, {&c->pg_offsets, B + 1, nullptr}, {&c->pg_after, B, nullptr}, {&c->pg_slot_map, rows, nullptr},
+        {&c->pg_row_pos, rows, nullptr}, {&c->pg_status, 1, nullptr}, {&c->pg_iota, rows, iota.data()}, {&c->pg_zeros, zeros.size(), zeros.data()}};
+    for (auto &l : lists) {
+        ALLOC(c, *l.p, l.words * 4);
+        if (l.from) HIP_TRY(c, hipMemcpy(*l.p, l.from, l.words * 4, hipMemcpyHostToDevice));
+    }
+    c->fresh_cap = ((int)Rp + ATTN_CHUNK - 1) / ATTN_CHUNK * ATTN_CHUNK;
+    ALLOC(c, c->fresh_k, (size_t)H * c->fresh_cap * dh * 2);
+    ALLOC(c, c->fresh_v, (size_t)H * c->fresh_cap * dh * 2);
+    // the attention's parts: passes of every length a step or prompt can have (more sequences never need less)
+    int64_t work = 0;
+    const int longest = c->Pmax > g.max_k + 1 ? c->Pmax : g.max_k + 1;
+    for (int m = 1; m <= longest; ++m) work = std::max(work, attend_paged_bytes(g.max_batch, c->blocks, H, H, dh, m));
+    ALLOC(c, c->attend_work, (size_t)work);
     return LLMA_OK;
 }
 
@@ -231,7 +288,8 @@ static int create_impl(llma_ctx *c, const llma_weights *w) {
     // ---- KV cache, zero-filled so that never-written positions hold finite values
     c->seq_cap = (g.max_seq + ATTN_CHUNK - 1) / ATTN_CHUNK * ATTN_CHUNK;
     const size_t kv_bytes = (size_t)g.max_batch * H * c->seq_cap * dh * es;
-    for (int l = 0; l < L; ++l) {
+    c->blocks = (g.max_seq + PAGE_POS - 1) / PAGE_POS;
+    for (int l = 0; l < L && !c->paged; ++l) {
         ALLOC(c, c->kc[l], kv_bytes);
         ALLOC(c, c->vc[l], kv_bytes);
         HIP_TRY(c, hipMemsetAsync(c->kc[l], 0, kv_bytes, c->st));
@@ -301,9 +359,13 @@ static int create_impl(llma_ctx *c, const llma_weights *w) {
             for (const GemmPlan *pl : {&c->plan_qkv, &c->plan_lm}) part = std::max(part, panel_part_bytes(*pl, few, tilek_groups(*pl)));
         }
         if (part > 0) ALLOC(c, c->part, part);
-        ALLOC(c, c->po, np * dh * 4);
-        ALLOC(c, c->pm, np * 4);
-        ALLOC(c, c->pl, np * 4);
+        if (c->paged) {
+            if ((rc = create_pages(c, Rp))) return rc;
+        } else {
+            ALLOC(c, c->po, np * dh * 4);
+            ALLOC(c, c->pm, np * 4);
+            ALLOC(c, c->pl, np * 4);
+        }
     } else {
         if ((rc = zalloc(&c->q, Rp * d * 4)) || (rc = zalloc(&c->att_hi, Rp * d * 4)) || (rc = zalloc(&c->act_hi, Rp * F * 4)))
             return rc;
@@ -376,6 +438,13 @@ static int create_impl(llma_ctx *c, const llma_weights *w) {
 // decoding-step GEMM arguments outside a forward (tuning, timing): matrix `which` of layer `layer`
 // (0 QKV, 1 O, 2 gate/up, 3 down, 4 LM head) over `rows` rows of whatever the scratch planes hold
 // ------------------------------------------------------------------------------------------------
+static void take_kv_target(llma_ctx *c, GemmArgs &ga, int layer) {       // where the QKV epilogue puts K and V
+    if (c->paged) {
+        ga.row_pos = c->pg_iota; ga.row_slot = c->pg_zeros; ga.max_seq = c->fresh_cap; ga.k_hi = c->fresh_k; ga.v_hi = c->fresh_v;
+    } else {
+        ga.k_hi = c->kc[layer]; ga.k_lo = c->kc_lo[layer]; ga.v_hi = c->vc[layer]; ga.v_lo = c->vc_lo[layer];
+    }
+}
 static GemmArgs step_gemm_args(llma_ctx *c, int which, int layer, int rows) {
     const llma_model_cfg &g = c->cfg;
     GemmArgs ga{};
@@ -385,7 +454,7 @@ static GemmArgs step_gemm_args(llma_ctx *c, int which, int layer, int rows) {
         case 0:
             ga.W = c->wqkv[layer]; ga.plan = c->plan_qkv; ga.Xhi = c->xhi; ga.Xlo = c->xlo; ga.epi = EPI_QKV; ga.ssq_in = c->ssq;
             ga.row_pos = c->s.row_pos; ga.row_slot = c->s.row_slot; ga.row_cs = c->s.row_cs; ga.q_hi = c->q; ga.q_lo = c->q_lo;
-            ga.k_hi = c->kc[layer]; ga.k_lo = c->kc_lo[layer]; ga.v_hi = c->vc[layer]; ga.v_lo = c->vc_lo[layer];
+            take_kv_target(c, ga, layer);
             break;
         case 1:
             ga.W = c->wo[layer]; ga.plan = c->plan_o; ga.Xhi = c->att_hi; ga.Xlo = c->att_lo; ga.epi = EPI_RESID; ga.out = c->h;
@@ -502,7 +571,8 @@ extern "C" int llma_create(const llma_model_cfg *cfg, const llma_weights *w, voi
     c->st = (hipStream_t)hip_stream;
     c->run_st = c->st;
     c->bf16 = cfg->dtype == LLMA_DTYPE_BF16;
-    c->kv_split = c->bf16 && cfg->kv_split != 0;
+    c->paged = c->bf16 && cfg->kv_split == LLMA_KV_PAGED;
+    c->kv_split = c->bf16 && cfg->kv_split != 0 && !c->paged;
     rc = create_impl(c, w);
     if (rc) {
         std::string e = c->err;
@@ -520,6 +590,7 @@ extern "C" int llma_destroy(llma_ctx *c) {
     for (auto &g : c->graphs) if (g.second.exec) (void)hipGraphExecDestroy(g.second.exec);
     if (c->cap_st) (void)hipStreamDestroy(c->cap_st);
     if (c->pin) (void)hipHostFree(c->pin);
+    if (c->pin_sample) (void)hipHostFree(c->pin_sample);
     for (int i = 0; i < 2; ++i) if (c->cnt_ev[i]) (void)hipEventDestroy(c->cnt_ev[i]);
     for (auto &e : c->events) { (void)hipEventDestroy(e.a); (void)hipEventDestroy(e.b); }
     for (void *p : c->allocs) (void)hipFree(p);
@@ -570,11 +641,35 @@ static int forward_f32(llma_ctx *c, int n_seqs, int m, bool lm_head) {
     }
     if (lm_head) {
         ga.W = c->lm_head; ga.Xhi = c->h; ga.N = V; ga.K = d; ga.epi = EPI_LMHEAD; ga.gain = c->final_norm;
-        ga.out = c->logits_dump; ga.pval = c->pval; ga.pidx = c->pidx; ga.n_part = c->n_part;
+        ga.out = c->logits_out; ga.pval = c->pval; ga.pidx = c->pidx; ga.n_part = c->n_part;
         launch_gemm_f32(ga, st);
     }
     HIP_TRY(c, hipGetLastError());
     return LLMA_OK;
+}
+
+// paged cache: the pass's pages and slots (once per pass), and a layer's fresh rows into its pages and the attention over them
+static void map_pass(llma_ctx *c, const PromptSeg *segs, int n_seqs, int m, int total_rows) {
+    c->pg_seqs = n_seqs;
+    c->pg_max_rows = m;
+    launch_pass_rows(segs, c->s.batch_slots, n_seqs, m, c->pg_rows, c->pg_slots, c->run_st);
+    MapArgs a{};
+    a.lens = c->s.T; a.rows = c->pg_rows; a.slots = c->pg_slots; a.n_seqs = n_seqs; a.n_slots = c->cfg.max_batch;
+    a.table = c->pg_table; a.max_blocks = c->blocks; a.owned = c->pg_owned; a.free_pages = c->pg_free; a.n_free = c->pg_n_free; a.n_pages = c->blocks * c->cfg.max_batch;
+    a.row_offsets = c->pg_offsets; a.lens_after = c->pg_after; a.slot_map = c->pg_slot_map; a.row_pos = c->pg_row_pos; a.max_rows = total_rows; a.status = c->pg_status;
+    launch_map_pages(a, c->run_st);
+}
+static void attend_pages(llma_ctx *c, int layer, int rows, const AttnArgs &aa) {
+    const llma_model_cfg &g = c->cfg;
+    const int64_t head = (int64_t)c->fresh_cap * g.head_dim;
+    launch_append_paged(AppendArgs{c->pages[layer], c->fresh_k, c->fresh_v, 0, head, 0, head, c->pg_slot_map, rows, ROWS_TILED}, c->run_st);
+    AttendArgs a{};
+    a.c = c->pages[layer];
+    a.q = aa.Qhi; a.q_lo = aa.Qlo; a.out = aa.out_hi; a.out_lo = aa.out_lo; a.type = ROWS_TILED; a.n_heads = g.n_heads;
+    a.tile_ksp = g.d_model / 32; a.tile_out_ksp = aa.out_KSp; a.quads = aa.quads;
+    a.table = c->pg_table; a.slots = c->pg_slots; a.lens = c->pg_after; a.row_offsets = c->pg_offsets;
+    a.n_seqs = c->pg_seqs; a.n_slots = g.max_batch; a.max_blocks = c->blocks; a.n_rows = rows; a.max_rows = c->pg_max_rows; a.scale = aa.scale; a.work = c->attend_work;
+    launch_attend_paged(a, c->run_st);
 }
 
 // bf16: per layer  QKV GEMM (+RMSNorm scale, RoPE, KV append) -> attention -> O GEMM (+residual,
@@ -622,11 +717,15 @@ static int forward_bf16(llma_ctx *c, int n_seqs, int m, int n_chunks, bool lm_he
         GemmArgs ga = base;
         ga.W = c->wqkv[l]; ga.plan = c->plan_qkv; ga.Xhi = c->xhi; ga.Xlo = c->xlo; ga.epi = EPI_QKV; ga.ssq_in = c->ssq;
         ga.row_pos = c->s.row_pos; ga.row_slot = c->s.row_slot; ga.row_cs = c->s.row_cs; ga.q_hi = c->q; ga.q_lo = c->q_lo;
-        ga.k_hi = c->kc[l]; ga.k_lo = c->kc_lo[l]; ga.v_hi = c->vc[l]; ga.v_lo = c->vc_lo[l];
+        take_kv_target(c, ga, l);
         if (panel) { panel_norm_gemm(ga); }
         else { ga.rstd_out = c->rstd; tilek_gemm(ga); }
-        aa.Khi = c->kc[l]; aa.Klo = c->kc_lo[l]; aa.Vhi = c->vc[l]; aa.Vlo = c->vc_lo[l];
-        launch_attn_bf16(aa, st);
+        if (c->paged) {
+            attend_pages(c, l, R, aa);
+        } else {
+            aa.Khi = c->kc[l]; aa.Klo = c->kc_lo[l]; aa.Vhi = c->vc[l]; aa.Vlo = c->vc_lo[l];
+            launch_attn_bf16(aa, st);
+        }
         ga = base;
         ga.W = c->wo[l]; ga.plan = c->plan_o; ga.Xhi = c->att_hi; ga.Xlo = c->att_lo; ga.epi = EPI_RESID; ga.out = c->h;
         ga.gain = c->n2[l]; ga.nx_hi = c->xhi; ga.nx_lo = c->xlo; ga.ssq_out = c->ssq;
@@ -655,7 +754,7 @@ static int forward_bf16(llma_ctx *c, int n_seqs, int m, int n_chunks, bool lm_he
     if (lm_head) {
         GemmArgs ga = base;
         ga.W = c->lm_head; ga.plan = c->plan_lm; ga.Xhi = c->xhi; ga.Xlo = c->xlo; ga.epi = EPI_LMHEAD; ga.ssq_in = c->ssq;
-        ga.out = c->logits_dump; ga.pval = c->pval; ga.pidx = c->pidx; ga.n_part = c->n_part;
+        ga.out = c->logits_out; ga.pval = c->pval; ga.pidx = c->pidx; ga.n_part = c->n_part;
         if (panel) { panel_norm_gemm(ga); }
         else { ga.rstd_out = c->rstd; tilek_gemm(ga); }
     }
@@ -666,6 +765,22 @@ static int forward_bf16(llma_ctx *c, int n_seqs, int m, int n_chunks, bool lm_he
 
 static int forward(llma_ctx *c, int n_seqs, int m, int n_chunks, bool lm_head, int slot) {
     return c->bf16 ? forward_bf16(c, n_seqs, m, n_chunks, lm_head, slot) : forward_f32(c, n_seqs, m, lm_head);
+}
+
+// device words of a sampled step: [temperature | u_sample | n_accepted | next][max_batch], [u_accept][max_batch * max_k], [emitted][max_batch * (max_k + 1)]; the inputs
+// ([temperature | u_sample][n_seqs], [u_accept][n_seqs * k]) come from pinned memory
+static void sample_step(llma_ctx *c, int n_seqs, int m) {
+    const size_t B = c->cfg.max_batch, mk = c->cfg.max_k;
+    const int k = m - 1;
+    int *const d = c->sample_dev, *const results = d + B * (2 + mk);
+    launch_take_words(c->pin_sample_dev, d, n_seqs * (2 + k), c->run_st);
+    SampledArgs a{};
+    a.logits = c->logits_out; a.row_stride = c->cfg.vocab; a.type = ROWS_F32; a.vocab = c->cfg.vocab; a.n_seqs = n_seqs; a.k = k;
+    a.drafts = c->s.draft; a.draft_stride = (int)mk; a.n_draft = c->s.keff;
+    a.temperature = (const float *)d; a.u_sample = a.temperature + n_seqs; a.u_accept = a.u_sample + n_seqs;
+    a.n_accepted = results; a.next = results + B; a.emitted = results + 2 * B; a.emit_stride = m; a.work = c->sample_work;
+    launch_verify_sampled(a, c->run_st);
+    launch_commit_sampled(CommitArgs{a.n_accepted, a.next, a.emitted, m, c->s.batch_slots, c->s.T, c->s.pending, c->s.io.nacc, c->s.io.next, c->s.io.emit, (int)mk + 1, n_seqs}, c->run_st);
 }
 
 // One step = row set-up + forward + bookkeeping, always the same launches for a given
@@ -679,9 +794,11 @@ static int step_body(llma_ctx *c, int kind, int n_seqs, int m, int n_chunks, int
     e.embed = c->embed; e.h = c->h; e.d = c->cfg.d_model;
     if (c->bf16) { e.gain = c->n1[0]; e.nx_hi = c->xhi; e.nx_lo = c->xlo; e.ssq_out = c->ssq; e.KSp = c->plan_qkv.KSp; e.quads = n_seqs * m > XTILE_ROWWISE; }
     c->rows_live = nullptr;
+    c->logits_out = c->logits_dump ? c->logits_dump : kind == STEP_SAMPLED ? (float *)c->sample_logits : nullptr;
     if (kind == STEP_PREFILL || kind == STEP_PROMPTS) {
         if (kind == STEP_PROMPTS) { c->n_segs = e.n_segs = n_seqs; e.segs = (const PromptSeg *)c->gen_segs; }
         launch_setup_prefill_rows(c->s, c->gen_prompt, c->gen_counters + 4 * c->cfg.max_batch, m, slot, c->cs_table, c->cfg.head_dim / 2, e, st);
+        if (c->paged) map_pass(c, kind == STEP_PROMPTS ? e.segs : nullptr, kind == STEP_PROMPTS ? n_seqs : 1, m, m);
         int rc = forward(c, 1, m, n_chunks, false, slot);
         c->n_segs = 0;
         if (rc || kind == STEP_PROMPTS) return rc;              // (whose lengths differ from pass to pass of the same shape)
@@ -694,8 +811,13 @@ static int step_body(llma_ctx *c, int kind, int n_seqs, int m, int n_chunks, int
     if (!gen) launch_take_step(c->s, n_seqs, mk, st);
     else if (c->gen_spans > 1) launch_trigger_scan(gen, n_seqs, c->gen_spans, part, st);
     launch_setup_step_rows(c->s, n_seqs, m, mk, c->cs_table, c->cfg.head_dim / 2, e, gen, part, c->gen_spans, st);
+    if (c->paged) map_pass(c, nullptr, n_seqs, m, n_seqs * m);
     int rc = forward(c, n_seqs, m, n_chunks, true, slot);
     if (rc) return rc;
+    if (kind == STEP_SAMPLED) {
+        sample_step(c, n_seqs, m);
+        return LLMA_OK;
+    }
     launch_argmax_accept(c->pval, c->pidx, c->n_part, c->s, n_seqs, m, mk, c->cfg.vocab, gen, st);
     return LLMA_OK;
 }
@@ -833,6 +955,23 @@ extern "C" int llma_kv_import(llma_ctx *c, int32_t seq, int32_t layer, const voi
     if (layer < 0 || layer >= c->cfg.n_layers) return fail(c, LLMA_E_RANGE, "llma_kv_import: layer %d", layer);
     if (len < 0 || len > c->cfg.max_seq) return fail(c, LLMA_E_RANGE, "llma_kv_import: len %d > max_seq %d", len, c->cfg.max_seq);
     const llma_model_cfg &g = c->cfg;
+    if (c->paged) {
+        if (len > 0) {
+            // the slot's pages for len positions (all layers have the same), then the rows into this layer's
+            HIP_TRY(c, hipMemcpyAsync(c->pg_rows, &len, 4, hipMemcpyHostToDevice, c->st));
+            HIP_TRY(c, hipMemcpyAsync(c->pg_slots, &seq, 4, hipMemcpyHostToDevice, c->st));
+            launch_map_pages(MapArgs{c->pg_zeros, c->pg_rows, c->pg_slots, 1, g.max_batch, c->pg_table, c->blocks, c->pg_owned, c->pg_free, c->pg_n_free, c->blocks * g.max_batch,
+                                     c->pg_offsets, c->pg_after, c->pg_slot_map, c->pg_row_pos, len, c->pg_status}, c->st);
+            const int64_t head = (int64_t)len * g.head_dim;
+            launch_append_paged(AppendArgs{c->pages[layer], k, v, g.head_dim, head, g.head_dim, head, c->pg_slot_map, len, ROWS_BF16}, c->st);
+            HIP_TRY(c, hipStreamSynchronize(c->st));        // (len and seq are this call's)
+        }
+        HIP_TRY(c, hipGetLastError());
+        c->imp_len[(size_t)seq * g.n_layers + layer] = len;
+        if (layer != g.n_layers - 1) return LLMA_OK;
+        c->T_host[seq] = len;
+        return push_state(c, seq);
+    }
     const size_t es = c->bf16 ? 2 : 4;
     const size_t slot_off = (size_t)seq * g.n_heads * c->seq_cap * g.head_dim * es;
     void *kc = (char *)c->kc[layer] + slot_off, *vc = (char *)c->vc[layer] + slot_off;
@@ -968,8 +1107,25 @@ static int drained(llma_ctx *c, int rc) {
     return rc;
 }
 
-extern "C" int llma_verify_step_batch(llma_ctx *c, int32_t n_seqs, const int32_t *seqs, const int32_t *drafts, int32_t k,
-                                      int32_t *n_accepted, int32_t *next_token, int32_t *emitted) {
+// random numbers of a sampled step (temperature null: a greedy one)
+struct SampleIn { const float *temperature, *u_accept, *u_sample; };
+
+// memory of sampled steps of up to `rows` rows
+static int ensure_sampling(llma_ctx *c, int n_seqs, int k) {
+    const size_t B = c->cfg.max_batch, mk = c->cfg.max_k;
+    if (!c->pin_sample) {
+        if (!c->sample_dev) ALLOC(c, c->sample_dev, B * (2 + mk + 2 + mk + 1) * 4);
+        HIP_TRY(c, hipHostMalloc((void **)&c->pin_sample, B * (2 + mk) * 4, hipHostMallocMapped | hipHostMallocCoherent));
+        HIP_TRY(c, hipHostGetDevicePointer((void **)&c->pin_sample_dev, c->pin_sample, 0));
+    }
+    int rc = LLMA_OK;
+    if (!c->logits_dump) rc = ensure_cap(c, &c->sample_logits, &c->cap_sample_logits, (size_t)n_seqs * (k + 1) * c->cfg.vocab);
+    if (!rc) rc = ensure_cap(c, &c->sample_work, &c->cap_sample_work, ((size_t)verify_sampled_bytes(n_seqs, k, c->cfg.vocab) + 3) / 4);
+    return rc;
+}
+
+static int verify_batch(llma_ctx *c, int32_t n_seqs, const int32_t *seqs, const int32_t *drafts, int32_t k, const SampleIn *sample,
+                        int32_t *n_accepted, int32_t *next_token, int32_t *emitted) {
     if (!c) return fail(nullptr, LLMA_E_INVAL, "llma_verify_step: null context");
     const llma_model_cfg &g = c->cfg;
     if (!seqs || n_seqs < 1 || n_seqs > g.max_batch) return fail(c, LLMA_E_INVAL, "llma_verify_step: bad slot list");
@@ -992,6 +1148,15 @@ extern "C" int llma_verify_step_batch(llma_ctx *c, int32_t n_seqs, const int32_t
     }
     if (c->logits_dump && n_seqs * (k + 1) > c->dump_rows)
         return fail(c, LLMA_E_RANGE, "llma_verify_step: logits dump holds %d rows, step has %d", c->dump_rows, n_seqs * (k + 1));
+    if (sample) {
+        if (!launch_verify_sampled) return fail(c, LLMA_E_INVAL, "llma_verify_step_sampled: built without sampling");
+        int rc = ensure_sampling(c, n_seqs, k);
+        if (rc) return rc;
+        float *const w = (float *)c->pin_sample;
+        std::copy(sample->temperature, sample->temperature + n_seqs, w);
+        std::copy(sample->u_sample, sample->u_sample + n_seqs, w + n_seqs);
+        if (k > 0) std::copy(sample->u_accept, sample->u_accept + (size_t)n_seqs * k, w + 2 * n_seqs);
+    }
     const int m = k + 1, mk = g.max_k;
     const HostIo &io = c->host;                // (nothing on the device reads or writes it now: every step is waited for, failed ones too)
     for (int b = 0; b < n_seqs; ++b) {
@@ -1004,7 +1169,7 @@ extern "C" int llma_verify_step_batch(llma_ctx *c, int32_t n_seqs, const int32_t
         io.nacc[b] = -1;                       // (checked below)
     }
     for (int b = 0; b < n_seqs; ++b) forget_imports(c, seqs[b]);
-    int rc = run_step(c, STEP_VERIFY, n_seqs, m, t_max, n_seqs == 1 ? seqs[0] : 0);
+    int rc = run_step(c, sample ? STEP_SAMPLED : STEP_VERIFY, n_seqs, m, t_max, n_seqs == 1 ? seqs[0] : 0);
     if (rc) return drained(c, rc);
     HIP_TRY(c, hipStreamSynchronize(c->st));
     HIP_TRY(c, hipGetLastError());
@@ -1024,6 +1189,29 @@ extern "C" int llma_verify_step_batch(llma_ctx *c, int32_t n_seqs, const int32_t
             for (int j = 0; j <= nacc[b]; ++j) emitted[(size_t)b * (k + 1) + j] = em[(size_t)b * (mk + 1) + j];
     }
     return LLMA_OK;
+}
+
+extern "C" int llma_verify_step_batch(llma_ctx *c, int32_t n_seqs, const int32_t *seqs, const int32_t *drafts, int32_t k,
+                                      int32_t *n_accepted, int32_t *next_token, int32_t *emitted) {
+    return verify_batch(c, n_seqs, seqs, drafts, k, nullptr, n_accepted, next_token, emitted);
+}
+
+extern "C" int llma_verify_step_sampled_batch(llma_ctx *c, int32_t n_seqs, const int32_t *seqs, const int32_t *drafts, int32_t k, const float *temperature,
+                                              const float *u_accept, const float *u_sample, int32_t *n_accepted, int32_t *next_token, int32_t *emitted) {
+    if (!c) return fail(nullptr, LLMA_E_INVAL, "llma_verify_step_sampled: null context");
+    if (!temperature || !u_sample || (k > 0 && !u_accept)) return fail(c, LLMA_E_INVAL, "llma_verify_step_sampled: null temperature or random numbers");
+    const SampleIn in{temperature, u_accept, u_sample};
+    for (int b = 0; b < n_seqs && n_seqs <= c->cfg.max_batch; ++b) {
+        bool ok = u_sample[b] >= 0.f && u_sample[b] < 1.f && temperature[b] >= 0.f && temperature[b] <= 3.402823466e38f;
+        for (int j = 0; j < k && k <= c->cfg.max_k; ++j) ok = ok && u_accept[(size_t)b * k + j] >= 0.f && u_accept[(size_t)b * k + j] < 1.f;
+        if (!ok) return fail(c, LLMA_E_RANGE, "llma_verify_step_sampled: random numbers outside [0,1) or a temperature that is negative or not finite for sequence %d", b);
+    }
+    return verify_batch(c, n_seqs, seqs, drafts, k, &in, n_accepted, next_token, emitted);
+}
+
+extern "C" int llma_verify_step_sampled(llma_ctx *c, int32_t seq, const int32_t *draft, int32_t k, float temperature, const float *u_accept, float u_sample,
+                                        int32_t *n_accepted, int32_t *next_token, int32_t *emitted) {
+    return llma_verify_step_sampled_batch(c, 1, &seq, draft, k, &temperature, u_accept, &u_sample, n_accepted, next_token, emitted);
 }
 
 extern "C" int llma_verify_step(llma_ctx *c, int32_t seq, const int32_t *draft, int32_t k, int32_t *n_accepted,

@@ -2,6 +2,10 @@
 #pragma once
 #include "common.h"
 
+// (weak: the host side is also linked against stand-ins of the launchers that a context cannot do without; one without these refuses
+// paged contexts and sampled steps)
+#define OPTIONAL __attribute__((weak))
+
 #define PAGE_POS 64              // positions of a page (LLMA_PAGE)
 
 // ---- the paged cache ---------------------------------------------------------------------------
@@ -31,7 +35,9 @@ struct MapArgs {
     int max_rows;
     int *status;
 };
-void launch_map_pages(const MapArgs &a, hipStream_t st);
+OPTIONAL void launch_map_pages(const MapArgs &a, hipStream_t st);
+// a context's pass as the calls above take it: rows[b] and slots[b] from its segments, or m rows of each of batch_slots
+OPTIONAL void launch_pass_rows(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots, hipStream_t st);
 
 struct AppendArgs {
     PagedCache c;
@@ -41,7 +47,7 @@ struct AppendArgs {
     int n_rows;
     int type;
 };
-void launch_append_paged(const AppendArgs &a, hipStream_t st);
+OPTIONAL void launch_append_paged(const AppendArgs &a, hipStream_t st);
 
 struct AttendArgs {
     PagedCache c;
@@ -55,8 +61,8 @@ struct AttendArgs {
     float scale;
     void *work;
 };
-int64_t attend_paged_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows);
-void launch_attend_paged(const AttendArgs &a, hipStream_t st);
+OPTIONAL int64_t attend_paged_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows);
+OPTIONAL void launch_attend_paged(const AttendArgs &a, hipStream_t st);
 
 struct SampledArgs {
     const void *logits;                  // [n_seqs * (k + 1)] rows of `vocab`, row_stride elements apart
@@ -72,5 +78,16 @@ struct SampledArgs {
     void *work;
 };
 #define SAMPLED_MAX_K 63                 // (a lane per row)
-int64_t verify_sampled_bytes(int n_seqs, int k, int vocab);
-void launch_verify_sampled(const SampledArgs &a, hipStream_t st);
+OPTIONAL int64_t verify_sampled_bytes(int n_seqs, int k, int vocab);
+OPTIONAL void launch_verify_sampled(const SampledArgs &a, hipStream_t st);
+// words of a sampled step's inputs from pinned host memory into the device's
+OPTIONAL void launch_take_words(const int *pinned, int *dev, int words, hipStream_t st);
+struct CommitArgs {                      // what a sampled step leaves in its context
+    const int *n_accepted, *next, *emitted;
+    int emit_stride;
+    const int *batch_slots;
+    int *T, *pending;                    // [max_batch]
+    int *io_nacc, *io_next, *io_emit;    // pinned, as the host reads them
+    int io_stride, n_seqs;
+};
+OPTIONAL void launch_commit_sampled(const CommitArgs &a, hipStream_t st);

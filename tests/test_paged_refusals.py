@@ -101,3 +101,9 @@ def test_the_binding_refuses_host_tensors_and_wrong_shapes():
         llma.llma_attend_paged(None, z, z, z, z, 1, 1.0, z)
     with pytest.raises(llma.LlmaError):
         llma.llma_verify_sampled(z, z, z, z, z, z, z)
+
+
+def test_sampled_steps_without_a_context(lib):
+    f = (ctypes.c_float * 2)(0.5, 0.5)
+    assert lib.llma_verify_step_sampled(None, 0, None, 0, 1.0, None, 0.5, None, None, None) == I
+    assert lib.llma_verify_step_sampled_batch(None, 1, None, None, 0, f, f, f, None, None, None) == I
