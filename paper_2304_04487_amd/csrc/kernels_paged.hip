@@ -394,7 +394,7 @@ void launch_append_paged(const AppendArgs &a, hipStream_t st) {
 // The pages of all sequences, end to end, are cut into equal shares, one per workgroup and key head: ragged lengths load the chip
 // evenly, and a share's four waves take its pages in turn and meet in LDS at a sequence's end.  A sequence that lies in one share
 // is finished there; the others' parts are joined by attend_join_kernel.
-#define ATTEND_SHARES 512        // workgroups wanted: two per compute unit
+#define ATTEND_CUS 256           // compute units; two workgroups each, one where four tiles fill the registers
 #define ATTEND_MIN_PAGES 4       // of a share: a page per wave
 
 struct AttendPlan { int nt, tiles, shares; };
@@ -404,7 +404,7 @@ static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_he
     p.nt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
     p.tiles = (int)((r + 16 * p.nt - 1) / (16 * p.nt));
     const int64_t pages = (int64_t)n_seqs * max_blocks, most = (pages + ATTEND_MIN_PAGES - 1) / ATTEND_MIN_PAGES;
-    int64_t shares = ATTEND_SHARES / ((int64_t)kv_heads * p.tiles);
+    int64_t shares = (p.nt < 4 ? 2 : 1) * ATTEND_CUS / ((int64_t)kv_heads * p.tiles);
     if (shares > most) shares = most;
     p.shares = shares < 1 ? 1 : (int)shares;
     return p;
@@ -527,7 +527,7 @@ template <int TYPE> constexpr int attend_nq = TYPE == ROWS_BF16 ? 1 : TYPE == RO
 template <int TYPE> constexpr int attend_np = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
 
 template <int DH, int NT, int TYPE>
-__global__ __launch_bounds__(256) void attend_paged_kernel(AttendArgs a, AttendPlan plan) {
+__global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(AttendArgs a, AttendPlan plan) {
     constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE>;
     constexpr int TD = DH / 64, DT = DH / 16, PIECES = NT * TD * 2 * 64;
     constexpr int JOIN = 2 * NT * DT * 64;                       // two waves' sums, in 16-byte pieces
@@ -600,18 +600,29 @@ __global__ __launch_bounds__(256) void attend_paged_kernel(AttendArgs a, AttendP
                 vs = a.c.v_scale[(size_t)id * a.c.heads + head];
             }
             const int n_here = (last - i0 + 3) / 4 < 64 ? (last - i0 + 3) / 4 : 64;
-            for (int it = 0; it < n_here; ++it) {
-                const int page = __builtin_amdgcn_readlane(id, it), base = (i0 + 4 * it) * PAGE_POS;
-                if (page < 0) continue;                          // no such page: its positions are not seen
-                const float pks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), it)), pvs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), it));
-                const size_t block = ((size_t)page * a.c.heads + head) * (PAGE_POS * DH);
-                u32x4 kc[4][TD], vc[DT];
+            // A page's bytes are requested a page ahead: K's as soon as this page's scores are out, V's as its products go by.  (A page that
+            // is none: page 0's bytes, and none of its positions is seen.)
+            u32x4 kc[4][TD], vc[DT];
+            const auto block_of = [&](int it) {
+                const int page = __builtin_amdgcn_readlane(id, it);
+                return ((size_t)(page < 0 ? 0 : page) * a.c.heads + head) * (PAGE_POS * DH);
+            };
+            const auto take_k = [&](size_t block) {
 #pragma unroll
                 for (int g = 0; g < 4; ++g)
 #pragma unroll
                     for (int t = 0; t < TD; ++t) kc[g][t] = *(const u32x4 *)(a.c.k + block + k_off + 4 * g * DH + 64 * t);
+            };
+            take_k(block_of(0));
 #pragma unroll
-                for (int d = 0; d < DT; ++d) vc[d] = *(const u32x4 *)(a.c.v + block + v_off + 16 * d * PAGE_POS);
+            for (int d = 0; d < DT; ++d) vc[d] = *(const u32x4 *)(a.c.v + block_of(0) + v_off + 16 * d * PAGE_POS);
+            for (int it = 0; it < n_here; ++it) {
+                const int page = __builtin_amdgcn_readlane(id, it), base = (i0 + 4 * it) * PAGE_POS;
+                const float pks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), it)), pvs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), it));
+                const size_t next = block_of(it + 1 < n_here ? it + 1 : it);       // (the last page's once more: no branch around the loads)
+                // (several tiles' queries come from LDS for every page: kept in registers across pages they would push the sums out)
+                int ql = lane;
+                if constexpr (NT > 1) asm volatile("" : "+v"(ql));
                 f32x4 sc[NT][4];
 #pragma unroll
                 for (int n = 0; n < NT; ++n)
@@ -627,15 +638,16 @@ __global__ __launch_bounds__(256) void attend_paged_kernel(AttendArgs a, AttendP
                         for (int n = 0; n < NT; ++n)
 #pragma unroll
                             for (int pl = NQ - 1; pl >= 0; --pl) {
-                                sc[n][g] = mfma16x16x32(lo, q[pl * PIECES + ((n * TD + t) * 2) * 64 + lane], sc[n][g]);
-                                sc[n][g] = mfma16x16x32(hi, q[pl * PIECES + ((n * TD + t) * 2 + 1) * 64 + lane], sc[n][g]);
+                                sc[n][g] = mfma16x16x32(lo, q[pl * PIECES + ((n * TD + t) * 2) * 64 + ql], sc[n][g]);
+                                sc[n][g] = mfma16x16x32(hi, q[pl * PIECES + ((n * TD + t) * 2 + 1) * 64 + ql], sc[n][g]);
                             }
                     }
+                take_k(next);
                 const float by = to_log2 * pks;
-                const bool masked = base + PAGE_POS - 1 > seen;
+                const bool masked = page < 0 || base + PAGE_POS - 1 > seen;
                 bool nans = false;
                 if (masked) {
-                    const int there = s.len - base - 16 * kb;    // of the lane's 16 positions of V
+                    const int there = page < 0 ? 0 : s.len - base - 16 * kb;       // of the lane's 16 positions of V
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
 #pragma unroll
@@ -656,7 +668,7 @@ __global__ __launch_bounds__(256) void attend_paged_kernel(AttendArgs a, AttendP
 #pragma unroll
                         for (int r = 0; r < 4; ++r) {
                             float v = sc[n][g][r] * by;
-                            if (masked && base + 16 * kb + 4 * g + r > limit[n]) v = LLMA_NEG_INF;
+                            if (masked && (page < 0 || base + 16 * kb + 4 * g + r > limit[n])) v = LLMA_NEG_INF;
                             x[4 * g + r] = v;
                             top = fmaxf(top, v);
                         }
@@ -714,6 +726,7 @@ __global__ __launch_bounds__(256) void attend_paged_kernel(AttendArgs a, AttendP
                 for (int d = 0; d < DT; ++d) {
                     u32x4 lo, hi;
                     widen16(vc[d], pvs, lo, hi);
+                    vc[d] = *(const u32x4 *)(a.c.v + next + v_off + 16 * d * PAGE_POS);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
