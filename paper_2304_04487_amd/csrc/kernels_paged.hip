@@ -394,17 +394,17 @@ void launch_append_paged(const AppendArgs &a, hipStream_t st) {
 // The pages of all sequences, end to end, are cut into equal shares, one per workgroup and key head: ragged lengths load the chip
 // evenly, and a share's four waves take its pages in turn and meet in LDS at a sequence's end.  A sequence that lies in one share
 // is finished there; the others' parts are joined by attend_join_kernel.
-#define ATTEND_CUS 256           // compute units; two workgroups each, one where four tiles fill the registers
+#define ATTEND_CUS 256           // compute units; two workgroups each, one where three or four tiles fill the registers
 #define ATTEND_MIN_PAGES 4       // of a share: a page per wave
 
 struct AttendPlan { int nt, tiles, shares; };
 static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows) {
     const int64_t r = (int64_t)max_rows * (n_heads / kv_heads);
     AttendPlan p;
-    p.nt = r <= 16 ? 1 : r <= 32 ? 2 : 4;
+    p.nt = r <= 64 ? (int)((r + 15) / 16) : 4;
     p.tiles = (int)((r + 16 * p.nt - 1) / (16 * p.nt));
     const int64_t pages = (int64_t)n_seqs * max_blocks, most = (pages + ATTEND_MIN_PAGES - 1) / ATTEND_MIN_PAGES;
-    int64_t shares = (p.nt < 4 ? 2 : 1) * ATTEND_CUS / ((int64_t)kv_heads * p.tiles);
+    int64_t shares = (p.nt <= 2 ? 2 : 1) * ATTEND_CUS / ((int64_t)kv_heads * p.tiles);
     if (shares > most) shares = most;
     p.shares = shares < 1 ? 1 : (int)shares;
     return p;
@@ -432,45 +432,75 @@ __device__ __forceinline__ AttendSeq attend_seq(const AttendArgs &a, int b) {
     if (s.len < 0 || (unsigned)s.slot >= (unsigned)a.n_slots) s.len = 0;
     return s;
 }
+// (of one sequence for the whole wave: values that came through vector loads or LDS, into scalar registers)
+__device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
+__device__ __forceinline__ AttendSeq uniform(AttendSeq s) { return AttendSeq{uniform(s.slot), uniform(s.len), uniform(s.rows), uniform(s.row0)}; }
 __device__ __forceinline__ int attend_pages(const AttendSeq &s) {      // a sequence without positions still has rows to write
     if (s.rows <= 0) return 0;
     return s.len < 1 ? 1 : (s.len + PAGE_POS - 1) / PAGE_POS;
 }
 
-// q: 16-byte operand pieces in LDS, [plane][tile][64-dim group][half][lane]
-template <int DH, int NT, int NQ, int TYPE>
-__device__ __forceinline__ void attend_take_q(const AttendArgs &a, const AttendSeq &s, int head, int group, int r0, u32x4 *q) {
-    constexpr int PIECES = NT * (DH / 64) * 2 * 64;
-    for (int i = threadIdx.x; i < PIECES; i += 256) {
-        const int lane = i & 63, half = i >> 6 & 1, t = (i >> 7) % (DH / 64), nt = (i >> 7) / (DH / 64);
+// q: 16-byte operand pieces in LDS, [plane][tile][64-dim group][half][lane].  A thread's pieces on their way there: eight values each
+template <int DH, int NT> constexpr int attend_pieces = NT * (DH / 64) * 2 * 64;
+template <int DH, int NT> struct AttendQ { u32x4 raw[(attend_pieces<DH, NT> + 255) / 256][2]; };
+template <int DH, int NT, int TYPE>
+__device__ __forceinline__ void attend_load_q(const AttendArgs &a, const AttendSeq &s, int head, int group, int r0, AttendQ<DH, NT> &q) {
+#pragma unroll
+    for (int u = 0; u < (attend_pieces<DH, NT> + 255) / 256; ++u) {
+        const int i = u * 256 + threadIdx.x, lane = i & 63, half = i >> 6 & 1, t = (i >> 7) % (DH / 64), nt = (i >> 7) / (DH / 64);
         const int r = r0 + nt * 16 + (lane & 15), d = 64 * t + 16 * (lane >> 4) + 8 * half;
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = 0.f;
-        u32x4 p[3] = {(u32x4){0, 0, 0, 0}, (u32x4){0, 0, 0, 0}, (u32x4){0, 0, 0, 0}};
-        if (r < s.rows * group) {
-            const int row = s.row0 + r / group, h = head * group + r % group;
-            if constexpr (TYPE == ROWS_TILED) {
-                const size_t at = xtile_off(row, h * DH + d, a.tile_ksp, a.quads);
-                p[0] = *(const u32x4 *)((const bf16_t *)a.q + at);
-                p[1] = *(const u32x4 *)((const bf16_t *)a.q_lo + at);
+        q.raw[u][0] = q.raw[u][1] = (u32x4){0, 0, 0, 0};
+        if (i >= attend_pieces<DH, NT> || r >= s.rows * group) continue;
+        const int row = s.row0 + r / group, h = head * group + r % group;
+        if constexpr (TYPE == ROWS_TILED) {
+            const size_t at = xtile_off(row, h * DH + d, a.tile_ksp, a.quads);
+            q.raw[u][0] = *(const u32x4 *)((const bf16_t *)a.q + at);
+            q.raw[u][1] = *(const u32x4 *)((const bf16_t *)a.q_lo + at);
+        } else {
+            const int64_t at = (int64_t)row * a.q_row + h * a.q_head + d;
+            if constexpr (TYPE == ROWS_F32) {
+                q.raw[u][0] = *(const u32x4 *)((const float *)a.q + at);
+                q.raw[u][1] = *(const u32x4 *)((const float *)a.q + at + 4);
             } else {
-                row8<TYPE>(a.q, (int64_t)row * a.q_row + h * a.q_head + d, v);
+                q.raw[u][0] = *(const u32x4 *)((const bf16_t *)a.q + at);
             }
         }
-        if constexpr (TYPE != ROWS_TILED) {
+    }
+}
+template <int DH, int NT, int NQ, int TYPE>
+__device__ __forceinline__ void attend_put_q(const AttendQ<DH, NT> &q, u32x4 *lds) {
+    constexpr int PIECES = attend_pieces<DH, NT>;
 #pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                float x = v[2 * w], y = v[2 * w + 1];
+    for (int u = 0; u < (PIECES + 255) / 256; ++u) {
+        const int i = u * 256 + threadIdx.x;
+        if (i >= PIECES) continue;
+        if constexpr (TYPE == ROWS_BF16) {
+            lds[i] = q.raw[u][0];
+        } else if constexpr (TYPE == ROWS_TILED) {
+            lds[i] = q.raw[u][0];
+            lds[PIECES + i] = q.raw[u][1];
+        } else {
+            float v[8];
+            if constexpr (TYPE == ROWS_F32) {
 #pragma unroll
-                for (int n = 0; n < NQ; ++n) {
-                    p[n][w] = bf16_pair(x, y);
-                    if (n + 1 < NQ) { x -= __uint_as_float(p[n][w] << 16); y -= __uint_as_float(p[n][w] & 0xffff0000u); }
+                for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(q.raw[u][e / 4][e % 4]);
+            } else {
+                const f16x8 h = __builtin_bit_cast(f16x8, q.raw[u][0]);
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
+            }
+#pragma unroll
+            for (int n = 0; n < NQ; ++n) {
+                u32x4 p;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    p[w] = bf16_pair(v[2 * w], v[2 * w + 1]);
+                    v[2 * w] -= __uint_as_float(p[w] << 16);
+                    v[2 * w + 1] -= __uint_as_float(p[w] & 0xffff0000u);
                 }
+                lds[n * PIECES + i] = p;
             }
         }
-#pragma unroll
-        for (int n = 0; n < NQ; ++n) q[n * PIECES + i] = p[n];
     }
 }
 // 16 codes as two operands of eight bf16, times a power of two
@@ -483,21 +513,10 @@ __device__ __forceinline__ void widen16(u32x4 c, float scale, u32x4 &lo, u32x4 &
         hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 + w], scale, true));
     }
 }
-// ones where one of 16 codes is NaN, as bf16 operands; *any: whether there is one.  The codes themselves become zero there
-__device__ __forceinline__ void take_nans(u32x4 &c, u32x4 &lo, u32x4 &hi, bool &any) {
-#pragma unroll
-    for (int w = 0; w < 4; ++w) {
-        uint32_t m = 0;
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-            if ((c[w] >> (8 * e) & 0x7f) == 0x7f) m |= 0xffu << (8 * e);
-        c[w] &= ~m;
-        any |= m != 0;
-        const uint32_t a = (m & 1 ? 0x3f80u : 0) | (m & 0x100 ? 0x3f800000u : 0), b = (m & 0x10000 ? 0x3f80u : 0) | (m & 0x1000000 ? 0x3f800000u : 0);
-        if (w < 2) { lo[2 * w] = a; lo[2 * w + 1] = b; }
-        else { hi[2 * w - 4] = a; hi[2 * w - 3] = b; }
-    }
-}
+// the NaN codes among four: 0x80 in their bytes
+__device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+// four such bytes as the ones of two words of bf16
+__device__ __forceinline__ u32x2 ones_of(uint32_t m) { return (u32x2){(m >> 7 & 1) * 0x3f80u | (m >> 15 & 1) * 0x3f800000u, (m >> 23 & 1) * 0x3f80u | (m >> 31) * 0x3f800000u}; }
 
 template <int TYPE>
 __device__ __forceinline__ void attend_store(const AttendArgs &a, int row, int h, int d, f32x4 v) {      // four neighbouring features
@@ -526,18 +545,23 @@ __device__ __forceinline__ void attend_store(const AttendArgs &a, int row, int h
 template <int TYPE> constexpr int attend_nq = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
 template <int TYPE> constexpr int attend_np = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
 
+// a share's part of one sequence: pages first .. last - 1 of it (none: last = 0)
+struct AttendSeg { AttendSeq s; int b, first, last, pages; };
+
+template <int DH, int NT, int TYPE> constexpr int attend_lds = 16 * (attend_nq<TYPE> * attend_pieces<DH, NT> > 4 * NT * (DH / 16) * 64 ? attend_nq<TYPE> * attend_pieces<DH, NT> : 4 * NT * (DH / 16) * 64);
+#define ATTEND_KEPT 256          // sequences whose lengths and rows the workgroup keeps in LDS
+
 template <int DH, int NT, int TYPE>
-__global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(AttendArgs a, AttendPlan plan) {
+__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(AttendArgs a, AttendPlan plan) {
     constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE>;
-    constexpr int TD = DH / 64, DT = DH / 16, PIECES = NT * TD * 2 * 64;
-    constexpr int JOIN = 2 * NT * DT * 64;                       // two waves' sums, in 16-byte pieces
+    constexpr int TD = DH / 64, DT = DH / 16, PIECES = attend_pieces<DH, NT>;
     extern __shared__ u32x4 lds[];
-    constexpr int BIG = NQ * PIECES > JOIN ? NQ * PIECES : JOIN;
     u32x4 *const q = lds;
-    f32x4 *const osum = (f32x4 *)lds;                            // (the queries' place, once they are used)
-    __shared__ float ml[2][2][NT * 16];
+    f32x4 *const osum = (f32x4 *)lds;                            // the four waves' sums, in the queries' place once they are used
+    __shared__ float ml[4][2][NT * 16];
     __shared__ int part[4];
-    int *const starts = (int *)(lds + BIG);                      // [n_seqs + 1]
+    __shared__ AttendSeq kept[ATTEND_KEPT];
+    int *const starts = (int *)((char *)lds + attend_lds<DH, NT, TYPE>);         // [n_seqs + 1]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int share = blockIdx.x % plan.shares, head = blockIdx.x / plan.shares % a.c.heads, tile = blockIdx.x / plan.shares / a.c.heads;
     const int group = a.n_heads / a.c.heads, r0 = tile * NT * 16;
@@ -545,15 +569,21 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
     int total = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += 256) {
         const int b = b0 + threadIdx.x;
-        int sum;
-        const int at = block_scan<4>(b < a.n_seqs ? attend_pages(attend_seq(a, b)) : 0, part, &sum);
+        int sum, pages = 0;
+        if (b < a.n_seqs) {
+            const AttendSeq s = attend_seq(a, b);
+            pages = attend_pages(s);
+            if (b < ATTEND_KEPT) kept[b] = s;
+        }
+        const int at = block_scan<4>(pages, part, &sum);
         if (b < a.n_seqs) starts[b] = total + at;
         total += sum;
     }
     if (threadIdx.x == 0) starts[a.n_seqs] = total;
     __syncthreads();
-    if (plan.shares > 1 && blockIdx.x == 0)        // (for attend_join_kernel)
+    if (plan.shares > 1 && blockIdx.x == 0)                      // (for attend_join_kernel)
         for (int b = threadIdx.x; b <= a.n_seqs; b += 256) ((int *)a.work)[b] = starts[b];
+    total = uniform(total);
     int per = (total + plan.shares - 1) / plan.shares;
     per = per < ATTEND_MIN_PAGES ? ATTEND_MIN_PAGES : per;
     const int64_t from = (int64_t)share * per;
@@ -561,16 +591,73 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
     const int p0 = (int)from, p1 = p0 + per < total ? p0 + per : total;
     const float to_log2 = a.scale * 1.44269504088896340736f;
     const int kb = lane >> 4, col = lane & 15;
-    const int k_off = (16 * (col >> 2) + (col & 3)) * DH + 16 * kb, v_off = col * PAGE_POS + 16 * kb;
+    const uint32_t k_off = (16 * (col >> 2) + (col & 3)) * DH + 16 * kb, v_off = col * PAGE_POS + 16 * kb;
 
-    for (int b = count_le(starts, a.n_seqs + 1, p0) - 1; b < a.n_seqs && starts[b] < p1; ++b) {
-        const int first = p0 > starts[b] ? p0 - starts[b] : 0, pages = starts[b + 1] - starts[b];
-        const int last = (p1 < starts[b + 1] ? p1 : starts[b + 1]) - starts[b];
-        const AttendSeq s = attend_seq(a, b);
-        if (first >= last || r0 >= s.rows * group) continue;     // (uniform)
+    // the share's part of sequence b, or of the next that has rows in this tile
+    const auto segment = [&](int b) {
+        AttendSeg g{};
+        for (; b < a.n_seqs; ++b) {
+            const int begin = uniform(starts[b]), end = uniform(starts[b + 1]);
+            if (begin >= p1) break;
+            const int first = p0 > begin ? p0 - begin : 0, last = (p1 < end ? p1 : end) - begin;
+            if (first >= last) continue;
+            const AttendSeq s = uniform(b < ATTEND_KEPT ? kept[b] : attend_seq(a, b));
+            if (r0 < s.rows * group) return AttendSeg{s, b, first, last, end - begin};
+        }
+        return g;
+    };
+    // 64 pages of this wave, every fourth from i0 on: their numbers (-1: none)
+    const auto page_ids = [&](const AttendSeg &g, int i0) {
+        const int i = i0 + 4 * lane;
+        int id = -1;
+        if (i < g.last && i < (g.s.len + PAGE_POS - 1) / PAGE_POS) id = a.table[(size_t)g.s.slot * a.max_blocks + i];
+        return (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
+    };
+    // A page's bytes are requested a page ahead: K's as soon as a page's scores are out, V's as its products go by, the first page's of the next
+    // sequence before the waves' sums of this one meet.  (A page that is none: page 0's bytes, and none of its positions is seen.)
+    u32x4 kc[4][TD], vc[DT];
+    const auto block_of = [&](int page) { return ((size_t)(page < 0 ? 0 : page) * a.c.heads + head) * (PAGE_POS * DH); };
+    const auto take_k = [&](size_t block) {
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+#pragma unroll
+            for (int t = 0; t < TD; ++t) kc[g][t] = *(const u32x4 *)((a.c.k + block + 4 * g * DH + 64 * t) + k_off);
+    };
+    const auto take_v = [&](size_t block, int d) { vc[d] = *(const u32x4 *)((a.c.v + block + 16 * d * PAGE_POS) + v_off); };
+    const auto take_page = [&](int page) {
+        take_k(block_of(page));
+#pragma unroll
+        for (int d = 0; d < DT; ++d) take_v(block_of(page), d);
+    };
+    float ks = 0.f, vs = 0.f;
+    const auto take_scales = [&](int id) {
+        ks = vs = 0.f;
+        if (id >= 0) {
+            ks = a.c.k_scale[(size_t)id * a.c.heads + head];
+            vs = a.c.v_scale[(size_t)id * a.c.heads + head];
+        }
+    };
+
+    AttendSeg seg = segment(uniform(count_le(starts, a.n_seqs + 1, p0) - 1));
+    AttendQ<DH, NT> qr;
+    int id = -1;
+    if (seg.last > 0) {
+        id = page_ids(seg, seg.first + wave);
+        attend_load_q<DH, NT, TYPE>(a, seg.s, head, group, r0, qr);
+        if (seg.first + wave < seg.last) take_page(__builtin_amdgcn_readlane(id, 0));
+        take_scales(id);
+    }
+    while (seg.last > 0) {
+        const AttendSeq s = seg.s;
         __syncthreads();
-        attend_take_q<DH, NT, NQ, TYPE>(a, s, head, group, r0, q);
+        attend_put_q<DH, NT, NQ, TYPE>(qr, q);
         __syncthreads();
+        const AttendSeg after = segment(seg.b + 1);
+        int id_after = -1;
+        if (after.last > 0) {
+            id_after = page_ids(after, after.first + wave);
+            attend_load_q<DH, NT, TYPE>(a, after.s, head, group, r0, qr);
+        }
         // the last position that every column sees, and each lane's columns' own
         const int seen = s.len - s.rows;
         int limit[NT];
@@ -588,38 +675,12 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[n][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        for (int i0 = first + wave; i0 < last; i0 += 256) {      // 64 pages of this wave: their numbers and scales
-            int id = -1;
-            float ks = 0.f, vs = 0.f;
-            if (i0 + 4 * lane < last && (i0 + 4 * lane) * PAGE_POS < s.len) {
-                id = a.table[(size_t)s.slot * a.max_blocks + i0 + 4 * lane];
-                if ((unsigned)id >= (unsigned)a.c.n_pages) id = -1;
-            }
-            if (id >= 0) {
-                ks = a.c.k_scale[(size_t)id * a.c.heads + head];
-                vs = a.c.v_scale[(size_t)id * a.c.heads + head];
-            }
-            const int n_here = (last - i0 + 3) / 4 < 64 ? (last - i0 + 3) / 4 : 64;
-            // A page's bytes are requested a page ahead: K's as soon as this page's scores are out, V's as its products go by.  (A page that
-            // is none: page 0's bytes, and none of its positions is seen.)
-            u32x4 kc[4][TD], vc[DT];
-            const auto block_of = [&](int it) {
-                const int page = __builtin_amdgcn_readlane(id, it);
-                return ((size_t)(page < 0 ? 0 : page) * a.c.heads + head) * (PAGE_POS * DH);
-            };
-            const auto take_k = [&](size_t block) {
-#pragma unroll
-                for (int g = 0; g < 4; ++g)
-#pragma unroll
-                    for (int t = 0; t < TD; ++t) kc[g][t] = *(const u32x4 *)(a.c.k + block + k_off + 4 * g * DH + 64 * t);
-            };
-            take_k(block_of(0));
-#pragma unroll
-            for (int d = 0; d < DT; ++d) vc[d] = *(const u32x4 *)(a.c.v + block_of(0) + v_off + 16 * d * PAGE_POS);
+        for (int i0 = seg.first + wave; i0 < seg.last; i0 += 256) {
+            const int n_here = (seg.last - i0 + 3) / 4 < 64 ? (seg.last - i0 + 3) / 4 : 64;
             for (int it = 0; it < n_here; ++it) {
                 const int page = __builtin_amdgcn_readlane(id, it), base = (i0 + 4 * it) * PAGE_POS;
                 const float pks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), it)), pvs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), it));
-                const size_t next = block_of(it + 1 < n_here ? it + 1 : it);       // (the last page's once more: no branch around the loads)
+                const size_t next = block_of(__builtin_amdgcn_readlane(id, it + 1 < n_here ? it + 1 : it));      // (the last page's once more: no branch around the loads)
                 // (several tiles' queries come from LDS for every page: kept in registers across pages they would push the sums out)
                 int ql = lane;
                 if constexpr (NT > 1) asm volatile("" : "+v"(ql));
@@ -642,21 +703,25 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
                                 sc[n][g] = mfma16x16x32(hi, q[pl * PIECES + ((n * TD + t) * 2 + 1) * 64 + ql], sc[n][g]);
                             }
                     }
+                __builtin_amdgcn_sched_barrier(0);
                 take_k(next);
+                __builtin_amdgcn_sched_barrier(0);
                 const float by = to_log2 * pks;
                 const bool masked = page < 0 || base + PAGE_POS - 1 > seen;
-                bool nans = false;
+                uint32_t nans = 0;
                 if (masked) {
                     const int there = page < 0 ? 0 : s.len - base - 16 * kb;       // of the lane's 16 positions of V
+                    uint32_t is[4];
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) is[w] = there - 4 * w >= 4 ? ~0u : there - 4 * w <= 0 ? 0u : ~(~0u << (8 * (there - 4 * w)));
+                    // what lies behind the last position may be anything, and a NaN that only later rows see must not reach the others through 0 * NaN
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
 #pragma unroll
                         for (int w = 0; w < 4; ++w) {
-                            const int n = there - 4 * w;
-                            vc[d][w] &= n >= 4 ? ~0u : n <= 0 ? 0u : ~(~0u << (8 * n));
-                            // a NaN that only later rows see must not reach the others through 0 * NaN
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) nans |= (vc[d][w] >> (8 * e) & 0x7f) == 0x7f;
+                            const uint32_t c = vc[d][w] & is[w], m = nan_bytes(c);
+                            nans |= m;
+                            vc[d][w] = c & ~(m | (m - (m >> 7)));
                         }
                 }
                 u32x4 pb[NT][NP][2];
@@ -697,28 +762,37 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
                             }
                         }
                 }
-                if (masked && __ballot(nans) != 0) {             // rare: rows that see a NaN get it, the others do not
-#pragma unroll
+                __builtin_amdgcn_sched_barrier(0);
+                if (masked && __ballot(nans != 0) != 0) {        // rare: rows that see a NaN get it.  Products of ones find them
+#pragma unroll 1
                     for (int d = 0; d < DT; ++d) {
-                        u32x4 lo, hi;
-                        bool any = false;
-                        take_nans(vc[d], lo, hi, any);
+                        const u32x4 c = *(const u32x4 *)(a.c.v + block_of(page) + 16 * d * PAGE_POS + v_off);
+                        u32x4 ones[2];
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const int n = s.len - base - 16 * kb - 4 * w;
+                            const u32x2 o2 = ones_of(nan_bytes(c[w] & (n >= 4 ? ~0u : n <= 0 ? 0u : ~(~0u << (8 * n)))));
+                            ones[w / 2][2 * (w & 1)] = o2[0];
+                            ones[w / 2][2 * (w & 1) + 1] = o2[1];
+                        }
 #pragma unroll
                         for (int n = 0; n < NT; ++n) {
-                            u32x4 vis[2];
+                            f32x4 hit = (f32x4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-                            for (int u = 0; u < 2; ++u)
+                            for (int u = 0; u < 2; ++u) {
+                                u32x4 sees;
 #pragma unroll
                                 for (int w = 0; w < 4; ++w) {
                                     const int p = base + 16 * kb + 8 * u + 2 * w;
-                                    vis[u][w] = (p <= limit[n] ? 0x3f80u : 0) | (p + 1 <= limit[n] ? 0x3f800000u : 0);
+                                    sees[w] = (p <= limit[n] ? 0x3f80u : 0) | (p + 1 <= limit[n] ? 0x3f800000u : 0);
                                 }
-                            f32x4 hit = (f32x4){0.f, 0.f, 0.f, 0.f};
-                            hit = mfma16x16x32(lo, vis[0], hit);
-                            hit = mfma16x16x32(hi, vis[1], hit);
+                                hit = mfma16x16x32(ones[u], sees, hit);
+                            }
 #pragma unroll
-                            for (int r = 0; r < 4; ++r)
-                                if (hit[r] > 0.f) o[n][d][r] = __builtin_nanf("");
+                            for (int e = 0; e < DT; ++e)
+#pragma unroll
+                                for (int r = 0; r < 4; ++r)
+                                    if (e == d && hit[r] > 0.f) o[n][e][r] = __builtin_nanf("");
                         }
                     }
                 }
@@ -726,7 +800,7 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
                 for (int d = 0; d < DT; ++d) {
                     u32x4 lo, hi;
                     widen16(vc[d], pvs, lo, hi);
-                    vc[d] = *(const u32x4 *)(a.c.v + next + v_off + 16 * d * PAGE_POS);
+                    take_v(next, d);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -736,59 +810,62 @@ __global__ __launch_bounds__(256, NT < 4 ? 2 : 1) void attend_paged_kernel(Atten
                         }
                 }
             }
+            if (i0 + 256 < seg.last) {                           // (a share of more than 256 pages of one sequence)
+                id = page_ids(seg, i0 + 256);
+                take_page(__builtin_amdgcn_readlane(id, 0));
+                take_scales(id);
+            }
         }
+        id = id_after;
+        if (after.last > 0) {
+            if (after.first + wave < after.last) take_page(__builtin_amdgcn_readlane(id, 0));
+            take_scales(id);
+        }
+        // ---- the waves' sums meet
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             l[n] += lane_xor<16>(l[n]);
             l[n] += lane_xor<32>(l[n]);
+            if (kb == 0) { ml[wave][0][n * 16 + col] = m[n]; ml[wave][1][n * 16 + col] = l[n]; }
         }
-        // ---- the waves' sums meet: 2 and 3 with 0 and 1, then 1 with 0
+        __syncthreads();
+        float top[NT], sum[NT];
 #pragma unroll
-        for (int step = 2; step >= 1; step /= 2) {
-            __syncthreads();
-            if (wave >= step && wave < 2 * step) {
+        for (int n = 0; n < NT; ++n) {
+            const float *const am = &ml[0][0][n * 16 + col];
+            top[n] = fmaxf(fmaxf(am[0], am[2 * NT * 16]), fmaxf(am[4 * NT * 16], am[6 * NT * 16]));
+            const float ref = top[n] == LLMA_NEG_INF ? 0.f : top[n];
+            sum[n] = 0.f;
 #pragma unroll
-                for (int n = 0; n < NT; ++n) {
+            for (int w = 0; w < 4; ++w) sum[n] += am[(2 * w + 1) * NT * 16] * __builtin_amdgcn_exp2f(am[2 * w * NT * 16] - ref);
+            const float f = __builtin_amdgcn_exp2f(m[n] - ref);
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) osum[((wave - step) * NT * DT + n * DT + d) * 64 + lane] = o[n][d];
-                    if (kb == 0) { ml[wave - step][0][n * 16 + col] = m[n]; ml[wave - step][1][n * 16 + col] = l[n]; }
-                }
-            }
-            __syncthreads();
-            if (wave < step) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    const float om = ml[wave][0][n * 16 + col], ol = ml[wave][1][n * 16 + col];
-                    const float mn = fmaxf(m[n], om), ref = mn == LLMA_NEG_INF ? 0.f : mn;
-                    const float f0 = __builtin_amdgcn_exp2f(m[n] - ref), f1 = __builtin_amdgcn_exp2f(om - ref);
-                    m[n] = mn;
-                    l[n] = l[n] * f0 + ol * f1;
-#pragma unroll
-                    for (int d = 0; d < DT; ++d) o[n][d] = o[n][d] * f0 + osum[(wave * NT * DT + n * DT + d) * 64 + lane] * f1;
-                }
-            }
+            for (int d = 0; d < DT; ++d) osum[((wave * NT + n) * DT + d) * 64 + lane] = o[n][d] * f;
         }
-        if (wave == 0) {
-            const bool whole = first == 0 && last == pages;
-            // the part's place: a share has at most one sequence that began before it (0) and one that goes on behind it (1)
-            const int64_t at = (((int64_t)share * 2 + (first == 0)) * a.c.heads + head) * plan.tiles + tile;
-            float *const po = (float *)a.work + (a.n_seqs + 1 + 63) / 64 * 64;
-            float *const pm = po + attend_parts(plan, a.c.heads) * 16 * NT * DH, *const pl = pm + attend_parts(plan, a.c.heads) * 16 * NT;
+        __syncthreads();
+        const bool whole = seg.first == 0 && seg.last == seg.pages;
+        // the part's place: a share has at most one sequence that began before it (0) and one that goes on behind it (1)
+        const int64_t at = (((int64_t)share * 2 + (seg.first == 0)) * a.c.heads + head) * plan.tiles + tile;
+        float *const po = (float *)a.work + (a.n_seqs + 1 + 63) / 64 * 64;
+        float *const pm = po + attend_parts(plan, a.c.heads) * 16 * NT * DH, *const pl = pm + attend_parts(plan, a.c.heads) * 16 * NT;
 #pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                const int r = r0 + 16 * n + col;
-                if (r >= s.rows * group) continue;
-                if (whole) {
-                    const float inv = l[n] == 0.f ? 0.f : 1.f / l[n];
+        for (int n = 0; n < NT; ++n) {
+            const int r = r0 + 16 * n + col;
+            if (r >= s.rows * group) continue;
+            const int row = s.row0 + r / group, h = head * group + r % group;
+            const float inv = sum[n] == 0.f ? 0.f : 1.f / sum[n];
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 16 * d + 4 * kb, o[n][d] * inv);
-                } else {
+            for (int u = 0; u < DT / 4; ++u) {
+                const int d = 4 * u + wave;
+                f32x4 v = osum[(n * DT + d) * 64 + lane];
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) *(f32x4 *)(po + (at * 16 * NT + 16 * n + col) * DH + 16 * d + 4 * kb) = o[n][d];
-                    if (kb == 0) { pm[at * 16 * NT + 16 * n + col] = m[n]; pl[at * 16 * NT + 16 * n + col] = l[n]; }
-                }
+                for (int w = 1; w < 4; ++w) v += osum[((w * NT + n) * DT + d) * 64 + lane];
+                if (whole) attend_store<TYPE>(a, row, h, 16 * d + 4 * kb, v * inv);
+                else *(f32x4 *)(po + (at * 16 * NT + 16 * n + col) * DH + 16 * d + 4 * kb) = v;
             }
+            if (!whole && wave == 0 && kb == 0) { pm[at * 16 * NT + 16 * n + col] = top[n]; pl[at * 16 * NT + 16 * n + col] = sum[n]; }
         }
+        seg = after;
     }
 }
 
@@ -835,8 +912,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, AttendPl
 
 template <int DH, int NT, int TYPE>
 static void launch_attend_nt(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
-    constexpr int NQ = attend_nq<TYPE>, PIECES = NT * (DH / 64) * 2 * 64, JOIN = 2 * NT * (DH / 16) * 64;
-    const size_t bytes = (size_t)(NQ * PIECES > JOIN ? NQ * PIECES : JOIN) * 16 + (size_t)(a.n_seqs + 1) * 4;
+    const size_t bytes = (size_t)attend_lds<DH, NT, TYPE> + (size_t)(a.n_seqs + 1) * 4;
     hipLaunchKernelGGL((attend_paged_kernel<DH, NT, TYPE>), dim3(p.shares * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
 }
 template <int DH, int TYPE>
@@ -844,6 +920,7 @@ static void launch_attend_type(const AttendArgs &a, hipStream_t st) {
     const AttendPlan p = attend_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
+    else if (p.nt == 3) launch_attend_nt<DH, 3, TYPE>(a, p, st);
     else launch_attend_nt<DH, 4, TYPE>(a, p, st);
     if (p.shares > 1)
         hipLaunchKernelGGL((attend_join_kernel<DH, TYPE>), dim3((a.max_rows * (a.n_heads / a.c.heads) + 3) / 4, a.c.heads, a.n_seqs), dim3(256), 0, st, a, p);
