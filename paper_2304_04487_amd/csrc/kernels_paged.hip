@@ -515,8 +515,47 @@ __device__ __forceinline__ void widen16(u32x4 c, float scale, u32x4 &lo, u32x4 &
 }
 // the NaN codes among four: 0x80 in their bytes
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
+__device__ __forceinline__ uint32_t whole_bytes(uint32_t m) { return m | (m - (m >> 7)); }
+// a word's first n bytes (all for n >= 4, none for n <= 0)
+__device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : ~(~0u << (8 * n)); }
 // four such bytes as the ones of two words of bf16
 __device__ __forceinline__ u32x2 ones_of(uint32_t m) { return (u32x2){(m >> 7 & 1) * 0x3f80u | (m >> 15 & 1) * 0x3f800000u, (m >> 23 & 1) * 0x3f80u | (m >> 31) * 0x3f800000u}; }
+
+// rare: a page's V holds NaN where not all rows see it.  The rows that see one get it in that feature; products of ones find them.  codes: the page's V at the lane's place
+template <int DH, int NT>
+__device__ __forceinline__ void attend_nans(const uint8_t *codes, int base, int len, const int (&limit)[NT], f32x4 (&o)[NT][DH / 16]) {
+    const int kb = (threadIdx.x & 63) >> 4;
+#pragma unroll 1
+    for (int d = 0; d < DH / 16; ++d) {
+        const u32x4 c = *(const u32x4 *)(codes + 16 * d * PAGE_POS);
+        u32x4 ones[2];
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const u32x2 o2 = ones_of(nan_bytes(c[w] & bytes_below(len - base - 16 * kb - 4 * w)));
+            ones[w / 2][2 * (w & 1)] = o2[0];
+            ones[w / 2][2 * (w & 1) + 1] = o2[1];
+        }
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            f32x4 hit = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+                u32x4 sees;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const int p = base + 16 * kb + 8 * u + 2 * w;
+                    sees[w] = (p <= limit[n] ? 0x3f80u : 0) | (p + 1 <= limit[n] ? 0x3f800000u : 0);
+                }
+                hit = mfma16x16x32(ones[u], sees, hit);
+            }
+#pragma unroll
+            for (int e = 0; e < DH / 16; ++e)
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+                    if (e == d && hit[r] > 0.f) o[n][e][r] = __builtin_nanf("");
+        }
+    }
+}
 
 template <int TYPE>
 __device__ __forceinline__ void attend_store(const AttendArgs &a, int row, int h, int d, f32x4 v) {      // four neighbouring features
@@ -675,8 +714,11 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
 #pragma unroll
             for (int d = 0; d < DT; ++d) o[n][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
         }
-        for (int i0 = seg.first + wave; i0 < seg.last; i0 += 256) {
-            const int n_here = (seg.last - i0 + 3) / 4 < 64 ? (seg.last - i0 + 3) / 4 : 64;
+        // (pages behind the tile's last row are not seen by any of it)
+        const int r_last = (r0 + 16 * NT < s.rows * group ? r0 + 16 * NT : s.rows * group) - 1, furthest = seen + r_last / group;
+        const int stop = furthest < 0 ? 0 : seg.last < furthest / PAGE_POS + 1 ? seg.last : furthest / PAGE_POS + 1;
+        for (int i0 = seg.first + wave; i0 < stop; i0 += 256) {
+            const int n_here = (stop - i0 + 3) / 4 < 64 ? (stop - i0 + 3) / 4 : 64;
             for (int it = 0; it < n_here; ++it) {
                 const int page = __builtin_amdgcn_readlane(id, it), base = (i0 + 4 * it) * PAGE_POS;
                 const float pks = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(ks), it)), pvs = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(vs), it));
@@ -713,7 +755,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                     const int there = page < 0 ? 0 : s.len - base - 16 * kb;       // of the lane's 16 positions of V
                     uint32_t is[4];
 #pragma unroll
-                    for (int w = 0; w < 4; ++w) is[w] = there - 4 * w >= 4 ? ~0u : there - 4 * w <= 0 ? 0u : ~(~0u << (8 * (there - 4 * w)));
+                    for (int w = 0; w < 4; ++w) is[w] = bytes_below(there - 4 * w);
                     // what lies behind the last position may be anything, and a NaN that only later rows see must not reach the others through 0 * NaN
 #pragma unroll
                     for (int d = 0; d < DT; ++d)
@@ -721,7 +763,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                         for (int w = 0; w < 4; ++w) {
                             const uint32_t c = vc[d][w] & is[w], m = nan_bytes(c);
                             nans |= m;
-                            vc[d][w] = c & ~(m | (m - (m >> 7)));
+                            vc[d][w] = c & ~whole_bytes(m);
                         }
                 }
                 u32x4 pb[NT][NP][2];
@@ -729,14 +771,14 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                 for (int n = 0; n < NT; ++n) {
                     float x[16], top = LLMA_NEG_INF;
 #pragma unroll
-                    for (int g = 0; g < 4; ++g)
+                    for (int e = 0; e < 16; ++e) x[e] = sc[n][e / 4][e % 4] * by;
+                    if (masked) {
+                        const int left = (page < 0 ? -1 : limit[n]) - base - 16 * kb;
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
-                            float v = sc[n][g][r] * by;
-                            if (masked && (page < 0 || base + 16 * kb + 4 * g + r > limit[n])) v = LLMA_NEG_INF;
-                            x[4 * g + r] = v;
-                            top = fmaxf(top, v);
-                        }
+                        for (int e = 0; e < 16; ++e) x[e] = e > left ? LLMA_NEG_INF : x[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, x[e]);
                     top = fmaxf(top, lane_xor<16>(top));
                     top = fmaxf(top, lane_xor<32>(top));
                     const float mn = fmaxf(m[n], top), ref = mn == LLMA_NEG_INF ? 0.f : mn;
@@ -763,39 +805,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                         }
                 }
                 __builtin_amdgcn_sched_barrier(0);
-                if (masked && __ballot(nans != 0) != 0) {        // rare: rows that see a NaN get it.  Products of ones find them
-#pragma unroll 1
-                    for (int d = 0; d < DT; ++d) {
-                        const u32x4 c = *(const u32x4 *)(a.c.v + block_of(page) + 16 * d * PAGE_POS + v_off);
-                        u32x4 ones[2];
-#pragma unroll
-                        for (int w = 0; w < 4; ++w) {
-                            const int n = s.len - base - 16 * kb - 4 * w;
-                            const u32x2 o2 = ones_of(nan_bytes(c[w] & (n >= 4 ? ~0u : n <= 0 ? 0u : ~(~0u << (8 * n)))));
-                            ones[w / 2][2 * (w & 1)] = o2[0];
-                            ones[w / 2][2 * (w & 1) + 1] = o2[1];
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            f32x4 hit = (f32x4){0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                            for (int u = 0; u < 2; ++u) {
-                                u32x4 sees;
-#pragma unroll
-                                for (int w = 0; w < 4; ++w) {
-                                    const int p = base + 16 * kb + 8 * u + 2 * w;
-                                    sees[w] = (p <= limit[n] ? 0x3f80u : 0) | (p + 1 <= limit[n] ? 0x3f800000u : 0);
-                                }
-                                hit = mfma16x16x32(ones[u], sees, hit);
-                            }
-#pragma unroll
-                            for (int e = 0; e < DT; ++e)
-#pragma unroll
-                                for (int r = 0; r < 4; ++r)
-                                    if (e == d && hit[r] > 0.f) o[n][e][r] = __builtin_nanf("");
-                        }
-                    }
-                }
+                if (masked && __ballot(nans != 0) != 0) attend_nans<DH, NT>(a.c.v + block_of(page) + v_off, base, s.len, limit, o);
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     u32x4 lo, hi;
@@ -810,7 +820,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                         }
                 }
             }
-            if (i0 + 256 < seg.last) {                           // (a share of more than 256 pages of one sequence)
+            if (i0 + 256 < stop) {                               // (a share of more than 256 pages of one sequence)
                 id = page_ids(seg, i0 + 256);
                 take_page(__builtin_amdgcn_readlane(id, 0));
                 take_scales(id);
@@ -869,6 +879,264 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
     }
 }
 
+// ---- many rows -----------------------------------------------------------------------------------
+// Which calls take it: those with more rows a key head than the shares' kernel holds (64) and at least this many row blocks.  Fewer leave compute units
+// without work, where shares cut the pages too.  Both at 32 heads of 128, bf16, 1000 positions before 512 / 640 / 768 rows (128, 160, 192 blocks) 54 / 57 / 61
+// us here, 42 / 70 / 74 in shares; 16 sequences of 18 x 4 rows over 4000 positions (128) 111 and 85, 64 of 20 x 4 over 1000 (512) 48 and 127.
+#define ROWS_MIN 160
+// Prompts: a workgroup takes 64 NT rows of a sequence's key head and all pages they see.  Each page is widened once, for all four waves, into LDS as the
+// operands' images (16 KB of K, 16 KB of V at head_dim 128); a page is requested two ahead, widened one ahead, one barrier a page.  A wave holds its rows' queries and
+// sums in registers and meets nobody at the end.  Pages behind a wave's rows are skipped; the longest row blocks start first, and a key head's on one XCD.
+// The reference of the exponentials moves only when a maximum passes it by 2^8: the sums are rescaled once or twice a row instead of once a page.
+template <int DH> constexpr int rows_images = (4 * (DH / 64) * 2 + (DH / 16) * 2) * 64;       // 16-byte pieces of a page
+template <int DH, int NT, int TYPE>
+__global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int blocks) {
+    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE>, TD = DH / 64, DT = DH / 16;
+    extern __shared__ u32x4 lds[];                               // [2] pages
+    __shared__ int nan_seen[2][4];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, b = rest % a.n_seqs, block = blocks - 1 - rest / a.n_seqs;
+    const int group = a.n_heads / a.c.heads, r0 = block * 64 * NT;
+    const AttendSeq s = uniform(attend_seq(a, b));
+    const int R = s.rows * group, seen = s.len - s.rows;
+    if (r0 >= R) return;
+    const int r1 = r0 + 64 * NT < R ? r0 + 64 * NT : R, furthest = seen + (r1 - 1) / group;        // the block's last position
+    const int pages = furthest < 0 ? 0 : furthest / PAGE_POS + 1;
+    const int kb = lane >> 4, col = lane & 15, w0 = r0 + wave * 16 * NT;
+    const int w1 = w0 + 16 * NT < R ? w0 + 16 * NT : R;
+    const int wave_first = w0 < R ? seen + w0 / group : -1, wave_last = w0 < R ? seen + (w1 - 1) / group : -1, block_first = seen + r0 / group;
+    const uint32_t k_off = (16 * (col >> 2) + (col & 3)) * DH + 16 * kb, v_off = col * PAGE_POS + 16 * kb;
+    // ---- the wave's queries.  A negative scale turns their signs, so that the largest score is the largest product
+    u32x4 q[NQ][NT][TD][2];
+    const uint32_t turn = a.scale < 0.f ? 0x80008000u : 0u;
+    int limit[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = w0 + 16 * n + col;
+        limit[n] = r < R ? seen + r / group : -1;
+#pragma unroll
+        for (int t = 0; t < TD; ++t)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                float v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = 0.f;
+#pragma unroll
+                for (int p = 0; p < NQ; ++p) q[p][n][t][h] = (u32x4){0, 0, 0, 0};
+                if (r < R) {
+                    const int row = s.row0 + r / group, hq = head * group + r % group, d = 64 * t + 16 * kb + 8 * h;
+                    if constexpr (TYPE == ROWS_TILED) {
+                        const size_t at = xtile_off(row, hq * DH + d, a.tile_ksp, a.quads);
+                        q[0][n][t][h] = *(const u32x4 *)((const bf16_t *)a.q + at);
+                        q[1][n][t][h] = *(const u32x4 *)((const bf16_t *)a.q_lo + at);
+                    } else {
+                        row8<TYPE>(a.q, (int64_t)row * a.q_row + hq * a.q_head + d, v);
+#pragma unroll
+                        for (int p = 0; p < NQ; ++p)
+#pragma unroll
+                            for (int w = 0; w < 4; ++w) {
+                                const uint32_t x = bf16_pair(v[2 * w], v[2 * w + 1]);
+                                q[p][n][t][h][w] = x;
+                                v[2 * w] -= __uint_as_float(x << 16);
+                                v[2 * w + 1] -= __uint_as_float(x & 0xffff0000u);
+                            }
+                    }
+#pragma unroll
+                    for (int p = 0; p < NQ; ++p) q[p][n][t][h] ^= turn;
+                }
+            }
+    }
+    // ---- page numbers and scales, 64 pages a lane at a time: the present 64 and the next
+    struct Pages { int id; float ks, vs; };
+    const auto pages_from = [&](int i0) {
+        Pages g{-1, 0.f, 0.f};
+        const int i = i0 + lane;
+        if (i < pages) g.id = a.table[(size_t)s.slot * a.max_blocks + i];
+        if ((unsigned)g.id >= (unsigned)a.c.n_pages) g.id = -1;
+        if (g.id >= 0) {
+            g.ks = a.c.k_scale[(size_t)g.id * a.c.heads + head];
+            g.vs = a.c.v_scale[(size_t)g.id * a.c.heads + head];
+        }
+        return g;
+    };
+    Pages now = pages_from(0), later = pages_from(64);
+    int now_at = 0;                                              // the first page of `now`
+    const auto id_of = [&](int i) { return i < now_at + 64 ? __builtin_amdgcn_readlane(now.id, i - now_at) : __builtin_amdgcn_readlane(later.id, i - now_at - 64); };
+    const auto scale_of = [&](float x, float y, int i) {
+        return __uint_as_float(i < now_at + 64 ? __builtin_amdgcn_readlane(__float_as_uint(x), i - now_at) : __builtin_amdgcn_readlane(__float_as_uint(y), i - now_at - 64));
+    };
+    // a thread's share of a page: score tile `wave`, feature tiles of V 4 u + wave
+    u32x4 kc[TD], vc[DT / 4];
+    const auto take = [&](int i) {
+        const int id = id_of(i);
+        const size_t at = ((size_t)(id < 0 ? 0 : id) * a.c.heads + head) * (PAGE_POS * DH);
+#pragma unroll
+        for (int t = 0; t < TD; ++t) kc[t] = *(const u32x4 *)((a.c.k + at + 4 * wave * DH + 64 * t) + k_off);
+#pragma unroll
+        for (int u = 0; u < DT / 4; ++u) vc[u] = *(const u32x4 *)((a.c.v + at + 16 * (4 * u + wave) * PAGE_POS) + v_off);
+    };
+    const auto widen = [&](int i) {
+        u32x4 *const to = lds + (i & 1) * rows_images<DH>;
+#pragma unroll
+        for (int t = 0; t < TD; ++t) {
+            u32x4 lo, hi;
+            widen16(kc[t], 1.f, lo, hi);
+            to[((wave * TD + t) * 2) * 64 + lane] = lo;
+            to[((wave * TD + t) * 2 + 1) * 64 + lane] = hi;
+        }
+        const float vs = scale_of(now.vs, later.vs, i);
+        uint32_t nans = 0;
+        if (i * PAGE_POS + PAGE_POS - 1 > block_first || id_of(i) < 0) {       // positions that some row does not see
+            const int there = id_of(i) < 0 ? 0 : s.len - i * PAGE_POS - 16 * kb;
+#pragma unroll
+            for (int u = 0; u < DT / 4; ++u)
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const uint32_t c = vc[u][w] & bytes_below(there - 4 * w), m = nan_bytes(c);
+                    nans |= m;
+                    vc[u][w] = c & ~whole_bytes(m);
+                }
+        }
+        nans = __ballot(nans != 0) != 0;
+        if (lane == 0) nan_seen[i & 1][wave] = (int)nans;
+#pragma unroll
+        for (int u = 0; u < DT / 4; ++u) {
+            u32x4 lo, hi;
+            widen16(vc[u], vs, lo, hi);
+            to[4 * TD * 2 * 64 + ((4 * u + wave) * 2) * 64 + lane] = lo;
+            to[4 * TD * 2 * 64 + ((4 * u + wave) * 2 + 1) * 64 + lane] = hi;
+        }
+    };
+    f32x4 o[NT][DT];
+    float m[NT];
+    f32x4 l[NT];                                                 // the rows' sums, by products with ones
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = LLMA_NEG_INF;
+        l[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[n][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    const float to_log2 = fabsf(a.scale) * 1.44269504088896340736f;
+    if (pages > 0) {
+        take(0);
+        widen(0);
+        if (pages > 1) take(1);
+    }
+    __syncthreads();
+    for (int i = 0; i < pages; ++i) {
+        if (i + 1 < pages) widen(i + 1);
+        if (i + 2 < pages) take(i + 2);
+        const int base = i * PAGE_POS;
+        if (base <= wave_last) {                                 // (the wave's rows see some of it)
+            // operands come from LDS eight ahead of their products, V's first ones behind K's last
+            constexpr int KI = 4 * TD * 2, VI = DT * 2;
+            const u32x4 *const img = lds + (i & 1) * rows_images<DH> + lane;
+            u32x4 w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = img[j * 64];
+            const int id = id_of(i);
+            const bool masked = id < 0 || base + PAGE_POS - 1 > wave_first;
+            // (not 0: minus infinity has to stay that)
+            const float by = fmaxf(to_log2 * scale_of(now.ks, later.ks, i), 1e-37f);
+            u32x4 pb[NT][NP][2];
+            f32x4 sc[NT][4];
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int g = 0; g < 4; ++g) sc[n][g] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int j = 0; j < KI; ++j) {
+                const int g = j / (2 * TD), t = j / 2 % TD, h = j % 2;
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sc[n][g] = mfma16x16x32(w[j % 8], q[p][n][t][h], sc[n][g]);
+                w[j % 8] = img[(j + 8) * 64];
+                __builtin_amdgcn_sched_group_barrier(0x008, NT * NQ, 0);       // (products, then a load: as written)
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            if (masked) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int left = (id < 0 ? -1 : limit[n]) - base - 16 * kb;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sc[n][e / 4][e % 4] = e > left ? LLMA_NEG_INF : sc[n][e / 4][e % 4];
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float top = LLMA_NEG_INF;
+#pragma unroll
+                for (int g = 0; g < 4; ++g)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[n][g][r]);
+                top = fmaxf(top, lane_xor<16>(top));
+                top = fmaxf(top, lane_xor<32>(top)) * by;
+                if (__ballot(top > m[n] + 8.f) != 0) {
+                    const float mn = fmaxf(m[n], top), keep = __builtin_amdgcn_exp2f(m[n] - (mn == LLMA_NEG_INF ? 0.f : mn));
+                    m[n] = mn;
+                    l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+                }
+                const float ref = m[n] == LLMA_NEG_INF ? 0.f : m[n];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int g = 2 * u + w / 2, r = 2 * (w & 1);
+                        float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][g][r], by, -ref)), z = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][g][r + 1], by, -ref));
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            pb[n][p][u][w] = bf16_pair(y, z);
+                            if (p + 1 < NP) { y -= __uint_as_float(pb[n][p][u][w] << 16); z -= __uint_as_float(pb[n][p][u][w] & 0xffff0000u); }
+                        }
+                    }
+            }
+            if (masked && (nan_seen[i & 1][0] | nan_seen[i & 1][1] | nan_seen[i & 1][2] | nan_seen[i & 1][3]))
+                attend_nans<DH, NT>(a.c.v + ((size_t)(id < 0 ? 0 : id) * a.c.heads + head) * (PAGE_POS * DH) + v_off, base, id < 0 ? 0 : s.len, limit, o);
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) l[n] = mfma16x16x32((u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, pb[n][p][u], l[n]);
+#pragma unroll
+            for (int j = 0; j < VI; ++j) {
+                const int d = j / 2, u = j % 2;
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) o[n][d] = mfma16x16x32(w[(KI + j) % 8], pb[n][p][u], o[n][d]);
+                if (j + 8 < VI) {
+                    w[(KI + j) % 8] = img[(KI + j + 8) * 64];
+                    __builtin_amdgcn_sched_group_barrier(0x008, NT * NP, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (i + 1 == now_at + 64) {
+            now = later;
+            now_at += 64;
+            later = pages_from(now_at + 64);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = w0 + 16 * n + col;
+        if (r >= R) continue;
+        const float inv = l[n][0] == 0.f ? 0.f : 1.f / l[n][0];
+#pragma unroll
+        for (int d = 0; d < DT; ++d) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 16 * d + 4 * kb, o[n][d] * inv);
+    }
+}
+
 // a wave per row of a sequence that lies in several shares
 template <int DH, int TYPE>
 __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, AttendPlan plan) {
@@ -915,8 +1183,21 @@ static void launch_attend_nt(const AttendArgs &a, const AttendPlan &p, hipStream
     const size_t bytes = (size_t)attend_lds<DH, NT, TYPE> + (size_t)(a.n_seqs + 1) * 4;
     hipLaunchKernelGGL((attend_paged_kernel<DH, NT, TYPE>), dim3(p.shares * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
 }
+// row blocks of a call, at most: what blocks of 64 nt rows make of max_rows everywhere, or of all rows and a remainder per sequence
+static int64_t attend_row_blocks(const AttendArgs &a, int nt) {
+    const int64_t group = a.n_heads / a.c.heads, rows = 64 * nt;
+    const int64_t by_max = a.n_seqs * ((a.max_rows * group + rows - 1) / rows), by_all = a.n_rows * group / rows + a.n_seqs;
+    return (by_max < by_all ? by_max : by_all) * a.c.heads;
+}
+template <int DH, int NT, int TYPE>
+static void launch_attend_rows(const AttendArgs &a, hipStream_t st) {
+    const int group = a.n_heads / a.c.heads, blocks = (a.max_rows * group + 64 * NT - 1) / (64 * NT);
+    hipLaunchKernelGGL((attend_rows_kernel<DH, NT, TYPE>), dim3((unsigned)blocks * a.n_seqs * a.c.heads), dim3(256), 2 * rows_images<DH> * 16, st, a, blocks);
+}
 template <int DH, int TYPE>
 static void launch_attend_type(const AttendArgs &a, hipStream_t st) {
+    constexpr int ROWS_NT = TYPE == ROWS_F32 ? 1 : 2;            // (three planes of queries and probabilities leave room for one tile)
+    if ((int64_t)a.max_rows * (a.n_heads / a.c.heads) > 64 && attend_row_blocks(a, ROWS_NT) >= ROWS_MIN) return launch_attend_rows<DH, ROWS_NT, TYPE>(a, st);
     const AttendPlan p = attend_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
