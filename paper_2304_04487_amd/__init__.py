@@ -191,65 +191,80 @@ def _refuse(msg: str):
     raise LlmaError(LLMA_E_INVAL, msg)
 
 
+_torch = None
+_ROW_TYPES = {}
+
+
+def _import_torch():
+    global _torch
+    import torch
+    _ROW_TYPES.update({torch.bfloat16: LLMA_DTYPE_BF16, torch.float16: LLMA_DTYPE_F16, torch.float32: LLMA_DTYPE_F32})
+    _torch = torch
+
+
 class _Call:
-    """Checks a call's tensors -- all on one device, of the type and shape they should have -- and names its stream."""
+    """Checks a call's tensors -- all on one device, of the type and shape they should have -- and names its stream.  The kernels of the smallest calls take a few
+    microseconds, so what is asked of a tensor is asked in one line each (attend: 20 us a call with the stream looked up as an object and loops over shapes)."""
+    __slots__ = ("who", "device", "given", "stream", "lib")
 
     def __init__(self, who: str, first, stream):
-        import torch
-        self.torch, self.who = torch, who
-        if not isinstance(first, torch.Tensor) or not first.is_cuda:
+        if _torch is None:
+            _import_torch()
+        self.who = who
+        if not isinstance(first, _torch.Tensor) or not first.is_cuda:
             _refuse(f"{who}: device tensors are wanted")
+        self.lib = _lib or load_library()
         self.device = first.device
-        if stream is not None and getattr(stream, "device", self.device) != self.device:
-            _refuse(f"{who}: the stream is not on the tensors' device")
         self.given = stream
-        self.stream = stream if stream is not None else torch.cuda.current_stream(self.device)
+        if stream is None:
+            self.stream = _torch._C._cuda_getCurrentRawStream(self.device.index)
+        else:
+            if getattr(stream, "device", self.device) != self.device:
+                _refuse(f"{who}: the stream is not on the tensors' device")
+            self.stream = stream.cuda_stream
 
     def ptr(self, name, t, dtype, shape):
-        """a contiguous tensor's address; shape: sizes, None where any will do"""
-        if t.dtype is not dtype or t.device != self.device or not t.is_contiguous() or t.dim() != len(shape):
-            _refuse(f"{self.who}: {name} has to be a contiguous {dtype} tensor of {len(shape)} dimensions on {self.device}")
-        for have, want in zip(t.shape, shape):
-            if want is not None and have != want:
-                _refuse(f"{self.who}: {name} has shape {tuple(t.shape)}, wanted {shape}")
-        return t.data_ptr()
+        """a contiguous tensor's address"""
+        if t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
+            return t.data_ptr()
+        _refuse(f"{self.who}: {name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def rows(self, name, t, shape):
         """(address, dtype code) of rows whose features lie together, any other strides"""
-        codes = {self.torch.bfloat16: LLMA_DTYPE_BF16, self.torch.float16: LLMA_DTYPE_F16, self.torch.float32: LLMA_DTYPE_F32}
-        if t.dtype not in codes or t.device != self.device or t.dim() != len(shape) or (t.numel() and t.stride(-1) != 1):
-            _refuse(f"{self.who}: {name} has to be a bf16, fp16 or fp32 tensor of {len(shape)} dimensions on {self.device} whose features lie together")
-        for have, want in zip(t.shape, shape):
-            if want is not None and have != want:
-                _refuse(f"{self.who}: {name} has shape {tuple(t.shape)}, wanted {shape}")
-        return t.data_ptr(), codes[t.dtype]
+        code = _ROW_TYPES.get(t.dtype)
+        if code is not None and t.shape == shape and t.device == self.device and (t.stride(-1) == 1 or t.numel() == 0):
+            return t.data_ptr(), code
+        _refuse(f"{self.who}: {name} has to be a bf16, fp16 or fp32 tensor of shape {tuple(shape)} on {self.device} whose features lie together, not {t.dtype} {tuple(t.shape)}, "
+                f"strides {t.stride()}, on {t.device}")
 
     def cache(self, c):
-        t = self.torch
-        if c.k.dim() != 4 or c.k.shape[2] != LLMA_PAGE:
+        k, u8, f32 = c.k, _torch.uint8, _torch.float32
+        if k.dim() != 4:
             _refuse(f"{self.who}: cache.k has to be [n_pages, n_kv_heads, {LLMA_PAGE}, head_dim]")
-        P, H, _, D = c.k.shape
-        return PagedCacheC(self.ptr("cache.k", c.k, t.uint8, (P, H, LLMA_PAGE, D)), self.ptr("cache.v", c.v, t.uint8, (P, H, D, LLMA_PAGE)),
-                           self.ptr("cache.k_scale", c.k_scale, t.float32, (P, H)), self.ptr("cache.v_scale", c.v_scale, t.float32, (P, H)), P, H, D)
+        P, H, _, D = k.shape
+        return PagedCacheC(self.ptr("cache.k", k, u8, (P, H, LLMA_PAGE, D)), self.ptr("cache.v", c.v, u8, (P, H, D, LLMA_PAGE)),
+                           self.ptr("cache.k_scale", c.k_scale, f32, (P, H)), self.ptr("cache.v_scale", c.v_scale, f32, (P, H)), P, H, D)
 
     def workspace(self, given, size: int):
         """a workspace of the caller's, or one that lives until the stream has used it (the allocator orders its reuse on the stream)"""
         _check(size)
         if given is not None:
-            if not given.is_cuda or given.device != self.device or not given.is_contiguous():
+            if given.device != self.device or not given.is_contiguous():
                 _refuse(f"{self.who}: workspace has to be a contiguous tensor on {self.device}")
             return given, given.numel() * given.element_size()
         if self.given is None:
-            return self.torch.empty(size, dtype=self.torch.uint8, device=self.device), size
-        with self.torch.cuda.stream(self.given):
-            return self.torch.empty(size, dtype=self.torch.uint8, device=self.device), size
+            return _torch.empty(size, dtype=_torch.uint8, device=self.device), size
+        with _torch.cuda.stream(self.given):
+            return _torch.empty(size, dtype=_torch.uint8, device=self.device), size
 
     def run(self, fn, *args):
-        if self.device.index == self.torch.cuda.current_device():
-            _check(fn(*args, c_void_p(self.stream.cuda_stream)))
+        if self.device.index == _torch.cuda.current_device():
+            rc = fn(*args, self.stream)
         else:
-            with self.torch.cuda.device(self.device):
-                _check(fn(*args, c_void_p(self.stream.cuda_stream)))
+            with _torch.cuda.device(self.device):
+                rc = fn(*args, self.stream)
+        if rc < 0:
+            _check(rc)
 
 
 def llma_map_pages(pages, lens, rows, row_offsets, lens_after, slot_map, row_pos, status, slots=None, stream=None):
@@ -257,17 +272,16 @@ def llma_map_pages(pages, lens, rows, row_offsets, lens_after, slot_map, row_pos
     rows [n_seqs], slots [n_seqs] or None; written: row_offsets [n_seqs + 1], lens_after [n_seqs], slot_map and row_pos [max_rows] (or both None), status [1].
     Enqueues on `stream` (None: torch's current stream of the tensors' device) and returns without synchronising."""
     c = _Call("llma_map_pages", lens, stream)
-    i32, p = c.torch.int32, c.ptr
-    table = p("pages.table", pages.table, i32, (None, None))
-    S, blocks = pages.table.shape
+    i32, p = _torch.int32, c.ptr
+    S, blocks = pages.table.shape if pages.table.dim() == 2 else (-1, -1)
     B, P = rows.numel(), pages.free_pages.numel()
     if (slot_map is None) != (row_pos is None):
         _refuse("llma_map_pages: slot_map and row_pos come together")
     n = 0 if slot_map is None else slot_map.numel()
-    c.run(load_library().llma_map_pages, p("lens", lens, i32, (S,)), p("rows", rows, i32, (B,)), None if slots is None else p("slots", slots, i32, (B,)), B, S, table, blocks,
-          p("pages.owned", pages.owned, i32, (S,)), p("pages.free_pages", pages.free_pages, i32, (P,)), p("pages.n_free", pages.n_free, i32, (1,)), P,
-          p("row_offsets", row_offsets, i32, (B + 1,)), p("lens_after", lens_after, i32, (B,)), None if n == 0 else p("slot_map", slot_map, i32, (n,)),
-          None if n == 0 else p("row_pos", row_pos, i32, (n,)), n, p("status", status, i32, (1,)))
+    c.run(c.lib.llma_map_pages, p("lens", lens, i32, (S,)), p("rows", rows, i32, (B,)), None if slots is None else p("slots", slots, i32, (B,)), B, S,
+          p("pages.table", pages.table, i32, (S, blocks)), blocks, p("pages.owned", pages.owned, i32, (S,)), p("pages.free_pages", pages.free_pages, i32, (P,)),
+          p("pages.n_free", pages.n_free, i32, (1,)), P, p("row_offsets", row_offsets, i32, (B + 1,)), p("lens_after", lens_after, i32, (B,)),
+          None if n == 0 else p("slot_map", slot_map, i32, (n,)), None if n == 0 else p("row_pos", row_pos, i32, (n,)), n, p("status", status, i32, (1,)))
 
 
 def llma_append_paged(cache, k, v, slot_map, stream=None):
@@ -275,13 +289,13 @@ def llma_append_paged(cache, k, v, slot_map, stream=None):
     cache at slot_map (int32 [n_rows], negative: nowhere); see llma.h.  Enqueues and returns without synchronising."""
     c = _Call("llma_append_paged", k, stream)
     d = c.cache(cache)
-    shape = (k.shape[0], d.n_kv_heads, d.head_dim)
+    shape = (slot_map.numel(), d.n_kv_heads, d.head_dim)
     kp, kt = c.rows("k", k, shape)
     vp, vt = c.rows("v", v, shape)
     if kt != vt:
         _refuse("llma_append_paged: k and v have different types")
-    c.run(load_library().llma_append_paged, byref(d), kp, vp, kt, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-          c.ptr("slot_map", slot_map, c.torch.int32, (shape[0],)), shape[0])
+    c.run(c.lib.llma_append_paged, byref(d), kp, vp, kt, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
+          c.ptr("slot_map", slot_map, _torch.int32, (shape[0],)), shape[0])
 
 
 def llma_attend_paged(cache, q, table, lens, row_offsets, max_rows: int, scale: float, out, slots=None, workspace=None, stream=None):
@@ -290,18 +304,18 @@ def llma_attend_paged(cache, q, table, lens, row_offsets, max_rows: int, scale: 
     rows.  workspace: at least llma_attend_paged_workspace() bytes of device memory, None: allocated for the call.  Enqueues
     and returns without synchronising.  Returns out."""
     c = _Call("llma_attend_paged", q, stream)
-    i32, d = c.torch.int32, c.cache(cache)
-    qp, qt = c.rows("q", q, (None, None, d.head_dim))
-    n, heads = q.shape[0], q.shape[1]
-    op, ot = c.rows("out", out, (n, heads, d.head_dim))
+    i32, p, d = _torch.int32, c.ptr, c.cache(cache)
+    shape = (q.shape[0], q.shape[1], d.head_dim) if q.dim() == 3 else (-1,)
+    qp, qt = c.rows("q", q, shape)
+    op, ot = c.rows("out", out, shape)
     if qt != ot:
         _refuse("llma_attend_paged: out and q have different types")
     B = lens.numel()
-    tp = c.ptr("table", table, i32, (None, None))
-    lib = load_library()
-    ws, size = c.workspace(workspace, lib.llma_attend_paged_workspace(B, table.shape[1], heads, d.n_kv_heads, d.head_dim, max_rows))
-    c.run(lib.llma_attend_paged, byref(d), qp, qt, heads, q.stride(0), q.stride(1), tp, None if slots is None else c.ptr("slots", slots, i32, (B,)),
-          table.shape[0], table.shape[1], c.ptr("lens", lens, i32, (B,)), c.ptr("row_offsets", row_offsets, i32, (B + 1,)), B, n, max_rows, scale,
+    S, blocks = table.shape if table.dim() == 2 else (-1, -1)
+    tp = p("table", table, i32, (S, blocks))
+    ws, size = c.workspace(workspace, c.lib.llma_attend_paged_workspace(B, blocks, shape[1], d.n_kv_heads, d.head_dim, max_rows))
+    c.run(c.lib.llma_attend_paged, byref(d), qp, qt, shape[1], q.stride(0), q.stride(1), tp, None if slots is None else p("slots", slots, i32, (B,)),
+          S, blocks, p("lens", lens, i32, (B,)), p("row_offsets", row_offsets, i32, (B + 1,)), B, shape[0], max_rows, scale,
           op, out.stride(0), out.stride(1), ws.data_ptr(), size)
     return out
 
@@ -317,18 +331,18 @@ def llma_verify_sampled(logits, drafts, u_accept, u_sample, n_accepted, next_tok
     [n_seqs, k, vocab], temperature fp32 [n_seqs]; written, int32: n_accepted, next_token [n_seqs], emitted [n_seqs, k + 1].  workspace: at least
     llma_verify_sampled_workspace() bytes of device memory, None: allocated for the call.  Enqueues and returns without synchronising."""
     c = _Call("llma_verify_sampled", logits, stream)
-    i32, f32 = c.torch.int32, c.torch.float32
-    lp, lt = c.rows("logits", logits, (None, None, None))
-    B, k, V = logits.shape[0], logits.shape[1] - 1, logits.shape[2]
+    i32, f32, p = _torch.int32, _torch.float32, c.ptr
+    shape = logits.shape if logits.dim() == 3 else (-1, 0, -1)
+    lp, lt = c.rows("logits", logits, shape)
+    B, k, V = shape[0], shape[1] - 1, shape[2]
     if k < 0 or (B > 1 and logits.stride(0) != (k + 1) * logits.stride(1)):
         _refuse("llma_verify_sampled: logits has to be [n_seqs, k + 1, vocab] with all rows the same stride apart")
     row = logits.stride(1) if k > 0 else logits.stride(0)
-    lib = load_library()
-    ws, size = c.workspace(workspace, lib.llma_verify_sampled_workspace(B, k, V))
-    c.run(lib.llma_verify_sampled, lp, lt, row if B * (k + 1) > 1 else max(row, V), V, B, k, c.ptr("drafts", drafts, i32, (B, k)),
-          None if n_draft is None else c.ptr("n_draft", n_draft, i32, (B,)), None if draft_probs is None else c.ptr("draft_probs", draft_probs, f32, (B, k, V)),
-          None if temperature is None else c.ptr("temperature", temperature, f32, (B,)), c.ptr("u_accept", u_accept, f32, (B, k)), c.ptr("u_sample", u_sample, f32, (B,)),
-          c.ptr("n_accepted", n_accepted, i32, (B,)), c.ptr("next_token", next_token, i32, (B,)), c.ptr("emitted", emitted, i32, (B, k + 1)), ws.data_ptr(), size)
+    ws, size = c.workspace(workspace, c.lib.llma_verify_sampled_workspace(B, k, V))
+    c.run(c.lib.llma_verify_sampled, lp, lt, row if B * (k + 1) > 1 else max(row, V), V, B, k, p("drafts", drafts, i32, (B, k)),
+          None if n_draft is None else p("n_draft", n_draft, i32, (B,)), None if draft_probs is None else p("draft_probs", draft_probs, f32, (B, k, V)),
+          None if temperature is None else p("temperature", temperature, f32, (B,)), p("u_accept", u_accept, f32, (B, k)), p("u_sample", u_sample, f32, (B,)),
+          p("n_accepted", n_accepted, i32, (B,)), p("next_token", next_token, i32, (B,)), p("emitted", emitted, i32, (B, k + 1)), ws.data_ptr(), size)
 
 
 def llma_verify_sampled_workspace(n_seqs: int, k: int, vocab: int) -> int:
