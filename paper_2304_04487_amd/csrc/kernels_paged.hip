@@ -54,139 +54,170 @@ __device__ __forceinline__ int count_le(const P *p, int n, int v) {
 #define MAP_ROWS_HERE 8192       // rows whose slots the same workgroup writes; more take a launch of many
 #define MAP_MAX_SLOTS 65536      // (bits of LDS that find a slot listed twice)
 
+// what is known of a sequence: of the workgroup's present 1024, and where they begin in three sums
 struct MapSeq { int slot, len, rows, own, need; };
-__device__ __forceinline__ MapSeq map_seq(const MapArgs &a, int b, bool ok) {
-    MapSeq s{0, 0, 0, 0, 0};
-    if (b >= a.n_seqs || !ok) return s;
-    s.slot = a.slots ? a.slots[b] : b;
-    s.len = a.lens[s.slot];
-    s.rows = a.rows[b];
-    s.own = a.owned[s.slot];
-    s.need = (int)(((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS);
-    return s;
-}
+struct MapTile { MapSeq seq[MAP_THREADS]; int first[MAP_THREADS]; };
+struct MapSums { int back, more, rows; };
 
-__device__ __forceinline__ void map_row(const MapArgs &a, int i, int total, const int *offsets) {
-    if (i >= total) {
-        a.slot_map[i] = -1;
-        a.row_pos[i] = 0;
-        return;
-    }
-    const int b = count_le(offsets + 1, a.n_seqs, i);
-    const int slot = a.slots ? a.slots[b] : b;
-    const int pos = a.lens[slot] + i - offsets[b];
+// exclusive prefix sums of three numbers over the workgroup, *total the sums
+__device__ __forceinline__ MapSums block_scan3(MapSums v, MapSums *part, MapSums *total) {
+    constexpr int NW = MAP_THREADS / 64;
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const MapSums in = {wave_scan(v.back), wave_scan(v.more), wave_scan(v.rows)};
+    __syncthreads();
+    if (lane == 63) part[wave] = in;
+    __syncthreads();
+    // (a wave's lanes look at the waves' sums side by side)
+    const MapSums p = lane < NW ? part[lane] : MapSums{0, 0, 0};
+    const MapSums c = {wave_scan(p.back), wave_scan(p.more), wave_scan(p.rows)};
+    const MapSums up_to = {__shfl(c.back, wave), __shfl(c.more, wave), __shfl(c.rows, wave)}, own = {__shfl(p.back, wave), __shfl(p.more, wave), __shfl(p.rows, wave)};
+    *total = MapSums{__shfl(c.back, NW - 1), __shfl(c.more, NW - 1), __shfl(c.rows, NW - 1)};
+    return MapSums{up_to.back - own.back + in.back - v.back, up_to.more - own.more + in.more - v.more, up_to.rows - own.rows + in.rows - v.rows};
+}
+__device__ __forceinline__ void map_row(const MapArgs &a, int i, int slot, int pos) {
     const int page = a.table[(size_t)slot * a.max_blocks + pos / PAGE_POS];
     a.slot_map[i] = (unsigned)page < (unsigned)a.n_pages ? page * PAGE_POS + pos % PAGE_POS : -1;      // (a free list that holds no page's number)
     a.row_pos[i] = pos;
 }
 
 __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
-    constexpr int NW = MAP_THREADS / 64;
-    __shared__ int part[NW];
+    __shared__ MapSums part[MAP_THREADS / 64];
     __shared__ unsigned listed[MAP_MAX_SLOTS / 32];
-    __shared__ int first[MAP_THREADS + 1];
+    __shared__ MapTile tile;
     __shared__ int bad;
-    __shared__ unsigned long long sums[3];                       // pages back, pages granted, rows
     const int t = threadIdx.x;
-    if (t == 0) { bad = 0; sums[0] = sums[1] = sums[2] = 0; }
+    const int top = *a.n_free;
+    if (t == 0) bad = 0;
     if (a.slots)
         for (int w = t; w < (a.n_slots + 31) / 32; w += MAP_THREADS) listed[w] = 0;
     __syncthreads();
-    // ---- what the lists ask for, and whether they make sense
-    for (int b = t; b < a.n_seqs; b += MAP_THREADS) {
-        const int slot = a.slots ? a.slots[b] : b;
-        if ((unsigned)slot >= (unsigned)a.n_slots) { atomicMin(&bad, LLMA_E_RANGE); continue; }
-        if (a.slots && (atomicOr(&listed[slot / 32], 1u << (slot % 32)) >> (slot % 32) & 1)) { atomicMin(&bad, LLMA_E_INVAL); continue; }
-        const int len = a.lens[slot], rows = a.rows[b], own = a.owned[slot];
-        if (len < 0 || rows < 0 || own < 0 || own > a.max_blocks) { atomicMin(&bad, LLMA_E_INVAL); continue; }
-        const long long need = ((long long)len + rows + PAGE_POS - 1) / PAGE_POS;
-        if (need > a.max_blocks) { atomicMin(&bad, LLMA_E_RANGE); continue; }
-        if (own > need) atomicAdd(&sums[0], (unsigned long long)(own - need));
-        if (need > own) atomicAdd(&sums[1], (unsigned long long)(need - own));
-        atomicAdd(&sums[2], (unsigned long long)rows);
+    // ---- what the lists ask for, and whether they make sense.  (Sums of 32 bits: a sequence asks for max_blocks pages at most, so 64-bit sums are
+    // taken over the tiles; a tile's are below 1024 * 2^25.)
+    const auto load = [&](int b) {
+        MapSeq s{-1, 0, 0, 0, 0};
+        if (b >= a.n_seqs) return s;
+        s.slot = a.slots ? a.slots[b] : b;
+        if ((unsigned)s.slot >= (unsigned)a.n_slots) { s.slot = -2; return s; }
+        s.len = a.lens[s.slot];
+        s.rows = a.rows[b];
+        s.own = a.owned[s.slot];
+        s.need = (int)(((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS);
+        return s;
+    };
+    MapSeq mine{};                                               // of the first tile, which is all there is up to 1024 sequences
+    long long back = 0, more = 0, rows = 0;
+    for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
+        MapSeq s = load(b0 + t);
+        int code = 0;
+        if (s.slot == -2) code = LLMA_E_RANGE;
+        else if (s.slot >= 0) {
+            const bool twice = a.slots && (atomicOr(&listed[s.slot / 32], 1u << (s.slot % 32)) >> (s.slot % 32) & 1);
+            if (twice || s.len < 0 || s.rows < 0 || s.own < 0 || s.own > a.max_blocks) code = LLMA_E_INVAL;
+            else if (((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS > a.max_blocks) code = LLMA_E_RANGE;
+        }
+        if (code) { atomicMin(&bad, code); s.own = s.need = s.rows = 0; }
+        // (rows above 2^20 in one sequence are summed apart: 1024 of them stay below 2^31)
+        MapSums sums;
+        (void)block_scan3(MapSums{s.own > s.need ? s.own - s.need : 0, s.need > s.own ? s.need - s.own : 0, s.rows & 0xfffff}, part, &sums);
+        back += sums.back; more += sums.more; rows += sums.rows;
+        (void)block_scan3(MapSums{0, 0, s.rows >> 20}, part, &sums);
+        rows += (long long)sums.rows << 20;
+        if (b0 == 0) mine = s;
     }
     __syncthreads();
-    const int top = *a.n_free;
     int status = bad;
-    if (status == 0 && (top < 0 || sums[0] > (unsigned long long)a.n_pages || top > a.n_pages - (int)sums[0])) status = LLMA_E_INVAL;
+    if (status == 0 && (top < 0 || back > a.n_pages || top > a.n_pages - (int)back)) status = LLMA_E_INVAL;
     // (without a slot map only the tables and offsets are wanted: any number of rows)
-    if (status == 0 && (sums[2] > 0x7fffffffull || (a.max_rows > 0 && sums[2] > (unsigned long long)a.max_rows))) status = LLMA_E_RANGE;
-    const int stack = top + (status == 0 ? (int)sums[0] : 0);    // its height once everything is back
-    if (status == 0 && sums[1] > (unsigned long long)stack) status = (int)(sums[1] - (unsigned long long)stack);
-    const bool ok = status == 0;
-    const int total = ok ? (int)sums[2] : 0;
+    if (status == 0 && (rows > 0x7fffffffll || (a.max_rows > 0 && rows > a.max_rows))) status = LLMA_E_RANGE;
+    const int stack = top + (status == 0 ? (int)back : 0);       // its height once everything is back
+    if (status == 0 && more > stack) status = (int)(more - stack);
+    const bool ok = status == 0, here = a.max_rows <= MAP_ROWS_HERE;
     if (t == 0) *a.status = status;
-    if (ok) {
+    // a tile's sequences and their places, for threads that look them up by page or row
+    const auto look = [&](int b0) {
+        const MapSeq s = b0 == 0 ? mine : load(b0 + t);
+        __syncthreads();
+        tile.seq[t] = s;
+        return s;
+    };
+    if (ok && back > 0) {
         // ---- pages that go back: the j-th of them in granting order lies j below the stack's new top
         int before = 0;
         for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
-            const MapSeq s = map_seq(a, b0 + t, true);
-            int sum;
-            const int at = block_scan<NW>(s.own > s.need ? s.own - s.need : 0, part, &sum);
-            first[t] = at;
-            if (t == 0) first[MAP_THREADS] = sum;
+            const MapSeq s = look(b0);
+            MapSums sum;
+            tile.first[t] = block_scan3(MapSums{s.own > s.need ? s.own - s.need : 0, 0, 0}, part, &sum).back;
             __syncthreads();
-            for (int i = t; i < sum; i += MAP_THREADS) {
-                const int q = count_le(first, MAP_THREADS, i) - 1;
-                const MapSeq o = map_seq(a, b0 + q, true);
-                int *entry = a.table + (size_t)o.slot * a.max_blocks + o.need + (i - first[q]);
+            for (int i = t; i < sum.back; i += MAP_THREADS) {
+                const int q = count_le(tile.first, MAP_THREADS, i) - 1;
+                int *entry = a.table + (size_t)tile.seq[q].slot * a.max_blocks + tile.seq[q].need + (i - tile.first[q]);
                 a.free_pages[stack - 1 - (before + i)] = *entry;
                 *entry = -1;
             }
-            before += sum;
-            __syncthreads();
+            before += sum.back;
         }
         __syncthreads();
-        // ---- pages that are granted
-        before = 0;
-        for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
-            const MapSeq s = map_seq(a, b0 + t, true);
-            int sum;
-            const int at = block_scan<NW>(s.need > s.own ? s.need - s.own : 0, part, &sum);
-            first[t] = at;
-            if (t == 0) first[MAP_THREADS] = sum;
-            __syncthreads();
-            for (int i = t; i < sum; i += MAP_THREADS) {
-                const int q = count_le(first, MAP_THREADS, i) - 1;
-                const MapSeq o = map_seq(a, b0 + q, true);
-                a.table[(size_t)o.slot * a.max_blocks + o.own + (i - first[q])] = a.free_pages[stack - 1 - (before + i)];
-            }
-            before += sum;
-            __syncthreads();                                     // (everyone has read owned)
-            if (b0 + t < a.n_seqs) a.owned[s.slot] = s.need;
-        }
-        if (t == 0) *a.n_free = stack - before;
     }
-    // ---- rows
-    int before = 0;
+    // ---- pages that are granted, and the rows
+    int granted = 0, row0 = 0;
     for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
-        const int b = b0 + t;
-        int len = 0, rows = 0;
-        if (b < a.n_seqs) {
-            const int slot = a.slots ? a.slots[b] : b;
-            if ((unsigned)slot < (unsigned)a.n_slots) len = a.lens[slot];
-            if (ok) rows = a.rows[b];
+        MapSeq s = look(b0);
+        if (!ok) s.rows = 0;
+        MapSums sum;
+        const MapSums at = block_scan3(MapSums{0, ok && s.need > s.own ? s.need - s.own : 0, s.rows}, part, &sum);
+        if (b0 + t < a.n_seqs) {
+            a.row_offsets[b0 + t] = row0 + at.rows;
+            a.lens_after[b0 + t] = s.len + s.rows;
         }
-        int sum;
-        const int at = block_scan<NW>(rows, part, &sum);
-        if (b < a.n_seqs) {
-            a.row_offsets[b] = before + at;
-            a.lens_after[b] = len + rows;
+        if (sum.more > 0) {                                      // (uniform)
+            tile.first[t] = at.more;
+            __syncthreads();
+            for (int i = t; i < sum.more; i += MAP_THREADS) {
+                const int q = count_le(tile.first, MAP_THREADS, i) - 1;
+                a.table[(size_t)tile.seq[q].slot * a.max_blocks + tile.seq[q].own + (i - tile.first[q])] = a.free_pages[stack - 1 - (granted + i)];
+            }
+            granted += sum.more;
+            __syncthreads();
         }
-        before += sum;
+        if (ok && s.slot >= 0) a.owned[s.slot] = s.need;
+        if (here && sum.rows > 0) {
+            tile.first[t] = at.rows;
+            __syncthreads();
+            for (int i = t; i < sum.rows; i += MAP_THREADS) {
+                const int q = count_le(tile.first, MAP_THREADS, i) - 1;
+                map_row(a, row0 + i, tile.seq[q].slot, tile.seq[q].len + i - tile.first[q]);
+            }
+        }
+        row0 += sum.rows;
     }
-    if (t == 0) a.row_offsets[a.n_seqs] = before;
-    __syncthreads();
-    if (a.max_rows > MAP_ROWS_HERE) return;
-    for (int i = t; i < a.max_rows; i += MAP_THREADS) map_row(a, i, total, a.row_offsets);
+    if (t == 0) {
+        a.row_offsets[a.n_seqs] = row0;
+        if (ok) *a.n_free = stack - granted;
+    }
+    if (here)
+        for (int i = row0 + t; i < a.max_rows; i += MAP_THREADS) { a.slot_map[i] = -1; a.row_pos[i] = 0; }
 }
+#define MAP_OFFSETS 8192         // sequences whose offsets a workgroup of map_rows_kernel keeps in LDS
 __global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
-    const int total = a.row_offsets[a.n_seqs];
-    for (int i = blockIdx.x * 1024 + threadIdx.x; i < a.max_rows && i < (int)(blockIdx.x + 1) * 1024; i += 256) map_row(a, i, total, a.row_offsets);
+    __shared__ int offsets[MAP_OFFSETS + 1];
+    const bool kept = a.n_seqs <= MAP_OFFSETS;
+    if (kept)
+        for (int b = threadIdx.x; b <= a.n_seqs; b += 256) offsets[b] = a.row_offsets[b];
+    __syncthreads();
+    const int total = kept ? offsets[a.n_seqs] : a.row_offsets[a.n_seqs];
+    for (int i = blockIdx.x * 512 + threadIdx.x; i < a.max_rows && i < (int)(blockIdx.x + 1) * 512; i += 256) {
+        if (i >= total) {
+            a.slot_map[i] = -1;
+            a.row_pos[i] = 0;
+            continue;
+        }
+        const int b = kept ? count_le(offsets + 1, a.n_seqs, i) : count_le(a.row_offsets + 1, a.n_seqs, i), slot = a.slots ? a.slots[b] : b;
+        map_row(a, i, slot, a.lens[slot] + i - (kept ? offsets[b] : a.row_offsets[b]));
+    }
 }
 void launch_map_pages(const MapArgs &a, hipStream_t st) {
     hipLaunchKernelGGL(map_pages_kernel, dim3(1), dim3(MAP_THREADS), 0, st, a);
-    if (a.max_rows > MAP_ROWS_HERE) hipLaunchKernelGGL(map_rows_kernel, dim3((a.max_rows + 1023) / 1024), dim3(256), 0, st, a);
+    if (a.max_rows > MAP_ROWS_HERE) hipLaunchKernelGGL(map_rows_kernel, dim3((a.max_rows + 511) / 512), dim3(256), 0, st, a);
 }
 
 __global__ __launch_bounds__(256) void pass_rows_kernel(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots) {
@@ -227,8 +258,9 @@ __device__ __forceinline__ void row8(const void *p, int64_t at, float v[8]) {
 // values); a run that starts inside its page keeps the page's scale where that is larger, and where s is larger the
 // codes before it are rounded again to the new scale.  code = x / s rounded to nearest even: the division is exact, so the one rounding
 // to four significant bits is the format's.  +-inf become +-448, NaN stays NaN.
-// A wave per run and head holds the run in registers: 16 (8) lanes share a row's 128 (64) features, eight each, and a lane
-// has four neighbouring positions in turn, so that a dim's four codes leave as one word of the transposed V.
+// 16 (8) lanes share a row's 128 (64) features, eight each, and a lane has four neighbouring positions, so that a dim's four codes leave as one word
+// of the transposed V: a wave holds 16 (32) positions.  A prompt's pages take a wave for each 16 (32) positions, which agree on the maximum in LDS; a step's
+// runs, a few rows long, one wave.
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 // exponent of the scale: -64 .. 120
 __device__ __forceinline__ int scale_exponent(float amax) {
@@ -243,56 +275,65 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
 }
 __device__ __forceinline__ float code_value(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
 
-template <int DH, int TYPE, bool KEYS>
-__device__ __forceinline__ void append_run(const AppendArgs &a, int head, int row0, int n, int page, int off) {
+template <int DH, int TYPE, bool KEYS, int WAVES>
+__device__ __forceinline__ void append_run(const AppendArgs &a, int head, int row0, int n, int page, int off, float *shared_max) {
     constexpr int LPR = DH / 8;                     // lanes per row
     constexpr int QUADS = 64 / LPR;                 // groups of four positions a wave has at once
-    constexpr int ROUNDS = PAGE_POS / (4 * QUADS);
-    const int lane = threadIdx.x & 63, d0 = lane % LPR * 8, quad = lane / LPR;
+    const int lane = threadIdx.x & 63, wave = WAVES > 1 ? __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : 0;
+    const int d0 = lane % LPR * 8;
     const size_t block = (size_t)page * a.c.heads + head;
     uint8_t *const codes = (KEYS ? a.c.k : a.c.v) + block * (PAGE_POS * DH);
     float *const scale = (KEYS ? a.c.k_scale : a.c.v_scale) + block;
     const float old = off > 0 ? *scale : 0.f;
     const void *const src = KEYS ? a.k : a.v;
     const int64_t rs = KEYS ? a.k_row : a.v_row, hs = KEYS ? a.k_head : a.v_head;
-    float x[ROUNDS][4][8];
-    float amax = 0.f;
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r)
+    const int quad0 = off / 4, rounds = ((off + n - 1) / 4 - quad0) / QUADS + 1;      // (the run's groups, QUADS a round)
+    float x[4][8];
+    const auto load = [&](int r) {
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int i = 4 * (quad + r * QUADS) + j - off;
+            const int i = 4 * (quad0 + r * QUADS + lane / LPR) + j - off;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[r][j][e] = 0.f;
+            for (int e = 0; e < 8; ++e) x[j][e] = 0.f;
             if (i < 0 || i >= n) continue;
             if constexpr (TYPE == ROWS_TILED) {
                 const bf16_t *p = (const bf16_t *)src + head * hs;
                 if constexpr (KEYS) {
-                    row8<ROWS_BF16>(p, (int64_t)kcache_off(row0 + i, d0, DH), x[r][j]);
+                    row8<ROWS_BF16>(p, (int64_t)kcache_off(row0 + i, d0, DH), x[j]);
                 } else {
 #pragma unroll
-                    for (int e = 0; e < 8; ++e) x[r][j][e] = bf16_to_f32(p[vcache_off(row0 + i, d0 + e, DH)]);
+                    for (int e = 0; e < 8; ++e) x[j][e] = bf16_to_f32(p[vcache_off(row0 + i, d0 + e, DH)]);
                 }
             } else {
-                row8<TYPE>(src, (int64_t)(row0 + i) * rs + head * hs + d0, x[r][j]);
+                row8<TYPE>(src, (int64_t)(row0 + i) * rs + head * hs + d0, x[j]);
             }
         }
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r)
+    };
+    float amax = 0.f;
+    for (int r = wave; r < rounds; r += WAVES) {
+        load(r);
 #pragma unroll
         for (int j = 0; j < 4; ++j)
 #pragma unroll
             for (int e = 0; e < 8; ++e) {
-                const float m = fabsf(x[r][j][e]);
+                const float m = fabsf(x[j][e]);
                 amax = m < __builtin_huge_valf() ? fmaxf(amax, m) : amax;          // (false for NaN)
             }
+    }
     butterfly<32>([&](auto o) { amax = fmaxf(amax, lane_xor<o.value>(amax)); });
+    if constexpr (WAVES > 1) {
+        __syncthreads();                            // (the last run's maxima have been read)
+        if (lane == 0) shared_max[wave] = amax;
+        __syncthreads();
+#pragma unroll
+        for (int w = 0; w < WAVES; ++w) amax = fmaxf(amax, shared_max[w]);
+    }
     float s = pow2(scale_exponent(amax));
     if (off > 0) {
         if (s > old) {
             // the codes before the run, byte by byte: those of its own positions are not touched
             const float by = old / s;
-            for (int i = lane; i < off * DH; i += 64) {
+            for (int i = wave * 64 + lane; i < off * DH; i += 64 * WAVES) {
                 uint8_t *const c = KEYS ? codes + i : codes + (size_t)(i / off) * PAGE_POS + i % off;
                 *c = (uint8_t)codes4(code_value(*c) * by, 0.f, 0.f, 0.f);
             }
@@ -300,16 +341,16 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int head, int ro
             s = old;
         }
     }
-    if (lane == 0) *scale = s;
+    if (wave == 0 && lane == 0) *scale = s;
     const float inv = 1.f / s;                      // (exact)
-#pragma unroll
-    for (int r = 0; r < ROUNDS; ++r) {
-        const int p0 = 4 * (quad + r * QUADS);      // the lane's positions in the page
+    for (int r = wave; r < rounds; r += WAVES) {
+        if (rounds > WAVES) load(r);                // (a wave with several rounds has kept none)
+        const int p0 = 4 * (quad0 + r * QUADS + lane / LPR);     // the lane's positions in the page
         if (p0 + 3 < off || p0 >= off + n) continue;
         uint32_t w[4][2];                           // [position]: eight dims' codes
 #pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const float *v = x[r][j];
+            const float *v = x[j];
             w[j][0] = codes4(v[0] * inv, v[1] * inv, v[2] * inv, v[3] * inv);
             w[j][1] = codes4(v[4] * inv, v[5] * inv, v[6] * inv, v[7] * inv);
         }
@@ -335,53 +376,59 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int head, int ro
     }
 }
 
-// a wave per (window of rows, head, K or V): the runs that begin in the window, one after the other
-template <int DH, int TYPE>
-__global__ __launch_bounds__(256) void append_paged_kernel(AppendArgs a, int window, int n_windows) {
-    const int unit = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+// WAVES waves (WAVES > 1: a workgroup) per window of rows, head, and K or V: the runs that begin in the window, one after the other
+template <int DH, int TYPE, int WAVES>
+__global__ __launch_bounds__(WAVES == 1 ? 256 : 64 * WAVES) void append_paged_kernel(AppendArgs a, int window, int n_windows) {
+    __shared__ float shared_max[WAVES];
+    const int unit = WAVES == 1 ? blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6) : blockIdx.x;
     const int lane = threadIdx.x & 63;
     const int win = unit / (2 * a.c.heads), head = unit % (2 * a.c.heads) / 2;
     if (win >= n_windows) return;
-    const int r0 = win * window, r1 = r0 + window < a.n_rows ? r0 + window : a.n_rows;
-    const int i = r0 + lane;
-    int slot = -1, prev = -1;
-    if (i < r1) {
-        slot = a.slot_map[i];
-        prev = i > 0 ? a.slot_map[i - 1] : -1;
-    }
-    const bool live = slot >= 0 && slot / PAGE_POS < a.c.n_pages;
-    unsigned long long begins = __ballot(live && (prev < 0 || slot != prev + 1 || slot % PAGE_POS == 0));
+    const int r0 = win * window;
+    // the slots of the window and of the rows a run from it can reach; which of them go on from the row before
+    const auto slot_of = [&](int i) { return i >= 0 && i < a.n_rows ? a.slot_map[i] : -1; };
+    const int slot = slot_of(r0 + lane), behind = slot_of(r0 + 64 + lane);
+    int prev = __shfl_up(slot, 1), prev_behind = __shfl_up(behind, 1);
+    const int before = slot_of(r0 - 1), last = __builtin_amdgcn_readlane(slot, 63);
+    if (lane == 0) { prev = before; prev_behind = last; }
+    const auto goes_on = [&](int s, int p) { return p >= 0 && s == p + 1 && s % PAGE_POS != 0; };
+    const unsigned long long on = __ballot(goes_on(slot, prev)), on_behind = __ballot(goes_on(behind, prev_behind));
+    unsigned long long begins = __ballot(lane < window && slot >= 0 && slot / PAGE_POS < a.c.n_pages) & ~on;
     while (begins) {
         const int at = __builtin_ctzll(begins);
         begins &= begins - 1;
         const int first = __builtin_amdgcn_readlane(slot, at), off = first % PAGE_POS;
-        // its length: rows that follow with the slots that follow, to the page's end
-        const int left = PAGE_POS - off, j = r0 + at + lane;
-        const bool follows = lane < left && j < a.n_rows && a.slot_map[j < a.n_rows ? j : 0] == first + lane;
-        const unsigned long long same = __ballot(follows);
-        const int n = ~same == 0 ? 64 : __builtin_ctzll(~same);
-        if (unit & 1) append_run<DH, TYPE, false>(a, head, r0 + at, n, first / PAGE_POS, off);
-        else append_run<DH, TYPE, true>(a, head, r0 + at, n, first / PAGE_POS, off);
+        // its length: the rows that go on, 64 at most
+        const unsigned long long rest = at == 63 ? on_behind : (on >> (at + 1)) | (on_behind << (63 - at));
+        const int n = ~rest == 0 ? 64 : __builtin_ctzll(~rest) + 1;
+        if (unit & 1) append_run<DH, TYPE, false, WAVES>(a, head, r0 + at, n, first / PAGE_POS, off, shared_max);
+        else append_run<DH, TYPE, true, WAVES>(a, head, r0 + at, n, first / PAGE_POS, off, shared_max);
     }
 }
 
 void launch_append_paged(const AppendArgs &a, hipStream_t st) {
     if (a.n_rows < 1) return;
-    // a wave takes up to 64 rows' runs (a prompt's page); fewer while the chip has room for more waves (a step's runs are short)
+    // Windows of 64 rows (a prompt's pages) as long as they give the chip its waves, with all of a page's waves at work; else windows so small that there are
+    // enough of them, a wave each: a step's runs are short.
+    const int units = 2 * a.c.heads, waves = a.c.dh == 128 ? 4 : 2;
+    const bool pages = (int64_t)((a.n_rows + 63) / 64) * units * waves >= 2048;
     int window = 64;
-    while (window > 1 && (int64_t)((a.n_rows + window - 1) / window) * 2 * a.c.heads < 4096) window /= 2;
+    while (!pages && window > 1 && (int64_t)((a.n_rows + window - 1) / window) * units < 4096) window /= 2;
     const int n_windows = (a.n_rows + window - 1) / window;
-    const dim3 grid((unsigned)(((int64_t)n_windows * 2 * a.c.heads + 3) / 4));
-    auto go = [&](auto kernel) { hipLaunchKernelGGL(kernel, grid, dim3(256), 0, st, a, window, n_windows); };
-    auto of = [&](auto dh) {
-        constexpr int DH = decltype(dh)::value;
-        if (a.type == ROWS_BF16) go(append_paged_kernel<DH, ROWS_BF16>);
-        else if (a.type == ROWS_F16) go(append_paged_kernel<DH, ROWS_F16>);
-        else if (a.type == ROWS_F32) go(append_paged_kernel<DH, ROWS_F32>);
-        else go(append_paged_kernel<DH, ROWS_TILED>);
+    const int64_t n = (int64_t)n_windows * units;
+    auto of = [&](auto dh, auto type) {
+        constexpr int DH = decltype(dh)::value, TYPE = decltype(type)::value, W = DH == 128 ? 4 : 2;
+        if (pages) hipLaunchKernelGGL((append_paged_kernel<DH, TYPE, W>), dim3((unsigned)n), dim3(64 * W), 0, st, a, window, n_windows);
+        else hipLaunchKernelGGL((append_paged_kernel<DH, TYPE, 1>), dim3((unsigned)((n + 3) / 4)), dim3(256), 0, st, a, window, n_windows);
     };
-    if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
-    else of(std::integral_constant<int, 64>{});
+    auto typed = [&](auto dh) {
+        if (a.type == ROWS_BF16) of(dh, std::integral_constant<int, ROWS_BF16>{});
+        else if (a.type == ROWS_F16) of(dh, std::integral_constant<int, ROWS_F16>{});
+        else if (a.type == ROWS_F32) of(dh, std::integral_constant<int, ROWS_F32>{});
+        else of(dh, std::integral_constant<int, ROWS_TILED>{});
+    };
+    if (a.c.dh == 128) typed(std::integral_constant<int, 128>{});
+    else typed(std::integral_constant<int, 64>{});
 }
 
 // ---------------------------------------------------------------------------------------------

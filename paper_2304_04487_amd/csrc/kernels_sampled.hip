@@ -50,7 +50,7 @@ __device__ __forceinline__ double weight64(float x, float top, double inv_t) {
 struct RowPart { float top, sum; int where; };                   // of a chunk: maximum, sum of 2^((x - top) log2(e) / T), first index of the maximum
 
 // work: RowPart[rows][chunks] | per sequence: Choice | double weight sums [n_seqs][picks] (and, with draft probabilities, exponentials' sums before them)
-struct Choice { int accepted, row, token, residual; float top; int greedy; double sum; };
+struct Choice { int accepted, row, token, residual; float top; int greedy; double sum, inv_sum; };
 
 struct SampledPlan { int chunk_blocks, chunks, picks; int64_t at_choice, at_sums, bytes; };
 static SampledPlan sampled_plan(int n_seqs, int k, int vocab, int epb) {
@@ -129,9 +129,9 @@ __global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a
     }
 }
 
+template <int OFF> __device__ __forceinline__ double lane_xor64(double v) { return __longlong_as_double((long long)lane_xor<OFF>((unsigned long long)__double_as_longlong(v))); }
 __device__ __forceinline__ double block_sum(double v, double *part) {       // over 256 threads; part: LDS of four words
-#pragma unroll
-    for (int d = 32; d >= 1; d /= 2) v += __shfl_xor(v, d);
+    butterfly<32>([&](auto o) { v += lane_xor64<o.value>(v); });
     __syncthreads();
     if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = v;
     __syncthreads();
@@ -140,13 +140,20 @@ __device__ __forceinline__ double block_sum(double v, double *part) {       // o
 // inclusive prefix sum over 256 threads, *total the sum
 __device__ __forceinline__ double scan64(double v, double *part, double *total) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const double o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    double all = v;                              // of the lane's group of 1, 2, 4 .. lanes
+    const auto step = [&](auto o) {
+        const double other = lane_xor64<o.value>(all);
+        if (lane & o.value) v += other;
+        all += other;
+    };
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 8>{});
+    step(std::integral_constant<int, 16>{});
+    step(std::integral_constant<int, 32>{});
     __syncthreads();
-    if (lane == 63) part[wave] = v;
+    if (lane == 0) part[wave] = all;
     __syncthreads();
     double before = 0.0, sum = 0.0;
 #pragma unroll
@@ -184,43 +191,59 @@ __device__ __forceinline__ float logit_at(const SampledArgs &a, int64_t row, int
 
 // How many drafts of sequence b hold, and which row its token comes from.  All threads of a workgroup call it and get the same; lane j looks at
 // row j.  The sums of the rows' chunks are fp32: a test whose sides are nearer than 2^-15 of each other is decided
-// again with the row's sum in 64 bits (the sums are off by 4e-6 at most: 2e-7 of the exponent, which has 17 bits where weights still matter).
+// again with the row's sum in 64 bits (the sums are off by 5e-6 at most: 2e-7 of the exponent, which is up to 17 where weights still matter, and of a chunk's factor).
 template <int TYPE>
 __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, double *part) {
     const int lane = threadIdx.x & 63;
-    const int n_draft = drafts_of(a, b);
+    const int64_t row = (int64_t)b * (a.k + 1) + lane;
+    const bool in = lane <= a.k, tested = lane < a.k;
+    // everything that needs no other value first: a row's chunks eight at a time (those of rows that no draft leads to hold anything)
+    const RowPart *const p = (const RowPart *)a.work + (in ? row : (int64_t)b * (a.k + 1)) * plan.chunks;
     const float temp = a.temperature ? a.temperature[b] : 1.f;
+    int draft = -1;
+    float q = 1.f, u = 0.f;
+    if (tested) {
+        draft = a.drafts[(int64_t)b * a.draft_stride + lane];
+        u = a.u_accept[(int64_t)b * a.k + lane];
+    }
+    const int n_draft = drafts_of(a, b);
     const bool greedy = !(temp > 0.f);
     const double inv_t = greedy ? 0.0 : 1.0 / (double)temp;
-    float top = LLMA_NEG_INF;
-    double sum = 0.0;
-    int where = 0x7fffffff, draft = -1;
-    const int64_t row = (int64_t)b * (a.k + 1) + lane;
-    if (lane <= n_draft) {
-        const RowPart *p = (const RowPart *)a.work + row * plan.chunks;
-        for (int c = 0; c < plan.chunks; ++c) top = fmaxf(top, p[c].top);
-        for (int c = 0; c < plan.chunks; ++c) {
-            if (p[c].top == top && p[c].where < where) where = p[c].where;
-            if (!greedy && p[c].top > LLMA_NEG_INF)
-                sum += (double)p[c].sum * (p[c].top == top ? 1.0 : exp(((double)p[c].top - (double)top) * inv_t));
+    const float by = greedy ? 0.f : 1.44269504088896340736f / temp;
+    const bool fits = tested && (unsigned)draft < (unsigned)a.vocab;
+    const float logit = fits ? logit_at<TYPE>(a, row, draft) : 0.f;
+    if (fits && a.probs) q = a.probs[((int64_t)b * a.k + lane) * a.vocab + draft];
+    float top = LLMA_NEG_INF, sum = 0.f;
+    int where = 0x7fffffff;
+    for (int c0 = 0; c0 < plan.chunks; c0 += 8) {
+        RowPart x[8];
+#pragma unroll
+        for (int c = 0; c < 8; ++c) x[c] = p[c0 + c < plan.chunks ? c0 + c : c0];
+        float here = top;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) here = fmaxf(here, x[c].top);
+        // (a top that is infinite counts 1 by itself and leaves nothing to lower ones)
+        sum *= top == here ? 1.f : __builtin_amdgcn_exp2f((top - here) * by);
+        if (top != here) where = 0x7fffffff;
+        if (top == LLMA_NEG_INF) sum = 0.f;
+        top = here;
+#pragma unroll
+        for (int c = 0; c < 8; ++c) {
+            if (c0 + c >= plan.chunks) continue;
+            if (x[c].top == here && x[c].where < where) where = x[c].where;
+            if (x[c].top > LLMA_NEG_INF) sum += x[c].sum * (x[c].top == here ? 1.f : __builtin_amdgcn_exp2f((x[c].top - here) * by));
         }
     }
     double left = 0.0, right = 0.0;                              // u q sum < e
     bool ok = false, near = false;
-    float q = 1.f, u = 0.f;
-    if (lane < n_draft) {
-        draft = a.drafts[(int64_t)b * a.draft_stride + lane];
-        if ((unsigned)draft < (unsigned)a.vocab && top > LLMA_NEG_INF) {
-            if (greedy) {
-                ok = draft == where;
-            } else {
-                u = a.u_accept[(int64_t)b * a.k + lane];
-                if (a.probs) q = a.probs[((int64_t)b * a.k + lane) * a.vocab + draft];
-                right = weight64(logit_at<TYPE>(a, row, draft), top, inv_t);
-                left = (double)u * (double)q * sum;
-                ok = left < right;
-                near = right > 0.0 && fabs(left - right) <= 3e-5 * right;
-            }
+    if (lane < n_draft && fits && top > LLMA_NEG_INF) {
+        if (greedy) {
+            ok = draft == where;
+        } else {
+            right = weight64(logit, top, inv_t);
+            left = (double)u * (double)q * (double)sum;
+            ok = left < right;
+            near = right > 0.0 && fabs(left - right) <= 3e-5 * right;
         }
     }
     unsigned long long yes = __ballot(ok), unsure = __ballot(near);
@@ -246,7 +269,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
     c.top = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), n));
     c.token = c.residual ? __builtin_amdgcn_readlane(draft, n) : -1;       // the rejected draft
     if (greedy) c.token = __builtin_amdgcn_readlane(where, n);             // (0x7fffffff: nothing to choose)
-    c.sum = 0.0;
+    c.sum = c.inv_sum = 0.0;
     return c;
 }
 
@@ -263,7 +286,7 @@ __device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice
         if (blk < blocks && id >= 0 && id < a.vocab) {
             y = weight64(logit_of(x[e]), c.top, inv_t);
             if (minus) {
-                if (q) y = fmax(y / c.sum - (double)q[id], 0.0);
+                if (q) y = fmax(y * c.inv_sum - (double)q[id], 0.0);
                 else if (id == c.token) y = 0.0;
             }
         }
@@ -290,7 +313,11 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
         double s = 0.0;
         for (int i = threadIdx.x; i < plan.picks; i += 256) s += sums[i];
         c.sum = block_sum(s, part);
-        if (blockIdx.y == 0 && threadIdx.x == 0) choice->sum = c.sum;       // (the other fields are read by all, this one by the next kernel)
+        c.inv_sum = 1.0 / c.sum;
+        if (blockIdx.y == 0 && threadIdx.x == 0) {                          // (the other fields are read by all, these by the next kernel)
+            choice->sum = c.sum;
+            choice->inv_sum = c.inv_sum;
+        }
     }
     if (c.greedy) return;
     const double inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
@@ -317,37 +344,41 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
     __shared__ double part[4];
     __shared__ double s_range_before;
     __shared__ int s_range, s_token, s_last;
-    const int b = blockIdx.x, t = threadIdx.x, lane = t & 63;
-    Choice c = ((const Choice *)((const char *)a.work + plan.at_choice))[b];
+    const int b = blockIdx.x, t = threadIdx.x;
     const double *const base = (const double *)((const char *)a.work + plan.at_sums) + (int64_t)b * 2 * plan.picks;
+    // requested together: the choice, the first 256 ranges' sums of both passes, the random number, the drafts
+    const Choice c = ((const Choice *)((const char *)a.work + plan.at_choice))[b];
+    const double all0 = t < plan.picks ? base[t] : 0.0, left0 = a.probs && t < plan.picks ? base[plan.picks + t] : 0.0;
+    const double u = (double)a.u_sample[b], inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
+    const int draft = t < a.k ? a.drafts[(int64_t)b * a.draft_stride + t] : -1;
     int token = -1;
     if (c.greedy) {
         token = c.token == 0x7fffffff ? -1 : c.token;
     } else {
         const bool with_q = c.residual && a.probs != nullptr;
-        bool minus = c.residual;
-        const double *sums = with_q ? base + plan.picks : base;
+        bool minus = c.residual, all = !with_q;                  // which weights, which sums
+        const auto sum_of = [&](int i) { return i < plan.picks ? (i == t ? (all ? all0 : left0) : base[(all ? 0 : plan.picks) + i]) : 0.0; };
         double s = 0.0;
-        for (int i = t; i < plan.picks; i += 256) s += sums[i];
+        for (int i = t; i < plan.picks; i += 256) s += sum_of(i);
         double total = block_sum(s, part);
         if (c.residual && !(total > 0.0)) {                      // p nowhere above q: p itself
             minus = false;
             if (with_q) {
-                sums = base;
+                all = true;
                 total = c.sum;
             } else if (c.top > LLMA_NEG_INF) {
                 token = c.token;                                 // (the rejected token is the only one there is)
             }
         }
         if (total > 0.0) {
-            const double target = (double)a.u_sample[b] * total;
+            const double target = u * total;
             if (t == 0) { s_range = 0x7fffffff; s_last = -1; s_token = 0x7fffffff; }
             // the first range whose cumulative sum passes the target, else the last with a weight: 256 ranges at a time
             double before = 0.0, mine_before = 0.0;
             int mine = -1;                                       // the thread's first range that passes, else its last with a weight; what lies before it
             bool passed = false;
             for (int i0 = 0; i0 < plan.picks; i0 += 256) {
-                const double w = i0 + t < plan.picks ? sums[i0 + t] : 0.0, up_to = before + scan64(w, part, &s);
+                const double w = sum_of(i0 + t), up_to = before + scan64(w, part, &s);
                 before += s;
                 if (w > 0.0 && !passed) { mine = i0 + t; mine_before = up_to - w; passed = up_to > target; }
                 if (w > 0.0 && up_to > target) atomicMin(&s_range, i0 + t);
@@ -359,7 +390,6 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
             __syncthreads();
             if (t == 0) s_last = -1;
             __syncthreads();
-            const double inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
             const RowView v = row_view<TYPE>(a, c.row);
             const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
             const float *const q = with_q && minus ? a.probs + ((int64_t)b * a.k + c.accepted) * a.vocab : nullptr;
@@ -393,7 +423,7 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
     }
     if (t <= a.k) {
         int e = -1;
-        if (t < c.accepted) e = a.drafts[(int64_t)b * a.draft_stride + t];
+        if (t < c.accepted) e = draft;
         else if (t == c.accepted) e = token;
         a.emitted[(int64_t)b * a.emit_stride + t] = e;
     }
