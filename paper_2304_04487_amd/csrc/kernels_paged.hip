@@ -5,13 +5,20 @@
 // ---------------------------------------------------------------------------------------------
 // sums over a workgroup
 // ---------------------------------------------------------------------------------------------
-__device__ __forceinline__ int wave_scan(int v) {              // inclusive
+__device__ __forceinline__ int wave_scan(int v) {              // inclusive, by register moves: a lane's group of 1, 2, 4 .. lanes and what lies before it
     const int lane = threadIdx.x & 63;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-        const int o = __shfl_up(v, d);
-        if (lane >= d) v += o;
-    }
+    int all = v;
+    const auto step = [&](auto o) {
+        const int other = lane_xor<o.value>(all);
+        v += lane & o.value ? other : 0;
+        all += other;
+    };
+    step(std::integral_constant<int, 1>{});
+    step(std::integral_constant<int, 2>{});
+    step(std::integral_constant<int, 4>{});
+    step(std::integral_constant<int, 8>{});
+    step(std::integral_constant<int, 16>{});
+    step(std::integral_constant<int, 32>{});
     return v;
 }
 // exclusive prefix sum of v over the workgroup's NW waves, *total the sum; part: LDS of at least NW words, free again after the next barrier
@@ -56,23 +63,27 @@ __device__ __forceinline__ int count_le(const P *p, int n, int v) {
 
 // what is known of a sequence: of the workgroup's present 1024, and where they begin in three sums
 struct MapSeq { int slot, len, rows, own, need; };
-struct MapTile { MapSeq seq[MAP_THREADS]; int first[MAP_THREADS]; };
+template <int N> struct MapTile { MapSeq seq[N]; int first[N]; };
 struct MapSums { int back, more, rows; };
 
-// exclusive prefix sums of three numbers over the workgroup, *total the sums
+// exclusive prefix sums of three numbers over the workgroup's NW waves, *total the sums
+template <int NW>
 __device__ __forceinline__ MapSums block_scan3(MapSums v, MapSums *part, MapSums *total) {
-    constexpr int NW = MAP_THREADS / 64;
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const MapSums in = {wave_scan(v.back), wave_scan(v.more), wave_scan(v.rows)};
     __syncthreads();
     if (lane == 63) part[wave] = in;
     __syncthreads();
-    // (a wave's lanes look at the waves' sums side by side)
-    const MapSums p = lane < NW ? part[lane] : MapSums{0, 0, 0};
-    const MapSums c = {wave_scan(p.back), wave_scan(p.more), wave_scan(p.rows)};
-    const MapSums up_to = {__shfl(c.back, wave), __shfl(c.more, wave), __shfl(c.rows, wave)}, own = {__shfl(p.back, wave), __shfl(p.more, wave), __shfl(p.rows, wave)};
-    *total = MapSums{__shfl(c.back, NW - 1), __shfl(c.more, NW - 1), __shfl(c.rows, NW - 1)};
-    return MapSums{up_to.back - own.back + in.back - v.back, up_to.more - own.more + in.more - v.more, up_to.rows - own.rows + in.rows - v.rows};
+    MapSums before{0, 0, 0}, all{0, 0, 0};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+        const MapSums p = part[w];
+        const int in_front = w < wave ? -1 : 0;
+        before.back += p.back & in_front; before.more += p.more & in_front; before.rows += p.rows & in_front;
+        all.back += p.back; all.more += p.more; all.rows += p.rows;
+    }
+    *total = all;
+    return MapSums{before.back + in.back - v.back, before.more + in.more - v.more, before.rows + in.rows - v.rows};
 }
 __device__ __forceinline__ void map_row(const MapArgs &a, int i, int slot, int pos) {
     const int page = a.table[(size_t)slot * a.max_blocks + pos / PAGE_POS];
@@ -80,34 +91,37 @@ __device__ __forceinline__ void map_row(const MapArgs &a, int i, int slot, int p
     a.row_pos[i] = pos;
 }
 
-__global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
-    __shared__ MapSums part[MAP_THREADS / 64];
+template <int N>
+__global__ __launch_bounds__(N) void map_pages_kernel(MapArgs a) {
+    constexpr int NW = N / 64;
+    __shared__ MapSums part[NW];
     __shared__ unsigned listed[MAP_MAX_SLOTS / 32];
-    __shared__ MapTile tile;
-    __shared__ int bad;
+    __shared__ MapTile<N> tile;
+    __shared__ int bad, many;
     const int t = threadIdx.x;
     const int top = *a.n_free;
-    if (t == 0) bad = 0;
-    if (a.slots)
-        for (int w = t; w < (a.n_slots + 31) / 32; w += MAP_THREADS) listed[w] = 0;
-    __syncthreads();
-    // ---- what the lists ask for, and whether they make sense.  (Sums of 32 bits: a sequence asks for max_blocks pages at most, so 64-bit sums are
-    // taken over the tiles; a tile's are below 1024 * 2^25.)
     const auto load = [&](int b) {
         MapSeq s{-1, 0, 0, 0, 0};
         if (b >= a.n_seqs) return s;
+        s.rows = a.rows[b];
         s.slot = a.slots ? a.slots[b] : b;
         if ((unsigned)s.slot >= (unsigned)a.n_slots) { s.slot = -2; return s; }
         s.len = a.lens[s.slot];
-        s.rows = a.rows[b];
         s.own = a.owned[s.slot];
         s.need = (int)(((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS);
         return s;
     };
-    MapSeq mine{};                                               // of the first tile, which is all there is up to 1024 sequences
+    const auto sums_of = [](const MapSeq &s) { return MapSums{s.own > s.need ? s.own - s.need : 0, s.need > s.own ? s.need - s.own : 0, s.rows}; };
+    MapSeq mine = load(t);                                       // of the first tile, which is all there is up to N sequences
+    if (t == 0) bad = many = 0;
+    if (a.slots)
+        for (int w = t; w < (a.n_slots + 31) / 32; w += N) listed[w] = 0;
+    __syncthreads();
+    // ---- what the lists ask for, and whether they make sense
+    MapSums at_mine{}, sum_mine{};
     long long back = 0, more = 0, rows = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
-        MapSeq s = load(b0 + t);
+    for (int b0 = 0; b0 < a.n_seqs; b0 += N) {
+        MapSeq s = b0 == 0 ? mine : load(b0 + t);
         int code = 0;
         if (s.slot == -2) code = LLMA_E_RANGE;
         else if (s.slot >= 0) {
@@ -116,15 +130,24 @@ __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
             else if (((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS > a.max_blocks) code = LLMA_E_RANGE;
         }
         if (code) { atomicMin(&bad, code); s.own = s.need = s.rows = 0; }
-        // (rows above 2^20 in one sequence are summed apart: 1024 of them stay below 2^31)
-        MapSums sums;
-        (void)block_scan3(MapSums{s.own > s.need ? s.own - s.need : 0, s.need > s.own ? s.need - s.own : 0, s.rows & 0xfffff}, part, &sums);
-        back += sums.back; more += sums.more; rows += sums.rows;
-        (void)block_scan3(MapSums{0, 0, s.rows >> 20}, part, &sums);
-        rows += (long long)sums.rows << 20;
-        if (b0 == 0) mine = s;
+        if (s.rows > 1 << 20) many = 1;                          // (their sum may pass 32 bits; a tile's pages do not: 1024 times 2^25 would, but 2^25 are all there can be)
+        MapSums sum;
+        const MapSums at = block_scan3<NW>(sums_of(s), part, &sum);
+        back += sum.back; more += sum.more; rows += sum.rows;
+        if (b0 == 0) { at_mine = at; sum_mine = sum; }
     }
     __syncthreads();
+    if (many) {                                                  // rare: the rows once more, in pieces of 20 bits
+        rows = 0;
+        for (int b0 = 0; b0 < a.n_seqs; b0 += N) {
+            const MapSeq s = b0 == 0 ? mine : load(b0 + t);
+            const int r = s.slot >= 0 && s.rows > 0 ? s.rows : 0;
+            MapSums sum;
+            (void)block_scan3<NW>(MapSums{r & 0xfffff, r >> 20, 0}, part, &sum);
+            rows += sum.back + ((long long)sum.more << 20);
+        }
+        __syncthreads();
+    }
     int status = bad;
     if (status == 0 && (top < 0 || back > a.n_pages || top > a.n_pages - (int)back)) status = LLMA_E_INVAL;
     // (without a slot map only the tables and offsets are wanted: any number of rows)
@@ -134,8 +157,10 @@ __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
     const bool ok = status == 0, here = a.max_rows <= MAP_ROWS_HERE;
     if (t == 0) *a.status = status;
     // a tile's sequences and their places, for threads that look them up by page or row
-    const auto look = [&](int b0) {
+    const auto look = [&](int b0, MapSums *at, MapSums *sum) {
         const MapSeq s = b0 == 0 ? mine : load(b0 + t);
+        if (b0 == 0) { *at = at_mine; *sum = sum_mine; }
+        else *at = block_scan3<NW>(sums_of(s), part, sum);
         __syncthreads();
         tile.seq[t] = s;
         return s;
@@ -143,13 +168,13 @@ __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
     if (ok && back > 0) {
         // ---- pages that go back: the j-th of them in granting order lies j below the stack's new top
         int before = 0;
-        for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
-            const MapSeq s = look(b0);
-            MapSums sum;
-            tile.first[t] = block_scan3(MapSums{s.own > s.need ? s.own - s.need : 0, 0, 0}, part, &sum).back;
+        for (int b0 = 0; b0 < a.n_seqs; b0 += N) {
+            MapSums at, sum;
+            (void)look(b0, &at, &sum);
+            tile.first[t] = at.back;
             __syncthreads();
-            for (int i = t; i < sum.back; i += MAP_THREADS) {
-                const int q = count_le(tile.first, MAP_THREADS, i) - 1;
+            for (int i = t; i < sum.back; i += N) {
+                const int q = count_le(tile.first, N, i) - 1;
                 int *entry = a.table + (size_t)tile.seq[q].slot * a.max_blocks + tile.seq[q].need + (i - tile.first[q]);
                 a.free_pages[stack - 1 - (before + i)] = *entry;
                 *entry = -1;
@@ -160,20 +185,19 @@ __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
     }
     // ---- pages that are granted, and the rows
     int granted = 0, row0 = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += MAP_THREADS) {
-        MapSeq s = look(b0);
-        if (!ok) s.rows = 0;
-        MapSums sum;
-        const MapSums at = block_scan3(MapSums{0, ok && s.need > s.own ? s.need - s.own : 0, s.rows}, part, &sum);
+    for (int b0 = 0; b0 < a.n_seqs; b0 += N) {
+        MapSums at, sum;
+        const MapSeq s = look(b0, &at, &sum);
+        if (!ok) at = sum = MapSums{0, 0, 0};
         if (b0 + t < a.n_seqs) {
             a.row_offsets[b0 + t] = row0 + at.rows;
-            a.lens_after[b0 + t] = s.len + s.rows;
+            a.lens_after[b0 + t] = s.len + (ok ? s.rows : 0);
         }
         if (sum.more > 0) {                                      // (uniform)
             tile.first[t] = at.more;
             __syncthreads();
-            for (int i = t; i < sum.more; i += MAP_THREADS) {
-                const int q = count_le(tile.first, MAP_THREADS, i) - 1;
+            for (int i = t; i < sum.more; i += N) {
+                const int q = count_le(tile.first, N, i) - 1;
                 a.table[(size_t)tile.seq[q].slot * a.max_blocks + tile.seq[q].own + (i - tile.first[q])] = a.free_pages[stack - 1 - (granted + i)];
             }
             granted += sum.more;
@@ -183,8 +207,8 @@ __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
         if (here && sum.rows > 0) {
             tile.first[t] = at.rows;
             __syncthreads();
-            for (int i = t; i < sum.rows; i += MAP_THREADS) {
-                const int q = count_le(tile.first, MAP_THREADS, i) - 1;
+            for (int i = t; i < sum.rows; i += N) {
+                const int q = count_le(tile.first, N, i) - 1;
                 map_row(a, row0 + i, tile.seq[q].slot, tile.seq[q].len + i - tile.first[q]);
             }
         }
@@ -195,7 +219,7 @@ __global__ __launch_bounds__(MAP_THREADS) void map_pages_kernel(MapArgs a) {
         if (ok) *a.n_free = stack - granted;
     }
     if (here)
-        for (int i = row0 + t; i < a.max_rows; i += MAP_THREADS) { a.slot_map[i] = -1; a.row_pos[i] = 0; }
+        for (int i = row0 + t; i < a.max_rows; i += N) { a.slot_map[i] = -1; a.row_pos[i] = 0; }
 }
 #define MAP_OFFSETS 8192         // sequences whose offsets a workgroup of map_rows_kernel keeps in LDS
 __global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
@@ -216,7 +240,9 @@ __global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
     }
 }
 void launch_map_pages(const MapArgs &a, hipStream_t st) {
-    hipLaunchKernelGGL(map_pages_kernel, dim3(1), dim3(MAP_THREADS), 0, st, a);
+    // (a step of a few sequences: four waves wait for each other sooner than sixteen)
+    if (a.n_seqs <= 256 && a.max_rows <= 2048) hipLaunchKernelGGL(map_pages_kernel<256>, dim3(1), dim3(256), 0, st, a);
+    else hipLaunchKernelGGL(map_pages_kernel<MAP_THREADS>, dim3(1), dim3(MAP_THREADS), 0, st, a);
     if (a.max_rows > MAP_ROWS_HERE) hipLaunchKernelGGL(map_rows_kernel, dim3((a.max_rows + 511) / 512), dim3(256), 0, st, a);
 }
 

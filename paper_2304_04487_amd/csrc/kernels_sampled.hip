@@ -42,10 +42,31 @@ __device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? LLMA_NEG_INF : x; }           // NaN: a token that cannot be
-// e^((x - top) / T) in 64 bits; the top itself (also +inf) counts 1, minus infinity 0
-__device__ __forceinline__ double weight64(float x, float top, double inv_t) {
-    return x == top ? (x == LLMA_NEG_INF ? 0.0 : 1.0) : x == LLMA_NEG_INF ? 0.0 : exp(((double)x - (double)top) * inv_t);
+// 2^y in 64 bits, y <= 0: the series of 2^f about 0 to f^11 for |f| <= 1/2 (the rest is below (ln 2 / 2)^12 / 12! = 7e-15 of it)
+__device__ __forceinline__ double exp2_64(double y) {
+    constexpr double L = 0.69314718055994530942;
+    y = fmax(y, -2000.0);                                        // (2^-2000 is 0; minus infinity)
+    const double k = __builtin_rint(y), f = (y - k) * L;
+    double p = 1.0 / 39916800.0;
+    p = __builtin_fma(p, f, 1.0 / 3628800.0);
+    p = __builtin_fma(p, f, 1.0 / 362880.0);
+    p = __builtin_fma(p, f, 1.0 / 40320.0);
+    p = __builtin_fma(p, f, 1.0 / 5040.0);
+    p = __builtin_fma(p, f, 1.0 / 720.0);
+    p = __builtin_fma(p, f, 1.0 / 120.0);
+    p = __builtin_fma(p, f, 1.0 / 24.0);
+    p = __builtin_fma(p, f, 1.0 / 6.0);
+    p = __builtin_fma(p, f, 0.5);
+    p = __builtin_fma(p, f, 1.0);
+    p = __builtin_fma(p, f, 1.0);
+    return __builtin_amdgcn_ldexp(p, (int)k);
 }
+// e^((x - top) / T) in 64 bits, by = log2(e) / T; the top itself (also +inf) counts 1, minus infinity 0
+__device__ __forceinline__ double weight64(float x, float top, double by) {
+    const double w = exp2_64(((double)x - (double)top) * by);
+    return x == LLMA_NEG_INF ? 0.0 : x == top ? 1.0 : w;
+}
+__device__ __forceinline__ double log2_scale(const SampledArgs &a, int b) { return 1.4426950408889634074 / (double)(a.temperature ? a.temperature[b] : 1.f); }
 
 struct RowPart { float top, sum; int where; };                   // of a chunk: maximum, sum of 2^((x - top) log2(e) / T), first index of the maximum
 
@@ -80,44 +101,78 @@ __global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a
     const bool greedy = !(temp > 0.f);
     const RowView v = row_view<TYPE>(a, row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB, first = blockIdx.y * plan.chunk_blocks;
-    float x[NB][EPB];
+    // the pieces stay as they come (unpacked twice they cost less than the registers of their values): requested together, then maximum, then sum
+    u32x4 x[NB];
     float top = LLMA_NEG_INF;
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
         const int blk = first + i * ROW_THREADS + t;
-        piece_values<TYPE>(v.base[blk < blocks ? blk : 0], x[i]);
+        x[i] = v.base[blk < blocks ? blk : 0];
     }
+    const int id0 = (first + t) * EPB - v.skip;                  // of the thread's first logit
+    // all pieces of the chunk wholly the row's: nothing to mask
+    const bool inside = first * EPB >= v.skip && (first + NB * ROW_THREADS) * (int64_t)EPB - v.skip <= a.vocab;
+    const auto values = [&](int i, float (&f)[EPB]) {
+        piece_values<TYPE>(x[i], f);
+        if (!inside) {
+#pragma unroll
+            for (int e = 0; e < EPB; ++e) {
+                const int id = id0 + i * ROW_THREADS * EPB + e;
+                f[e] = id >= 0 && id < a.vocab ? f[e] : LLMA_NEG_INF;
+            }
+        }
+    };
 #pragma unroll
     for (int i = 0; i < NB; ++i) {
-        const int id0 = (first + i * ROW_THREADS + t) * EPB - v.skip;
+        float f[EPB];
+        values(i, f);
 #pragma unroll
-        for (int e = 0; e < EPB; ++e) {
-            x[i][e] = id0 + e >= 0 && id0 + e < a.vocab ? logit_of(x[i][e]) : LLMA_NEG_INF;
-            top = fmaxf(top, x[i][e]);
-        }
+        for (int e = 0; e < EPB; ++e) top = fmaxf(top, f[e]);     // (passes over NaN)
     }
     butterfly<32>([&](auto o) { top = fmaxf(top, lane_xor<o.value>(top)); });
     if (lane == 0) parts[t >> 6].top = top;
     __syncthreads();
     top = fmaxf(fmaxf(parts[0].top, parts[1].top), fmaxf(parts[2].top, parts[3].top));
+    // (or the compiler would keep the values of the first pass)
+#pragma unroll
+    for (int i = 0; i < NB; ++i) asm volatile("" : "+v"(x[i]));
     float sum = 0.f;
     int where = 0x7fffffff;
     if (greedy) {
 #pragma unroll
-        for (int i = NB - 1; i >= 0; --i)
+        for (int i = NB - 1; i >= 0; --i) {
+            float f[EPB];
+            values(i, f);
 #pragma unroll
             for (int e = EPB - 1; e >= 0; --e)
-                if (x[i][e] == top && top != LLMA_NEG_INF) where = (first + i * ROW_THREADS + t) * EPB - v.skip + e;
+                if (f[e] == top && top != LLMA_NEG_INF) where = id0 + i * ROW_THREADS * EPB + e;
+        }
         butterfly<32>([&](auto o) { const int w = lane_xor<o.value>(where); where = w < where ? w : where; });
     } else {
         const float by = 1.44269504088896340736f / temp;
 #pragma unroll
-        for (int i = 0; i < NB; ++i)
+        for (int i = 0; i < NB; ++i) {
+            float f[EPB];
+            values(i, f);
 #pragma unroll
-            for (int e = 0; e < EPB; ++e) {
-                const float w = x[i][e] == top ? 1.f : __builtin_amdgcn_exp2f((x[i][e] - top) * by);
-                sum += x[i][e] == LLMA_NEG_INF ? 0.f : w;
+            for (int e = 0; e < EPB; ++e) sum += __builtin_amdgcn_exp2f((f[e] - top) * by);
+        }
+        if (sum != sum) {                                        // a NaN among them, or an infinite top: token by token
+            sum = 0.f;
+#pragma unroll 1
+            for (int i = 0; i < NB; ++i) {
+                float f[EPB];
+                const int blk = first + i * ROW_THREADS + t;
+                piece_values<TYPE>(v.base[blk < blocks ? blk : 0], f);
+#pragma unroll
+                for (int e = 0; e < EPB; ++e) {
+                    const int id = id0 + i * ROW_THREADS * EPB + e;
+                    const float l = id >= 0 && id < a.vocab ? logit_of(f[e]) : LLMA_NEG_INF;
+                    const float w = l == top ? 1.f : __builtin_amdgcn_exp2f((l - top) * by);
+                    sum += l == LLMA_NEG_INF ? 0.f : w;
+                }
             }
+        }
         butterfly<32>([&](auto o) { sum += lane_xor<o.value>(sum); });
     }
     if (lane == 0) { parts[t >> 6].sum = sum; parts[t >> 6].where = where; }
@@ -165,7 +220,7 @@ __device__ __forceinline__ double scan64(double v, double *part, double *total) 
     return before + v;
 }
 template <int TYPE>
-__device__ double row_sum64(const SampledArgs &a, int64_t row, float top, double inv_t, double *part) {
+__device__ double row_sum64(const SampledArgs &a, int64_t row, float top, double by, double *part) {
     constexpr int EPB = sampled_epb<TYPE>;
     const RowView v = row_view<TYPE>(a, row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
@@ -176,7 +231,7 @@ __device__ double row_sum64(const SampledArgs &a, int64_t row, float top, double
 #pragma unroll
         for (int e = 0; e < EPB; ++e) {
             const int id = blk * EPB - v.skip + e;
-            if (id >= 0 && id < a.vocab) s += weight64(logit_of(x[e]), top, inv_t);
+            if (id >= 0 && id < a.vocab) s += weight64(logit_of(x[e]), top, by);
         }
     }
     return block_sum(s, part);
@@ -208,8 +263,8 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
     }
     const int n_draft = drafts_of(a, b);
     const bool greedy = !(temp > 0.f);
-    const double inv_t = greedy ? 0.0 : 1.0 / (double)temp;
-    const float by = greedy ? 0.f : 1.44269504088896340736f / temp;
+    const double by64 = greedy ? 0.0 : 1.4426950408889634074 / (double)temp;
+    const float by = (float)by64;
     const bool fits = tested && (unsigned)draft < (unsigned)a.vocab;
     const float logit = fits ? logit_at<TYPE>(a, row, draft) : 0.f;
     if (fits && a.probs) q = a.probs[((int64_t)b * a.k + lane) * a.vocab + draft];
@@ -240,7 +295,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
         if (greedy) {
             ok = draft == where;
         } else {
-            right = weight64(logit, top, inv_t);
+            right = weight64(logit, top, by64);
             left = (double)u * (double)q * (double)sum;
             ok = left < right;
             near = right > 0.0 && fabs(left - right) <= 3e-5 * right;
@@ -256,7 +311,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
         const int j = __builtin_ctzll(look);
         unsure &= ~(1ull << j);
         const float tj = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(top), j));
-        const double s = row_sum64<TYPE>(a, (int64_t)b * (a.k + 1) + j, tj, inv_t, part);
+        const double s = row_sum64<TYPE>(a, (int64_t)b * (a.k + 1) + j, tj, by64, part);
         const unsigned long long again = __ballot(lane == j && (double)u * (double)q * s < right);
         yes = (yes & ~(1ull << j)) | again;
     }
@@ -275,7 +330,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
 
 // the weights of a piece of the sampled row: e, or what is left of p once q is taken off
 template <int TYPE>
-__device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice &c, const RowView &v, int blocks, int blk, double inv_t, bool minus, const float *q, double w[sampled_epb<TYPE>]) {
+__device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice &c, const RowView &v, int blocks, int blk, double by, bool minus, const float *q, double w[sampled_epb<TYPE>]) {
     constexpr int EPB = sampled_epb<TYPE>;
     float x[EPB];
     piece_values<TYPE>(v.base[blk < blocks ? blk : 0], x);
@@ -284,7 +339,7 @@ __device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice
         const int id = blk * EPB - v.skip + e;
         double y = 0.0;
         if (blk < blocks && id >= 0 && id < a.vocab) {
-            y = weight64(logit_of(x[e]), c.top, inv_t);
+            y = weight64(logit_of(x[e]), c.top, by);
             if (minus) {
                 if (q) y = fmax(y * c.inv_sum - (double)q[id], 0.0);
                 else if (id == c.token) y = 0.0;
@@ -320,7 +375,7 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
         }
     }
     if (c.greedy) return;
-    const double inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
+    const double by = log2_scale(a, b);
     const RowView v = row_view<TYPE>(a, c.row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
     const bool minus = PASS == 1 || (a.probs == nullptr && c.residual);
@@ -329,7 +384,7 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
 #pragma unroll
     for (int i = 0; i < PICK_BLOCKS / 256; ++i) {
         double w[EPB];
-        piece_weights<TYPE>(a, c, v, blocks, blockIdx.y * PICK_BLOCKS + i * 256 + threadIdx.x, inv_t, minus, q, w);
+        piece_weights<TYPE>(a, c, v, blocks, blockIdx.y * PICK_BLOCKS + i * 256 + threadIdx.x, by, minus, q, w);
 #pragma unroll
         for (int e = 0; e < EPB; ++e) s += w[e];
     }
@@ -337,19 +392,40 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
     if (threadIdx.x == 0) sums[PASS * plan.picks + blockIdx.y] = s;
 }
 
-// a workgroup per sequence: the range the random number falls into, then the token in it
+// The first thread, in order, whose `hit` is set hands its two values to the workgroup, else the last whose `some` is; false if there is neither.  slots: LDS of eight
+struct Found { double at; int id; };
+__device__ __forceinline__ bool first_of(bool hit, bool some, double at, int id, Found *slots, Found *out) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    const unsigned long long hits = __ballot(hit), any = __ballot(some);
+    const int who = hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : -1;
+    if (lane == (who < 0 ? 0 : who)) slots[wave] = Found{at, who < 0 ? -1 : id};
+    if (lane == 0) slots[4 + wave].id = hits != 0;
+    __syncthreads();
+    int best = -1;
+#pragma unroll
+    for (int w = 3; w >= 0; --w)
+        if (slots[4 + w].id) best = w;
+    if (best < 0) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+            if (slots[w].id >= 0) best = w;
+    }
+    if (best >= 0) *out = slots[best];
+    return best >= 0;
+}
+// A workgroup per sequence: the range the random number falls into, then the token in it.  Bound by its chain: the choice and the ranges' sums, a scan, the range's
+// pieces (8 or 16 exponentials a thread), a scan.  With separate sums and scans, and atomics that look for the first hit, one sequence over 32000 tokens took 9.8 us where it takes 4.6.
 template <int TYPE>
 __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, SampledPlan plan) {
     constexpr int EPB = sampled_epb<TYPE>, PER = PICK_BLOCKS / 256;
     __shared__ double part[4];
-    __shared__ double s_range_before;
-    __shared__ int s_range, s_token, s_last;
+    __shared__ Found ranges[8], tokens[8];
     const int b = blockIdx.x, t = threadIdx.x;
     const double *const base = (const double *)((const char *)a.work + plan.at_sums) + (int64_t)b * 2 * plan.picks;
     // requested together: the choice, the first 256 ranges' sums of both passes, the random number, the drafts
     const Choice c = ((const Choice *)((const char *)a.work + plan.at_choice))[b];
     const double all0 = t < plan.picks ? base[t] : 0.0, left0 = a.probs && t < plan.picks ? base[plan.picks + t] : 0.0;
-    const double u = (double)a.u_sample[b], inv_t = 1.0 / (double)(a.temperature ? a.temperature[b] : 1.f);
+    const double u = (double)a.u_sample[b], by = log2_scale(a, b);
     const int draft = t < a.k ? a.drafts[(int64_t)b * a.draft_stride + t] : -1;
     int token = -1;
     if (c.greedy) {
@@ -358,52 +434,50 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
         const bool with_q = c.residual && a.probs != nullptr;
         bool minus = c.residual, all = !with_q;                  // which weights, which sums
         const auto sum_of = [&](int i) { return i < plan.picks ? (i == t ? (all ? all0 : left0) : base[(all ? 0 : plan.picks) + i]) : 0.0; };
-        double s = 0.0;
-        for (int i = t; i < plan.picks; i += 256) s += sum_of(i);
-        double total = block_sum(s, part);
+        double total, up_to, sum;                                // (up to 256 ranges: one scan gives both)
+        const auto add_up = [&]() {
+            up_to = scan64(sum_of(t), part, &total);
+            for (int i0 = 256; i0 < plan.picks; i0 += 256) total += block_sum(sum_of(i0 + t), part);
+        };
+        add_up();
         if (c.residual && !(total > 0.0)) {                      // p nowhere above q: p itself
             minus = false;
             if (with_q) {
                 all = true;
-                total = c.sum;
+                add_up();
             } else if (c.top > LLMA_NEG_INF) {
                 token = c.token;                                 // (the rejected token is the only one there is)
             }
         }
         if (total > 0.0) {
             const double target = u * total;
-            if (t == 0) { s_range = 0x7fffffff; s_last = -1; s_token = 0x7fffffff; }
-            // the first range whose cumulative sum passes the target, else the last with a weight: 256 ranges at a time
-            double before = 0.0, mine_before = 0.0;
-            int mine = -1;                                       // the thread's first range that passes, else its last with a weight; what lies before it
-            bool passed = false;
+            // the first range whose cumulative sum passes the target, else the last with a weight; what lies before it
+            Found range{0.0, -1}, found{0.0, -1};
+            double before = 0.0;
             for (int i0 = 0; i0 < plan.picks; i0 += 256) {
-                const double w = sum_of(i0 + t), up_to = before + scan64(w, part, &s);
-                before += s;
-                if (w > 0.0 && !passed) { mine = i0 + t; mine_before = up_to - w; passed = up_to > target; }
-                if (w > 0.0 && up_to > target) atomicMin(&s_range, i0 + t);
-                if (w > 0.0) atomicMax(&s_last, i0 + t);
+                const double w = sum_of(i0 + t);
+                if (i0 > 0) {
+                    __syncthreads();                             // (the last 256's answer has been read)
+                    up_to = before + scan64(w, part, &sum);
+                }
+                if (first_of(w > 0.0 && up_to > target, w > 0.0, up_to - w, i0 + t, ranges, &found)) range = found;
+                if (range.id >= 0 && range.at + sum_of(range.id) > target) break;
+                before = i0 == 0 ? part[0] + part[1] + part[2] + part[3] : before + sum;
             }
-            __syncthreads();
-            const int range = s_range != 0x7fffffff ? s_range : s_last;
-            if (mine == range) s_range_before = mine_before;
-            __syncthreads();
-            if (t == 0) s_last = -1;
-            __syncthreads();
             const RowView v = row_view<TYPE>(a, c.row);
             const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
             const float *const q = with_q && minus ? a.probs + ((int64_t)b * a.k + c.accepted) * a.vocab : nullptr;
             // a thread's pieces are neighbours, so that cumulative sums run along the threads
             double w[PER][EPB], own = 0.0;
-            const int blk0 = range * PICK_BLOCKS + t * PER;
+            const int blk0 = range.id * PICK_BLOCKS + t * PER;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                piece_weights<TYPE>(a, c, v, blocks, blk0 + i, inv_t, minus, q, w[i]);
+                piece_weights<TYPE>(a, c, v, blocks, blk0 + i, by, minus, q, w[i]);
 #pragma unroll
                 for (int e = 0; e < EPB; ++e) own += w[i][e];
             }
-            double run = s_range_before + scan64(own, part, &s) - own;
-            int found = 0x7fffffff, last = -1;
+            double run = range.at + scan64(own, part, &sum) - own;
+            int mine = -1, last = -1;
 #pragma unroll
             for (int i = 0; i < PER; ++i)
 #pragma unroll
@@ -412,13 +486,10 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
                     run += w[i][e];
                     if (w[i][e] > 0.0) {
                         last = id;
-                        if (run > target && found == 0x7fffffff) found = id;
+                        if (run > target && mine < 0) mine = id;
                     }
                 }
-            atomicMin(&s_token, found);
-            atomicMax(&s_last, last);
-            __syncthreads();
-            token = s_token != 0x7fffffff ? s_token : s_last;
+            if (first_of(mine >= 0, last >= 0, 0.0, mine >= 0 ? mine : last, tokens, &found)) token = found.id;
         }
     }
     if (t <= a.k) {
