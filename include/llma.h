@@ -296,8 +296,8 @@ int llma_append_paged(const llma_paged_cache *cache, const void *k, const void *
 /* Causal attention of a step's rows over the cache.  Rows row_offsets[b] .. row_offsets[b+1]-1 of q are sequence b's; row j of
  * m sees positions 0 .. lens[b] - m + j of the pages table[slots[b]] (lens counts the step's own rows, which
  * llma_append_paged has written).  out = softmax(scale * q K^T) V per head; query head h reads key head h / (n_heads /
- * n_kv_heads).  q, out: n_rows x n_heads x head_dim of dtype, strides in elements, pointers and strides multiples of 16 bytes; out may not overlap q.
- * max_rows: at least the rows of every sequence (further rows are not written); rows behind the last sequence's stay as they are.
+ * n_kv_heads).  q, out: n_rows x n_heads x head_dim of dtype, strides in elements, pointers and strides multiples of 16 bytes; rows of out may overlap neither each other nor q.
+ * max_rows: at least the rows of every sequence (a sequence's further rows are not written); rows behind the last sequence's stay as they are.
  * A row that sees nothing becomes 0.  Positions whose page number is outside [0, n_pages) are not seen.
  * work: llma_attend_paged_workspace(...) bytes, 16-byte aligned. */
 int64_t llma_attend_paged_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);

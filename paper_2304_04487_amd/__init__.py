@@ -225,12 +225,16 @@ class _Call:
 
     def ptr(self, name, t, dtype, shape):
         """a contiguous tensor's address"""
+        if not isinstance(t, _torch.Tensor):
+            _refuse(f"{self.who}: {name} has to be a tensor")
         if t.dtype is dtype and t.shape == shape and t.device == self.device and t.is_contiguous():
             return t.data_ptr()
         _refuse(f"{self.who}: {name} has to be a contiguous {dtype} tensor of shape {tuple(shape)} on {self.device}, not {t.dtype} {tuple(t.shape)} on {t.device}")
 
     def rows(self, name, t, shape):
         """(address, dtype code) of rows whose features lie together, any other strides"""
+        if not isinstance(t, _torch.Tensor):
+            _refuse(f"{self.who}: {name} has to be a tensor")
         code = _ROW_TYPES.get(t.dtype)
         if code is not None and t.shape == shape and t.device == self.device and (t.stride(-1) == 1 or t.numel() == 0):
             return t.data_ptr(), code

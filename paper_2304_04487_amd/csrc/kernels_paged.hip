@@ -489,12 +489,13 @@ int64_t attend_paged_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads
     return ((int64_t)(n_seqs + 1 + 63) / 64 * 64 + attend_parts(p, kv_heads) * 16 * p.nt * (dh + 2)) * 4;
 }
 
-struct AttendSeq { int slot, len, rows, row0; };
+struct AttendSeq { int slot, len, rows, row0, seen; };          // seen: the last position that its first row sees
 // a sequence as the kernels take it: whatever the lists hold, nothing outside the buffers is reached
 __device__ __forceinline__ AttendSeq attend_seq(const AttendArgs &a, int b) {
     AttendSeq s;
     s.row0 = a.row_offsets[b];
     s.rows = a.row_offsets[b + 1] - s.row0;
+    const int all = s.rows;
     s.rows = s.rows > a.max_rows ? a.max_rows : s.rows;
     if (s.row0 < 0 || s.row0 > a.n_rows) s.rows = 0;
     else if (s.rows > a.n_rows - s.row0) s.rows = a.n_rows - s.row0;
@@ -503,11 +504,12 @@ __device__ __forceinline__ AttendSeq attend_seq(const AttendArgs &a, int b) {
     const int64_t most = (int64_t)a.max_blocks * PAGE_POS;
     if (s.len > most) s.len = (int)most;
     if (s.len < 0 || (unsigned)s.slot >= (unsigned)a.n_slots) s.len = 0;
+    s.seen = s.rows > 0 ? s.len - all : 0;
     return s;
 }
 // (of one sequence for the whole wave: values that came through vector loads or LDS, into scalar registers)
 __device__ __forceinline__ int uniform(int v) { return __builtin_amdgcn_readfirstlane(v); }
-__device__ __forceinline__ AttendSeq uniform(AttendSeq s) { return AttendSeq{uniform(s.slot), uniform(s.len), uniform(s.rows), uniform(s.row0)}; }
+__device__ __forceinline__ AttendSeq uniform(AttendSeq s) { return AttendSeq{uniform(s.slot), uniform(s.len), uniform(s.rows), uniform(s.row0), uniform(s.seen)}; }
 __device__ __forceinline__ int attend_pages(const AttendSeq &s) {      // a sequence without positions still has rows to write
     if (s.rows <= 0) return 0;
     return s.len < 1 ? 1 : (s.len + PAGE_POS - 1) / PAGE_POS;
@@ -771,7 +773,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
             attend_load_q<DH, NT, TYPE>(a, after.s, head, group, r0, qr);
         }
         // the last position that every column sees, and each lane's columns' own
-        const int seen = s.len - s.rows;
+        const int seen = s.seen;
         int limit[NT];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
@@ -971,7 +973,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
     const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, b = rest % a.n_seqs, block = blocks - 1 - rest / a.n_seqs;
     const int group = a.n_heads / a.c.heads, r0 = block * 64 * NT;
     const AttendSeq s = uniform(attend_seq(a, b));
-    const int R = s.rows * group, seen = s.len - s.rows;
+    const int R = s.rows * group, seen = s.seen;
     if (r0 >= R) return;
     const int r1 = r0 + 64 * NT < R ? r0 + 64 * NT : R, furthest = seen + (r1 - 1) / group;        // the block's last position
     const int pages = furthest < 0 ? 0 : furthest / PAGE_POS + 1;
@@ -1270,7 +1272,8 @@ static void launch_attend_rows(const AttendArgs &a, hipStream_t st) {
 template <int DH, int TYPE>
 static void launch_attend_type(const AttendArgs &a, hipStream_t st) {
     constexpr int ROWS_NT = TYPE == ROWS_F32 ? 1 : 2;            // (three planes of queries and probabilities leave room for one tile)
-    if ((int64_t)a.max_rows * (a.n_heads / a.c.heads) > 64 && attend_row_blocks(a, ROWS_NT) >= ROWS_MIN) return launch_attend_rows<DH, ROWS_NT, TYPE>(a, st);
+    const int64_t group_rows = (int64_t)a.max_rows * (a.n_heads / a.c.heads), launched = (group_rows + 64 * ROWS_NT - 1) / (64 * ROWS_NT) * a.n_seqs * a.c.heads;
+    if (group_rows > 64 && attend_row_blocks(a, ROWS_NT) >= ROWS_MIN && launched < 1 << 23) return launch_attend_rows<DH, ROWS_NT, TYPE>(a, st);
     const AttendPlan p = attend_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);

@@ -956,6 +956,7 @@ extern "C" int llma_kv_import(llma_ctx *c, int32_t seq, int32_t layer, const voi
     if (len < 0 || len > c->cfg.max_seq) return fail(c, LLMA_E_RANGE, "llma_kv_import: len %d > max_seq %d", len, c->cfg.max_seq);
     const llma_model_cfg &g = c->cfg;
     if (c->paged) {
+        if (((uintptr_t)k | (uintptr_t)v) & 15) return fail(c, LLMA_E_INVAL, "llma_kv_import: k and v have to be 16-byte aligned for a paged cache");
         if (len > 0) {
             // the slot's pages for len positions (all layers have the same), then the rows into this layer's
             HIP_TRY(c, hipMemcpyAsync(c->pg_rows, &len, 4, hipMemcpyHostToDevice, c->st));

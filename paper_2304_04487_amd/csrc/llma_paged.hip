@@ -44,6 +44,7 @@ extern "C" int llma_map_pages(const int32_t *lens, const int32_t *rows, const in
     if (!lens || !rows || !table || !owned || !free_pages || !n_free || !row_offsets || !lens_after || !status) return refuse(LLMA_E_INVAL, "%s: null pointer", who);
     if (n_seqs < 1 || n_slots < 1 || max_blocks < 1 || n_pages < 1 || max_rows < 0) return refuse(LLMA_E_INVAL, "%s: need n_seqs, n_slots, max_blocks, n_pages >= 1 and max_rows >= 0", who);
     if (max_rows > 0 && (!slot_map || !row_pos)) return refuse(LLMA_E_INVAL, "%s: null slot_map or row_pos with max_rows > 0", who);
+    if (max_rows > 1 << 30) return refuse(LLMA_E_RANGE, "%s: max_rows %d, at most 2^30", who, max_rows);
     if (n_slots > 65536) return refuse(LLMA_E_RANGE, "%s: %d slots, at most 65536", who, n_slots);
     if (n_seqs > n_slots) return refuse(LLMA_E_RANGE, "%s: %d sequences in %d slots", who, n_seqs, n_slots);
     if (n_pages > 0x7fffffff / LLMA_PAGE || max_blocks > 0x7fffffff / LLMA_PAGE) return refuse(LLMA_E_RANGE, "%s: pages pass 32-bit slots", who);
@@ -65,7 +66,7 @@ extern "C" int llma_append_paged(const llma_paged_cache *cache, const void *k, c
     const int64_t es = item(type);
     if (!aligned(k) || !aligned(v) || !stride_ok(k_row_stride, es) || !stride_ok(k_head_stride, es) || !stride_ok(v_row_stride, es) || !stride_ok(v_head_stride, es))
         return refuse(LLMA_E_INVAL, "%s: rows must be 16-byte aligned (pointers and strides)", who);
-    if ((int64_t)n_rows * cache->n_kv_heads > (int64_t)1 << 33) return refuse(LLMA_E_RANGE, "%s: %d rows of %d heads in one call", who, n_rows, cache->n_kv_heads);
+    if ((int64_t)n_rows * cache->n_kv_heads > (int64_t)1 << 28) return refuse(LLMA_E_RANGE, "%s: %d rows of %d heads in one call", who, n_rows, cache->n_kv_heads);
     launch_append_paged(AppendArgs{taken(cache), k, v, k_row_stride, k_head_stride, v_row_stride, v_head_stride, slot_map, n_rows, type}, (hipStream_t)hip_stream);
     return enqueued(who);
 }
@@ -102,6 +103,10 @@ extern "C" int llma_attend_paged(const llma_paged_cache *cache, const void *q, i
     if (!aligned(q) || !aligned(out) || !stride_ok(q_row_stride, es) || !stride_ok(q_head_stride, es) || !stride_ok(out_row_stride, es) || !stride_ok(out_head_stride, es))
         return refuse(LLMA_E_INVAL, "%s: rows must be 16-byte aligned (pointers and strides)", who);
     if (out == q) return refuse(LLMA_E_INVAL, "%s: out is q", who);
+    // (rows of q may lie on top of each other, rows of out may not)
+    const bool heads_inside = out_head_stride >= cache->head_dim && (n_rows == 1 || out_row_stride >= (n_heads - 1) * out_head_stride + cache->head_dim);
+    const bool rows_inside = out_row_stride >= cache->head_dim && (n_heads == 1 || out_head_stride >= (n_rows - 1) * out_row_stride + cache->head_dim);
+    if (!(heads_inside || rows_inside || n_rows * (int64_t)n_heads == 1)) return refuse(LLMA_E_INVAL, "%s: rows of out overlap", who);
     const int64_t need = attend_paged_bytes(n_seqs, max_blocks, n_heads, cache->n_kv_heads, cache->head_dim, max_rows);
     if (!aligned(work) || work_bytes < need) return refuse(LLMA_E_INVAL, "%s: needs a 16-byte aligned workspace of %lld bytes", who, (long long)need);
     AttendArgs a{};
@@ -116,7 +121,7 @@ extern "C" int llma_attend_paged(const llma_paged_cache *cache, const void *q, i
 static int check_sampled(int n_seqs, int k, int vocab, const char *who) {
     if (n_seqs < 0 || k < 0 || vocab < 1) return refuse(LLMA_E_INVAL, "%s: need n_seqs, k >= 0 and vocab >= 1", who);
     if (k > LLMA_SAMPLED_MAX_K) return refuse(LLMA_E_RANGE, "%s: k %d, at most %d", who, k, LLMA_SAMPLED_MAX_K);
-    if (vocab > 1 << 24 || n_seqs > 1 << 20) return refuse(LLMA_E_RANGE, "%s: vocab %d, %d sequences (at most 2^24, 2^20)", who, vocab, n_seqs);
+    if (vocab > 1 << 24 || (int64_t)n_seqs * (k + 1) > 1 << 22) return refuse(LLMA_E_RANGE, "%s: vocab %d, %d sequences of %d rows (at most 2^24, 2^22 rows)", who, vocab, n_seqs, k + 1);
     return LLMA_OK;
 }
 extern "C" int64_t llma_verify_sampled_workspace(int32_t n_seqs, int32_t k, int32_t vocab) {

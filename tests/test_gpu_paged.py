@@ -387,6 +387,23 @@ def test_attend_strides_workspace_and_streams(llma):
     assert torch.equal(plain, o2)
 
 
+@pytest.mark.parametrize("heads,kv,rows,most", [(8, 4, [9, 5], 6), (96, 96, [90, 70], 68)])
+def test_attend_writes_max_rows_of_a_sequence_at_most(llma, heads, kv, rows, most):
+    """what is written is what a call for all rows writes there; q that ends inside the last sequence likewise"""
+    lens = [130, 75]
+    c, q, table, slots, off = attend_case(llma, lens, rows, heads, kv, 64, "bf16", 73)
+    args = (i32(table), i32(lens), i32(off))
+    full = llma.llma_attend_paged(c, q, *args, max(rows), 0.125, torch.empty_like(q), slots=i32(slots))
+    some = llma.llma_attend_paged(c, q, *args, most, 0.125, torch.full_like(q, 7.0), slots=i32(slots))
+    for b in range(2):
+        a, e = off[b], off[b + 1]
+        m = min(most, rows[b])
+        assert (some[a:a + m].float() - full[a:a + m].float()).abs().max() <= 2.0 ** -6 * full.float().abs().max()      # (another form may have computed it)
+        assert (some[a + m:e] == 7.0).all()
+    short = llma.llma_attend_paged(c, q[:off[1] + 2], *args, max(rows), 0.125, torch.full_like(q, 7.0)[:off[1] + 2], slots=i32(slots))
+    assert (short.float() - full[:off[1] + 2].float()).abs().max() <= 2.0 ** -6 * full.float().abs().max()
+
+
 def test_attend_pages_past_32_bits(llma):
     """pages whose bytes lie more than 2^32 behind the cache's start"""
     H, D = 8, 128

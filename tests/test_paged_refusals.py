@@ -38,7 +38,7 @@ def call(lib, name, base, change):
 @pytest.mark.parametrize("change,code", [
     (dict(lens=None), I), (dict(rows=None), I), (dict(table=None), I), (dict(owned=None), I), (dict(free_pages=None), I), (dict(n_free=None), I), (dict(row_offsets=None), I),
     (dict(lens_after=None), I), (dict(status=None), I), (dict(slot_map=None), I), (dict(row_pos=None), I), (dict(n_seqs=0), I), (dict(n_slots=0), I), (dict(max_blocks=0), I),
-    (dict(n_pages=0), I), (dict(max_rows=-1), I), (dict(n_slots=65537), R), (dict(n_seqs=3), R), (dict(n_pages=1 << 25), R), (dict(max_blocks=1 << 25), R), (dict(lens_after=P), I)])
+    (dict(n_pages=0), I), (dict(max_rows=-1), I), (dict(n_slots=65537), R), (dict(n_seqs=3), R), (dict(n_pages=1 << 25), R), (dict(max_blocks=1 << 25), R), (dict(lens_after=P), I), (dict(max_rows=(1 << 30) + 1), R)])
 def test_map_pages(lib, change, code):
     assert call(lib, "llma_map_pages", MAP, change) == code
     assert b"llma_map_pages" in lib.llma_last_error(None)
@@ -48,7 +48,7 @@ def test_map_pages(lib, change, code):
     (dict(cache="null"), I), (dict(cache=cache(k=None)), I), (dict(cache=cache(v_scale=None)), I), (dict(cache=cache(head_dim=96)), I), (dict(cache=cache(n_pages=0)), I),
     (dict(cache=cache(n_kv_heads=0)), I), (dict(cache=cache(n_kv_heads=1025)), I), (dict(cache=cache(n_pages=1 << 25)), R), (dict(cache=cache(v=P + 8)), I), (dict(k=None), I), (dict(v=None), I),
     (dict(slot_map=None), I), (dict(dtype=3), I), (dict(dtype=-1), I), (dict(n_rows=-1), I), (dict(k=P + 2), I), (dict(v_row=60), I), (dict(k_head=4), I), (dict(k_row=-64), I),
-    (dict(cache=cache(n_kv_heads=1024), n_rows=1 << 24), R)])
+    (dict(cache=cache(n_kv_heads=1024), n_rows=1 << 24), R), (dict(n_rows=(1 << 28) + 1), R)])
 def test_append_paged(lib, change, code):
     assert call(lib, "llma_append_paged", APPEND, change) == code
     assert b"llma_append_paged" in lib.llma_last_error(None)
@@ -58,7 +58,7 @@ def test_append_paged(lib, change, code):
     (dict(cache="null"), I), (dict(cache=cache(head_dim=32)), I), (dict(q=None), I), (dict(out=None), I), (dict(table=None), I), (dict(lens=None), I), (dict(row_offsets=None), I), (dict(work=None), I),
     (dict(dtype=7), I), (dict(n_heads=3), I), (dict(n_heads=0), I), (dict(n_seqs=-1), I), (dict(n_rows=-1), I), (dict(max_rows=-1), I), (dict(max_blocks=0), I), (dict(n_seqs=4097), R),
     (dict(n_slots=1), R), (dict(slots=P, n_slots=0), R), (dict(max_blocks=1 << 25), R), (dict(max_rows=1 << 25), R), (dict(q=P + 8), I), (dict(out=P + 4), I), (dict(q_row=7), I), (dict(out_head=68), I),
-    (dict(out=P), I), (dict(work_bytes=100), I), (dict(work=P + 4), I)])
+    (dict(out=P), I), (dict(out_row=128), I), (dict(out_row=0), I), (dict(out_head=0), I), (dict(out_row=64, out_head=320), I), (dict(work_bytes=100), I), (dict(work=P + 4), I)])
 def test_attend_paged(lib, change, code):
     assert call(lib, "llma_attend_paged", ATTEND, change) == code
     assert b"llma_attend_paged" in lib.llma_last_error(None)
@@ -66,11 +66,17 @@ def test_attend_paged(lib, change, code):
 
 @pytest.mark.parametrize("change,code", [
     (dict(logits=None), I), (dict(drafts=None), I), (dict(u_accept=None), I), (dict(u_sample=None), I), (dict(n_accepted=None), I), (dict(next_token=None), I), (dict(emitted=None), I), (dict(work=None), I),
-    (dict(dtype=5), I), (dict(n_seqs=-1), I), (dict(k=-1), I), (dict(vocab=0), I), (dict(k=64), R), (dict(vocab=(1 << 24) + 1, row_stride=1 << 25), R), (dict(n_seqs=(1 << 20) + 1), R), (dict(row_stride=99), I),
+    (dict(dtype=5), I), (dict(n_seqs=-1), I), (dict(k=-1), I), (dict(vocab=0), I), (dict(k=64), R), (dict(vocab=(1 << 24) + 1, row_stride=1 << 25), R), (dict(n_seqs=(1 << 20) + 1), R), (dict(k=0, n_seqs=(1 << 22) + 1), R), (dict(row_stride=99), I),
     (dict(logits=P + 2), I), (dict(work_bytes=16), I), (dict(work=P + 8), I)])
 def test_verify_sampled(lib, change, code):
     assert call(lib, "llma_verify_sampled", VERIFY, change) == code
     assert b"llma_verify_sampled" in lib.llma_last_error(None)
+
+
+def test_out_with_heads_outermost_is_not_refused(lib):
+    """(the next check is what refuses: a workspace that is too small)"""
+    assert call(lib, "llma_attend_paged", ATTEND, dict(out_row=64, out_head=384, work_bytes=0)) == I
+    assert b"workspace" in lib.llma_last_error(None)
 
 
 def test_calls_without_rows_are_done_at_once(lib):
