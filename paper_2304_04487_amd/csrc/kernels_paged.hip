@@ -467,25 +467,37 @@ void launch_append_paged(const AppendArgs &a, hipStream_t st) {
 // The pages of all sequences, end to end, are cut into equal shares, one per workgroup and key head: ragged lengths load the chip
 // evenly, and a share's four waves take its pages in turn and meet in LDS at a sequence's end.  A sequence that lies in one share
 // is finished there; the others' parts are joined by attend_join_kernel.
+// Short sequences are not cut: a workgroup per sequence and key head, no count of the others' pages, nothing to join.  It is bound by what one compute unit
+// takes in, 44 KB a microsecond, so it pays while a table's row holds few pages more than an equal share would.  us, cut and whole, 9 rows of 32 heads of 128, bf16:
+// one sequence of 512 / 1001 / 1500 positions 10.5 / 11.0 / 11.8 and 9.8 / 11.1 / 13.7; six 17.7 / 19.7 / 21.7 and 10.8 / 13.2 / 15.9, of 2500 27.4 and 21.8; 16
+// 24.1 / 29.2 / 34 and 16.4 / 21.7 / 29.8; 64 of 1001 / 1900 / 3900 90 / 144 / 256 and 86 / 139 / 262.  Four of 5 rows, 8 key heads, 1001 / 2000: 13.5 / 13.2 and 11.2 / 16.6.
+// Eight waves for one compute unit instead of four changed nothing.
 #define ATTEND_CUS 256           // compute units; two workgroups each, one where three or four tiles fill the registers
 #define ATTEND_MIN_PAGES 4       // of a share: a page per wave
 
-struct AttendPlan { int nt, tiles, shares; };
-static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows) {
+#define ATTEND_WHOLE_PAGES 40    // whole sequences: of a table's row, at most
+struct AttendPlan { int nt, tiles, shares; bool whole; };        // whole: sequences in place of shares
+static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
     const int64_t r = (int64_t)max_rows * (n_heads / kv_heads);
     AttendPlan p;
     p.nt = r <= 64 ? (int)((r + 15) / 16) : 4;
     p.tiles = (int)((r + 16 * p.nt - 1) / (16 * p.nt));
+    const int64_t groups = (p.nt <= 2 ? 2 : 1) * ATTEND_CUS, columns = (int64_t)kv_heads * p.tiles;
     const int64_t pages = (int64_t)n_seqs * max_blocks, most = (pages + ATTEND_MIN_PAGES - 1) / ATTEND_MIN_PAGES;
-    int64_t shares = (p.nt <= 2 ? 2 : 1) * ATTEND_CUS / ((int64_t)kv_heads * p.tiles);
+    int64_t shares = groups / columns;
     if (shares > most) shares = most;
     p.shares = shares < 1 ? 1 : (int)shares;
+    // pages beyond an equal share, at 16 KB of K and V each: 512 KB, or where whole sequences leave half of the compute units without work 256 KB and, of a
+    // single one (which costs the least when cut), 192 KB
+    const int64_t beyond = (max_blocks - pages * columns / groups) * dh;
+    p.whole = max_blocks <= ATTEND_WHOLE_PAGES && n_seqs * columns < 1 << 23 && beyond <= 128 * (n_seqs * columns >= ATTEND_CUS / 2 ? 32 : n_seqs > 1 ? 16 : 12);
     return p;
 }
-// work: [pages before every sequence, n_seqs + 1 ints, rounded up to 64][parts' O][parts' m][parts' l]
+// work: [pages before every sequence, n_seqs + 1 ints, rounded up to 64][parts' O][parts' m][parts' l].  (Also where sequences stay whole: a workspace
+// for some number of sequences does for fewer)
 __host__ __device__ static inline int64_t attend_parts(const AttendPlan &p, int kv_heads) { return p.shares > 1 ? (int64_t)p.shares * 2 * kv_heads * p.tiles : 0; }
 int64_t attend_paged_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
-    const AttendPlan p = attend_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows);
+    const AttendPlan p = attend_plan(n_seqs, max_blocks, n_heads, kv_heads, dh, max_rows);
     return ((int64_t)(n_seqs + 1 + 63) / 64 * 64 + attend_parts(p, kv_heads) * 16 * p.nt * (dh + 2)) * 4;
 }
 
@@ -677,11 +689,20 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
     __shared__ AttendSeq kept[ATTEND_KEPT];
     int *const starts = (int *)((char *)lds + attend_lds<DH, NT, TYPE>);         // [n_seqs + 1]
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int share = blockIdx.x % plan.shares, head = blockIdx.x / plan.shares % a.c.heads, tile = blockIdx.x / plan.shares / a.c.heads;
+    const int shares = plan.whole ? a.n_seqs : plan.shares, share = blockIdx.x % shares, head = blockIdx.x / shares % a.c.heads, tile = blockIdx.x / shares / a.c.heads;
     const int group = a.n_heads / a.c.heads, r0 = tile * NT * 16;
     // ---- where the sequences' pages begin
+    const int n_seqs = plan.whole ? 1 : a.n_seqs;
     int total = 0;
-    for (int b0 = 0; b0 < a.n_seqs; b0 += 256) {
+    if (plan.whole) {
+        const AttendSeq s = attend_seq(a, share);
+        total = attend_pages(s);
+        if (threadIdx.x == 0) {
+            kept[0] = s;
+            starts[0] = 0;
+        }
+    }
+    for (int b0 = 0; b0 < a.n_seqs && !plan.whole; b0 += 256) {
         const int b = b0 + threadIdx.x;
         int sum, pages = 0;
         if (b < a.n_seqs) {
@@ -693,14 +714,14 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
         if (b < a.n_seqs) starts[b] = total + at;
         total += sum;
     }
-    if (threadIdx.x == 0) starts[a.n_seqs] = total;
+    if (threadIdx.x == 0) starts[n_seqs] = total;
     __syncthreads();
-    if (plan.shares > 1 && blockIdx.x == 0)                      // (for attend_join_kernel)
+    if (plan.shares > 1 && !plan.whole && blockIdx.x == 0)       // (for attend_join_kernel)
         for (int b = threadIdx.x; b <= a.n_seqs; b += 256) ((int *)a.work)[b] = starts[b];
     total = uniform(total);
-    int per = (total + plan.shares - 1) / plan.shares;
+    int per = plan.whole ? total : (total + plan.shares - 1) / plan.shares;
     per = per < ATTEND_MIN_PAGES ? ATTEND_MIN_PAGES : per;
-    const int64_t from = (int64_t)share * per;
+    const int64_t from = plan.whole ? 0 : (int64_t)share * per;
     if (from >= total) return;
     const int p0 = (int)from, p1 = p0 + per < total ? p0 + per : total;
     const float to_log2 = a.scale * 1.44269504088896340736f;
@@ -710,7 +731,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
     // the share's part of sequence b, or of the next that has rows in this tile
     const auto segment = [&](int b) {
         AttendSeg g{};
-        for (; b < a.n_seqs; ++b) {
+        for (; b < n_seqs; ++b) {
             const int begin = uniform(starts[b]), end = uniform(starts[b + 1]);
             if (begin >= p1) break;
             const int first = p0 > begin ? p0 - begin : 0, last = (p1 < end ? p1 : end) - begin;
@@ -752,7 +773,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
         }
     };
 
-    AttendSeg seg = segment(uniform(count_le(starts, a.n_seqs + 1, p0) - 1));
+    AttendSeg seg = segment(uniform(count_le(starts, n_seqs + 1, p0) - 1));
     AttendQ<DH, NT> qr;
     int id = -1;
     if (seg.last > 0) {
@@ -1256,7 +1277,7 @@ __global__ __launch_bounds__(256) void attend_join_kernel(AttendArgs a, AttendPl
 template <int DH, int NT, int TYPE>
 static void launch_attend_nt(const AttendArgs &a, const AttendPlan &p, hipStream_t st) {
     const size_t bytes = (size_t)attend_lds<DH, NT, TYPE> + (size_t)(a.n_seqs + 1) * 4;
-    hipLaunchKernelGGL((attend_paged_kernel<DH, NT, TYPE>), dim3(p.shares * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
+    hipLaunchKernelGGL((attend_paged_kernel<DH, NT, TYPE>), dim3((p.whole ? a.n_seqs : p.shares) * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
 }
 // row blocks of a call, at most: what blocks of 64 nt rows make of max_rows everywhere, or of all rows and a remainder per sequence
 static int64_t attend_row_blocks(const AttendArgs &a, int nt) {
@@ -1274,12 +1295,12 @@ static void launch_attend_type(const AttendArgs &a, hipStream_t st) {
     constexpr int ROWS_NT = TYPE == ROWS_F32 ? 1 : 2;            // (three planes of queries and probabilities leave room for one tile)
     const int64_t group_rows = (int64_t)a.max_rows * (a.n_heads / a.c.heads), launched = (group_rows + 64 * ROWS_NT - 1) / (64 * ROWS_NT) * a.n_seqs * a.c.heads;
     if (group_rows > 64 && attend_row_blocks(a, ROWS_NT) >= ROWS_MIN && launched < 1 << 23) return launch_attend_rows<DH, ROWS_NT, TYPE>(a, st);
-    const AttendPlan p = attend_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows);
+    const AttendPlan p = attend_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, DH, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
     else if (p.nt == 3) launch_attend_nt<DH, 3, TYPE>(a, p, st);
     else launch_attend_nt<DH, 4, TYPE>(a, p, st);
-    if (p.shares > 1)
+    if (p.shares > 1 && !p.whole)
         hipLaunchKernelGGL((attend_join_kernel<DH, TYPE>), dim3((a.max_rows * (a.n_heads / a.c.heads) + 3) / 4, a.c.heads, a.n_seqs), dim3(256), 0, st, a, p);
 }
 void launch_attend_paged(const AttendArgs &a, hipStream_t st) {
