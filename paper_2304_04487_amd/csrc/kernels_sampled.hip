@@ -42,29 +42,28 @@ __device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? LLMA_NEG_INF : x; }           // NaN: a token that cannot be
-// 2^y in 64 bits, y <= 0: the series of 2^f about 0 to f^11 for |f| <= 1/2 (the rest is below (ln 2 / 2)^12 / 12! = 7e-15 of it)
-__device__ __forceinline__ double exp2_64(double y) {
-    constexpr double L = 0.69314718055994530942;
-    y = fmax(y, -2000.0);                                        // (2^-2000 is 0; minus infinity)
-    const double k = __builtin_rint(y), f = (y - k) * L;
-    double p = 1.0 / 39916800.0;
-    p = __builtin_fma(p, f, 1.0 / 3628800.0);
-    p = __builtin_fma(p, f, 1.0 / 362880.0);
-    p = __builtin_fma(p, f, 1.0 / 40320.0);
-    p = __builtin_fma(p, f, 1.0 / 5040.0);
-    p = __builtin_fma(p, f, 1.0 / 720.0);
-    p = __builtin_fma(p, f, 1.0 / 120.0);
-    p = __builtin_fma(p, f, 1.0 / 24.0);
-    p = __builtin_fma(p, f, 1.0 / 6.0);
-    p = __builtin_fma(p, f, 0.5);
+// A row's weights e^((x - top) / T) in 64 bits, as 2^((x - top) by), by = log2(e) / T.  2^f for |f| <= 1/2 by the polynomial of degree 10 that is 1 at 0 and meets it
+// at the ten Chebyshev points of the interval (off by 6e-16 of it); a whole number is split off by adding 1.5 2^52, whose low word it becomes.
+// The top itself counts 1, also an infinite one; minus infinity, NaN and what is below 2^-2000 count 0 (fmax passes over a NaN).
+struct Weigher { float top; double by, least; };
+__device__ __forceinline__ Weigher weigher(float top, double by) { return Weigher{top, by, -2000.0 / by}; }
+__device__ __forceinline__ double weight64(float x, const Weigher &w) {
+    constexpr double whole = 6755399441055744.0;
+    const double d = fmax((double)x - (double)w.top, w.least);
+    const double t = __builtin_fma(d, w.by, whole), f = __builtin_fma(d, w.by, whole - t);
+    double p = 7.070977866508138e-09;
+    p = __builtin_fma(p, f, 1.0205905413765595e-07);
+    p = __builtin_fma(p, f, 1.3215451633221434e-06);
+    p = __builtin_fma(p, f, 1.5252672924850737e-05);
+    p = __builtin_fma(p, f, 0.00015403530424776529);
+    p = __builtin_fma(p, f, 0.0013333558200794592);
+    p = __builtin_fma(p, f, 0.009618129107618665);
+    p = __builtin_fma(p, f, 0.05550410866465167);
+    p = __builtin_fma(p, f, 0.24022650695910075);
+    p = __builtin_fma(p, f, 0.6931471805599462);
     p = __builtin_fma(p, f, 1.0);
-    p = __builtin_fma(p, f, 1.0);
-    return __builtin_amdgcn_ldexp(p, (int)k);
-}
-// e^((x - top) / T) in 64 bits, by = log2(e) / T; the top itself (also +inf) counts 1, minus infinity 0
-__device__ __forceinline__ double weight64(float x, float top, double by) {
-    const double w = exp2_64(((double)x - (double)top) * by);
-    return x == LLMA_NEG_INF ? 0.0 : x == top ? 1.0 : w;
+    p = __builtin_amdgcn_ldexp(p, (int)__double_as_longlong(t));
+    return w.top == -LLMA_NEG_INF && x == w.top ? 1.0 : p;
 }
 __device__ __forceinline__ double log2_scale(const SampledArgs &a, int b) { return 1.4426950408889634074 / (double)(a.temperature ? a.temperature[b] : 1.f); }
 
@@ -224,6 +223,7 @@ __device__ double row_sum64(const SampledArgs &a, int64_t row, float top, double
     constexpr int EPB = sampled_epb<TYPE>;
     const RowView v = row_view<TYPE>(a, row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
+    const Weigher weigh = weigher(top, by);
     double s = 0.0;
     for (int blk = threadIdx.x; blk < blocks; blk += 256) {
         float x[EPB];
@@ -231,7 +231,7 @@ __device__ double row_sum64(const SampledArgs &a, int64_t row, float top, double
 #pragma unroll
         for (int e = 0; e < EPB; ++e) {
             const int id = blk * EPB - v.skip + e;
-            if (id >= 0 && id < a.vocab) s += weight64(logit_of(x[e]), top, by);
+            if (id >= 0 && id < a.vocab) s += weight64(x[e], weigh);
         }
     }
     return block_sum(s, part);
@@ -295,7 +295,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
         if (greedy) {
             ok = draft == where;
         } else {
-            right = weight64(logit, top, by64);
+            right = weight64(logit, weigher(top, by64));
             left = (double)u * (double)q * (double)sum;
             ok = left < right;
             near = right > 0.0 && fabs(left - right) <= 3e-5 * right;
@@ -329,23 +329,32 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
 }
 
 // the weights of a piece of the sampled row: e, or what is left of p once q is taken off
+typedef __attribute__((ext_vector_type(4), aligned(4))) float f32x4_any;
 template <int TYPE>
-__device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice &c, const RowView &v, int blocks, int blk, double by, bool minus, const float *q, double w[sampled_epb<TYPE>]) {
+__device__ __forceinline__ void piece_weights(const SampledArgs &a, const Choice &c, const RowView &v, int blocks, int blk, const Weigher &weigh, bool minus, const float *q, double w[sampled_epb<TYPE>]) {
     constexpr int EPB = sampled_epb<TYPE>;
-    float x[EPB];
+    const int id0 = blk * EPB - v.skip;
+    const bool edge = id0 < 0 || blk * (int64_t)EPB - v.skip + EPB > a.vocab;       // not wholly the row's
+    float x[EPB], taken[EPB];
     piece_values<TYPE>(v.base[blk < blocks ? blk : 0], x);
+    if (minus && q) {
+        if (edge) {
 #pragma unroll
-    for (int e = 0; e < EPB; ++e) {
-        const int id = blk * EPB - v.skip + e;
-        double y = 0.0;
-        if (blk < blocks && id >= 0 && id < a.vocab) {
-            y = weight64(logit_of(x[e]), c.top, by);
-            if (minus) {
-                if (q) y = fmax(y * c.inv_sum - (double)q[id], 0.0);
-                else if (id == c.token) y = 0.0;
-            }
+            for (int e = 0; e < EPB; ++e) taken[e] = blk < blocks && id0 + e >= 0 && id0 + e < a.vocab ? q[id0 + e] : 0.f;
+        } else {
+#pragma unroll
+            for (int e = 0; e < EPB; e += 4) *(f32x4 *)(taken + e) = *(const f32x4_any *)(q + id0 + e);
         }
-        w[e] = y;
+    }
+    if (edge) {
+#pragma unroll
+        for (int e = 0; e < EPB; ++e) x[e] = blk < blocks && id0 + e >= 0 && id0 + e < a.vocab ? x[e] : LLMA_NEG_INF;
+    }
+#pragma unroll
+    for (int e = 0; e < EPB; ++e) w[e] = weight64(x[e], weigh);
+    if (minus) {
+#pragma unroll
+        for (int e = 0; e < EPB; ++e) w[e] = q ? fmax(__builtin_fma(w[e], c.inv_sum, -(double)taken[e]), 0.0) : id0 + e == c.token ? 0.0 : w[e];
     }
 }
 
@@ -375,7 +384,7 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
         }
     }
     if (c.greedy) return;
-    const double by = log2_scale(a, b);
+    const Weigher weigh = weigher(c.top, log2_scale(a, b));
     const RowView v = row_view<TYPE>(a, c.row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
     const bool minus = PASS == 1 || (a.probs == nullptr && c.residual);
@@ -384,7 +393,7 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
 #pragma unroll
     for (int i = 0; i < PICK_BLOCKS / 256; ++i) {
         double w[EPB];
-        piece_weights<TYPE>(a, c, v, blocks, blockIdx.y * PICK_BLOCKS + i * 256 + threadIdx.x, by, minus, q, w);
+        piece_weights<TYPE>(a, c, v, blocks, blockIdx.y * PICK_BLOCKS + i * 256 + threadIdx.x, weigh, minus, q, w);
 #pragma unroll
         for (int e = 0; e < EPB; ++e) s += w[e];
     }
@@ -425,7 +434,8 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
     // requested together: the choice, the first 256 ranges' sums of both passes, the random number, the drafts
     const Choice c = ((const Choice *)((const char *)a.work + plan.at_choice))[b];
     const double all0 = t < plan.picks ? base[t] : 0.0, left0 = a.probs && t < plan.picks ? base[plan.picks + t] : 0.0;
-    const double u = (double)a.u_sample[b], by = log2_scale(a, b);
+    const double u = (double)a.u_sample[b];
+    const Weigher weigh = weigher(c.top, log2_scale(a, b));
     const int draft = t < a.k ? a.drafts[(int64_t)b * a.draft_stride + t] : -1;
     int token = -1;
     if (c.greedy) {
@@ -472,7 +482,7 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
             const int blk0 = range.id * PICK_BLOCKS + t * PER;
 #pragma unroll
             for (int i = 0; i < PER; ++i) {
-                piece_weights<TYPE>(a, c, v, blocks, blk0 + i, by, minus, q, w[i]);
+                piece_weights<TYPE>(a, c, v, blocks, blk0 + i, weigh, minus, q, w[i]);
 #pragma unroll
                 for (int e = 0; e < EPB; ++e) own += w[i][e];
             }
