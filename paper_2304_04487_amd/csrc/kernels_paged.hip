@@ -57,6 +57,7 @@ __device__ __forceinline__ int count_le(const P *p, int n, int v) {
 // order of granting (a grant taken back leaves the stack as it was); what it lacks comes off the stack's top, sequence by sequence.
 // Places are prefix sums, so the result does not depend on the order of execution.  One workgroup, a thread per sequence
 // and then a thread per page and per row: all of it is a chain of dependent reads, a few microseconds however little there is to do.
+// 16 sequences of 9 rows 3.9 us, 512 prompts of 130 rows (33 thousand) 5.6 and 5.0 for the rows in a launch of their own, of which an empty launch is 2.
 #define MAP_THREADS 1024
 #define MAP_ROWS_HERE 8192       // rows whose slots the same workgroup writes; more take a launch of many
 #define MAP_MAX_SLOTS 65536      // (bits of LDS that find a slot listed twice)
@@ -287,6 +288,8 @@ __device__ __forceinline__ void row8(const void *p, int64_t at, float v[8]) {
 // 16 (8) lanes share a row's 128 (64) features, eight each, and a lane has four neighbouring positions, so that a dim's four codes leave as one word
 // of the transposed V: a wave holds 16 (32) positions.  A prompt's pages take a wave for each 16 (32) positions, which agree on the maximum in LDS; a step's
 // runs, a few rows long, one wave.
+// Prompts are bound by memory: 4 of up to 2011 fp32 rows of 8 heads of 128, 62 MB read and written, 17 us = 3.6 TB/s.  Steps by their chain of slots, rows, maximum and
+// scale: 16 sequences of 9 rows of 32 heads 9.5 us, of which 8.0 for a single sequence too.
 __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)(e + 127) << 23); }
 // exponent of the scale: -64 .. 120
 __device__ __forceinline__ int scale_exponent(float amax) {
@@ -299,7 +302,10 @@ __device__ __forceinline__ uint32_t codes4(float a, float b, float c, float d) {
     uint32_t w = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_input(a), code_input(b), 0, false);
     return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(code_input(c), code_input(d), (int)w, true);
 }
-__device__ __forceinline__ float code_value(uint32_t byte) { return __builtin_amdgcn_cvt_f32_fp8((int)byte, 0); }
+// four codes' values times `by`, as codes
+__device__ __forceinline__ uint32_t codes_by(uint32_t c, float by) {
+    return codes4(__builtin_amdgcn_cvt_f32_fp8((int)c, 0) * by, __builtin_amdgcn_cvt_f32_fp8((int)c, 1) * by, __builtin_amdgcn_cvt_f32_fp8((int)c, 2) * by, __builtin_amdgcn_cvt_f32_fp8((int)c, 3) * by);
+}
 
 template <int DH, int TYPE, bool KEYS, int WAVES>
 __device__ __forceinline__ void append_run(const AppendArgs &a, int head, int row0, int n, int page, int off, float *shared_max) {
@@ -357,11 +363,42 @@ __device__ __forceinline__ void append_run(const AppendArgs &a, int head, int ro
     float s = pow2(scale_exponent(amax));
     if (off > 0) {
         if (s > old) {
-            // the codes before the run, byte by byte: those of its own positions are not touched
+            // The codes before the run, 16 bytes a lane and four of them at once: off rows of K, the first off bytes of V's rows, where 16 bytes that the run begins
+            // in are written byte by byte (another wave may be writing its positions).  By single bytes a step into 32
+            // heads' pages of 60 positions that all had to grow took 22 us more than one into pages that had not; so 4
             const float by = old / s;
-            for (int i = wave * 64 + lane; i < off * DH; i += 64 * WAVES) {
-                uint8_t *const c = KEYS ? codes + i : codes + (size_t)(i / off) * PAGE_POS + i % off;
-                *c = (uint8_t)codes4(code_value(*c) * by, 0.f, 0.f, 0.f);
+            const int per = KEYS ? 1 : (off + 15) / 16, pieces = KEYS ? off * DH / 16 : DH * per;
+            for (int i0 = wave * 64 + lane; i0 < pieces; i0 += 4 * 64 * WAVES) {
+                u32x4 c[4];
+                u32x4 *at[4];
+                int mine[4];                        // bytes before the run
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const int i = i0 + u * 64 * WAVES;
+                    const int piece = i < pieces ? i : i0;
+                    at[u] = (u32x4 *)(KEYS ? codes + piece * 16 : codes + piece / per * PAGE_POS + piece % per * 16);
+                    mine[u] = i >= pieces ? 0 : KEYS ? 16 : off - piece % per * 16;
+                    c[u] = *at[u];
+                }
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) c[u][w] = codes_by(c[u][w], by);
+                    if (mine[u] >= 16) {
+                        *at[u] = c[u];
+                    } else {
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            if (mine[u] >= 4 * w + 4) {
+                                ((uint32_t *)at[u])[w] = c[u][w];
+                                continue;
+                            }
+#pragma unroll
+                            for (int e = 0; e < 3; ++e)
+                                if (4 * w + e < mine[u]) ((uint8_t *)at[u])[4 * w + e] = (uint8_t)(c[u][w] >> 8 * e);
+                        }
+                    }
+                }
             }
         } else {
             s = old;
@@ -467,6 +504,8 @@ void launch_append_paged(const AppendArgs &a, hipStream_t st) {
 // The pages of all sequences, end to end, are cut into equal shares, one per workgroup and key head: ragged lengths load the chip
 // evenly, and a share's four waves take its pages in turn and meet in LDS at a sequence's end.  A sequence that lies in one share
 // is finished there; the others' parts are joined by attend_join_kernel.
+// Steps are bound by one read of the cache: 16 sequences of up to 4096 positions, 9 rows of 32 heads of 128, 361 MB in 74 us of kernels = 4.9 TB/s, 61 of 5 rows, four
+// query heads a key head, fp16, 671 MB in 146 = 4.6; a kernel of the same mapping that only loads is within 3 to 10 % of that.
 // Short sequences are not cut: a workgroup per sequence and key head, no count of the others' pages, nothing to join.  It is bound by what one compute unit
 // takes in, 44 KB a microsecond, so it pays while a table's row holds few pages more than an equal share would.  us, cut and whole, 9 rows of 32 heads of 128, bf16:
 // one sequence of 512 / 1001 / 1500 positions 10.5 / 11.0 / 11.8 and 9.8 / 11.1 / 13.7; six 17.7 / 19.7 / 21.7 and 10.8 / 13.2 / 15.9, of 2500 27.4 and 21.8; 16
@@ -984,6 +1023,9 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
 // operands' images (16 KB of K, 16 KB of V at head_dim 128); a page is requested two ahead, widened one ahead, one barrier a page.  A wave holds its rows' queries and
 // sums in registers and meets nobody at the end.  Pages behind a wave's rows are skipped; the longest row blocks start first, and a key head's on one XCD.
 // The reference of the exponentials moves only when a maximum passes it by 2^8: the sums are rescaled once or twice a row instead of once a page.
+// Bound by issue: two sequences of up to 2047 rows, 32 query and 8 key heads of 128, over up to 2900 positions before, bf16, 136 GFLOP in 267 us = 0.51 PFLOP/s, vector instructions
+// in 46 % of the cycles, matrix instructions in 34 %.  The exponentials of one page beside the products of the next spilled (330 to 430 us); eight waves a page, 256
+// rows, 2 % faster there and 10 % slower for prompts without a cache (84 us against 76 for 2047 rows of 32 heads).
 template <int DH> constexpr int rows_images = (4 * (DH / 64) * 2 + (DH / 16) * 2) * 64;       // 16-byte pieces of a page
 template <int DH, int NT, int TYPE>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int blocks) {
