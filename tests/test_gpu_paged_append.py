@@ -52,3 +52,19 @@ def test_prompts_that_begin_inside_a_page(llma, D, rows, dtype):  # noqa: F811
     assert at <= P
     x = torch.tensor(rng.standard_normal((rows, 2, H, D)) * 300).to(DT[dtype]).cuda()
     assert check(llma, c, x, slot_map).any()
+
+
+@pytest.mark.parametrize("D", [64, 128])
+def test_short_and_long_runs_together(llma, D):  # noqa: F811
+    """steps of many sequences: runs of 1 to 64 rows at any offset, several in a window of 64 rows, some over its end"""
+    rng = np.random.default_rng(D)
+    H, P = 32, 110
+    c = random_cache(llma, P, H, D, 19)
+    slot_map = []
+    for i, page in enumerate(rng.permutation(P)[:100]):
+        off = int(rng.integers(0, PAGE)) if i % 3 else 0
+        n = int(min(PAGE - off, rng.integers(1, 6) if i % 4 else rng.integers(14, 65)))
+        slot_map += [int(page) * PAGE + off + j for j in range(n)] + [-1] * (i % 5 == 0)
+    slot_map += [-1] * max(0, 1100 - len(slot_map))        # (the form with several waves a page)
+    x = torch.tensor(rng.standard_normal((len(slot_map), 2, H, D)) * 10.0 ** rng.integers(0, 4, (len(slot_map), 2, H, 1))).bfloat16().cuda()
+    assert check(llma, c, x, slot_map).any()
