@@ -155,7 +155,7 @@ __global__ __launch_bounds__(N) void map_pages_kernel(MapArgs a) {
     if (status == 0 && (rows > 0x7fffffffll || (a.max_rows > 0 && rows > a.max_rows))) status = LLMA_E_RANGE;
     const int stack = top + (status == 0 ? (int)back : 0);       // its height once everything is back
     if (status == 0 && more > stack) status = (int)(more - stack);
-    const bool ok = status == 0, here = a.max_rows <= MAP_ROWS_HERE;
+    const bool ok = status == 0, here = a.max_rows > 0 && a.max_rows <= MAP_ROWS_HERE;      // (no map: no row has a place in one)
     if (t == 0) *a.status = status;
     // a tile's sequences and their places, for threads that look them up by page or row
     const auto look = [&](int b0, MapSums *at, MapSums *sum) {
