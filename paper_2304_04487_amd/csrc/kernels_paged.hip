@@ -1247,7 +1247,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
                         }
                     }
             }
-            if (masked && (nan_seen[i & 1][0] | nan_seen[i & 1][1] | nan_seen[i & 1][2] | nan_seen[i & 1][3]))
+            // (taken out of the image where the block's first row does not see all of the page: also for waves whose rows all do)
+            if (base + PAGE_POS - 1 > block_first && (nan_seen[i & 1][0] | nan_seen[i & 1][1] | nan_seen[i & 1][2] | nan_seen[i & 1][3]))
                 attend_nans<DH, NT>(a.c.v + ((size_t)(id < 0 ? 0 : id) * a.c.heads + head) * (PAGE_POS * DH) + v_off, base, id < 0 ? 0 : s.len, limit, o);
             __builtin_amdgcn_s_setprio(1);
 #pragma unroll
