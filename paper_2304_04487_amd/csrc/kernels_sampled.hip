@@ -406,9 +406,9 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
     if (threadIdx.x == 0) sums[PASS * plan.picks + blockIdx.y] = s;
 }
 
-// The first thread, in order, whose `hit` is set hands its two values to the workgroup, else the last whose `some` is; false if there is neither.  slots: LDS of eight
+// The first thread, in order, whose `hit` is set hands its two values to the workgroup (2), else the last whose `some` is (1); 0 if there is neither.  slots: LDS of eight
 struct Found { double at; int id; };
-__device__ __forceinline__ bool first_of(bool hit, bool some, double at, int id, Found *slots, Found *out) {
+__device__ __forceinline__ int first_of(bool hit, bool some, double at, int id, Found *slots, Found *out) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     const unsigned long long hits = __ballot(hit), any = __ballot(some);
     const int who = hits ? __builtin_ctzll(hits) : any ? 63 - __builtin_clzll(any) : -1;
@@ -419,13 +419,14 @@ __device__ __forceinline__ bool first_of(bool hit, bool some, double at, int id,
 #pragma unroll
     for (int w = 3; w >= 0; --w)
         if (slots[4 + w].id) best = w;
-    if (best < 0) {
+    const bool is_hit = best >= 0;
+    if (!is_hit) {
 #pragma unroll
         for (int w = 0; w < 4; ++w)
             if (slots[w].id >= 0) best = w;
     }
     if (best >= 0) *out = slots[best];
-    return best >= 0;
+    return best < 0 ? 0 : is_hit ? 2 : 1;
 }
 // A workgroup per sequence: the range the random number falls into, then the token in it.  Bound by its chain: the choice and the ranges' sums, a scan, the range's
 // pieces (8 or 16 exponentials a thread), a scan.  With separate sums and scans, and atomics that look for the first hit, one sequence over 32000 tokens took 9.8 us where it takes 4.1.
@@ -449,9 +450,10 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
         const bool with_q = c.residual && a.probs != nullptr;
         bool minus = c.residual, all = !with_q;                  // which weights, which sums
         const auto sum_of = [&](int i) { return i < plan.picks ? (i == t ? (all ? all0 : left0) : base[(all ? 0 : plan.picks) + i]) : 0.0; };
-        double total, up_to, sum;                                // (up to 256 ranges: one scan gives both)
+        double total, up_to, sum, first;                         // (up to 256 ranges: one scan gives both; first: the sum of the first 256)
         const auto add_up = [&]() {
-            up_to = scan64(sum_of(t), part, &total);
+            up_to = scan64(sum_of(t), part, &first);
+            total = first;
             for (int i0 = 256; i0 < plan.picks; i0 += 256) total += block_sum(sum_of(i0 + t), part);
         };
         add_up();
@@ -475,9 +477,10 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
                     __syncthreads();                             // (the last 256's answer has been read)
                     up_to = before + scan64(w, part, &sum);
                 }
-                if (first_of(w > 0.0 && up_to > target, w > 0.0, up_to - w, i0 + t, ranges, &found)) range = found;
-                if (range.id >= 0 && range.at + sum_of(range.id) > target) break;
-                before = i0 == 0 ? part[0] + part[1] + part[2] + part[3] : before + sum;
+                const int is = first_of(w > 0.0 && up_to > target, w > 0.0, up_to - w, i0 + t, ranges, &found);
+                if (is) range = found;
+                if (is == 2) break;
+                before += i0 == 0 ? first : sum;
             }
             const RowView v = row_view<TYPE>(a, c.row);
             const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
