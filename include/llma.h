@@ -190,7 +190,7 @@ int llma_verify_step_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs,
 /* The step with sampling in place of the arg max: the same forward, then llma_verify_sampled on its logits with the drafts as copied
  * tokens (accepted with probability p(draft) / 1, else a token from p without it), so that emitted tokens are distributed as the model's
  * own at that temperature.  temperature, u_sample: HOST float[n_seqs]; u_accept: HOST float[n_seqs*k]; u in [0, 1), temperature >= 0 (0: the
- * greedy step's tokens), finite, else RANGE.  Everything else as above.  The first call allocates device memory for the logits (grown when a
+ * greedy step's tokens), finite, else RANGE, as are models of more than 2^24 tokens.  Everything else as above.  The first call allocates device memory for the logits (grown when a
  * step has more rows; with a logits dump set they are written there). */
 int llma_verify_step_sampled(llma_ctx *ctx, int32_t seq, const int32_t *draft, int32_t k, float temperature, const float *u_accept, float u_sample,
                              int32_t *n_accepted, int32_t *next_token, int32_t *emitted);
@@ -312,7 +312,7 @@ int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtyp
  * (NULL: a copied token, q = 1).  The next token is drawn from max(p - q, 0) at the first rejection (copied token: p without it; p itself
  * where nothing is left), from p of row n_draft when all were accepted: the smallest v whose cumulative weight passes u_sample[b] times
  * the sum.  u in [0, 1).  temperature NULL: 1; not above 0: the arg max, lowest id on ties, as llma_verify_step has it.
- * NaN logits count as minus infinity; drafts outside [0, vocab) are rejected.
+ * NaN logits count as minus infinity; drafts outside [0, vocab) are rejected.  vocab <= 2^24, n_seqs * (k + 1) <= 2^22, else RANGE.
  * Outputs: n_accepted[b] = a, next_token[b] (-1: a row without a logit above minus infinity), emitted[b][0 .. k]: the accepted drafts, the next token, then -1. */
 int64_t llma_verify_sampled_workspace(int32_t n_seqs, int32_t k, int32_t vocab);
 int llma_verify_sampled(const void *logits, int32_t dtype, int64_t row_stride, int32_t vocab, int32_t n_seqs, int32_t k,

@@ -1150,6 +1150,8 @@ static int verify_batch(llma_ctx *c, int32_t n_seqs, const int32_t *seqs, const 
     if (c->logits_dump && n_seqs * (k + 1) > c->dump_rows)
         return fail(c, LLMA_E_RANGE, "llma_verify_step: logits dump holds %d rows, step has %d", c->dump_rows, n_seqs * (k + 1));
     if (sample) {
+        if (g.vocab > SAMPLED_MAX_VOCAB || (int64_t)n_seqs * (k + 1) > SAMPLED_MAX_ROWS)
+            return fail(c, LLMA_E_RANGE, "llma_verify_step_sampled: vocab %d, %d sequences of %d rows (at most 2^24, 2^22 rows)", g.vocab, n_seqs, k + 1);
         if (!launch_verify_sampled) return fail(c, LLMA_E_INVAL, "llma_verify_step_sampled: built without sampling");
         int rc = ensure_sampling(c, n_seqs, k);
         if (rc) return rc;

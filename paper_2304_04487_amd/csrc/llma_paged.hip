@@ -121,7 +121,7 @@ extern "C" int llma_attend_paged(const llma_paged_cache *cache, const void *q, i
 static int check_sampled(int n_seqs, int k, int vocab, const char *who) {
     if (n_seqs < 0 || k < 0 || vocab < 1) return refuse(LLMA_E_INVAL, "%s: need n_seqs, k >= 0 and vocab >= 1", who);
     if (k > LLMA_SAMPLED_MAX_K) return refuse(LLMA_E_RANGE, "%s: k %d, at most %d", who, k, LLMA_SAMPLED_MAX_K);
-    if (vocab > 1 << 24 || (int64_t)n_seqs * (k + 1) > 1 << 22) return refuse(LLMA_E_RANGE, "%s: vocab %d, %d sequences of %d rows (at most 2^24, 2^22 rows)", who, vocab, n_seqs, k + 1);
+    if (vocab > SAMPLED_MAX_VOCAB || (int64_t)n_seqs * (k + 1) > SAMPLED_MAX_ROWS) return refuse(LLMA_E_RANGE, "%s: vocab %d, %d sequences of %d rows (at most 2^24, 2^22 rows)", who, vocab, n_seqs, k + 1);
     return LLMA_OK;
 }
 extern "C" int64_t llma_verify_sampled_workspace(int32_t n_seqs, int32_t k, int32_t vocab) {
