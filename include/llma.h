@@ -190,8 +190,9 @@ int llma_verify_step_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs,
 /* The step with sampling in place of the arg max: the same forward, then llma_verify_sampled on its logits with the drafts as copied
  * tokens (accepted with probability p(draft) / 1, else a token from p without it), so that emitted tokens are distributed as the model's
  * own at that temperature.  temperature, u_sample: HOST float[n_seqs]; u_accept: HOST float[n_seqs*k]; u in [0, 1), temperature >= 0 (0: the
- * greedy step's tokens), finite, else RANGE, as are models of more than 2^24 tokens.  Everything else as above.  The first call allocates device memory for the logits (grown when a
- * step has more rows; with a logits dump set they are written there). */
+ * greedy step's tokens), finite, else RANGE, as are models of more than 2^24 tokens.  A sequence whose row has no logit above minus infinity
+ * fails the step (HIP): all of its slots stay as they were.  Everything else as above.  The first call allocates device memory for the
+ * logits (grown when a step has more rows; with a logits dump set they are written there). */
 int llma_verify_step_sampled(llma_ctx *ctx, int32_t seq, const int32_t *draft, int32_t k, float temperature, const float *u_accept, float u_sample,
                              int32_t *n_accepted, int32_t *next_token, int32_t *emitted);
 int llma_verify_step_sampled_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs, const int32_t *drafts, int32_t k, const float *temperature,

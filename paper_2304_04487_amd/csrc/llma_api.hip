@@ -1171,19 +1171,20 @@ static int verify_batch(llma_ctx *c, int32_t n_seqs, const int32_t *seqs, const 
         for (int j = 0; j < k; ++j) io.draft[(size_t)b * mk + j] = drafts[(size_t)b * k + j];
         io.nacc[b] = -1;                       // (checked below)
     }
-    for (int b = 0; b < n_seqs; ++b) forget_imports(c, seqs[b]);
+    // (until the step is known to be good the device's lengths and tokens may be its: a step that fails is undone for all of its slots)
+    for (int b = 0; b < n_seqs; ++b) { forget_imports(c, seqs[b]); c->stale[seqs[b]] = 1; }
     int rc = run_step(c, sample ? STEP_SAMPLED : STEP_VERIFY, n_seqs, m, t_max, n_seqs == 1 ? seqs[0] : 0);
     if (rc) return drained(c, rc);
     HIP_TRY(c, hipStreamSynchronize(c->st));
     HIP_TRY(c, hipGetLastError());
     const int *const nacc = io.nacc, *const nxt = io.next, *const em = io.emit;
-    for (int b = 0; b < n_seqs; ++b) c->stale[seqs[b]] = 0;
     for (int b = 0; b < n_seqs; ++b) {
         bool ok = nacc[b] >= 0 && nacc[b] <= k && nxt[b] >= 0 && nxt[b] < g.vocab;
         for (int j = 0; ok && j <= nacc[b]; ++j) ok = em[(size_t)b * (mk + 1) + j] >= 0 && em[(size_t)b * (mk + 1) + j] < g.vocab;
         if (!ok) return fail(c, LLMA_E_HIP, "llma_verify_step: device returned accepted count %d / token %d outside their ranges for slot %d", nacc[b], nxt[b], seqs[b]);
     }
     for (int b = 0; b < n_seqs; ++b) {
+        c->stale[seqs[b]] = 0;
         c->T_host[seqs[b]] += nacc[b] + 1;
         c->pending_host[seqs[b]] = nxt[b];
         if (n_accepted) n_accepted[b] = nacc[b];
