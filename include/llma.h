@@ -275,7 +275,7 @@ typedef struct {
  * Outputs: row_offsets[n_seqs+1] (sums of rows), lens_after[n_seqs] = lens + rows; for row i of sequence b, at row_offsets[b] + i:
  * row_pos = lens + i and slot_map = 64 * page + position in the page; entries behind the last row up to max_rows: 0 and -1.
  * With max_rows = 0 no row is mapped: slot_map and row_pos may be NULL, rows may be any, and all else is written as it is with a map.
- * *status: 0; the number of pages that were missing; or a negative LLMA_E_* (INVAL: a negative length, a slot listed twice, counts that do not fit the table or the stack; RANGE: a slot outside [0, n_slots),
+ * *status: 0; the number of pages that were missing (2^31 - 1: as many or more); or a negative LLMA_E_* (INVAL: a negative length, a slot listed twice, counts that do not fit the table or the stack; RANGE: a slot outside [0, n_slots),
  * more than max_blocks pages, max_rows rows (unless that is 0) or 2^31 - 1).  Unless it is 0, table, owned and the stack stay as they were and
  * the call describes a step without rows.  lens_after may not be lens.  n_slots <= 65536. */
 int llma_map_pages(const int32_t *lens, const int32_t *rows, const int32_t *slots, int32_t n_seqs, int32_t n_slots,

@@ -131,21 +131,26 @@ __global__ __launch_bounds__(N) void map_pages_kernel(MapArgs a) {
             else if (((long long)s.len + s.rows + PAGE_POS - 1) / PAGE_POS > a.max_blocks) code = LLMA_E_RANGE;
         }
         if (code) { atomicMin(&bad, code); s.own = s.need = s.rows = 0; }
-        if (s.rows > 1 << 20) many = 1;                          // (their sum may pass 32 bits; a tile's pages do not: 1024 times 2^25 would, but 2^25 are all there can be)
+        if (s.rows > 1 << 20 || s.own > 1 << 20 || s.need > 1 << 20) many = 1;       // (1024 of them may pass 32 bits)
         MapSums sum;
         const MapSums at = block_scan3<NW>(sums_of(s), part, &sum);
         back += sum.back; more += sum.more; rows += sum.rows;
         if (b0 == 0) { at_mine = at; sum_mine = sum; }
     }
     __syncthreads();
-    if (many) {                                                  // rare: the rows once more, in pieces of 20 bits
-        rows = 0;
+    // Rare: all of them once more, in pieces of 20 bits.  (Where the step is granted, the tiles' sums of pages are right: no more than 2^26 go back or are taken, so
+    // none of them had passed 32 bits)
+    if (many) {
+        back = more = rows = 0;
         for (int b0 = 0; b0 < a.n_seqs; b0 += N) {
             const MapSeq s = b0 == 0 ? mine : load(b0 + t);
-            const int r = s.slot >= 0 && s.rows > 0 ? s.rows : 0;
-            MapSums sum;
-            (void)block_scan3<NW>(MapSums{r & 0xfffff, r >> 20, 0}, part, &sum);
-            rows += sum.back + ((long long)sum.more << 20);
+            const MapSums v = s.slot >= 0 ? sums_of(s) : MapSums{0, 0, 0};       // (of lists that make no sense: not used)
+            MapSums low, high;
+            (void)block_scan3<NW>(MapSums{v.back & 0xfffff, v.more & 0xfffff, v.rows & 0xfffff}, part, &low);
+            (void)block_scan3<NW>(MapSums{v.back >> 20, v.more >> 20, v.rows >> 20}, part, &high);
+            back += low.back + ((long long)high.back << 20);
+            more += low.more + ((long long)high.more << 20);
+            rows += low.rows + ((long long)high.rows << 20);
         }
         __syncthreads();
     }
@@ -154,7 +159,7 @@ __global__ __launch_bounds__(N) void map_pages_kernel(MapArgs a) {
     // (without a slot map only the tables and offsets are wanted: any number of rows)
     if (status == 0 && (rows > 0x7fffffffll || (a.max_rows > 0 && rows > a.max_rows))) status = LLMA_E_RANGE;
     const int stack = top + (status == 0 ? (int)back : 0);       // its height once everything is back
-    if (status == 0 && more > stack) status = (int)(more - stack);
+    if (status == 0 && more > stack) status = (int)(more - stack < 0x7fffffff ? more - stack : 0x7fffffff);
     const bool ok = status == 0, here = a.max_rows > 0 && a.max_rows <= MAP_ROWS_HERE;      // (no map: no row has a place in one)
     if (t == 0) *a.status = status;
     // a tile's sequences and their places, for threads that look them up by page or row

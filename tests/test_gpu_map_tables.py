@@ -42,3 +42,23 @@ def test_a_map_of_one_entry_is_not_no_map(llma):  # noqa: F811
     got = outputs(2, 1)
     llma.llma_map_pages(pages, i32([5, 60]), i32([1, 1]), *got)
     assert got[4].item() == llma.LLMA_E_RANGE and got[0].tolist() == [0, 0, 0] and got[2].item() == -1 and pages.n_free.item() == 8
+
+
+@pytest.mark.parametrize("B", [64, 65, 128, 129, 1024, 1100])
+def test_page_counts_past_32_bits(llma, B):  # noqa: F811
+    """sequences that each want, or own, all of a table's width: their sums pass 2^31 and 2^32.  Missing pages are counted (2^31 - 1 at most), nothing is changed"""
+    total = 130 << 25                                                    # entries of a table, 17 GB (never touched: no page is granted)
+    blocks = min((1 << 25) - 1, total // B)
+    free = 10
+    pages = llma.PageTable(torch.empty((B, blocks), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda"),
+                           torch.arange(free, dtype=torch.int32, device="cuda"), i32([free]))
+    for lens, rows in ((blocks * 64 - 5, 3), (0, blocks * 64), (blocks * 64, 0)):
+        got = outputs(B, 0)
+        llma.llma_map_pages(pages, i32([lens] * B), i32([rows] * B), got[0], got[1], None, None, got[4])
+        missing, too_many = B * blocks - free, B * rows > 0x7fffffff
+        assert got[4].item() == (llma.LLMA_E_RANGE if too_many else min(missing, 0x7fffffff))
+        assert not got[0].any() and (got[1] == lens).all() and not pages.owned.any() and pages.n_free.item() == free
+    pages.owned.fill_(blocks)                                            # more pages than there are
+    got = outputs(B, 0)
+    llma.llma_map_pages(pages, i32([0] * B), i32([1] * B), got[0], got[1], None, None, got[4])
+    assert got[4].item() == llma.LLMA_E_INVAL and (pages.owned == blocks).all() and pages.n_free.item() == free
