@@ -312,7 +312,8 @@ int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtyp
  * Draft j of n_draft[b] (NULL: k everywhere) is accepted while u_accept[b][j] * q(draft) < p(draft), q = draft_probs[b][j] [vocab]
  * (NULL: a copied token, q = 1).  The next token is drawn from max(p - q, 0) at the first rejection (copied token: p without it; p itself
  * where nothing is left), from p of row n_draft when all were accepted: the smallest v whose cumulative weight passes u_sample[b] times
- * the sum.  u in [0, 1).  temperature NULL: 1; not above 0: the arg max, lowest id on ties, as llma_verify_step has it.
+ * the sum.  u in [0, 1).  temperature NULL: 1; not above 0: the arg max, lowest id on ties, as llma_verify_step has it;
+ * infinite: all tokens with a logit above minus infinity alike.
  * NaN logits count as minus infinity; drafts outside [0, vocab) are rejected.  vocab <= 2^24, n_seqs * (k + 1) <= 2^22, else RANGE.
  * Outputs: n_accepted[b] = a, next_token[b] (-1: a row without a logit above minus infinity), emitted[b][0 .. k]: the accepted drafts, the next token, then -1. */
 int64_t llma_verify_sampled_workspace(int32_t n_seqs, int32_t k, int32_t vocab);

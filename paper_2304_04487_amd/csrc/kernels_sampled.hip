@@ -41,6 +41,11 @@ __device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
     const int n = a.n_draft ? a.n_draft[b] : a.k;
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
+// an infinite temperature counts as the largest there is: 0 times minus infinity, of a masked logit, would be no weight at all
+__device__ __forceinline__ float temperature_of(const SampledArgs &a, int b) {
+    const float t = a.temperature ? a.temperature[b] : 1.f;
+    return t > 3.402823466e38f ? 3.402823466e38f : t;
+}
 __device__ __forceinline__ float logit_of(float x) { return x != x ? LLMA_NEG_INF : x; }           // NaN: a token that cannot be
 // A row's weights e^((x - top) / T) in 64 bits, as 2^((x - top) by), by = log2(e) / T.  2^f for |f| <= 1/2 by the polynomial of degree 10 that is 1 at 0 and meets it
 // at the ten Chebyshev points of the interval (off by 6e-16 of it); a whole number is split off by adding 1.5 2^52, whose low word it becomes.
@@ -65,7 +70,7 @@ __device__ __forceinline__ double weight64(float x, const Weigher &w) {
     p = __builtin_amdgcn_ldexp(p, (int)__double_as_longlong(t));
     return w.top == -LLMA_NEG_INF && x == w.top ? 1.0 : p;
 }
-__device__ __forceinline__ double log2_scale(const SampledArgs &a, int b) { return 1.4426950408889634074 / (double)(a.temperature ? a.temperature[b] : 1.f); }
+__device__ __forceinline__ double log2_scale(const SampledArgs &a, int b) { return 1.4426950408889634074 / (double)temperature_of(a, b); }
 
 struct RowPart { float top, sum; int where; };                   // of a chunk: maximum, sum of 2^((x - top) log2(e) / T), first index of the maximum
 
@@ -98,7 +103,7 @@ __global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a
     __shared__ RowPart parts[4];
     const int row = blockIdx.x, b = row / (a.k + 1), j = row % (a.k + 1), t = threadIdx.x, lane = t & 63;
     if (j > drafts_of(a, b)) return;                             // (a row that no draft leads to)
-    const float temp = a.temperature ? a.temperature[b] : 1.f;
+    const float temp = temperature_of(a, b);
     const bool greedy = !(temp > 0.f);
     const RowView v = row_view<TYPE>(a, row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB, first = blockIdx.y * plan.chunk_blocks;
@@ -256,7 +261,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
     const bool in = lane <= a.k, tested = lane < a.k;
     // everything that needs no other value first: a row's chunks eight at a time (those of rows that no draft leads to hold anything)
     const RowPart *const p = (const RowPart *)a.work + (in ? row : (int64_t)b * (a.k + 1)) * plan.chunks;
-    const float temp = a.temperature ? a.temperature[b] : 1.f;
+    const float temp = temperature_of(a, b);
     int draft = -1;
     float q = 1.f, u = 0.f;
     if (tested) {
