@@ -339,7 +339,7 @@ def llma_verify_sampled(logits, drafts, u_accept, u_sample, n_accepted, next_tok
     shape = logits.shape if logits.dim() == 3 else (-1, 0, -1)
     lp, lt = c.rows("logits", logits, shape)
     B, k, V = shape[0], shape[1] - 1, shape[2]
-    if k < 0 or (B > 1 and logits.stride(0) != (k + 1) * logits.stride(1)):
+    if k < 0 or (B > 1 and k > 0 and logits.stride(0) != (k + 1) * logits.stride(1)):
         _refuse("llma_verify_sampled: logits has to be [n_seqs, k + 1, vocab] with all rows the same stride apart")
     row = logits.stride(1) if k > 0 else logits.stride(0)
     ws, size = c.workspace(workspace, c.lib.llma_verify_sampled_workspace(B, k, V))
