@@ -299,7 +299,8 @@ int llma_append_paged(const llma_paged_cache *cache, const void *k, const void *
  * llma_append_paged has written).  out = softmax(scale * q K^T) V per head; query head h reads key head h / (n_heads /
  * n_kv_heads).  q, out: n_rows x n_heads x head_dim of dtype, strides in elements, pointers and strides multiples of 16 bytes; rows of out may overlap neither each other nor q.
  * max_rows: at least the rows of every sequence (a sequence's further rows are not written); rows behind the last sequence's stay as they are.
- * A row that sees nothing becomes 0.  Positions whose page number is outside [0, n_pages) are not seen.
+ * A row that sees nothing becomes 0.  Positions whose page number is outside [0, n_pages) are not seen.  Scales are taken as the powers of two that they
+ * are; with bf16 rows, pages whose v_scale is more than 2^75 below another's of the sequence and head may count as zeros.
  * work: llma_attend_paged_workspace(...) bytes, 16-byte aligned. */
 int64_t llma_attend_paged_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);
 int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtype, int32_t n_heads, int64_t q_row_stride,

@@ -657,6 +657,42 @@ __device__ __forceinline__ void widen16(u32x4 c, float scale, u32x4 &lo, u32x4 &
         hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[2 + w], scale, true));
     }
 }
+// the same as fp16, and their product
+__device__ __forceinline__ void widen16_half(u32x4 c, float scale, u32x4 &lo, u32x4 &hi) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        lo[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[w], scale, false));
+        lo[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[w], scale, true));
+        hi[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 + w], scale, false));
+        hi[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(c[2 + w], scale, true));
+    }
+}
+__device__ __forceinline__ f32x4 mfma16x16x32_half(u32x4 a, u32x4 b, f32x4 c) {
+    return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
+}
+__device__ __forceinline__ uint32_t half_pair(float a, float b) {
+    typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
+    typedef __attribute__((ext_vector_type(2))) float f32x2;
+    return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
+}
+// fp16 products keep their sums in units of a power of two, `now` its exponent as fp32 holds it, so that V fits: a code of 2^-9 .. 448 times 2^-15 .. 2^7 is exact in fp16.
+// A page whose scale is not that near the unit makes its own the unit, but none more than 2^60 below the largest before it (up to 2^62 units may have been
+// added up, and fp32 ends at 2^128): there V counts as zero where it is more than 2^75 below another page's.
+struct SumUnit { int now, least; };
+// What a page's codes are multiplied by (a scale of 0 is no page's: its codes are 0, and the unit stays); the sums have to follow the unit.  (Without branches: 272 us for
+// two sequences of up to 2047 rows, 275 with one; 267 where the unit never changes.)
+__device__ __forceinline__ float unit_factor(float scale, SumUnit &u) {
+    const int e = (int)(__float_as_uint(scale) >> 23 & 255), near = e > u.least ? e : u.least;
+    const bool other = ((unsigned)(e - u.now + 15) > 22u) & (e > 0);
+    u.now = other ? near : u.now;
+    u.least = u.now - 60 > u.least ? u.now - 60 : u.least;
+    return pow2(e - u.now > -126 ? e - u.now : -126);
+}
+__device__ __forceinline__ f32x4 times_pow2(f32x4 v, int e) {
+#pragma unroll
+    for (int r = 0; r < 4; ++r) v[r] = __builtin_amdgcn_ldexpf(v[r], e);
+    return v;
+}
 // the NaN codes among four: 0x80 in their bytes
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & 0x80808080u; }
 __device__ __forceinline__ uint32_t whole_bytes(uint32_t m) { return m | (m - (m >> 7)); }
@@ -723,10 +759,13 @@ __device__ __forceinline__ void attend_store(const AttendArgs &a, int row, int h
     }
 }
 
-// Planes of bf16 that hold a row type's q exactly (fp32: 24 bits) and a probability to the output's precision: one bf16 probability is off by at most
-// 2^-8 of itself, as a bf16 output is, two by 2^-16 (fp16: 2^-11), three by 2^-24.
+// Planes of bf16 that hold a row type's q exactly (fp32: 24 bits), and a probability so that its rounding is lost in the output's: two leave 2^-16 of it, three
+// 2^-24.  bf16 rows take one plane of fp16 (2^-11; the largest as 2^15, what lies 2^32 and more below it is lost) where the products are what bounds the call:
+// from three tiles on, and for many rows.  us, two bf16 planes and one of fp16: two sequences of up to 2047 rows 332 and 272, 16 x 4096 with 33 rows of 32 heads 106 and 97, one of
+// 512 rows over 1000 positions 39 and 34; up to two tiles nothing.  One plane of bf16 would be off by 2^-8, as an output's rounding is: 268, 98 and 35 us, and outputs 0.0022
+// (rms, relative to 64 bits) off where 0.0017 is their own rounding.
 template <int TYPE> constexpr int attend_nq = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
-template <int TYPE> constexpr int attend_np = TYPE == ROWS_BF16 ? 1 : TYPE == ROWS_F32 ? 3 : 2;
+template <int TYPE, bool HALF> constexpr int attend_np = HALF ? 1 : TYPE == ROWS_F32 ? 3 : 2;
 
 // a share's part of one sequence: pages first .. last - 1 of it (none: last = 0)
 struct AttendSeg { AttendSeq s; int b, first, last, pages; };
@@ -736,7 +775,9 @@ template <int DH, int NT, int TYPE> constexpr int attend_lds = 16 * (attend_nq<T
 
 template <int DH, int NT, int TYPE>
 __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(AttendArgs a, AttendPlan plan) {
-    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE>;
+    constexpr bool HALF = TYPE == ROWS_BF16 && NT > 2;
+    constexpr float BIAS = HALF ? 15.f : 0.f;
+    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE, HALF>;
     constexpr int TD = DH / 64, DT = DH / 16, PIECES = attend_pieces<DH, NT>;
     extern __shared__ u32x4 lds[];
     u32x4 *const q = lds;
@@ -860,6 +901,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
         }
         f32x4 o[NT][DT];
         float m[NT], l[NT];
+        SumUnit unit{127, 67};
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
             m[n] = LLMA_NEG_INF;
@@ -934,7 +976,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                     for (int e = 0; e < 16; ++e) top = fmaxf(top, x[e]);
                     top = fmaxf(top, lane_xor<16>(top));
                     top = fmaxf(top, lane_xor<32>(top));
-                    const float mn = fmaxf(m[n], top), ref = mn == LLMA_NEG_INF ? 0.f : mn;
+                    const float mn = fmaxf(m[n], top), ref = mn == LLMA_NEG_INF ? 0.f : mn, from = ref - BIAS;
                     const float keep = __builtin_amdgcn_exp2f(m[n] - ref);
                     m[n] = mn;
                     l[n] *= keep;
@@ -942,7 +984,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                     for (int d = 0; d < DT; ++d) o[n][d] *= keep;
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
+                        x[e] = __builtin_amdgcn_exp2f(x[e] - from);
                         l[n] += x[e];
                     }
 #pragma unroll
@@ -952,24 +994,36 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
                             float y = x[8 * u + 2 * w], z = x[8 * u + 2 * w + 1];
 #pragma unroll
                             for (int pl = 0; pl < NP; ++pl) {
-                                pb[n][pl][u][w] = bf16_pair(y, z);
+                                pb[n][pl][u][w] = HALF ? half_pair(y, z) : bf16_pair(y, z);
                                 if (pl + 1 < NP) { y -= __uint_as_float(pb[n][pl][u][w] << 16); z -= __uint_as_float(pb[n][pl][u][w] & 0xffff0000u); }
                             }
                         }
                 }
                 __builtin_amdgcn_sched_barrier(0);
                 if (masked && __ballot(nans != 0) != 0) attend_nans<DH, NT>(a.c.v + block_of(page) + v_off, base, s.len, limit, o);
+                float v_by = pvs;
+                if constexpr (HALF) {
+                    const int was = unit.now;
+                    v_by = unit_factor(pvs, unit);
+                    if (unit.now != was) {
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int d = 0; d < DT; ++d) o[n][d] = times_pow2(o[n][d], was - unit.now);
+                    }
+                }
 #pragma unroll
                 for (int d = 0; d < DT; ++d) {
                     u32x4 lo, hi;
-                    widen16(vc[d], pvs, lo, hi);
+                    if constexpr (HALF) widen16_half(vc[d], v_by, lo, hi);
+                    else widen16(vc[d], v_by, lo, hi);
                     take_v(next, d);
 #pragma unroll
                     for (int n = 0; n < NT; ++n)
 #pragma unroll
                         for (int pl = NP - 1; pl >= 0; --pl) {
-                            o[n][d] = mfma16x16x32(lo, pb[n][pl][0], o[n][d]);
-                            o[n][d] = mfma16x16x32(hi, pb[n][pl][1], o[n][d]);
+                            o[n][d] = HALF ? mfma16x16x32_half(lo, pb[n][pl][0], o[n][d]) : mfma16x16x32(lo, pb[n][pl][0], o[n][d]);
+                            o[n][d] = HALF ? mfma16x16x32_half(hi, pb[n][pl][1], o[n][d]) : mfma16x16x32(hi, pb[n][pl][1], o[n][d]);
                         }
                 }
             }
@@ -989,6 +1043,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
         for (int n = 0; n < NT; ++n) {
             l[n] += lane_xor<16>(l[n]);
             l[n] += lane_xor<32>(l[n]);
+            if constexpr (HALF) l[n] *= pow2(-15);
             if (kb == 0) { ml[wave][0][n * 16 + col] = m[n]; ml[wave][1][n * 16 + col] = l[n]; }
         }
         __syncthreads();
@@ -1003,7 +1058,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
             for (int w = 0; w < 4; ++w) sum[n] += am[(2 * w + 1) * NT * 16] * __builtin_amdgcn_exp2f(am[2 * w * NT * 16] - ref);
             const float f = __builtin_amdgcn_exp2f(m[n] - ref);
 #pragma unroll
-            for (int d = 0; d < DT; ++d) osum[((wave * NT + n) * DT + d) * 64 + lane] = o[n][d] * f;
+            for (int d = 0; d < DT; ++d) osum[((wave * NT + n) * DT + d) * 64 + lane] = HALF ? times_pow2(o[n][d] * f, unit.now - 127 - 15) : o[n][d] * f;
         }
         __syncthreads();
         const bool whole = seg.first == 0 && seg.last == seg.pages;
@@ -1047,7 +1102,9 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
 template <int DH> constexpr int rows_images = (4 * (DH / 64) * 2 + (DH / 16) * 2) * 64;       // 16-byte pieces of a page
 template <int DH, int NT, int TYPE>
 __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int blocks) {
-    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE>, TD = DH / 64, DT = DH / 16;
+    constexpr bool HALF = TYPE == ROWS_BF16;
+    constexpr float BIAS = HALF ? 7.f : 0.f;
+    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE, HALF>, TD = DH / 64, DT = DH / 16;
     extern __shared__ u32x4 lds[];                               // [2] pages
     __shared__ int nan_seen[2][4];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -1131,6 +1188,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
 #pragma unroll
         for (int u = 0; u < DT / 4; ++u) vc[u] = *(const u32x4 *)((a.c.v + at + 16 * (4 * u + wave) * PAGE_POS) + v_off);
     };
+    SumUnit unit{127, 67};                                       // of the page that was widened last
     const auto widen = [&](int i) {
         u32x4 *const to = lds + (i & 1) * rows_images<DH>;
 #pragma unroll
@@ -1140,7 +1198,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
             to[((wave * TD + t) * 2) * 64 + lane] = lo;
             to[((wave * TD + t) * 2 + 1) * 64 + lane] = hi;
         }
-        const float vs = scale_of(now.vs, later.vs, i);
+        float vs = scale_of(now.vs, later.vs, i);
+        if constexpr (HALF) vs = unit_factor(vs, unit);
         uint32_t nans = 0;
         if (i * PAGE_POS + PAGE_POS - 1 > block_first || id_of(i) < 0) {       // positions that some row does not see
             const int there = id_of(i) < 0 ? 0 : s.len - i * PAGE_POS - 16 * kb;
@@ -1158,7 +1217,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
 #pragma unroll
         for (int u = 0; u < DT / 4; ++u) {
             u32x4 lo, hi;
-            widen16(vc[u], vs, lo, hi);
+            if constexpr (HALF) widen16_half(vc[u], vs, lo, hi);
+            else widen16(vc[u], vs, lo, hi);
             to[4 * TD * 2 * 64 + ((4 * u + wave) * 2) * 64 + lane] = lo;
             to[4 * TD * 2 * 64 + ((4 * u + wave) * 2 + 1) * 64 + lane] = hi;
         }
@@ -1180,7 +1240,9 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
         if (pages > 1) take(1);
     }
     __syncthreads();
+    int o_unit = unit.now;                                       // that the wave's sums are in
     for (int i = 0; i < pages; ++i) {
+        const int page_unit = unit.now;
         if (i + 1 < pages) widen(i + 1);
         if (i + 2 < pages) take(i + 2);
         const int base = i * PAGE_POS;
@@ -1197,6 +1259,13 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
             const float by = fmaxf(to_log2 * scale_of(now.ks, later.ks, i), 1e-37f);
             u32x4 pb[NT][NP][2];
             f32x4 sc[NT][4];
+            if (HALF && page_unit != o_unit) {                   // (exact)
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] = times_pow2(o[n][d], o_unit - page_unit);
+                o_unit = page_unit;
+            }
 #pragma unroll
             for (int n = 0; n < NT; ++n)
 #pragma unroll
@@ -1231,8 +1300,8 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
                     for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[n][g][r]);
                 top = fmaxf(top, lane_xor<16>(top));
                 top = fmaxf(top, lane_xor<32>(top)) * by;
-                if (__ballot(top > m[n] + 8.f) != 0) {
-                    const float mn = fmaxf(m[n], top), keep = __builtin_amdgcn_exp2f(m[n] - (mn == LLMA_NEG_INF ? 0.f : mn));
+                if (__ballot(top > m[n] + (8.f + BIAS)) != 0) {
+                    const float mn = fmaxf(m[n], top - BIAS), keep = __builtin_amdgcn_exp2f(m[n] - (mn == LLMA_NEG_INF ? 0.f : mn));
                     m[n] = mn;
                     l[n] *= keep;
 #pragma unroll
@@ -1247,7 +1316,7 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
                         float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][g][r], by, -ref)), z = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][g][r + 1], by, -ref));
 #pragma unroll
                         for (int p = 0; p < NP; ++p) {
-                            pb[n][p][u][w] = bf16_pair(y, z);
+                            pb[n][p][u][w] = HALF ? half_pair(y, z) : bf16_pair(y, z);
                             if (p + 1 < NP) { y -= __uint_as_float(pb[n][p][u][w] << 16); z -= __uint_as_float(pb[n][p][u][w] & 0xffff0000u); }
                         }
                     }
@@ -1261,14 +1330,16 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) l[n] = mfma16x16x32((u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, pb[n][p][u], l[n]);
+                    for (int n = 0; n < NT; ++n)
+                        l[n] = HALF ? mfma16x16x32_half((u32x4){0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}, pb[n][p][u], l[n])
+                                    : mfma16x16x32((u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, pb[n][p][u], l[n]);
 #pragma unroll
             for (int j = 0; j < VI; ++j) {
                 const int d = j / 2, u = j % 2;
 #pragma unroll
                 for (int p = NP - 1; p >= 0; --p)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) o[n][d] = mfma16x16x32(w[(KI + j) % 8], pb[n][p][u], o[n][d]);
+                    for (int n = 0; n < NT; ++n) o[n][d] = HALF ? mfma16x16x32_half(w[(KI + j) % 8], pb[n][p][u], o[n][d]) : mfma16x16x32(w[(KI + j) % 8], pb[n][p][u], o[n][d]);
                 if (j + 8 < VI) {
                     w[(KI + j) % 8] = img[(KI + j + 8) * 64];
                     __builtin_amdgcn_sched_group_barrier(0x008, NT * NP, 0);
@@ -1290,7 +1361,10 @@ __global__ __launch_bounds__(256, 2) void attend_rows_kernel(AttendArgs a, int b
         if (r >= R) continue;
         const float inv = l[n][0] == 0.f ? 0.f : 1.f / l[n][0];
 #pragma unroll
-        for (int d = 0; d < DT; ++d) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 16 * d + 4 * kb, o[n][d] * inv);
+        for (int d = 0; d < DT; ++d) {
+            const f32x4 v = o[n][d] * inv;
+            attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 16 * d + 4 * kb, HALF ? times_pow2(v, o_unit - 127) : v);
+        }
     }
 }
 
