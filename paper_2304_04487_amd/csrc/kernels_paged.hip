@@ -86,9 +86,11 @@ __device__ __forceinline__ MapSums block_scan3(MapSums v, MapSums *part, MapSums
     *total = all;
     return MapSums{before.back + in.back - v.back, before.more + in.more - v.more, before.rows + in.rows - v.rows};
 }
-__device__ __forceinline__ void map_row(const MapArgs &a, int i, int slot, int pos) {
-    const int page = a.table[(size_t)slot * a.max_blocks + pos / PAGE_POS];
-    a.slot_map[i] = (unsigned)page < (unsigned)a.n_pages ? page * PAGE_POS + pos % PAGE_POS : -1;      // (a free list that holds no page's number)
+// row i of the call, row j of sequence b
+__device__ __forceinline__ void map_row(const MapArgs &a, int i, int b, int j, int slot, int len) {
+    const int pos = len + j, page = a.table[(size_t)slot * a.max_blocks + pos / PAGE_POS];
+    const bool mapped = a.last_live == nullptr || j <= a.last_live[b];
+    a.slot_map[i] = mapped && (unsigned)page < (unsigned)a.n_pages ? page * PAGE_POS + pos % PAGE_POS : -1;      // (a free list that holds no page's number)
     a.row_pos[i] = pos;
 }
 
@@ -215,7 +217,7 @@ __global__ __launch_bounds__(N) void map_pages_kernel(MapArgs a) {
             __syncthreads();
             for (int i = t; i < sum.rows; i += N) {
                 const int q = count_le(tile.first, N, i) - 1;
-                map_row(a, row0 + i, tile.seq[q].slot, tile.seq[q].len + i - tile.first[q]);
+                map_row(a, row0 + i, b0 + q, i - tile.first[q], tile.seq[q].slot, tile.seq[q].len);
             }
         }
         row0 += sum.rows;
@@ -242,7 +244,7 @@ __global__ __launch_bounds__(256) void map_rows_kernel(MapArgs a) {
             continue;
         }
         const int b = kept ? count_le(offsets + 1, a.n_seqs, i) : count_le(a.row_offsets + 1, a.n_seqs, i), slot = a.slots ? a.slots[b] : b;
-        map_row(a, i, slot, a.lens[slot] + i - (kept ? offsets[b] : a.row_offsets[b]));
+        map_row(a, i, b, i - (kept ? offsets[b] : a.row_offsets[b]), slot, a.lens[slot]);
     }
 }
 void launch_map_pages(const MapArgs &a, hipStream_t st) {
@@ -252,14 +254,14 @@ void launch_map_pages(const MapArgs &a, hipStream_t st) {
     if (a.max_rows > MAP_ROWS_HERE) hipLaunchKernelGGL(map_rows_kernel, dim3((a.max_rows + 511) / 512), dim3(256), 0, st, a);
 }
 
-__global__ __launch_bounds__(256) void pass_rows_kernel(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots) {
+__global__ __launch_bounds__(256) void pass_rows_kernel(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, const int *last_live, int *rows, int *slots) {
     for (int b = threadIdx.x; b < n_seqs; b += 256) {
-        rows[b] = segs ? segs[b].rows : m;
+        rows[b] = segs ? segs[b].rows : last_live && n_seqs == 1 && *last_live + 1 < m ? *last_live + 1 : m;
         slots[b] = segs ? segs[b].slot : batch_slots[b];
     }
 }
-void launch_pass_rows(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots, hipStream_t st) {
-    hipLaunchKernelGGL(pass_rows_kernel, dim3(1), dim3(256), 0, st, segs, batch_slots, n_seqs, m, rows, slots);
+void launch_pass_rows(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, const int *last_live, int *rows, int *slots, hipStream_t st) {
+    hipLaunchKernelGGL(pass_rows_kernel, dim3(1), dim3(256), 0, st, segs, batch_slots, n_seqs, m, last_live, rows, slots);
 }
 
 // ---------------------------------------------------------------------------------------------

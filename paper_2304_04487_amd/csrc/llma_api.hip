@@ -220,6 +220,11 @@ static int create_pages(llma_ctx *c, size_t Rp) {
         ALLOC(c, p.v, (size_t)n_pages * H * PAGE_POS * dh);
         ALLOC(c, p.k_scale, (size_t)n_pages * H * 4);
         ALLOC(c, p.v_scale, (size_t)n_pages * H * 4);
+        // (never-written positions hold finite values: a batch's rows without a token look at them)
+        HIP_TRY(c, hipMemsetAsync(p.k, 0, (size_t)n_pages * H * PAGE_POS * dh, c->st));
+        HIP_TRY(c, hipMemsetAsync(p.v, 0, (size_t)n_pages * H * PAGE_POS * dh, c->st));
+        HIP_TRY(c, hipMemsetAsync(p.k_scale, 0, (size_t)n_pages * H * 4, c->st));
+        HIP_TRY(c, hipMemsetAsync(p.v_scale, 0, (size_t)n_pages * H * 4, c->st));
         c->pages.push_back(p);
     }
     const size_t B = g.max_batch, rows = Rp > (size_t)g.max_seq ? Rp : (size_t)g.max_seq;
@@ -649,14 +654,16 @@ static int forward_f32(llma_ctx *c, int n_seqs, int m, bool lm_head) {
 }
 
 // paged cache: the pass's pages and slots (once per pass), and a layer's fresh rows into its pages and the attention over them
-static void map_pass(llma_ctx *c, const PromptSeg *segs, int n_seqs, int m, int total_rows) {
+// last_live: generations, whose rows behind that carry no token.  (One sequence's are not there at all; a batch's keep their places among the pass's rows and see what their pages hold)
+static void map_pass(llma_ctx *c, const PromptSeg *segs, int n_seqs, int m, int total_rows, const int *last_live) {
     c->pg_seqs = n_seqs;
     c->pg_max_rows = m;
-    launch_pass_rows(segs, c->s.batch_slots, n_seqs, m, c->pg_rows, c->pg_slots, c->run_st);
+    launch_pass_rows(segs, c->s.batch_slots, n_seqs, m, last_live, c->pg_rows, c->pg_slots, c->run_st);
     MapArgs a{};
     a.lens = c->s.T; a.rows = c->pg_rows; a.slots = c->pg_slots; a.n_seqs = n_seqs; a.n_slots = c->cfg.max_batch;
     a.table = c->pg_table; a.max_blocks = c->blocks; a.owned = c->pg_owned; a.free_pages = c->pg_free; a.n_free = c->pg_n_free; a.n_pages = c->blocks * c->cfg.max_batch;
     a.row_offsets = c->pg_offsets; a.lens_after = c->pg_after; a.slot_map = c->pg_slot_map; a.row_pos = c->pg_row_pos; a.max_rows = total_rows; a.status = c->pg_status;
+    a.last_live = last_live;
     launch_map_pages(a, c->run_st);
 }
 static void attend_pages(llma_ctx *c, int layer, int rows, const AttnArgs &aa) {
@@ -798,7 +805,7 @@ static int step_body(llma_ctx *c, int kind, int n_seqs, int m, int n_chunks, int
     if (kind == STEP_PREFILL || kind == STEP_PROMPTS) {
         if (kind == STEP_PROMPTS) { c->n_segs = e.n_segs = n_seqs; e.segs = (const PromptSeg *)c->gen_segs; }
         launch_setup_prefill_rows(c->s, c->gen_prompt, c->gen_counters + 4 * c->cfg.max_batch, m, slot, c->cs_table, c->cfg.head_dim / 2, e, st);
-        if (c->paged) map_pass(c, kind == STEP_PROMPTS ? e.segs : nullptr, kind == STEP_PROMPTS ? n_seqs : 1, m, m);
+        if (c->paged) map_pass(c, kind == STEP_PROMPTS ? e.segs : nullptr, kind == STEP_PROMPTS ? n_seqs : 1, m, m, nullptr);
         int rc = forward(c, 1, m, n_chunks, false, slot);
         c->n_segs = 0;
         if (rc || kind == STEP_PROMPTS) return rc;              // (whose lengths differ from pass to pass of the same shape)
@@ -811,7 +818,7 @@ static int step_body(llma_ctx *c, int kind, int n_seqs, int m, int n_chunks, int
     if (!gen) launch_take_step(c->s, n_seqs, mk, st);
     else if (c->gen_spans > 1) launch_trigger_scan(gen, n_seqs, c->gen_spans, part, st);
     launch_setup_step_rows(c->s, n_seqs, m, mk, c->cs_table, c->cfg.head_dim / 2, e, gen, part, c->gen_spans, st);
-    if (c->paged) map_pass(c, nullptr, n_seqs, m, n_seqs * m);
+    if (c->paged) map_pass(c, nullptr, n_seqs, m, n_seqs * m, gen ? c->s.keff : nullptr);
     int rc = forward(c, n_seqs, m, n_chunks, true, slot);
     if (rc) return rc;
     if (kind == STEP_SAMPLED) {

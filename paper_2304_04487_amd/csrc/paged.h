@@ -34,10 +34,11 @@ struct MapArgs {
     int *slot_map, *row_pos;             // [max_rows] each
     int max_rows;
     int *status;
+    const int *last_live;                // [n_seqs] or null: rows behind row last_live[b] of sequence b carry no token and are mapped nowhere
 };
 OPTIONAL void launch_map_pages(const MapArgs &a, hipStream_t st);
-// a context's pass as the calls above take it: rows[b] and slots[b] from its segments, or m rows of each of batch_slots
-OPTIONAL void launch_pass_rows(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, int *rows, int *slots, hipStream_t st);
+// a context's pass as the calls above take it: rows[b] and slots[b] from its segments, or m rows (one sequence with last_live: *last_live + 1) of each of batch_slots
+OPTIONAL void launch_pass_rows(const PromptSeg *segs, const int *batch_slots, int n_seqs, int m, const int *last_live, int *rows, int *slots, hipStream_t st);
 
 struct AppendArgs {
     PagedCache c;
