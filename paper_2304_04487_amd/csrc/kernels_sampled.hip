@@ -252,8 +252,9 @@ __device__ __forceinline__ float logit_at(const SampledArgs &a, int64_t row, int
 }
 
 // How many drafts of sequence b hold, and which row its token comes from.  All threads of a workgroup call it and get the same; lane j looks at
-// row j.  The sums of the rows' chunks are fp32: a test whose sides are nearer than 2^-15 of each other is decided
-// again with the row's sum in 64 bits (the sums are off by 5e-6 at most: 2e-7 of the exponent, which is up to 17 where weights still matter, and of a chunk's factor).
+// row j.  The sums of the rows' chunks are fp32: a test whose sides are nearer than 3e-5 of each other, and 2^-24 for each chunk, is decided
+// again with the row's sum in 64 bits.  (A chunk's sum is off by 5e-6 at most: 2e-7 of the exponent, which is up to 17 where weights still matter, 64 addends a thread, and its factor; each chunk
+// that is added rounds the sum by half of 2^-23.  2^24 tokens are up to 8192 chunks.)
 template <int TYPE>
 __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, double *part) {
     const int lane = threadIdx.x & 63;
@@ -305,7 +306,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
             right = weight64(logit, weigher(top, by64));
             left = (double)u * (double)q * (double)sum;
             ok = left < right;
-            near = right > 0.0 && fabs(left - right) <= 3e-5 * right;
+            near = right > 0.0 && fabs(left - right) <= (3e-5 + plan.chunks * 0x1p-24) * right;
         }
     }
     unsigned long long yes = __ballot(ok), unsure = __ballot(near);

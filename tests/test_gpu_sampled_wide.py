@@ -54,3 +54,23 @@ def test_tokens_left_by_draft_probabilities(llma, V, dtype, cover):  # noqa: F81
         n, token, emitted, near = oracle.verify(x, drafts[b], 1, pr, 1.0, ua[b], us[b])
         assert near > 1e-13 and n == 0
         assert (got[0][b], got[1][b]) == (n, token), (b, float(us[b]))
+
+
+@pytest.mark.parametrize("V,dtype", [(3000001, "fp32"), (1 << 23, "bf16")])
+def test_tests_next_to_their_border(llma, V, dtype):  # noqa: F811
+    """copied drafts with random numbers from 1e-7 to 1e-3 of their probability below and above it: sums over hundreds of chunks, all alike, do not tell the nearest"""
+    rows = torch.full((2, V), -1.2345)
+    rows[:, 77] = 6.0
+    rows = rows.to(DT[dtype])
+    x = rows.double().numpy()
+    w = np.exp(x[0] - x[0].max())
+    B = 24
+    ua = np.zeros((B, 1), np.float32)
+    draft = 77
+    p = w[draft] / w.sum()
+    for b in range(B):
+        off = 10.0 ** (-7 + b // 2 * 4 / 11)
+        ua[b, 0] = np.float32(p * (1 + (off if b % 2 else -off)))
+    logits = rows.cuda().expand(B, 2, V).contiguous()
+    got = call(llma, logits, np.full((B, 1), draft), ua, np.full(B, 0.3, np.float32))
+    assert got[0].tolist() == [int(float(u) < p) for u in ua[:, 0]] and 0 < got[0].sum() < B
