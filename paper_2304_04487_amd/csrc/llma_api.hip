@@ -1121,11 +1121,10 @@ struct SampleIn { const float *temperature, *u_accept, *u_sample; };
 // memory of sampled steps of up to `rows` rows
 static int ensure_sampling(llma_ctx *c, int n_seqs, int k) {
     const size_t B = c->cfg.max_batch, mk = c->cfg.max_k;
-    if (!c->pin_sample) {
-        if (!c->sample_dev) ALLOC(c, c->sample_dev, B * (2 + mk + 2 + mk + 1) * 4);
-        HIP_TRY(c, hipHostMalloc((void **)&c->pin_sample, B * (2 + mk) * 4, hipHostMallocMapped | hipHostMallocCoherent));
-        HIP_TRY(c, hipHostGetDevicePointer((void **)&c->pin_sample_dev, c->pin_sample, 0));
-    }
+    // (each by itself: what a failed call got is kept, what it did not get is asked for again)
+    if (!c->sample_dev) ALLOC(c, c->sample_dev, B * (2 + mk + 2 + mk + 1) * 4);
+    if (!c->pin_sample) HIP_TRY(c, hipHostMalloc((void **)&c->pin_sample, B * (2 + mk) * 4, hipHostMallocMapped | hipHostMallocCoherent));
+    if (!c->pin_sample_dev) HIP_TRY(c, hipHostGetDevicePointer((void **)&c->pin_sample_dev, c->pin_sample, 0));
     int rc = LLMA_OK;
     if (!c->logits_dump) rc = ensure_cap(c, &c->sample_logits, &c->cap_sample_logits, (size_t)n_seqs * (k + 1) * c->cfg.vocab);
     if (!rc) rc = ensure_cap(c, &c->sample_work, &c->cap_sample_work, ((size_t)verify_sampled_bytes(n_seqs, k, c->cfg.vocab) + 3) / 4);
