@@ -46,7 +46,9 @@ extern "C" {
                                 bytes of kv_split = 1, half of one bf16 plane.  Values are rounded to four significant bits, so
                                 logits are those of another, rounded cache (not within the tolerance of the two planes), and a
                                 rejected draft may have raised its page's scale, which rounds values below e4m3's normal range
-                                again: the tokens of k > 0 and k = 0 agree except at near-ties. */
+                                again: the tokens of k > 0 and k = 0 agree except at near-ties.  Fresh K and V go to bf16 first,
+                                as in the other caches, and from there to their codes.  (Before there was a paged cache every
+                                value but 0 meant the two planes: callers that gave 2 now give 1.) */
 
 typedef struct llma_ctx llma_ctx;           /* opaque; owns re-tiled weights, KV cache, scratch */
 
@@ -58,8 +60,8 @@ typedef struct {
     int32_t dtype;         /* LLMA_DTYPE_*                                                  */
     int32_t kv_split;      /* bf16 only: 1 = keep K and V as a bf16 hi plane plus an 8-bit lo plane
                               (the residual x - hi as fp8 e4m3 of 256 times it: 1.5 x the cache
-                              bytes, 12 significand bits), 0 = one bf16 plane, LLMA_KV_PAGED = pages of 8-bit
-                              values (below).  Ignored for fp32 */
+                              bytes, 12 significand bits; so does any other value), 0 = one bf16 plane,
+                              LLMA_KV_PAGED (2) = pages of 8-bit values (above).  Ignored for fp32 */
     float   rms_eps;       /* RMSNorm(x; g) = g * x / sqrt(mean(x^2) + rms_eps)              */
     float   rope_theta;    /* rotary base: feature i pairs with i + head_dim/2, angle
                               pos * rope_theta^(-2i/head_dim)                               */

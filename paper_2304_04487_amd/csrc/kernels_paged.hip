@@ -524,13 +524,15 @@ void launch_append_paged(const AppendArgs &a, hipStream_t st) {
 // The pages of all sequences, end to end, are cut into equal shares, one per workgroup and key head: ragged lengths load the chip
 // evenly, and a share's four waves take its pages in turn and meet in LDS at a sequence's end.  A sequence that lies in one share
 // is finished there; the others' parts are joined by attend_join_kernel.
-// Steps are bound by one read of the cache: 16 sequences of up to 4096 positions, 9 rows of 32 heads of 128, 361 MB in 74 us of kernels = 4.9 TB/s, 61 of 5 rows, four
-// query heads a key head, fp16, 671 MB in 146 = 4.6; a kernel of the same mapping that only loads is within 3 to 10 % of that.
+// Steps are bound by one read of the cache: 16 sequences of up to 4096 positions, 9 rows of 32 heads of 128, 361 MB in 76 to 83 us a call = 4.4 to 4.7 TB/s, 61 of 5 rows, four
+// query heads a key head, fp16, 671 MB in 148 to 155 = 4.3 to 4.5.  This kernel alone takes 79 and 148 us under the profiler, one of the same mapping that only loads 75 and 130.
 // Short sequences are not cut: a workgroup per sequence and key head, no count of the others' pages, nothing to join.  It is bound by what one compute unit
-// takes in, 44 KB a microsecond, so it pays while a table's row holds few pages more than an equal share would.  us, cut and whole, 9 rows of 32 heads of 128, bf16:
-// one sequence of 512 / 1001 / 1500 positions 10.5 / 11.0 / 11.8 and 9.8 / 11.1 / 13.7; six 17.7 / 19.7 / 21.7 and 10.8 / 13.2 / 15.9, of 2500 27.4 and 21.8; 16
-// 24.1 / 29.2 / 34 and 16.4 / 21.7 / 29.8; 64 of 1001 / 1900 / 3900 90 / 144 / 256 and 86 / 139 / 262.  Four of 5 rows, 8 key heads, 1001 / 2000: 13.5 / 13.2 and 11.2 / 16.6.
-// Eight waves for one compute unit instead of four changed nothing.
+// takes in, 44 KB a microsecond, so it pays while a table's row holds few pages more than an equal share would.  us inside a captured graph, cut and whole, 9 rows of 32 heads of 128:
+//                     1 x 512    1 x 1001   1 x 1500   6 x 1001   6 x 2000   16 x 512   16 x 1001  64 x 1001  64 x 1900
+//   bf16              11.5 10.5  12.0 11.9  12.5 14.5  20.7 13.6  27.5 20.4  24.5 17.1  30.0 22.0  85.3 81.4  153 150
+//   fp16              11.5 11.1  12.3 12.7  12.7 15.8  21.1 14.4  27.8 22.0  25.7 17.8  31.0 23.0  88.9 84.0  154 152
+//   fp32              11.9 11.7  12.6 13.5  13.1 17.0  22.2 15.3  29.0 23.4  26.1 18.9  32.1 23.4  91.8 91.2  160 161
+// and a bf16 call of its own, 64 of 3900 256 and 262, four of 5 rows, 8 key heads, 1001 / 2000 13.5 / 13.2 and 11.2 / 16.6.  Eight waves for one compute unit instead of four changed nothing.
 #define ATTEND_CUS 256           // compute units; two workgroups each, one where three or four tiles fill the registers
 #define ATTEND_MIN_PAGES 4       // of a share: a page per wave
 
@@ -1091,15 +1093,19 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_kernel(Atte
 
 // ---- many rows -----------------------------------------------------------------------------------
 // Which calls take it: those with more rows a key head than the shares' kernel holds (64) and at least this many row blocks.  Fewer leave compute units
-// without work, where shares cut the pages too.  Both at 32 heads of 128, bf16, 1000 positions before 512 / 640 / 768 rows (128, 160, 192 blocks) 54 / 57 / 61
-// us here, 42 / 70 / 74 in shares; 16 sequences of 18 x 4 rows over 4000 positions (128) 111 and 85, 64 of 20 x 4 over 1000 (512) 48 and 127.
+// without work, where shares cut the pages too.  us inside a captured graph, here and in shares, 32 heads of 128, 1000 positions before 512 / 640 / 768 rows (128, 160, 192 blocks; fp32
+// twice as many), 16 sequences of 18 x 4 rows over 4000 positions (128), 64 of 20 x 4 over 1000 (512):
+//   bf16  47.6 33.4   50.1 60.0   54.7 62.3   107 75   43 90
+//   fp16  62.2 43.6   65.3 78.8   71.1 81.6   142 96   57 117
+//   fp32  49.4 60.1   59.8 104    64.8 106    114 126  71 157
+// fp32 with 160 / 256 rows (96, 128 blocks) 38.9 / 42.0 and 45.2 / 46.9: its blocks would pay from fewer on.
 #define ROWS_MIN 160
 // Prompts: a workgroup takes 64 NT rows of a sequence's key head and all pages they see.  Each page is widened once, for all four waves, into LDS as the
 // operands' images (16 KB of K, 16 KB of V at head_dim 128); a page is requested two ahead, widened one ahead, one barrier a page.  A wave holds its rows' queries and
 // sums in registers and meets nobody at the end.  Pages behind a wave's rows are skipped; the longest row blocks start first, and a key head's on one XCD.
 // The reference of the exponentials moves only when a maximum passes it by 2^8: the sums are rescaled once or twice a row instead of once a page.
-// Bound by issue: two sequences of up to 2047 rows, 32 query and 8 key heads of 128, over up to 2900 positions before, bf16, 136 GFLOP in 267 us = 0.51 PFLOP/s, vector instructions
-// in 46 % of the cycles, matrix instructions in 34 %.  The exponentials of one page beside the products of the next spilled (330 to 430 us); eight waves a page, 256
+// Bound by issue: two sequences of up to 2047 rows, 32 query and 8 key heads of 128, over up to 2900 positions before, bf16, 136 GFLOP in 272 us = 0.50 PFLOP/s, vector instructions
+// in 46 % of the compute units' busy cycles, matrix instructions in 39 %, LDS in 28 %.  The exponentials of one page beside the products of the next spilled (330 to 430 us); eight waves a page, 256
 // rows, 2 % faster there and 10 % slower for prompts without a cache (84 us against 76 for 2047 rows of 32 heads).
 template <int DH> constexpr int rows_images = (4 * (DH / 64) * 2 + (DH / 16) * 2) * 64;       // 16-byte pieces of a page
 template <int DH, int NT, int TYPE>
