@@ -254,7 +254,7 @@ __device__ __forceinline__ float logit_at(const SampledArgs &a, int64_t row, int
 // How many drafts of sequence b hold, and which row its token comes from.  All threads of a workgroup call it and get the same; lane j looks at
 // row j.  The sums of the rows' chunks are fp32: a test whose sides are nearer than 3e-5 of each other, and 2^-24 for each chunk, is decided
 // again with the row's sum in 64 bits.  (A chunk's sum is off by 5e-6 at most: 2e-7 of the exponent, which is up to 17 where weights still matter, 64 addends a thread, and its factor; each chunk
-// that is added rounds the sum by half of 2^-23.  2^24 tokens are up to 8192 chunks.)
+// that is added rounds the sum by half of 2^-23.  A row has up to 4096.)
 template <int TYPE>
 __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, double *part) {
     const int lane = threadIdx.x & 63;

@@ -79,7 +79,7 @@ struct SampledArgs {
     void *work;
 };
 #define SAMPLED_MAX_K 63                 // (a lane per row)
-#define SAMPLED_MAX_VOCAB (1 << 24)      // (ids and pieces of a row in 32 bits, 16384 ranges of it in a grid's second dimension)
+#define SAMPLED_MAX_VOCAB (1 << 24)      // (ids and pieces of a row in 32 bits, 8192 ranges of it in a grid's second dimension)
 #define SAMPLED_MAX_ROWS (1 << 22)       // of a call
 OPTIONAL int64_t verify_sampled_bytes(int n_seqs, int k, int vocab);
 OPTIONAL void launch_verify_sampled(const SampledArgs &a, hipStream_t st);

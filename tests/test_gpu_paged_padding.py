@@ -99,3 +99,41 @@ def test_batched_generations_leave_no_padding_either(made):
         assert got[1] == want[1]
         assert np.abs(ctx.logits(1) - logits).max() <= 2.0 ** -16 * np.abs(logits).max(), float(np.abs(ctx.logits(1) - logits).max() / np.abs(logits).max())
     ctx.close(), one.close()
+
+
+@pytest.mark.parametrize("prompt", [1, 30, 64, 150])
+def test_steps_do_not_depend_on_what_ran_before(made, prompt):
+    """prompts, steps of several widths, batches and imports on a context whose pages and buffers other sequences have used, and on a new one"""
+    import torch
+    llma, make = made
+    rng = np.random.default_rng(prompt)
+    p, drafts = rng.integers(0, CFG.vocab, prompt), rng.integers(0, CFG.vocab, (4, 12))
+    shape = (CFG.n_heads, 70, CFG.head_dim)
+    kv = [[torch.tensor(rng.standard_normal(shape), dtype=torch.bfloat16, device="cuda") for _ in range(2)] for _ in range(2)]
+    seen = []
+    for used in (False, True):
+        ctx = make(12)
+        ctx.enable_logits_dump(26)
+        if used:
+            for s in range(2):
+                ctx.prefill(rng.integers(0, CFG.vocab, 170 - 60 * s), seq=s)
+                ctx.verify_step(rng.integers(0, CFG.vocab, 12), seq=s)
+            ctx.generate_batch([rng.integers(0, CFG.vocab, 33)] * 2, [None] * 2, 1, 12, 20)
+            for s in range(2):
+                ctx.reset(s)
+        out = []
+        ctx.prefill(p, seq=1)
+        for d in (drafts[0], drafts[1][:3], drafts[2][:0]):
+            out.append(ctx.verify_step(d, seq=1))
+            out.append(ctx.logits(len(d) + 1))
+        for l in range(2):
+            ctx.kv_import(0, l, *kv[l], 70)
+        ctx.set_pending(5, 0)
+        out.append([x.tolist() if hasattr(x, "tolist") else x for x in ctx.verify_step_batch([0, 1], drafts[:2])])
+        out.append(ctx.logits(26))
+        out.append(ctx.verify_step_sampled(drafts[3], 0.9, np.full(12, 0.01, np.float32), 0.37, seq=1))
+        out.append(ctx.logits(13))
+        seen.append(out)
+        ctx.close()
+    for a, b in zip(*seen):
+        assert np.array_equal(a, b) if isinstance(a, np.ndarray) else a == b
