@@ -257,6 +257,7 @@ int llma_generate_batch(llma_ctx *ctx, int32_t n_seqs, const int32_t *seqs,
 #define LLMA_DTYPE_F16 2         /* rows of these calls only: fp16 (a context is F32 or BF16) */
 #define LLMA_PAGED_MAX_SEQS 4096 /* sequences of one llma_attend_paged */
 #define LLMA_SAMPLED_MAX_K 63    /* drafts per sequence of one llma_verify_sampled */
+#define LLMA_LOGPROBS_MAX_TOP 64 /* alternatives per row of one llma_token_logprobs */
 
 /* A layer's cache.  k [n_pages][n_kv_heads][64][head_dim] and v [n_pages][n_kv_heads][head_dim][64] (transposed) hold
  * OCP fp8 e4m3 codes, k_scale and v_scale [n_pages][n_kv_heads] powers of two, one for each page and head; a cached value is
@@ -310,6 +311,42 @@ int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtyp
                       const int32_t *lens, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, int32_t max_rows, float scale,
                       void *out, int64_t out_row_stride, int64_t out_head_stride, void *work, int64_t work_bytes, void *hip_stream);
 
+/* Rows out of the cache: row row_offsets[b] + j (below row_offsets[b+1]) of k and v becomes position first[b] + j (first NULL: 0) of the pages
+ * table[slots[b]], all heads, in dtype (code * scale, rounded once).  For a cache in planes (llma_kv_import takes rows head by head: any strides will
+ * do), for another program, for a look at what is cached.  k and v as llma_append_paged takes them, but not the same memory and without
+ * rows on top of each other.  Positions outside the table, and those whose page number is outside [0, n_pages), read as 0; rows behind the
+ * last sequence's stay as they are.  n_seqs <= LLMA_PAGED_MAX_SEQS, n_rows * n_kv_heads <= 2^28. */
+int llma_read_paged(const llma_paged_cache *cache, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,
+                    const int32_t *first, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, void *k, void *v, int32_t dtype,
+                    int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, void *hip_stream);
+
+/* The same cache in 4 bits, about half of the bytes: e2m1 codes (0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives) with a scale for every 32
+ * neighbouring features of a position, a power of two held as its exponent plus 127 (255: NaN), as OCP microscaling's MXFP4 has it.
+ * k [n_pages][n_kv_heads][64][head_dim / 2] and v [n_pages][n_kv_heads][head_dim / 2][64] (transposed): byte j of a position holds feature
+ * 2j in its low half, 2j + 1 in its high half; k_scale and v_scale bytes [n_pages][n_kv_heads][head_dim / 32][64].  A cached value is
+ * code * 2^(scale - 127).  All four 16-byte aligned; pages, tables and slots are llma_map_pages' as with 8 bits. */
+typedef struct {
+    void *k, *v, *k_scale, *v_scale;
+    int32_t n_pages, n_kv_heads, head_dim;
+} llma_paged_mx_cache;
+
+/* Writes rows into the 4-bit cache; arguments as llma_append_paged has them.  Every row has scales of its own: per 32 features the smallest power of
+ * two (from 2^-64 to 2^120) s with max |x| / s <= 7 over the finite values; codes are x / s rounded to nearest even, +-6 beyond; +-inf become
+ * +-6, a NaN makes its 32 features NaN.  So a write changes nothing but its rows' positions, and rows may come in any
+ * order; a slot listed twice has either row's codes. */
+int llma_append_paged_mx(const llma_paged_mx_cache *cache, const void *k, const void *v, int32_t dtype, int64_t k_row_stride,
+                         int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot_map, int32_t n_rows,
+                         void *hip_stream);
+/* llma_attend_paged and llma_read_paged over it. */
+int64_t llma_attend_paged_mx_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);
+int llma_attend_paged_mx(const llma_paged_mx_cache *cache, const void *q, int32_t dtype, int32_t n_heads, int64_t q_row_stride,
+                         int64_t q_head_stride, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,
+                         const int32_t *lens, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, int32_t max_rows, float scale,
+                         void *out, int64_t out_row_stride, int64_t out_head_stride, void *work, int64_t work_bytes, void *hip_stream);
+int llma_read_paged_mx(const llma_paged_mx_cache *cache, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,
+                       const int32_t *first, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, void *k, void *v, int32_t dtype,
+                       int64_t k_row_stride, int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, void *hip_stream);
+
 /* Verification of drafted tokens against the target's probabilities, from given random numbers.  logits: n_seqs * (k + 1) rows of
  * vocab values of dtype, row_stride elements apart; row (b, j) follows drafts[b][0 .. j).  p = softmax(logits / temperature[b]).
  * Draft j of n_draft[b] (NULL: k everywhere) is accepted while u_accept[b][j] * q(draft) < p(draft), q = draft_probs[b][j] [vocab]
@@ -324,6 +361,21 @@ int llma_verify_sampled(const void *logits, int32_t dtype, int64_t row_stride, i
                         const int32_t *drafts, const int32_t *n_draft, const float *draft_probs, const float *temperature,
                         const float *u_accept, const float *u_sample, int32_t *n_accepted, int32_t *next_token, int32_t *emitted,
                         void *work, int64_t work_bytes, void *hip_stream);
+
+/* What a model answered, in probabilities: for each of n_rows rows of vocab logits of dtype, row_stride elements apart, p = softmax(logits /
+ * temperature[i]) (NULL, or a temperature not above 0: 1; infinite: all tokens with a logit above minus infinity alike), and of it
+ *   logprob[i]  log p of tokens[i] (minus infinity where p is 0, and for a token outside [0, vocab))
+ *   rank[i]     tokens before it by falling logit, ties by rising id: 0 for the arg max; -1 for a token outside [0, vocab)
+ *   entropy[i]  -sum p log p
+ *   top_tokens, top_logprobs [i][0 .. n_top): the first n_top tokens of that order and their log p; -1 and minus infinity behind the last with a logit above it
+ * (natural logarithms; logprob, rank, entropy may be NULL, tokens too without the first two; the alternatives are n_top > 0's, at most
+ * LLMA_LOGPROBS_MAX_TOP).  NaN logits count as minus infinity, several plus infinities share the probability.  A row without a logit above minus infinity:
+ * entropy 0, no alternatives.  vocab <= 2^24, n_rows <= 2^22, both together 2^40, else RANGE.
+ * work: llma_token_logprobs_workspace(...) bytes, 16-byte aligned. */
+int64_t llma_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top);
+int llma_token_logprobs(const void *logits, int32_t dtype, int64_t row_stride, int32_t vocab, int32_t n_rows, const int32_t *tokens,
+                        const float *temperature, int32_t n_top, float *logprob, int32_t *rank, float *entropy, int32_t *top_tokens,
+                        float *top_logprobs, void *work, int64_t work_bytes, void *hip_stream);
 
 /* --- inspection / measurement --------------------------------------------------------- */
 /* When dev_buf != NULL every later forward also writes its rows' logits, fp32

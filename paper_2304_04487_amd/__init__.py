@@ -27,10 +27,12 @@ EXPORTS = [
     "llma_get_kernel_timing", "llma_time_ffn_gemm", "llma_time_step_gemm", "llma_device_bytes", "llma_find_trigger_static", "llma_truncate",
     "llma_describe", "llma_map_pages", "llma_append_paged", "llma_attend_paged", "llma_attend_paged_workspace",
     "llma_verify_sampled", "llma_verify_sampled_workspace", "llma_verify_step_sampled", "llma_verify_step_sampled_batch",
+    "llma_read_paged", "llma_append_paged_mx", "llma_attend_paged_mx", "llma_attend_paged_mx_workspace", "llma_read_paged_mx",
+    "llma_token_logprobs", "llma_token_logprobs_workspace",
 ]
 LLMA_TRIGGER_STATIC_MAX_REF = 1 << 20
 LLMA_DTYPE_F16, LLMA_KV_PAGED = 2, 2
-LLMA_PAGE, LLMA_PAGED_MAX_SEQS, LLMA_SAMPLED_MAX_K = 64, 4096, 63
+LLMA_PAGE, LLMA_PAGED_MAX_SEQS, LLMA_SAMPLED_MAX_K, LLMA_LOGPROBS_MAX_TOP = 64, 4096, 63, 64
 
 
 class LlmaError(RuntimeError):
@@ -52,6 +54,11 @@ class WeightsC(ctypes.Structure):
 
 
 class PagedCacheC(ctypes.Structure):
+    _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
+                ("n_pages", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32)]
+
+
+class PagedMxCacheC(ctypes.Structure):
     _fields_ = [("k", c_void_p), ("v", c_void_p), ("k_scale", c_void_p), ("v_scale", c_void_p),
                 ("n_pages", c_int32), ("n_kv_heads", c_int32), ("head_dim", c_int32)]
 
@@ -100,10 +107,17 @@ def load_library() -> ctypes.CDLL:
     lib.llma_time_step_gemm.argtypes = [vp, c_int32, c_int32, c_int32, POINTER(c_double)]
     lib.llma_map_pages.argtypes = [vp, vp, vp, c_int32, c_int32, vp, c_int32, vp, vp, vp, c_int32, vp, vp, vp, vp, c_int32, vp, vp]
     lib.llma_append_paged.argtypes = [POINTER(PagedCacheC), vp, vp, c_int32, c_int64, c_int64, c_int64, c_int64, vp, c_int32, vp]
-    lib.llma_attend_paged_workspace.argtypes = [c_int32] * 6
-    lib.llma_attend_paged_workspace.restype = c_int64
+    lib.llma_append_paged_mx.argtypes = [POINTER(PagedMxCacheC)] + lib.llma_append_paged.argtypes[1:]
+    lib.llma_attend_paged_workspace.argtypes = lib.llma_attend_paged_mx_workspace.argtypes = [c_int32] * 6
+    lib.llma_attend_paged_workspace.restype = lib.llma_attend_paged_mx_workspace.restype = c_int64
     lib.llma_attend_paged.argtypes = [POINTER(PagedCacheC), vp, c_int32, c_int32, c_int64, c_int64, vp, vp, c_int32, c_int32, vp, vp,
                                       c_int32, c_int32, c_int32, c_float, vp, c_int64, c_int64, vp, c_int64, vp]
+    lib.llma_attend_paged_mx.argtypes = [POINTER(PagedMxCacheC)] + lib.llma_attend_paged.argtypes[1:]
+    lib.llma_read_paged.argtypes = [POINTER(PagedCacheC), vp, vp, c_int32, c_int32, vp, vp, c_int32, c_int32, vp, vp, c_int32, c_int64, c_int64, c_int64, c_int64, vp]
+    lib.llma_read_paged_mx.argtypes = [POINTER(PagedMxCacheC)] + lib.llma_read_paged.argtypes[1:]
+    lib.llma_token_logprobs_workspace.argtypes = [c_int32] * 3
+    lib.llma_token_logprobs_workspace.restype = c_int64
+    lib.llma_token_logprobs.argtypes = [vp, c_int32, c_int64, c_int32, c_int32, vp, vp, c_int32, vp, vp, vp, vp, vp, vp, c_int64, vp]
     lib.llma_verify_sampled_workspace.argtypes = [c_int32] * 3
     lib.llma_verify_sampled_workspace.restype = c_int64
     lib.llma_verify_sampled.argtypes = [vp, c_int32, c_int64, c_int32, c_int32, c_int32, vp, vp, vp, vp, vp, vp, vp, vp, vp, vp, c_int64, vp]
@@ -170,6 +184,22 @@ class PagedCache:
                    torch.empty((n_pages, n_kv_heads, head_dim, LLMA_PAGE), dtype=torch.uint8, device=device),
                    torch.empty((n_pages, n_kv_heads), dtype=torch.float32, device=device),
                    torch.empty((n_pages, n_kv_heads), dtype=torch.float32, device=device))
+
+
+class PagedMxCache:
+    """A layer's cache in 4 bits: uint8 tensors k [n_pages, n_kv_heads, 64, head_dim / 2], v [n_pages, n_kv_heads, head_dim / 2, 64], k_scale and v_scale
+    [n_pages, n_kv_heads, head_dim / 32, 64] (see llma.h)."""
+    __slots__ = ("k", "v", "k_scale", "v_scale")
+
+    def __init__(self, k, v, k_scale, v_scale):
+        self.k, self.v, self.k_scale, self.v_scale = k, v, k_scale, v_scale
+
+    @classmethod
+    def empty(cls, n_pages: int, n_kv_heads: int, head_dim: int, device="cuda"):
+        import torch
+        u8 = {"dtype": torch.uint8, "device": device}
+        return cls(torch.empty((n_pages, n_kv_heads, LLMA_PAGE, head_dim // 2), **u8), torch.empty((n_pages, n_kv_heads, head_dim // 2, LLMA_PAGE), **u8),
+                   torch.empty((n_pages, n_kv_heads, head_dim // 32, LLMA_PAGE), **u8), torch.empty((n_pages, n_kv_heads, head_dim // 32, LLMA_PAGE), **u8))
 
 
 class PageTable:
@@ -249,6 +279,15 @@ class _Call:
         return PagedCacheC(self.ptr("cache.k", k, u8, (P, H, LLMA_PAGE, D)), self.ptr("cache.v", c.v, u8, (P, H, D, LLMA_PAGE)),
                            self.ptr("cache.k_scale", c.k_scale, f32, (P, H)), self.ptr("cache.v_scale", c.v_scale, f32, (P, H)), P, H, D)
 
+    def mx_cache(self, c):
+        k, u8 = c.k, _torch.uint8
+        if k.dim() != 4:
+            _refuse(f"{self.who}: cache.k has to be [n_pages, n_kv_heads, {LLMA_PAGE}, head_dim / 2]")
+        P, H, _, D = k.shape
+        scales = (P, H, D // 16, LLMA_PAGE)
+        return PagedMxCacheC(self.ptr("cache.k", k, u8, (P, H, LLMA_PAGE, D)), self.ptr("cache.v", c.v, u8, (P, H, D, LLMA_PAGE)),
+                             self.ptr("cache.k_scale", c.k_scale, u8, scales), self.ptr("cache.v_scale", c.v_scale, u8, scales), P, H, 2 * D)
+
     def workspace(self, given, size: int):
         """a workspace of the caller's, or one that lives until the stream has used it (the allocator orders its reuse on the stream)"""
         _check(size)
@@ -288,18 +327,43 @@ def llma_map_pages(pages, lens, rows, row_offsets, lens_after, slot_map, row_pos
           None if n == 0 else p("slot_map", slot_map, i32, (n,)), None if n == 0 else p("row_pos", row_pos, i32, (n,)), n, p("status", status, i32, (1,)))
 
 
-def llma_append_paged(cache, k, v, slot_map, stream=None):
-    """Writes rows k, v [n_rows, n_kv_heads, head_dim] (bf16, fp16 or fp32; features together, other strides as they are) into the paged
-    cache at slot_map (int32 [n_rows], negative: nowhere); see llma.h.  Enqueues and returns without synchronising."""
-    c = _Call("llma_append_paged", k, stream)
-    d = c.cache(cache)
+def _append(c, fn, d, k, v, slot_map):
     shape = (slot_map.numel(), d.n_kv_heads, d.head_dim)
     kp, kt = c.rows("k", k, shape)
     vp, vt = c.rows("v", v, shape)
     if kt != vt:
-        _refuse("llma_append_paged: k and v have different types")
-    c.run(c.lib.llma_append_paged, byref(d), kp, vp, kt, k.stride(0), k.stride(1), v.stride(0), v.stride(1),
-          c.ptr("slot_map", slot_map, _torch.int32, (shape[0],)), shape[0])
+        _refuse(f"{c.who}: k and v have different types")
+    c.run(fn, byref(d), kp, vp, kt, k.stride(0), k.stride(1), v.stride(0), v.stride(1), c.ptr("slot_map", slot_map, _torch.int32, (shape[0],)), shape[0])
+
+
+def llma_append_paged(cache, k, v, slot_map, stream=None):
+    """Writes rows k, v [n_rows, n_kv_heads, head_dim] (bf16, fp16 or fp32; features together, other strides as they are) into the paged
+    cache at slot_map (int32 [n_rows], negative: nowhere); see llma.h.  Enqueues and returns without synchronising."""
+    c = _Call("llma_append_paged", k, stream)
+    _append(c, c.lib.llma_append_paged, c.cache(cache), k, v, slot_map)
+
+
+def llma_append_paged_mx(cache, k, v, slot_map, stream=None):
+    """The same into a PagedMxCache (4 bits; see llma.h)."""
+    c = _Call("llma_append_paged_mx", k, stream)
+    _append(c, c.lib.llma_append_paged_mx, c.mx_cache(cache), k, v, slot_map)
+
+
+def _attend(c, fn, size, d, q, table, lens, row_offsets, max_rows, scale, out, slots, workspace):
+    i32, p = _torch.int32, c.ptr
+    shape = (q.shape[0], q.shape[1], d.head_dim) if q.dim() == 3 else (-1,)
+    qp, qt = c.rows("q", q, shape)
+    op, ot = c.rows("out", out, shape)
+    if qt != ot:
+        _refuse(f"{c.who}: out and q have different types")
+    B = lens.numel()
+    S, blocks = table.shape if table.dim() == 2 else (-1, -1)
+    tp = p("table", table, i32, (S, blocks))
+    ws, size = c.workspace(workspace, size(B, blocks, shape[1], d.n_kv_heads, d.head_dim, max_rows))
+    c.run(fn, byref(d), qp, qt, shape[1], q.stride(0), q.stride(1), tp, None if slots is None else p("slots", slots, i32, (B,)),
+          S, blocks, p("lens", lens, i32, (B,)), p("row_offsets", row_offsets, i32, (B + 1,)), B, shape[0], max_rows, scale,
+          op, out.stride(0), out.stride(1), ws.data_ptr(), size)
+    return out
 
 
 def llma_attend_paged(cache, q, table, lens, row_offsets, max_rows: int, scale: float, out, slots=None, workspace=None, stream=None):
@@ -308,24 +372,49 @@ def llma_attend_paged(cache, q, table, lens, row_offsets, max_rows: int, scale: 
     rows.  workspace: at least llma_attend_paged_workspace() bytes of device memory, None: allocated for the call.  Enqueues
     and returns without synchronising.  Returns out."""
     c = _Call("llma_attend_paged", q, stream)
-    i32, p, d = _torch.int32, c.ptr, c.cache(cache)
-    shape = (q.shape[0], q.shape[1], d.head_dim) if q.dim() == 3 else (-1,)
-    qp, qt = c.rows("q", q, shape)
-    op, ot = c.rows("out", out, shape)
-    if qt != ot:
-        _refuse("llma_attend_paged: out and q have different types")
-    B = lens.numel()
-    S, blocks = table.shape if table.dim() == 2 else (-1, -1)
-    tp = p("table", table, i32, (S, blocks))
-    ws, size = c.workspace(workspace, c.lib.llma_attend_paged_workspace(B, blocks, shape[1], d.n_kv_heads, d.head_dim, max_rows))
-    c.run(c.lib.llma_attend_paged, byref(d), qp, qt, shape[1], q.stride(0), q.stride(1), tp, None if slots is None else p("slots", slots, i32, (B,)),
-          S, blocks, p("lens", lens, i32, (B,)), p("row_offsets", row_offsets, i32, (B + 1,)), B, shape[0], max_rows, scale,
-          op, out.stride(0), out.stride(1), ws.data_ptr(), size)
-    return out
+    return _attend(c, c.lib.llma_attend_paged, c.lib.llma_attend_paged_workspace, c.cache(cache), q, table, lens, row_offsets, max_rows, scale, out, slots, workspace)
 
 
 def llma_attend_paged_workspace(n_seqs: int, max_blocks: int, n_heads: int, n_kv_heads: int, head_dim: int, max_rows: int) -> int:
     return _check(load_library().llma_attend_paged_workspace(n_seqs, max_blocks, n_heads, n_kv_heads, head_dim, max_rows))
+
+
+def llma_attend_paged_mx(cache, q, table, lens, row_offsets, max_rows: int, scale: float, out, slots=None, workspace=None, stream=None):
+    """The same over a PagedMxCache (4 bits; see llma.h).  workspace: at least llma_attend_paged_mx_workspace() bytes."""
+    c = _Call("llma_attend_paged_mx", q, stream)
+    return _attend(c, c.lib.llma_attend_paged_mx, c.lib.llma_attend_paged_mx_workspace, c.mx_cache(cache), q, table, lens, row_offsets, max_rows, scale, out, slots, workspace)
+
+
+def llma_attend_paged_mx_workspace(n_seqs: int, max_blocks: int, n_heads: int, n_kv_heads: int, head_dim: int, max_rows: int) -> int:
+    return _check(load_library().llma_attend_paged_mx_workspace(n_seqs, max_blocks, n_heads, n_kv_heads, head_dim, max_rows))
+
+
+def _read(c, fn, d, table, first, row_offsets, k, v, slots):
+    i32, p = _torch.int32, c.ptr
+    shape = (k.shape[0] if k.dim() == 3 else -1, d.n_kv_heads, d.head_dim)
+    kp, kt = c.rows("k", k, shape)
+    vp, vt = c.rows("v", v, shape)
+    if kt != vt:
+        _refuse(f"{c.who}: k and v have different types")
+    B = row_offsets.numel() - 1
+    S, blocks = table.shape if table.dim() == 2 else (-1, -1)
+    c.run(fn, byref(d), p("table", table, i32, (S, blocks)), None if slots is None else p("slots", slots, i32, (B,)), S, blocks,
+          None if first is None else p("first", first, i32, (B,)), p("row_offsets", row_offsets, i32, (B + 1,)), B, shape[0], kp, vp, kt,
+          k.stride(0), k.stride(1), v.stride(0), v.stride(1))
+
+
+def llma_read_paged(cache, table, first, row_offsets, k, v, slots=None, stream=None):
+    """Rows out of the paged cache into k, v [n_rows, n_kv_heads, head_dim] (bf16, fp16 or fp32; features together, other strides as they are): rows
+    row_offsets[b] .. row_offsets[b + 1] - 1 become the positions from first[b] on of sequence b (see llma.h).  int32 tensors table [n_slots, max_blocks], first
+    [n_seqs] (None: 0), row_offsets [n_seqs + 1], slots [n_seqs] or None.  Enqueues and returns without synchronising."""
+    c = _Call("llma_read_paged", k, stream)
+    _read(c, c.lib.llma_read_paged, c.cache(cache), table, first, row_offsets, k, v, slots)
+
+
+def llma_read_paged_mx(cache, table, first, row_offsets, k, v, slots=None, stream=None):
+    """The same out of a PagedMxCache (4 bits; see llma.h)."""
+    c = _Call("llma_read_paged_mx", k, stream)
+    _read(c, c.lib.llma_read_paged_mx, c.mx_cache(cache), table, first, row_offsets, k, v, slots)
 
 
 def llma_verify_sampled(logits, drafts, u_accept, u_sample, n_accepted, next_token, emitted, n_draft=None, draft_probs=None, temperature=None,
@@ -351,6 +440,30 @@ def llma_verify_sampled(logits, drafts, u_accept, u_sample, n_accepted, next_tok
 
 def llma_verify_sampled_workspace(n_seqs: int, k: int, vocab: int) -> int:
     return _check(load_library().llma_verify_sampled_workspace(n_seqs, k, vocab))
+
+
+def llma_token_logprobs(logits, tokens, logprob, rank=None, entropy=None, top_tokens=None, top_logprobs=None, temperature=None, workspace=None, stream=None):
+    """Log probabilities of given tokens under softmax(logits / temperature), with ranks, entropy and the likeliest alternatives (see llma.h).  logits [n_rows, vocab]
+    (bf16, fp16 or fp32, rows any stride apart), tokens int32 [n_rows] (or None), temperature fp32 [n_rows]; written, each may be None: logprob, entropy fp32 [n_rows],
+    rank int32 [n_rows], top_tokens int32 and top_logprobs fp32 [n_rows, n_top] (both or none).  workspace: at least llma_token_logprobs_workspace() bytes
+    of device memory, None: allocated for the call.  Enqueues and returns without synchronising."""
+    c = _Call("llma_token_logprobs", logits, stream)
+    i32, f32, p = _torch.int32, _torch.float32, c.ptr
+    shape = logits.shape if logits.dim() == 2 else (-1, -1)
+    lp, lt = c.rows("logits", logits, shape)
+    n, V = shape
+    if (top_tokens is None) != (top_logprobs is None):
+        _refuse("llma_token_logprobs: top_tokens and top_logprobs come together")
+    top = 0 if top_tokens is None else top_tokens.shape[-1] if top_tokens.dim() == 2 else -1
+    ws, size = c.workspace(workspace, c.lib.llma_token_logprobs_workspace(n, V, top))
+    c.run(c.lib.llma_token_logprobs, lp, lt, logits.stride(0) if n > 1 else max(logits.stride(0), V), V, n, None if tokens is None else p("tokens", tokens, i32, (n,)),
+          None if temperature is None else p("temperature", temperature, f32, (n,)), top, None if logprob is None else p("logprob", logprob, f32, (n,)),
+          None if rank is None else p("rank", rank, i32, (n,)), None if entropy is None else p("entropy", entropy, f32, (n,)),
+          None if top == 0 else p("top_tokens", top_tokens, i32, (n, top)), None if top == 0 else p("top_logprobs", top_logprobs, f32, (n, top)), ws.data_ptr(), size)
+
+
+def llma_token_logprobs_workspace(n_rows: int, vocab: int, n_top: int) -> int:
+    return _check(load_library().llma_token_logprobs_workspace(n_rows, vocab, n_top))
 
 
 class Context:

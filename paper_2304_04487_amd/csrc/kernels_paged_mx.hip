@@ -1,0 +1,671 @@
+// The paged 4-bit cache: the write into it, attention of a step's rows over it; and rows read back out of it and out of the 8-bit cache.
+#include "paged_attend.h"
+
+// ---------------------------------------------------------------------------------------------
+// codes and scales
+// ---------------------------------------------------------------------------------------------
+// e2m1: 0, 0.5, 1, 1.5, 2, 3, 4, 6 and their negatives.  The conversions read a scale's exponent bits alone (255: NaN), so one of four scale bytes
+// gets into place by one shift, whatever its neighbours leave in the other bits.
+template <int T> __device__ __forceinline__ float scale_byte(uint32_t w) { return __uint_as_float(T == 3 ? w >> 1 : w << (23 - 8 * T)); }
+template <int T> __device__ __forceinline__ uint32_t widen2(uint32_t c, float scale) {       // byte T's two features as bf16
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(c, scale, T));
+}
+// eight neighbouring features: an operand
+__device__ __forceinline__ u32x4 widen8(uint32_t c, float scale) { return (u32x4){widen2<0>(c, scale), widen2<1>(c, scale), widen2<2>(c, scale), widen2<3>(c, scale)}; }
+__device__ __forceinline__ uint32_t nan_scales(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u; }      // 0x80 in the bytes that are 255
+// exponent of the smallest power of two s from 2^-64 to 2^120 with amax / s <= 7: 6 is the largest code, and what lies up to 7 rounds to it by half a step as elsewhere
+// (7 costs less than 6: 19.0 dB of normal values' blocks kept, 18.75 with 6, 18.8 with 8)
+__device__ __forceinline__ int mx_exponent(float amax) {
+    const uint32_t b = __float_as_uint(amax);
+    const int e = (int)(b >> 23) - 127 - 2 + ((b & 0x7fffffu) > 0x600000u);
+    return e < -64 ? -64 : e > 120 ? 120 : e;
+}
+
+// ---------------------------------------------------------------------------------------------
+// write into the cache
+// ---------------------------------------------------------------------------------------------
+// Per row, head and 32 features: s as above over the finite values, code = x / s rounded to nearest even (+-inf become +-6; a NaN makes the scale 255, the codes 0).
+// 16 (8) lanes share a row's 128 (64) features, eight each.  A lane has the rows of up to four neighbouring positions, a quad, so that a byte of the
+// transposed V leaves as one word for four positions, and so do the scales; a quad that is not whole leaves byte by byte.  A wave takes the quads that begin in its
+// window of rows, 4 (8) at once: a prompt's rows are quads from its second page position divisible by four on, wherever it begins.
+template <int DH, int TYPE, bool KEYS>
+__device__ __forceinline__ void append_mx_quad(const AppendMxArgs &a, int head, int row, int n, int slot, int oct) {
+    constexpr int FB = DH / 32;
+    const int page = slot / PAGE_POS, at = slot % PAGE_POS;
+    const size_t block = (size_t)page * a.c.heads + head;
+    float v[4][8];
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int i = row + (r < n ? r : 0);
+        if constexpr (KEYS) row8<TYPE>(a.k, i * a.k_row + head * a.k_head + 8 * oct, v[r]);
+        else row8<TYPE>(a.v, i * a.v_row + head * a.v_head + 8 * oct, v[r]);
+    }
+    uint32_t codes[4], scales = 0;
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        float amax = 0.f;
+        int nan = 0;
+#pragma unroll
+        for (int e = 0; e < 8; ++e) {
+            const float x = fabsf(v[r][e]);
+            amax = fmaxf(amax, x < __builtin_huge_valf() ? x : 0.f);
+            nan |= x != x;
+        }
+        amax = fmaxf(amax, lane_xor<1>(amax));
+        nan |= lane_xor<1>(nan);
+        amax = fmaxf(amax, lane_xor<2>(amax));
+        nan |= lane_xor<2>(nan);
+        const int e = mx_exponent(amax);
+        const float s = pow2(e);
+        uint32_t c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(0u, v[r][0], v[r][1], s, 0);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[r][2], v[r][3], s, 1);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[r][4], v[r][5], s, 2);
+        c = __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(c, v[r][6], v[r][7], s, 3);
+        codes[r] = nan ? 0u : c;
+        scales |= (uint32_t)(nan ? 255 : e + 127) << 8 * r;
+    }
+    uint8_t *const sc = (KEYS ? a.c.k_scale : a.c.v_scale) + (block * FB + oct / 4) * PAGE_POS + at;
+    const bool whole = n == 4;                                   // (then at is a multiple of four)
+    if (oct % 4 == 0) {
+        if (whole) *(uint32_t *)sc = scales;
+        else
+            for (int r = 0; r < n; ++r) sc[r] = (uint8_t)(scales >> 8 * r);
+    }
+    if constexpr (KEYS) {
+        uint32_t *const to = (uint32_t *)(a.c.k + (block * PAGE_POS + at) * (DH / 2)) + oct;
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (r < n) to[r * (DH / 8)] = codes[r];
+    } else {
+        uint8_t *const to = a.c.v + (block * (DH / 2) + 4 * oct) * PAGE_POS + at;
+        if (whole) {
+            // four rows' four bytes, turned
+            const uint32_t p = __builtin_amdgcn_perm(codes[1], codes[0], 0x05010400u), q = __builtin_amdgcn_perm(codes[3], codes[2], 0x05010400u);
+            const uint32_t t = __builtin_amdgcn_perm(codes[1], codes[0], 0x07030602u), u = __builtin_amdgcn_perm(codes[3], codes[2], 0x07030602u);
+            *(uint32_t *)to = __builtin_amdgcn_perm(q, p, 0x05040100u);
+            *(uint32_t *)(to + PAGE_POS) = __builtin_amdgcn_perm(q, p, 0x07060302u);
+            *(uint32_t *)(to + 2 * PAGE_POS) = __builtin_amdgcn_perm(u, t, 0x05040100u);
+            *(uint32_t *)(to + 3 * PAGE_POS) = __builtin_amdgcn_perm(u, t, 0x07060302u);
+        } else {
+#pragma unroll
+            for (int r = 0; r < 4; ++r)
+                if (r < n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) to[j * PAGE_POS + r] = (uint8_t)(codes[r] >> 8 * j);
+        }
+    }
+}
+#define APPEND_MX_WINDOW 16
+template <int DH, int TYPE>
+__global__ __launch_bounds__(256) void append_paged_mx_kernel(AppendMxArgs a, int n_windows) {
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int units = 2 * a.c.heads, unit = (int)(id % units);
+    if (id / units >= n_windows) return;
+    const int r0 = (int)(id / units) * APPEND_MX_WINDOW, head = unit >> 1;
+    // lanes 0 .. 19: the window's slots, and those of three rows behind it; lane 63: the row's before it
+    const int i = lane == 63 ? r0 - 1 : r0 + lane;
+    int slot = -1;
+    if ((lane < APPEND_MX_WINDOW + 3 || lane == 63) && i >= 0 && i < a.n_rows) slot = a.slot_map[i];
+    if (slot < 0 || slot / PAGE_POS >= a.c.n_pages) slot = -1;
+    const int before = __shfl(slot, (lane + 63) & 63);
+    const bool follows = slot >= 0 && before >= 0 && slot == before + 1 && slot % 4 != 0;         // the row before it, in its quad
+    const uint32_t on = (uint32_t)__ballot(follows && lane < 32);
+    uint32_t starts = (uint32_t)__ballot(slot >= 0 && !follows && lane < APPEND_MX_WINDOW);
+    constexpr int LANES = DH / 8, GROUPS = 64 / LANES;
+    const int oct = lane % LANES, group = lane / LANES;
+    while (starts) {
+        int mine = -1;
+#pragma unroll
+        for (int g = 0; g < GROUPS; ++g) {
+            if (starts && g == group) mine = __builtin_ctz(starts);
+            starts &= starts - 1;
+        }
+        const int from = mine < 0 ? 0 : mine, n = 1 + __builtin_ctz(~(on >> (from + 1)));         // (rows that follow: at most three, as a quad ends at a multiple of four)
+        const int first = __shfl(slot, from);
+        if (mine < 0) continue;
+        if (unit & 1) append_mx_quad<DH, TYPE, false>(a, head, r0 + from, n, first, oct);
+        else append_mx_quad<DH, TYPE, true>(a, head, r0 + from, n, first, oct);
+    }
+}
+void launch_append_paged_mx(const AppendMxArgs &a, hipStream_t st) {
+    if (a.n_rows < 1) return;
+    const int n_windows = (a.n_rows + APPEND_MX_WINDOW - 1) / APPEND_MX_WINDOW;
+    const int64_t blocks = ((int64_t)n_windows * 2 * a.c.heads + 3) / 4;
+    auto of = [&](auto dh) {
+        constexpr int DH = decltype(dh)::value;
+        if (a.type == ROWS_BF16) hipLaunchKernelGGL((append_paged_mx_kernel<DH, ROWS_BF16>), dim3((unsigned)blocks), dim3(256), 0, st, a, n_windows);
+        else if (a.type == ROWS_F16) hipLaunchKernelGGL((append_paged_mx_kernel<DH, ROWS_F16>), dim3((unsigned)blocks), dim3(256), 0, st, a, n_windows);
+        else hipLaunchKernelGGL((append_paged_mx_kernel<DH, ROWS_F32>), dim3((unsigned)blocks), dim3(256), 0, st, a, n_windows);
+    };
+    if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
+    else of(std::integral_constant<int, 64>{});
+}
+
+// ---------------------------------------------------------------------------------------------
+// rows out of the cache
+// ---------------------------------------------------------------------------------------------
+// Row j of sequence b is position first[b] + j.  A run = rows of one sequence inside one page; a workgroup takes one head of the runs that begin in its window of 64 rows (a long
+// sequence's: one).  K's rows lie as they leave.  V's lie across: a lane takes four positions of eight features, turns them in registers and has
+// eight neighbouring features of four rows.
+#define READ_WINDOW 64
+#define READ_KEPT 4097           // offsets in LDS: LLMA_PAGED_MAX_SEQS + 1
+struct ReadRun { int row, n, page, at; };                        // page -1: none, the rows become 0
+template <int TYPE>
+__device__ __forceinline__ void store8(void *p, int64_t at, const float v[8]) {
+    if constexpr (TYPE == ROWS_F32) {
+        *(f32x4 *)((float *)p + at) = (f32x4){v[0], v[1], v[2], v[3]};
+        *(f32x4 *)((float *)p + at + 4) = (f32x4){v[4], v[5], v[6], v[7]};
+    } else if constexpr (TYPE == ROWS_F16) {
+        *(u32x4 *)((bf16_t *)p + at) = (u32x4){half_pair(v[0], v[1]), half_pair(v[2], v[3]), half_pair(v[4], v[5]), half_pair(v[6], v[7])};
+    } else {
+        *(u32x4 *)((bf16_t *)p + at) = (u32x4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
+    }
+}
+typedef __attribute__((ext_vector_type(2))) float f32x2;
+template <int T> __device__ __forceinline__ f32x2 value2(uint32_t c, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, T); }
+// eight features: 4-bit, one word
+__device__ __forceinline__ void values8(uint32_t c, float scale, float v[8]) {
+    const f32x2 p[4] = {value2<0>(c, scale), value2<1>(c, scale), value2<2>(c, scale), value2<3>(c, scale)};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = p[e / 2][e % 2];
+}
+// 8-bit, two words
+__device__ __forceinline__ void values8(u32x2 c, float scale, float v[8]) {
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+        v[4 * w] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 0) * scale;
+        v[4 * w + 1] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 1) * scale;
+        v[4 * w + 2] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 2) * scale;
+        v[4 * w + 3] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 3) * scale;
+    }
+}
+// four words of four bytes, turned: word r gets byte r of each
+__device__ __forceinline__ void turn4(uint32_t w[4]) {
+    const uint32_t p = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), q = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+    const uint32_t t = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), u = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(q, p, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(q, p, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(u, t, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(u, t, 0x07060302u);
+}
+template <typename C, int DH, int TYPE>
+__device__ __forceinline__ void read_run(const ReadArgs<C> &a, int head, const ReadRun &r) {
+    constexpr bool MX = std::is_same_v<C, PagedMxCache>;
+    constexpr int OCTS = DH / 8, ROWS = 256 / OCTS, PASSES = PAGE_POS / ROWS;
+    const size_t block = (size_t)(r.page < 0 ? 0 : r.page) * a.c.heads + head;
+    const bool none = r.page < 0;
+    {
+        const int oct = threadIdx.x % OCTS, j0 = threadIdx.x / OCTS;
+        std::conditional_t<MX, uint32_t, u32x2> c[PASSES];
+        float s[PASSES];
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int j = j0 + p * ROWS, at = r.at + (j < r.n ? j : 0);
+            if constexpr (MX) {
+                c[p] = ((const uint32_t *)(a.c.k + (block * PAGE_POS + at) * (DH / 2)))[oct];
+                s[p] = __uint_as_float((uint32_t)a.c.k_scale[(block * (DH / 32) + oct / 4) * PAGE_POS + at] << 23);
+            } else {
+                c[p] = ((const u32x2 *)(a.c.k + (block * PAGE_POS + at) * DH))[oct];
+                s[p] = a.c.k_scale[block];
+            }
+        }
+#pragma unroll
+        for (int p = 0; p < PASSES; ++p) {
+            const int j = j0 + p * ROWS;
+            if (j >= r.n) continue;
+            float v[8];
+            values8(c[p], s[p], v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : v[e];
+            store8<TYPE>(a.k, (r.row + j) * a.k_row + head * a.k_head + 8 * oct, v);
+        }
+    }
+    // (lanes of a wave: neighbouring octets that fill 128 bytes of a row, times positions)
+    constexpr int NEAR = TYPE == ROWS_F32 ? 4 : 8, WORDS = MX ? 4 : 8;
+    for (int t = threadIdx.x; t < OCTS * (PAGE_POS / 4); t += 256) {
+        const int oct = t % NEAR + t / (NEAR * 16) * NEAR, quad = t / NEAR % 16;
+        if (4 * quad + 3 < r.at || 4 * quad >= r.at + r.n) continue;
+        uint32_t w[WORDS], sc = 0;
+        float s = 0.f;
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[j] = *(const uint32_t *)(a.c.v + (block * (MX ? DH / 2 : DH) + WORDS * oct + j) * PAGE_POS + 4 * quad);
+        if constexpr (MX) sc = *(const uint32_t *)(a.c.v_scale + (block * (DH / 32) + oct / 4) * PAGE_POS + 4 * quad);
+        else s = a.c.v_scale[block];
+        turn4(w);
+        if constexpr (!MX) turn4(w + 4);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int row = 4 * quad + j - r.at;
+            if (row < 0 || row >= r.n) continue;
+            float v[8];
+            if constexpr (MX) values8(w[j], __uint_as_float((sc >> 8 * j & 255u) << 23), v);
+            else values8((u32x2){w[j], w[j + 4]}, s, v);
+#pragma unroll
+            for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : v[e];
+            store8<TYPE>(a.v, (r.row + row) * a.v_row + head * a.v_head + 8 * oct, v);
+        }
+    }
+}
+template <typename C, int DH, int TYPE>
+__global__ __launch_bounds__(256) void read_paged_kernel(ReadArgs<C> a) {
+    __shared__ int offsets[READ_KEPT];
+    __shared__ ReadRun runs[READ_WINDOW];
+    __shared__ int n_runs;
+    const int head = blockIdx.x % a.c.heads, r0 = blockIdx.x / a.c.heads * READ_WINDOW;
+    for (int b = threadIdx.x; b <= a.n_seqs; b += 256) offsets[b] = a.row_offsets[b];
+    __syncthreads();
+    if (threadIdx.x < 64) {
+        const int i = r0 + threadIdx.x;
+        ReadRun run{i, 0, -1, 0};
+        bool begins = false;
+        if (i < a.n_rows && i >= offsets[0] && i < offsets[a.n_seqs]) {
+            int b = count_le(offsets, a.n_seqs + 1, i) - 1;
+            b = b < 0 ? 0 : b >= a.n_seqs ? a.n_seqs - 1 : b;
+            const int64_t pos = (int64_t)(a.first ? a.first[b] : 0) + i - offsets[b];
+            const int slot = a.slots ? a.slots[b] : b, in = (int)(pos & (PAGE_POS - 1));
+            begins = i == offsets[b] || in == 0;
+            if (begins) {
+                run.at = in;
+                const int64_t left = (int64_t)offsets[b + 1] - i, rest = a.n_rows - i;
+                run.n = PAGE_POS - in;
+                run.n = left < run.n ? (int)left : run.n;
+                run.n = rest < run.n ? (int)rest : run.n;
+                if (pos >= 0 && pos < (int64_t)a.max_blocks * PAGE_POS && (unsigned)slot < (unsigned)a.n_slots) run.page = a.table[(size_t)slot * a.max_blocks + pos / PAGE_POS];
+                if ((unsigned)run.page >= (unsigned)a.c.n_pages) run.page = -1;
+            }
+        }
+        const unsigned long long all = __ballot(begins);
+        if (begins) runs[__popcll(all & ((1ull << threadIdx.x) - 1))] = run;
+        if (threadIdx.x == 0) n_runs = __popcll(all);
+    }
+    __syncthreads();
+    for (int k = 0; k < n_runs; ++k) read_run<C, DH, TYPE>(a, head, runs[k]);
+}
+template <typename C>
+static void launch_read(const ReadArgs<C> &a, hipStream_t st) {
+    if (a.n_seqs < 1 || a.n_rows < 1) return;
+    const unsigned blocks = (unsigned)((a.n_rows + READ_WINDOW - 1) / READ_WINDOW * a.c.heads);
+    auto of = [&](auto dh) {
+        constexpr int DH = decltype(dh)::value;
+        if (a.type == ROWS_BF16) hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_BF16>), dim3(blocks), dim3(256), 0, st, a);
+        else if (a.type == ROWS_F16) hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_F16>), dim3(blocks), dim3(256), 0, st, a);
+        else hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_F32>), dim3(blocks), dim3(256), 0, st, a);
+    };
+    if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
+    else of(std::integral_constant<int, 64>{});
+}
+void launch_read_paged(const ReadArgs<PagedCache> &a, hipStream_t st) { launch_read(a, st); }
+void launch_read_paged(const ReadArgs<PagedMxCache> &a, hipStream_t st) { launch_read(a, st); }
+
+// ---------------------------------------------------------------------------------------------
+// attention over the pages
+// ---------------------------------------------------------------------------------------------
+// The products, shares, whole sequences and the join are those of the 8-bit cache's kernel: S^T = K Q^T, O^T = V^T P^T, 16 rows a tile, one pass with the running maximum and
+// sum of the softmax in fp32.  What differs is how a lane finds its operands:
+//   K: row r of score tile t is position 4 r + t of the page, so that the four tiles' scales of a lane's block of 32 features are the bytes of one word, and
+//   a lane's 16 probabilities those of 16 neighbouring positions, which its 16 bytes of V hold.  At head_dim 128 a lane has a block of 32 features (16 bytes), at 64 half of one.
+//   V: a byte is two features of a position.  Widened (with its position's scale) it is a pair across features; two positions' pairs, exchanged by halves, are
+//   pairs along the positions, of an even and of an odd feature: block jj of 32 features makes two operands, features 32 jj + 2 i and 32 jj + 2 i + 1.
+// Both products see exactly what codes and scales stand for.
+// rare: a page's V has scales that stand for NaN where not all rows see them.  The rows that see one get it in its 32 features.  seen: 0x80 in the bytes of the lane's 16 positions
+template <int DH, int NT>
+__device__ __forceinline__ void attend_mx_nans(const u32x4 (&nans)[DH / 32], int base, const int (&limit)[NT], f32x4 (&o)[NT][DH / 16]) {
+    const int kb = (threadIdx.x & 63) >> 4;
+#pragma unroll
+    for (int j = 0; j < DH / 32; ++j)
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            int hit = 0;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) hit |= (nans[j][w] & bytes_below(limit[n] + 1 - base - 16 * kb - 4 * w)) != 0;
+            hit |= lane_xor<16>(hit);
+            hit |= lane_xor<32>(hit);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                o[n][2 * j][r] = hit ? __builtin_nanf("") : o[n][2 * j][r];
+                o[n][2 * j + 1][r] = hit ? __builtin_nanf("") : o[n][2 * j + 1][r];
+            }
+        }
+}
+// words i = 2 u, 2 u + 1 of a lane's 16 bytes of V: the operands of its even and its odd feature
+__device__ __forceinline__ void widen_v(const u32x4 &c, const u32x4 &s, int u, u32x4 &even, u32x4 &odd) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+        const uint32_t w = c[2 * u + h], b = s[2 * u + h];
+        const uint32_t p0 = widen2<0>(w, scale_byte<0>(b)), p1 = widen2<1>(w, scale_byte<1>(b)), p2 = widen2<2>(w, scale_byte<2>(b)), p3 = widen2<3>(w, scale_byte<3>(b));
+        even[2 * h] = __builtin_amdgcn_perm(p1, p0, 0x05040100u);
+        odd[2 * h] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
+        even[2 * h + 1] = __builtin_amdgcn_perm(p3, p2, 0x05040100u);
+        odd[2 * h + 1] = __builtin_amdgcn_perm(p3, p2, 0x07060302u);
+    }
+}
+template <int DH, int NT, int TYPE> constexpr int attend_mx_lds = 16 * (attend_nq<TYPE> * attend_pieces<DH, NT> > 4 * NT * (DH / 16) * 64 ? attend_nq<TYPE> * attend_pieces<DH, NT> : 4 * NT * (DH / 16) * 64);
+#define ATTEND_KEPT 256          // sequences whose lengths and rows the workgroup keeps in LDS
+
+template <int DH, int NT, int TYPE>
+__global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(AttendMxArgs a, AttendPlan plan) {
+    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE, false>;
+    constexpr int STEPS = DH / 32, FB = DH / 32, DT = DH / 16, PIECES = attend_pieces<DH, NT>;     // STEPS: products a score takes, of 32 features
+    typedef std::conditional_t<DH == 128, u32x4, u32x2> KBytes;                                     // a lane's DH / 4 features of a position
+    extern __shared__ u32x4 lds[];
+    u32x4 *const q = lds;
+    f32x4 *const osum = (f32x4 *)lds;                            // the four waves' sums, in the queries' place once they are used
+    __shared__ float ml[4][2][NT * 16];
+    __shared__ int part[4];
+    __shared__ AttendSeq kept[ATTEND_KEPT];
+    int *const starts = (int *)((char *)lds + attend_mx_lds<DH, NT, TYPE>);         // [n_seqs + 1]
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int shares = plan.whole ? a.n_seqs : plan.shares, share = blockIdx.x % shares, head = blockIdx.x / shares % a.c.heads, tile = blockIdx.x / shares / a.c.heads;
+    const int group = a.n_heads / a.c.heads, r0 = tile * NT * 16;
+    // ---- where the sequences' pages begin
+    const int n_seqs = plan.whole ? 1 : a.n_seqs;
+    int total = 0;
+    if (plan.whole) {
+        const AttendSeq s = attend_seq(a, share);
+        total = attend_pages(s);
+        if (threadIdx.x == 0) {
+            kept[0] = s;
+            starts[0] = 0;
+        }
+    }
+    for (int b0 = 0; b0 < a.n_seqs && !plan.whole; b0 += 256) {
+        const int b = b0 + threadIdx.x;
+        int sum, pages = 0;
+        if (b < a.n_seqs) {
+            const AttendSeq s = attend_seq(a, b);
+            pages = attend_pages(s);
+            if (b < ATTEND_KEPT) kept[b] = s;
+        }
+        const int at = block_scan<4>(pages, part, &sum);
+        if (b < a.n_seqs) starts[b] = total + at;
+        total += sum;
+    }
+    if (threadIdx.x == 0) starts[n_seqs] = total;
+    __syncthreads();
+    if (plan.shares > 1 && !plan.whole && blockIdx.x == 0)       // (for attend_join_kernel)
+        for (int b = threadIdx.x; b <= a.n_seqs; b += 256) ((int *)a.work)[b] = starts[b];
+    total = uniform(total);
+    int per = plan.whole ? total : (total + plan.shares - 1) / plan.shares;
+    per = per < ATTEND_MIN_PAGES ? ATTEND_MIN_PAGES : per;
+    const int64_t from = plan.whole ? 0 : (int64_t)share * per;
+    if (from >= total) return;
+    const int p0 = (int)from, p1 = p0 + per < total ? p0 + per : total;
+    const float to_log2 = a.scale * 1.44269504088896340736f;
+    const int kb = lane >> 4, col = lane & 15;
+    const uint32_t k_off = 4 * col * (DH / 2) + kb * (DH / 8), ks_off = (kb * FB / 4) * PAGE_POS + 4 * col, v_off = col * PAGE_POS + 16 * kb;
+
+    // the share's part of sequence b, or of the next that has rows in this tile
+    const auto segment = [&](int b) {
+        AttendSeg g{};
+        for (; b < n_seqs; ++b) {
+            const int begin = uniform(starts[b]), end = uniform(starts[b + 1]);
+            if (begin >= p1) break;
+            const int first = p0 > begin ? p0 - begin : 0, last = (p1 < end ? p1 : end) - begin;
+            if (first >= last) continue;
+            const AttendSeq s = uniform(b < ATTEND_KEPT ? kept[b] : attend_seq(a, b));
+            if (r0 < s.rows * group) return AttendSeg{s, b, first, last, end - begin};
+        }
+        return g;
+    };
+    // 64 pages of this wave, every fourth from i0 on: their numbers (-1: none)
+    const auto page_ids = [&](const AttendSeg &g, int i0) {
+        const int i = i0 + 4 * lane;
+        int id = -1;
+        if (i < g.last && i < (g.s.len + PAGE_POS - 1) / PAGE_POS) id = a.table[(size_t)g.s.slot * a.max_blocks + i];
+        return (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
+    };
+    // A page's bytes are requested a page ahead: K's as soon as a page's scores are out, V's as its products go by, the first page's of the next
+    // sequence before the waves' sums of this one meet.  (A page that is none: page 0's bytes, and none of its positions is seen.)
+    KBytes kc[4];
+    u32x4 vc[FB], vs[FB];
+    uint32_t ks;
+    const auto block_of = [&](int page) { return (size_t)(page < 0 ? 0 : page) * a.c.heads + head; };
+    const auto take_k = [&](size_t block) {
+#pragma unroll
+        for (int t = 0; t < 4; ++t) kc[t] = *(const KBytes *)((a.c.k + block * (PAGE_POS * DH / 2) + t * (DH / 2)) + k_off);
+        ks = *(const uint32_t *)((a.c.k_scale + block * (FB * PAGE_POS)) + ks_off);
+    };
+    const auto take_v = [&](size_t block, int j) {
+        vc[j] = *(const u32x4 *)((a.c.v + block * (PAGE_POS * DH / 2) + 16 * j * PAGE_POS) + v_off);
+        vs[j] = *(const u32x4 *)((a.c.v_scale + (block * FB + j) * PAGE_POS) + 16 * kb);
+    };
+    const auto take_page = [&](int page) {
+        take_k(block_of(page));
+#pragma unroll
+        for (int j = 0; j < FB; ++j) take_v(block_of(page), j);
+    };
+
+    AttendSeg seg = segment(uniform(count_le(starts, n_seqs + 1, p0) - 1));
+    AttendQ<DH, NT> qr;
+    int id = -1;
+    if (seg.last > 0) {
+        id = page_ids(seg, seg.first + wave);
+        attend_load_q<DH, NT, TYPE, DH / 32>(a, seg.s, head, group, r0, qr);
+        if (seg.first + wave < seg.last) take_page(__builtin_amdgcn_readlane(id, 0));
+    }
+    while (seg.last > 0) {
+        const AttendSeq s = seg.s;
+        __syncthreads();
+        attend_put_q<DH, NT, NQ, TYPE>(qr, q);
+        __syncthreads();
+        const AttendSeg after = segment(seg.b + 1);
+        int id_after = -1;
+        if (after.last > 0) {
+            id_after = page_ids(after, after.first + wave);
+            attend_load_q<DH, NT, TYPE, DH / 32>(a, after.s, head, group, r0, qr);
+        }
+        // the last position that every column sees, and each lane's columns' own
+        const int seen = s.seen;
+        int limit[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = r0 + 16 * n + col;
+            limit[n] = r < s.rows * group ? seen + r / group : -1;
+        }
+        f32x4 o[NT][DT];
+        float m[NT], l[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            m[n] = LLMA_NEG_INF;
+            l[n] = 0.f;
+#pragma unroll
+            for (int d = 0; d < DT; ++d) o[n][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+        }
+        // (pages behind the tile's last row are not seen by any of it)
+        const int r_last = (r0 + 16 * NT < s.rows * group ? r0 + 16 * NT : s.rows * group) - 1, furthest = seen + r_last / group;
+        const int stop = furthest < 0 ? 0 : seg.last < furthest / PAGE_POS + 1 ? seg.last : furthest / PAGE_POS + 1;
+        for (int i0 = seg.first + wave; i0 < stop; i0 += 256) {
+            const int n_here = (stop - i0 + 3) / 4 < 64 ? (stop - i0 + 3) / 4 : 64;
+            for (int it = 0; it < n_here; ++it) {
+                const int page = __builtin_amdgcn_readlane(id, it), base = (i0 + 4 * it) * PAGE_POS;
+                const size_t next = block_of(__builtin_amdgcn_readlane(id, it + 1 < n_here ? it + 1 : it));      // (the last page's once more: no branch around the loads)
+                // (several tiles' queries come from LDS for every page: kept in registers across pages they would push the sums out)
+                int ql = lane;
+                if constexpr (NT > 1) asm volatile("" : "+v"(ql));
+                f32x4 sc[NT][4];
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) sc[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+                const float k_by[4] = {scale_byte<0>(ks), scale_byte<1>(ks), scale_byte<2>(ks), scale_byte<3>(ks)};
+#pragma unroll
+                for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const u32x4 w = widen8(kc[t][st], k_by[t]);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n)
+#pragma unroll
+                            for (int pl = NQ - 1; pl >= 0; --pl) sc[n][t] = mfma16x16x32(w, q[pl * PIECES + (n * STEPS + st) * 64 + ql], sc[n][t]);
+                    }
+                __builtin_amdgcn_sched_barrier(0);
+                take_k(next);
+                __builtin_amdgcn_sched_barrier(0);
+                const bool masked = page < 0 || base + PAGE_POS - 1 > seen;
+                u32x4 nans[FB];
+                uint32_t any = 0;
+                if (masked) {
+                    const int there = page < 0 ? 0 : s.len - base - 16 * kb;       // of the lane's 16 positions of V
+                    // what lies behind the last position may be anything, and a NaN that only later rows see must not reach the others through 0 * NaN
+#pragma unroll
+                    for (int j = 0; j < FB; ++j)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            const uint32_t c = vs[j][w] & bytes_below(there - 4 * w), x = nan_scales(c);
+                            any |= x;
+                            nans[j][w] = x;
+                            vs[j][w] = c & ~(x | (x - (x >> 7)));
+                        }
+                }
+                u32x4 pb[NT][NP][2];
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    float x[16], top = LLMA_NEG_INF;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) x[e] = sc[n][e % 4][e / 4] * to_log2;
+                    if (masked) {
+                        const int left = (page < 0 ? -1 : limit[n]) - base - 16 * kb;
+#pragma unroll
+                        for (int e = 0; e < 16; ++e) x[e] = e > left ? LLMA_NEG_INF : x[e];
+                    }
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) top = fmaxf(top, x[e]);
+                    top = fmaxf(top, lane_xor<16>(top));
+                    top = fmaxf(top, lane_xor<32>(top));
+                    const float mn = fmaxf(m[n], top), ref = mn == LLMA_NEG_INF ? 0.f : mn;
+                    const float keep = __builtin_amdgcn_exp2f(m[n] - ref);
+                    m[n] = mn;
+                    l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
+                        l[n] += x[e];
+                    }
+#pragma unroll
+                    for (int u = 0; u < 2; ++u)
+#pragma unroll
+                        for (int w = 0; w < 4; ++w) {
+                            float y = x[8 * u + 2 * w], z = x[8 * u + 2 * w + 1];
+#pragma unroll
+                            for (int pl = 0; pl < NP; ++pl) {
+                                pb[n][pl][u][w] = bf16_pair(y, z);
+                                if (pl + 1 < NP) { y -= __uint_as_float(pb[n][pl][u][w] << 16); z -= __uint_as_float(pb[n][pl][u][w] & 0xffff0000u); }
+                            }
+                        }
+                }
+                __builtin_amdgcn_sched_barrier(0);
+                if (masked && __ballot(any != 0) != 0) attend_mx_nans<DH, NT>(nans, base, limit, o);
+#pragma unroll
+                for (int j = 0; j < FB; ++j) {
+                    u32x4 even[2], odd[2];
+#pragma unroll
+                    for (int u = 0; u < 2; ++u) widen_v(vc[j], vs[j], u, even[u], odd[u]);
+                    take_v(next, j);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+#pragma unroll
+                        for (int pl = NP - 1; pl >= 0; --pl)
+#pragma unroll
+                            for (int u = 0; u < 2; ++u) {
+                                o[n][2 * j] = mfma16x16x32(even[u], pb[n][pl][u], o[n][2 * j]);
+                                o[n][2 * j + 1] = mfma16x16x32(odd[u], pb[n][pl][u], o[n][2 * j + 1]);
+                            }
+                }
+            }
+            if (i0 + 256 < stop) {                               // (a share of more than 256 pages of one sequence)
+                id = page_ids(seg, i0 + 256);
+                take_page(__builtin_amdgcn_readlane(id, 0));
+            }
+        }
+        id = id_after;
+        if (after.last > 0 && after.first + wave < after.last) take_page(__builtin_amdgcn_readlane(id, 0));
+        // ---- the waves' sums meet
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            l[n] += lane_xor<16>(l[n]);
+            l[n] += lane_xor<32>(l[n]);
+            if (kb == 0) { ml[wave][0][n * 16 + col] = m[n]; ml[wave][1][n * 16 + col] = l[n]; }
+        }
+        __syncthreads();
+        float top[NT], sum[NT];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const float *const am = &ml[0][0][n * 16 + col];
+            top[n] = fmaxf(fmaxf(am[0], am[2 * NT * 16]), fmaxf(am[4 * NT * 16], am[6 * NT * 16]));
+            const float ref = top[n] == LLMA_NEG_INF ? 0.f : top[n];
+            sum[n] = 0.f;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) sum[n] += am[(2 * w + 1) * NT * 16] * __builtin_amdgcn_exp2f(am[2 * w * NT * 16] - ref);
+            const float f = __builtin_amdgcn_exp2f(m[n] - ref);
+#pragma unroll
+            for (int d = 0; d < DT; ++d) osum[((wave * NT + n) * DT + d) * 64 + lane] = o[n][d] * f;
+        }
+        __syncthreads();
+        const bool whole = seg.first == 0 && seg.last == seg.pages;
+        // the part's place: a share has at most one sequence that began before it (0) and one that goes on behind it (1)
+        const int64_t at = (((int64_t)share * 2 + (seg.first == 0)) * a.c.heads + head) * plan.tiles + tile;
+        float *const po = (float *)a.work + (a.n_seqs + 1 + 63) / 64 * 64;
+        float *const pm = po + attend_parts(plan, a.c.heads) * 16 * NT * DH, *const pl = pm + attend_parts(plan, a.c.heads) * 16 * NT;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const int r = r0 + 16 * n + col;
+            if (r >= s.rows * group) continue;
+            const int row = s.row0 + r / group, h = head * group + r % group;
+            const float inv = sum[n] == 0.f ? 0.f : 1.f / sum[n];
+#pragma unroll
+            for (int u = 0; u < DT / 4; ++u) {
+                // block jj's features 8 kb + 4 hf .. + 3: two of the even operand's, two of the odd one's
+                const int jj = (4 * u + wave) / 2, hf = wave % 2, d = 32 * jj + 8 * kb + 4 * hf;
+                typedef __attribute__((ext_vector_type(2))) float f32x2_t;
+                f32x2_t e = (f32x2_t){0.f, 0.f}, f = e;
+#pragma unroll
+                for (int w = 0; w < 4; ++w) {
+                    const f32x2_t *const from_w = (const f32x2_t *)&osum[((w * NT + n) * DT + 2 * jj) * 64 + lane] + hf;
+                    e += from_w[0];
+                    f += from_w[2 * 64];
+                }
+                const f32x4 v = (f32x4){e[0], f[0], e[1], f[1]};
+                if (whole) attend_store<TYPE>(a, row, h, d, v * inv);
+                else *(f32x4 *)(po + (at * 16 * NT + 16 * n + col) * DH + d) = v;
+            }
+            if (!whole && wave == 0 && kb == 0) { pm[at * 16 * NT + 16 * n + col] = top[n]; pl[at * 16 * NT + 16 * n + col] = sum[n]; }
+        }
+        seg = after;
+    }
+}
+
+template <int DH, int NT, int TYPE>
+static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStream_t st) {
+    const size_t bytes = (size_t)attend_mx_lds<DH, NT, TYPE> + (size_t)(a.n_seqs + 1) * 4;
+    hipLaunchKernelGGL((attend_paged_mx_kernel<DH, NT, TYPE>), dim3((p.whole ? a.n_seqs : p.shares) * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
+}
+static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
+    return attend_plan(n_seqs, max_blocks, n_heads, kv_heads, dh / 2 + dh / 32, max_rows);
+}
+template <int DH, int TYPE>
+static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
+    const AttendPlan p = attend_mx_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, DH, a.max_rows);
+    if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
+    else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
+    else if (p.nt == 3) launch_attend_nt<DH, 3, TYPE>(a, p, st);
+    else launch_attend_nt<DH, 4, TYPE>(a, p, st);
+    if (p.shares > 1 && !p.whole)
+        hipLaunchKernelGGL((attend_join_kernel<DH, TYPE, AttendMxArgs>), dim3((a.max_rows * (a.n_heads / a.c.heads) + 3) / 4, a.c.heads, a.n_seqs), dim3(256), 0, st, a, p);
+}
+int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
+    return attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, dh, max_rows), n_seqs, kv_heads, dh);
+}
+void launch_attend_paged_mx(const AttendMxArgs &a, hipStream_t st) {
+    if (a.n_seqs < 1 || a.n_rows < 1 || a.max_rows < 1) return;
+    auto of = [&](auto dh) {
+        constexpr int DH = decltype(dh)::value;
+        if (a.type == ROWS_BF16) launch_attend_type<DH, ROWS_BF16>(a, st);
+        else if (a.type == ROWS_F16) launch_attend_type<DH, ROWS_F16>(a, st);
+        else launch_attend_type<DH, ROWS_F32>(a, st);
+    };
+    if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
+    else of(std::integral_constant<int, 64>{});
+}

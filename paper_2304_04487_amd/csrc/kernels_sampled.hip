@@ -6,37 +6,11 @@
 // for them is decided again with the row's sum in 64 bits.  The one row that is sampled is read again in 64 bits throughout, so that
 // a token does not depend on how the sums were cut: exponentials off by 1e-7 would move one sample in some hundreds.
 #include "../../include/llma.h"
-#include "paged.h"
+#include "row_pieces.h"
 
 #define ROW_THREADS 256
 #define PICK_BLOCKS 512          // 16-byte pieces of a row per workgroup when it is sampled (two a thread)
 
-template <int TYPE> constexpr int sampled_epb = TYPE == ROWS_F32 ? 4 : 8;        // logits of a 16-byte piece
-
-// Rows begin anywhere: a row is read in the aligned 16-byte pieces that hold it, and what of the first and last is not its own is masked
-// (both pieces hold a byte of the row, so they lie in its allocation).
-struct RowView { const u32x4 *base; int skip; };                // pieces from the one with the row's first logit; logits before it in there
-template <int TYPE>
-__device__ __forceinline__ RowView row_view(const SampledArgs &a, int64_t row) {
-    constexpr int SIZE = TYPE == ROWS_F32 ? 4 : 2;
-    const uintptr_t at = (uintptr_t)a.logits + (uintptr_t)(row * a.row_stride) * SIZE;
-    return RowView{(const u32x4 *)(at & ~(uintptr_t)15), (int)(at & 15) / SIZE};
-}
-template <int TYPE>
-__device__ __forceinline__ void piece_values(u32x4 p, float v[sampled_epb<TYPE>]) {
-    if constexpr (TYPE == ROWS_F32) {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) v[e] = __uint_as_float(p[e]);
-    } else if constexpr (TYPE == ROWS_F16) {
-        typedef __attribute__((ext_vector_type(8))) _Float16 f16x8;
-        const f16x8 h = __builtin_bit_cast(f16x8, p);
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = (float)h[e];
-    } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) { v[2 * e] = __uint_as_float(p[e] << 16); v[2 * e + 1] = __uint_as_float(p[e] & 0xffff0000u); }
-    }
-}
 __device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
     const int n = a.n_draft ? a.n_draft[b] : a.k;
     return n < 0 ? 0 : n > a.k ? a.k : n;

@@ -1,4 +1,4 @@
-// Argument structs and launchers of the paged 8-bit cache (kernels_paged.hip) and of sampled verification (kernels_sampled.hip).
+// Argument structs and launchers of the paged caches (kernels_paged.hip: 8 bits, kernels_paged_mx.hip: 4), of sampled verification (kernels_sampled.hip) and of log probabilities (kernels_logprobs.hip).
 #pragma once
 #include "common.h"
 
@@ -64,6 +64,69 @@ struct AttendArgs {
 };
 OPTIONAL int64_t attend_paged_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows);
 OPTIONAL void launch_attend_paged(const AttendArgs &a, hipStream_t st);
+
+// ---- the paged cache of 4 bits -----------------------------------------------------------------
+// The same pages, of e2m1 codes with a power of two for every 32 neighbouring features of a position, held as its exponent plus 127 (255: NaN):
+//   k [n_pages][heads][64][dh / 2]   v [n_pages][heads][dh / 2][64]   byte j of a position: features 2j (low half) and 2j + 1
+//   k_scale, v_scale [n_pages][heads][dh / 32][64] bytes; a cached value is code * 2^(scale - 127).
+// Each position has scales of its own: a write changes nothing but its rows, whatever was there before.  A byte holds two features of one position, not one of two, so that
+// no two positions share a byte of V either.  The conversion that widens codes (v_cvt_scalef32_pk_*_fp4) takes the scale as it lies, and the product is exact in bf16.
+struct PagedMxCache {
+    uint8_t *k, *v, *k_scale, *v_scale;
+    int n_pages, heads, dh;
+};
+struct AppendMxArgs {
+    PagedMxCache c;
+    const void *k, *v;
+    int64_t k_row, k_head, v_row, v_head;
+    const int *slot_map;
+    int n_rows;
+    int type;
+};
+OPTIONAL void launch_append_paged_mx(const AppendMxArgs &a, hipStream_t st);
+struct AttendMxArgs {
+    PagedMxCache c;
+    const void *q;
+    void *out;
+    int64_t q_row, q_head, out_row, out_head;
+    int type, n_heads;
+    const int *table, *slots, *lens, *row_offsets;
+    int n_seqs, n_slots, max_blocks, n_rows, max_rows;
+    float scale;
+    void *work;
+};
+OPTIONAL int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows);
+OPTIONAL void launch_attend_paged_mx(const AttendMxArgs &a, hipStream_t st);
+
+// rows out of either cache
+template <typename C>
+struct ReadArgs {
+    C c;
+    void *k, *v;
+    int64_t k_row, k_head, v_row, v_head;
+    const int *table, *slots, *first, *row_offsets;   // slots, first: or null
+    int n_seqs, n_slots, max_blocks, n_rows;
+    int type;
+};
+OPTIONAL void launch_read_paged(const ReadArgs<PagedCache> &a, hipStream_t st);
+OPTIONAL void launch_read_paged(const ReadArgs<PagedMxCache> &a, hipStream_t st);
+
+// ---- log probabilities of given tokens ---------------------------------------------------------
+struct LogprobArgs {
+    const void *logits;                  // [n_rows] rows of `vocab`, row_stride elements apart
+    int64_t row_stride;
+    int type, vocab, n_rows, n_top;
+    const int *tokens;                   // [n_rows] or null
+    const float *temperature;            // [n_rows] or null: 1
+    float *logprob, *entropy;            // [n_rows] or null
+    int *rank;                           // [n_rows] or null
+    int *top_tokens;                     // [n_rows][n_top]
+    float *top_logprobs;
+    void *work;
+};
+#define LOGPROB_MAX_TOP 64
+OPTIONAL int64_t token_logprobs_bytes(int n_rows, int vocab, int n_top);
+OPTIONAL void launch_token_logprobs(const LogprobArgs &a, hipStream_t st);
 
 struct SampledArgs {
     const void *logits;                  // [n_seqs * (k + 1)] rows of `vocab`, row_stride elements apart

@@ -1,0 +1,168 @@
+"""llma_token_logprobs on the GPU against the plain numpy form in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+import mx_oracle as mx
+
+pytestmark = pytest.mark.gpu
+DT = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}
+
+
+@pytest.fixture(scope="module")
+def llma():
+    import paper_2304_04487_amd as m
+    m.load_library()
+    return m
+
+
+def run(llma, logits, tokens, temperature=None, n_top=0, **kw):
+    n = logits.shape[0]
+    new = lambda *s, dt=torch.float32: torch.full(s, 77, dtype=dt, device="cuda")
+    out = {"logprob": new(n), "rank": new(n, dt=torch.int32), "entropy": new(n)}
+    if n_top:
+        out.update(top_tokens=new(n, n_top, dt=torch.int32), top_logprobs=new(n, n_top))
+    t = None if temperature is None else torch.tensor(temperature, dtype=torch.float32, device="cuda")
+    llma.llma_token_logprobs(logits, torch.tensor(tokens, dtype=torch.int32, device="cuda"), out["logprob"], temperature=t, **{k: v for k, v in out.items() if k != "logprob"}, **kw)
+    torch.cuda.synchronize()
+    return {k: v.cpu().numpy() for k, v in out.items()}
+
+
+def check(llma, logits, tokens, temperature=None, n_top=0, **kw):
+    got = run(llma, logits, tokens, temperature, n_top, **kw)
+    x = logits.double().cpu().numpy()
+    for i in range(len(x)):
+        t = 1.0 if temperature is None else float(np.float32(temperature[i]))
+        lp, rank, entropy, top, top_lp = mx.logprobs(x[i], int(tokens[i]), t, n_top)
+        assert got["rank"][i] == rank, i
+        # The sum of the row's terms: each off by 4 roundings of 2^-24 relative (2^x and its argument's last steps) and one for every power of two of its argument (up to 2^7 where
+        # the term still counts), then a rounding for each of a chunk's log2 levels of sums; its logarithm is off by as much absolutely.  The entropy has the same twice, and times
+        # the mean of |x - M| / T, at most the row's own spread of what counts (2^7).  Then the output's rounding.
+        err = 2.0 ** -24 * (4 + 128 + 20)
+        assert near(got["logprob"][i], lp, err), (i, got["logprob"][i], lp)
+        assert near(got["entropy"][i], entropy, 2 * err * (1 + min(entropy, 128.0))), (i, got["entropy"][i], entropy)
+        if n_top:
+            assert got["top_tokens"][i].tolist() == top, i
+            assert all(near(a, b, err) for a, b in zip(got["top_logprobs"][i], top_lp)), i
+    return got
+
+
+def near(got, want, err):
+    if not np.isfinite(want):
+        return got == want
+    return abs(got - want) <= err + 2.0 ** -23 * abs(want)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("rows,vocab,n_top", [(1, 1, 1), (1, 2, 3), (3, 5, 0), (2, 64, 64), (9, 999, 5), (4, 2048, 1), (1, 32000, 20), (9, 32000, 7), (300, 1001, 3), (40, 50257, 32), (2, 300001, 64)])
+def test_against_the_definition(llma, dtype, rows, vocab, n_top):
+    rng = np.random.default_rng(rows + vocab)
+    x = torch.tensor(3 * rng.standard_normal((rows, vocab)), dtype=torch.float32).to(DT[dtype]).cuda()
+    tokens = rng.integers(0, vocab, rows)
+    tokens[0] = int(x[0].float().argmax())
+    check(llma, x, tokens, None, n_top)
+    check(llma, x, tokens, rng.uniform(0.3, 2.0, rows), n_top)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_rows_of_any_stride_and_place(llma, dtype):
+    """rows that begin at every element of a 16-byte piece, inside wider ones"""
+    rng = np.random.default_rng(3)
+    wide = torch.tensor(2 * rng.standard_normal((9, 3011)), dtype=torch.float32).to(DT[dtype]).cuda()
+    for at in range(9):
+        view = wide[:, at:at + 2990 + at % 3]
+        check(llma, view, rng.integers(0, 2990, 9), None, 4)
+    check(llma, wide[2:3, 1:], [7], None, 4)
+    check(llma, wide[::4], [7, 8, 3010], None, 4)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+def test_masked_infinite_and_nan_logits(llma, dtype):
+    inf, nan = float("inf"), float("nan")
+    rng = np.random.default_rng(5)
+    V = 5000
+    x = 2 * rng.standard_normal((12, V))
+    x[0, 1:] = -inf                                                     # one token left
+    x[1] = -inf                                                         # none
+    x[2, ::2] = nan
+    x[3] = nan
+    x[4, 17] = inf                                                      # takes all
+    x[5, [17, 4000]] = inf                                              # share
+    x[6] = -inf
+    x[6, [4999, 0, 2500]] = 1.5, 1.5, -3.0
+    x[7] = 0.0                                                          # all alike
+    x[8] = np.where(rng.random(V) < 0.5, 0.0, -0.0)                     # zeros of both signs are alike
+    x[9] = np.arange(V) * 1e-3                                          # rising: every one is among the best so far
+    x[10] = -np.arange(V) * 1e-3
+    x[11, :] = -inf
+    x[11, 3] = nan
+    x = torch.tensor(x, dtype=torch.float32).to(DT[dtype]).cuda()
+    for tokens in ([0, 0, 1, 2, 17, 4000, 2500, 4999, 4998, 4999, 4999, 3], [1, 4999, 0, 0, 16, 17, 1, 0, 0, 0, 0, 0], [-1, V, 2 ** 31 - 1, -2 ** 31, 5, -1, 4999, 2500, 1, 3, V, V - 1]):
+        for n_top in (0, 1, 6, 64):
+            check(llma, x, tokens, None, n_top)
+    t = [0.7, 1, inf, 1, inf, inf, inf, 1e30, 0.0, -1.0, nan, 2.0]
+    check(llma, x, [0] * 12, [1.0 if not v > 0 else v for v in t], 5)
+    a, b = run(llma, x, [0] * 12, t, 5), run(llma, x, [0] * 12, [1.0 if not v > 0 else v for v in t], 5)
+    for k in a:
+        assert np.array_equal(a[k], b[k], equal_nan=True)               # not above zero, or NaN: 1
+
+
+def test_very_cold_and_very_hot(llma):
+    """temperatures whose inverse leaves fp32's range, and logits from one end of it to the other"""
+    rng = np.random.default_rng(6)
+    x = torch.tensor(rng.standard_normal((8, 3000)), dtype=torch.float32, device="cuda")
+    x[0, 5], x[1, 5] = 3e38, -3e38
+    x[2, 7], x[2, 8] = 9.0, 9.0
+    t = np.array([1.0, 1.0, 1e-30, 1e-38, 1e-45, 1e12, 1e25, 3e38], np.float32)
+    got = run(llma, x, [5, 5, 7, 0, 0, 0, 0, 0], t, 3)
+    assert got["logprob"][0] == 0 and got["entropy"][0] == 0 and got["logprob"][1] < -2.9e38
+    assert abs(got["logprob"][2] + np.log(2)) < 1e-6 and abs(got["entropy"][2] - np.log(2)) < 1e-6
+    for i in (3, 4):
+        assert got["entropy"][i] == 0 and got["top_logprobs"][i][0] == 0 and got["top_logprobs"][i][1] < -1e30
+    for i in (5, 6, 7):
+        assert abs(got["entropy"][i] - np.log(3000)) < 1e-5 and abs(got["logprob"][i] + np.log(3000)) < 1e-5
+    assert np.isfinite(got["entropy"]).all()
+
+
+@pytest.mark.parametrize("n_top", [1, 64])
+def test_many_equal_and_rising_logits(llma, n_top):
+    """more candidates than wait at a time: equal ones go to the lowest ids, rising ones to the last"""
+    V = 400000
+    x = torch.zeros((4, V), dtype=torch.bfloat16, device="cuda")
+    x[1] = torch.arange(V, device="cuda").float().mul(1e-3).to(torch.bfloat16)           # long runs of equal values that rise
+    x[2, V // 2:] = 1.0
+    x[3, 100:3300] = torch.arange(3200, device="cuda").to(torch.bfloat16)                # the best together in a few segments
+    check(llma, x, [V - 1, 5, V // 2 + 3, 3000], None, n_top)
+
+
+def test_workspace_streams_devices_and_what_is_left_out(llma):
+    rng = np.random.default_rng(8)
+    x = torch.tensor(rng.standard_normal((20, 4001)), dtype=torch.float32, device="cuda")
+    tokens = rng.integers(0, 4001, 20)
+    ws = torch.empty(llma.llma_token_logprobs_workspace(20, 4001, 8), dtype=torch.uint8, device="cuda")
+    full = check(llma, x, tokens, None, 8, workspace=ws)
+    st = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    side = run(llma, x, tokens, None, 8, stream=st)
+    for k in full:
+        assert np.array_equal(full[k], side[k]), k
+    t = torch.tensor(tokens, dtype=torch.int32, device="cuda")
+    lp, ent = torch.empty(20, device="cuda"), torch.empty(20, device="cuda")
+    top, top_lp = torch.empty((20, 8), dtype=torch.int32, device="cuda"), torch.empty((20, 8), device="cuda")
+    llma.llma_token_logprobs(x, t, lp)
+    llma.llma_token_logprobs(x, None, None, entropy=ent, top_tokens=top, top_logprobs=top_lp)
+    assert np.array_equal(lp.cpu().numpy(), full["logprob"]) and np.array_equal(ent.cpu().numpy(), full["entropy"])
+    assert np.array_equal(top.cpu().numpy(), full["top_tokens"]) and np.array_equal(top_lp.cpu().numpy(), full["top_logprobs"])
+    llma.llma_token_logprobs(x[:0], t[:0], lp[:0])                      # no rows: nothing to do
+
+
+def test_sampled_tokens_and_their_logprobs_agree(llma):
+    """what llma_verify_sampled emits at temperature 0 is rank 0; its row's chances are what the call says"""
+    rng = np.random.default_rng(9)
+    B, V = 6, 5003
+    x = torch.tensor(2 * rng.standard_normal((B, 1, V)), dtype=torch.bfloat16, device="cuda")
+    i = lambda *s: torch.empty(s, dtype=torch.int32, device="cuda")
+    n_acc, nxt, emitted = i(B), i(B), i(B, 1)
+    llma.llma_verify_sampled(x, i(B, 0), torch.empty((B, 0), device="cuda"), torch.zeros(B, device="cuda"), n_acc, nxt, emitted, temperature=torch.zeros(B, device="cuda"))
+    got = check(llma, x[:, 0], nxt.cpu().numpy(), None, 1)
+    assert (got["rank"] == 0).all() and np.array_equal(got["top_tokens"][:, 0], nxt.cpu().numpy())
