@@ -1,47 +1,48 @@
 // Log probabilities of given tokens, with the distribution's entropy, the tokens' ranks and the likeliest alternatives.
 //   p = softmax(x / T);  log p(t) = (x_t - M) / T - ln S,  H = ln S - (W / S) / T  with M = max x, S = sum e^((x - M) / T), W = sum e^((x - M) / T) (x - M);
 //   rank = tokens before t in the order of falling logits, ties by rising id, whose first n_top are the alternatives.
-// Bound by one read of the logits: workgroups take chunks of rows and leave (M, S, W, rank's count), in fp32, relative to the chunk's own maximum, and the maximum
-// of every segment of 4 U pieces.  A second launch, a workgroup per row, joins them in 64 bits and in a fixed order.  The n_top-th largest segment maximum bounds the alternatives from
-// below, so it reads again only segments that reach it: n_top of a few hundred.
+// Bound by one read of the logits: each wave takes a chunk of a row, all of it in registers, and leaves (R, S, W, the rank's count): sums of 2^t and 2^t t with t = x by - R,
+// by = log2(e) / T, R near the chunk's largest x by; and the maximum of every segment (16 or more pieces that lie together).  A second launch, a wave per row, joins them in 64 bits and in a fixed
+// order.  The n_top-th largest segment maximum bounds the alternatives from below, so it reads again only segments that reach it.
 #include "../../include/llma.h"
 #include "row_pieces.h"
 
-#define CHUNK_THREADS 256
-#define TOP_KEPT 2048            // candidates that may wait; a batch adds up to 2048 more
-#define TOP_LIST 1024            // segments that are looked through at a time
+#define CHUNK_PIECES(u) (64 * (u))                               // of a wave
+#define TOP_KEPT 256             // candidates that may wait; a piece a lane adds up to 512
+#define TOP_FEW 24               // alternatives
+#define TOP_AHEAD 4              // pieces a lane requests at once when it looks for them
+#define TOP_LIST 1024            // segments whose maxima a wave keeps in registers, and looks through at a time
+#define LOW (-1e30f)             // logits are raised to this where only sums and maxima are meant: it ends fewer sums in NaN than minus infinity, and NaN goes with it
 
-struct LogprobPlan { int u, chunks, segments; };                 // pieces a thread; chunks and segments of a row (64 a chunk)
+struct LogprobPlan { int u, lanes, chunks, segments; };          // pieces a lane; lanes of a segment; chunks and segments of a row
 static LogprobPlan logprob_plan(int n_rows, int vocab, int epb) {
     const int pieces = (vocab + epb - 1) / epb + 1;
-    LogprobPlan p{8, 0, 0};
-    const auto chunks = [&] { return (pieces + CHUNK_THREADS * p.u - 1) / (CHUNK_THREADS * p.u); };
-    while (p.u > 1 && (int64_t)n_rows * chunks() < 1024) p.u /= 2;
+    LogprobPlan p{8, 16, 0, 0};
+    const auto chunks = [&] { return (pieces + CHUNK_PIECES(p.u) - 1) / CHUNK_PIECES(p.u); };
+    while (p.u > 1 && (int64_t)n_rows * chunks() < 4096) p.u /= 2;
     p.chunks = chunks();
-    p.segments = 64 * p.chunks;
+    while (p.lanes < 64 && p.chunks * p.u * (64 / p.lanes) > TOP_LIST) p.lanes *= 2;
+    p.segments = p.chunks * p.u * (64 / p.lanes);
     return p;
 }
-static int64_t logprob_bytes(const LogprobPlan &p, int n_rows, int n_top) { return (int64_t)n_rows * (p.chunks * 16 + (n_top > 0 ? p.segments * 4 : 0)); }
+struct LogprobPart { double r; float s, w, tilt; int before, pad[2]; };      // tilt: (by - its fp32 value) by its fp32 value, where the sums were taken with that
+static int64_t logprob_bytes(const LogprobPlan &p, int n_rows, int n_top) { return (int64_t)n_rows * (p.chunks * (int64_t)sizeof(LogprobPart) + (n_top > 0 ? p.segments * 4ll : 0)); }
 int64_t token_logprobs_bytes(int n_rows, int vocab, int n_top) {
     const int64_t narrow = logprob_bytes(logprob_plan(n_rows, vocab, 8), n_rows, n_top), wide = logprob_bytes(logprob_plan(n_rows, vocab, 4), n_rows, n_top);
     return (narrow > wide ? narrow : wide) + 16;
 }
-struct LogprobPart { float m, s, w; int before; };
 
-// e^((x - M) / T) as 2^((x - M) by), by = log2(e) / T in two parts: its own rounding would tilt all terms of a row alike
-struct By { float hi, lo; double t; };
+// log2(e) / T; the sums are taken with its fp32 value, whose own rounding would tilt all terms of a row alike, and put right when the parts are joined
+struct By { double by; float hi; };
 __device__ __forceinline__ By by_of(const LogprobArgs &a, int row) {
     float t = a.temperature ? a.temperature[row] : 1.f;
     if (!(t > 0.f)) t = 1.f;                                     // (also NaN)
     t = t > 3.402823466e38f ? 3.402823466e38f : t;
-    const double by = 1.4426950408889634074 / (double)(t > 1e-37f ? t : 1e-37f);       // (below it only the maximum counts either way, and the range ends)
     By b;
-    b.hi = (float)by;
-    b.lo = (float)(by - (double)b.hi);
-    b.t = (double)t;
+    b.by = 1.4426950408889634074 / (double)t;
+    b.hi = (float)b.by;
     return b;
 }
-__device__ __forceinline__ float power(float d, const By &b) { return __builtin_amdgcn_exp2f(__builtin_fmaf(d, b.lo, d * b.hi)); }
 template <int TYPE> __device__ __forceinline__ float logit_at(const LogprobArgs &a, int64_t row, int i) {
     const int64_t at = row * a.row_stride + i;
     float x;
@@ -68,6 +69,12 @@ __device__ __forceinline__ u32x4 row_piece(const RowView &v, int p, int pieces, 
     }
     return w;
 }
+// x by, rounded: where logits are so large that this rounding shows, R has it too
+__device__ __forceinline__ double times_by(float x, const By &b) {
+#pragma clang fp contract(off)
+    const double z = (double)x * b.by;
+    return z;
+}
 // the smallest float above x (of plus infinity: NaN, which nothing reaches)
 __device__ __forceinline__ float next_above(float x) {
     const int b = (int)__float_as_uint(x);
@@ -75,263 +82,395 @@ __device__ __forceinline__ float next_above(float x) {
     if (x == 0.f) return __uint_as_float(1u);
     return __uint_as_float((uint32_t)(b < 0 ? b - 1 : b + 1));
 }
+// of numbers that are no NaN (fmaxf would first quiet both)
+__device__ __forceinline__ float larger(float a, float b) {
+    float r;
+    asm("v_max_f32 %0, %1, %2" : "=v"(r) : "v"(a), "v"(b));
+    return r;
+}
+// N numbers a lane of which each 16 lanes want the maxima: halves of the numbers go to halves of the lanes; lane l of 16 ends with number l N / 16
+template <int N, int BIT = 8>
+__device__ __forceinline__ float maxima16(const float (&m)[N]) {
+    float h[N > 1 ? N / 2 : 1];
+    if constexpr (N > 1) {
+        const bool upper = threadIdx.x & BIT;
+#pragma unroll
+        for (int u = 0; u < N / 2; ++u) h[u] = larger(upper ? m[u + N / 2] : m[u], lane_xor<BIT>(upper ? m[u] : m[u + N / 2]));
+    } else h[0] = larger(m[0], lane_xor<BIT>(m[0]));
+    if constexpr (BIT > 1) return maxima16<(N > 1 ? N / 2 : 1), BIT / 2>(h);
+    else return h[0];
+}
+template <typename F>
+__device__ __forceinline__ void add_over_wave(F &v) {
+    butterfly<32>([&](auto o) {
+        if constexpr (std::is_same_v<F, double>) v += __longlong_as_double((long long)lane_xor<o.value>((unsigned long long)__double_as_longlong(v)));
+        else v += lane_xor<o.value>(v);
+    });
+}
+
+// a maximum with any NaN, also a signalling one, is the other number from here on
+__device__ __forceinline__ void ieee_mode_off() { __builtin_amdgcn_s_setreg(1 | 9 << 6, 0); }      // (bit 9 of the mode register)
 
 template <int TYPE, int U>
-__global__ __launch_bounds__(CHUNK_THREADS) void logprob_chunk_kernel(LogprobArgs a, LogprobPlan plan) {
-    constexpr int EPB = sampled_epb<TYPE>;
-    __shared__ float tops[4];
-    __shared__ LogprobPart parts[4];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    const int row = blockIdx.x / plan.chunks, chunk = blockIdx.x % plan.chunks;
+__global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, LogprobPlan plan) {
+    constexpr int EPB = sampled_epb<TYPE>, N = U * EPB;
+    ieee_mode_off();
+    const int lane = threadIdx.x & 63;
+    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (id >= (int64_t)a.n_rows * plan.chunks) return;
+    const int row = (int)(id / plan.chunks), chunk = (int)(id % plan.chunks);
     const RowView view = row_view<TYPE>(a, row);
-    const int pieces = (view.skip + a.vocab + EPB - 1) / EPB, p0 = chunk * CHUNK_THREADS * U + threadIdx.x;
+    const int pieces = (view.skip + a.vocab + EPB - 1) / EPB, p0 = chunk * CHUNK_PIECES(U);
     u32x4 w[U];
+    // (only a row's first and last chunk hold what is not the row's)
+    if (p0 * EPB >= view.skip && (p0 + CHUNK_PIECES(U)) * EPB - view.skip <= a.vocab) {
 #pragma unroll
-    for (int u = 0; u < U; ++u) w[u] = row_piece<TYPE>(view, p0 + u * CHUNK_THREADS, pieces, a.vocab);
+        for (int u = 0; u < U; ++u) w[u] = view.base[p0 + 64 * u + lane];
+    } else {
+#pragma unroll
+        for (int u = 0; u < U; ++u) w[u] = row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab);
+    }
     const By by = by_of(a, row);
     const int token = a.tokens ? a.tokens[row] : -1;
-    const bool given = (unsigned)token < (unsigned)a.vocab;
+    const bool given = a.rank && (unsigned)token < (unsigned)a.vocab;
     const float xt = given ? logit_at<TYPE>(a, row, token) : 0.f;
-    // ---- maxima
-    float top = LLMA_NEG_INF;
+    float x[N], m[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        float x[EPB];
-        piece_values<TYPE>(w[u], x);
+        piece_values<TYPE>(w[u], x + u * EPB);
+        m[u] = LOW;
 #pragma unroll
-        for (int e = 0; e < EPB; ++e) top = fmaxf(top, x[e]);    // (passes over NaN)
+        for (int e = 0; e < EPB; ++e) {
+            asm("v_max_f32 %0, %1, %2" : "=v"(x[u * EPB + e]) : "v"(x[u * EPB + e]), "s"(LOW));       // (as fmaxf, which would first quiet its argument; one that is NaN gives way either way)
+            m[u] = fmaxf(m[u], x[u * EPB + e]);
+        }
     }
-    top = fmaxf(top, lane_xor<1>(top));
-    top = fmaxf(top, lane_xor<2>(top));
-    float *const segments = (float *)((LogprobPart *)a.work + (int64_t)a.n_rows * plan.chunks);
-    if (a.n_top > 0 && lane % 4 == 0) segments[(int64_t)row * plan.segments + chunk * 64 + threadIdx.x / 4] = top;
-    top = fmaxf(top, lane_xor<4>(top));
-    butterfly<32>([&](auto o) { if constexpr (o.value >= 8) top = fmaxf(top, lane_xor<o.value>(top)); });
-    if (lane == 0) tops[wave] = top;
-    __syncthreads();
-    const float M = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    // ---- sums.  Tokens at or above the given one's logit count before it when their id is lower, tokens above it always
-    const float above = given ? next_above(xt) : __builtin_nanf(""), same = given ? xt : __builtin_nanf("");
-    const int pt = given ? (token + view.skip) / EPB : 0;
-    // (far out: an infinite maximum, which counts 1 and all else 0, or a temperature whose inverse ends the range)
-    const bool far = M == -LLMA_NEG_INF || by.hi < 1e-20f;
-    float s = 0.f, sd = 0.f;
-    int before = 0;
-    if (far) {
+    // ---- maxima of segments, of the chunk
+    float M = m[0];
+#pragma unroll
+    for (int u = 1; u < U; ++u) M = fmaxf(M, m[u]);
+    float lowest = m[0];
+#pragma unroll
+    for (int u = 1; u < U; ++u) lowest = fminf(lowest, m[u]);
+    if (__ballot(lowest <= LOW) != 0) {                          // (a piece all masked: by minus infinity, or by something between)
+        M = LLMA_NEG_INF;
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[EPB];                                        // (read again: kept, the pieces would cost the registers of a wave in four)
+            piece_values<TYPE>(row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab), v);
+            m[u] = LLMA_NEG_INF;
+#pragma unroll
+            for (int e = 0; e < EPB; ++e) m[u] = fmaxf(m[u], v[e]);
+            M = fmaxf(M, m[u]);
+        }
+    }
+    if (a.n_top > 0) {
+        float *const segments = (float *)((LogprobPart *)a.work + (int64_t)a.n_rows * plan.chunks) + (int64_t)row * plan.segments + chunk * U * (64 / plan.lanes);
+        float mine = maxima16<U>(m);
+        if (plan.lanes >= 32) mine = fmaxf(mine, lane_xor<16>(mine));
+        if (plan.lanes >= 64) mine = fmaxf(mine, lane_xor<32>(mine));
+        const int log_lanes = __builtin_ctz(plan.lanes);
+        if ((lane & (16 / U - 1)) == 0 && (lane & (plan.lanes - 1)) < 16) segments[((lane & 15) / (16 / U) << (6 - log_lanes)) + (lane >> log_lanes)] = mine;
+    }
+    butterfly<32>([&](auto o) { M = fmaxf(M, lane_xor<o.value>(M)); });
+    // ---- sums
+    double R = LLMA_NEG_INF;
+    float s = 0.f, sw = 0.f, tilt = 0.f;
+    const float r = M * by.hi;
+    if (fabsf(M) < 1e30f && by.hi > 1e-20f && fabsf(r) < 4096.f) {
+        R = (double)r;
+        tilt = (float)((by.by - (double)by.hi) / (double)by.hi);
+#pragma unroll
+        for (int i = 0; i < N; ++i) {
+            const float t = __builtin_fmaf(x[i], by.hi, -r), y = __builtin_amdgcn_exp2f(t);
+            s += y;
+            sw = __builtin_fmaf(y, t, sw);
+        }
+    } else if (M != LLMA_NEG_INF) {                              // an infinite maximum (it counts 1, all else 0), large logits, cold or very hot rows: in 64 bits up to 2^t
+        R = times_by(M, by);
 #pragma unroll 1
         for (int u = 0; u < U; ++u) {
-            float x[EPB];
-            piece_values<TYPE>(row_piece<TYPE>(view, p0 + u * CHUNK_THREADS, pieces, a.vocab), x);
+            float v[EPB];
+            piece_values<TYPE>(row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab), v);
 #pragma unroll
             for (int e = 0; e < EPB; ++e) {
-                const float v = fmaxf(x[e], LLMA_NEG_INF), d = v == M ? 0.f : v - M, y = d == LLMA_NEG_INF ? 0.f : power(d, by);
+                const float z = fmaxf(v[e], LLMA_NEG_INF);
+                const double t = z == M ? 0. : ((double)z - (double)M) * by.by;
+                const float y = t < -1000. ? 0.f : __builtin_amdgcn_exp2f((float)t);
                 s += y;
-                sd += y > 0.f ? y * d : 0.f;
-            }
-        }
-    } else if (M != LLMA_NEG_INF) {
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            float x[EPB];
-            piece_values<TYPE>(w[u], x);
-#pragma unroll
-            for (int e = 0; e < EPB; ++e) {
-                const float d = fmaxf(x[e] - M, -1e30f), y = power(d, by);       // (minus infinity and NaN: 0)
-                s += y;
-                sd = __builtin_fmaf(y, d, sd);
+                sw += y > 0.f ? y * (float)t : 0.f;
             }
         }
     }
-    if (given && a.rank) {
+    // ---- tokens before the given one: those above it, and as large ones with a lower id
+    int before = 0;
+    if (given) {
+        const float above = next_above(xt);
+        const int pt = (token + view.skip) / EPB;
+        if (xt > LOW) {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int p = p0 + u * CHUNK_THREADS;
-            float x[EPB];
-            piece_values<TYPE>(w[u], x);
-            const float least = p < pt ? same : above;
-            // (minus infinity, if that is what is given, counts too, and what is not the row's would)
-            const int i0 = p * EPB - view.skip;
+            for (int u = 0; u < U; ++u) {
+                const int p = p0 + 64 * u;
+                if (pt >= p && pt < p + 64) {                    // (of the wave's pieces here)
 #pragma unroll
-            for (int e = 0; e < EPB; ++e) {
-                const float v = fmaxf(x[e], LLMA_NEG_INF);
-                before += (v >= least || (p == pt && v == same && i0 + e < token)) && (same != LLMA_NEG_INF || (i0 + e >= 0 && i0 + e < a.vocab));
+                    for (int e = 0; e < EPB; ++e) {
+                        const float v = x[u * EPB + e];
+                        before += __popcll(__ballot(v >= above || (v == xt && (p + lane) * EPB + e < token + view.skip)));
+                    }
+                } else {
+                    const float least = p > pt ? above : xt;
+                    if (__ballot(m[u] >= least) == 0) continue;  // (m: of lanes, or of their 16: few reach a token that is likely)
+#pragma unroll
+                    for (int e = 0; e < EPB; ++e) before += __popcll(__ballot(x[u * EPB + e] >= least));
+                }
+            }
+        } else {
+#pragma unroll 1
+            for (int u = 0; u < U; ++u) {
+                const int i0 = (p0 + 64 * u + lane) * EPB - view.skip;
+                float v[EPB];
+                piece_values<TYPE>(row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab), v);
+#pragma unroll
+                for (int e = 0; e < EPB; ++e) {
+                    const float z = fmaxf(v[e], LLMA_NEG_INF);
+                    before += __popcll(__ballot((z >= above || (z == xt && i0 + e < token)) && i0 + e >= 0 && i0 + e < a.vocab));
+                }
             }
         }
     }
-    butterfly<32>([&](auto o) {
-        s += lane_xor<o.value>(s);
-        sd += lane_xor<o.value>(sd);
-        before += lane_xor<o.value>(before);
-    });
-    if (lane == 0) parts[wave] = LogprobPart{0.f, s, sd, before};
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        LogprobPart t{M, 0.f, 0.f, 0};
-        for (int i = 0; i < 4; ++i) {
-            t.s += parts[i].s;
-            t.w += parts[i].w;
-            t.before += parts[i].before;
-        }
-        ((LogprobPart *)a.work)[(int64_t)row * plan.chunks + chunk] = t;
+    add_over_wave(s);
+    add_over_wave(sw);
+    if (lane == 0) {
+        LogprobPart t;
+        t.r = R;
+        t.s = s;
+        t.w = sw;
+        t.tilt = tilt;
+        t.before = before;
+        t.pad[0] = t.pad[1] = 0;
+        ((LogprobPart *)a.work)[id] = t;
     }
 }
 
-// floats as integers of the same order; minus infinity is the least but one that can be, NaN is not asked
+// floats as integers of the same order
 __device__ __forceinline__ uint32_t ordered(float x) {
     const uint32_t b = __float_as_uint(x + 0.f);                 // (minus zero is zero)
     return b & 0x80000000u ? ~b : b | 0x80000000u;
 }
 __device__ __forceinline__ float value_of(uint32_t k) { return __uint_as_float(k & 0x80000000u ? k & 0x7fffffffu : ~k); }
-// the n-th largest of `count` distinct keys in LDS, all threads of the workgroup
-__device__ __forceinline__ unsigned long long nth_key(const unsigned long long *keys, int count, int n, int *sums) {
+
+// the n-th largest of `count` distinct keys in LDS
+__device__ __forceinline__ unsigned long long nth_key(const unsigned long long *keys, int count, int n) {
     unsigned long long t = 0;
     for (int bit = 63; bit >= 0; --bit) {
         const unsigned long long c = t | 1ull << bit;
         int at = 0;
-        for (int i = threadIdx.x; i < count; i += CHUNK_THREADS) at += keys[i] >= c;
-        butterfly<32>([&](auto o) { at += lane_xor<o.value>(at); });
-        __syncthreads();
-        if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = at;
-        __syncthreads();
-        if (sums[0] + sums[1] + sums[2] + sums[3] >= n) t = c;
+        for (int i = 0; i < count; i += 64) {
+            const int j = i + (int)threadIdx.x;
+            at += __popcll(__ballot(j < count && keys[j < count ? j : 0] >= c));
+        }
+        if (at >= n) t = c;
     }
     return t;
 }
 
 template <int TYPE>
-__global__ __launch_bounds__(CHUNK_THREADS) void logprob_row_kernel(LogprobArgs a, LogprobPlan plan) {
-    constexpr int EPB = sampled_epb<TYPE>;
-    __shared__ float tops[4];
-    __shared__ double sums[4][2];
-    __shared__ int counts[4];
-    __shared__ unsigned long long keys[TOP_KEPT + 8 * CHUNK_THREADS];
+__global__ __launch_bounds__(64) void logprob_row_kernel(LogprobArgs a, LogprobPlan plan) {
+    constexpr int EPB = sampled_epb<TYPE>, HELD = TOP_LIST / 64;
+    __shared__ unsigned long long keys[TOP_KEPT + 64 * EPB];
     __shared__ int list[TOP_LIST];
-    __shared__ int n_keys, n_list, cut[4];
-    __shared__ uint32_t least_segment;
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, row = blockIdx.x;
+    __shared__ u32x4 ahead[TOP_AHEAD][64];
+    __shared__ int ahead_at[TOP_AHEAD][64];
+    ieee_mode_off();
+    const int lane = threadIdx.x, row = blockIdx.x;
     const LogprobPart *const parts = (const LogprobPart *)a.work + (int64_t)row * plan.chunks;
+    const float *const segments = (const float *)((const LogprobPart *)a.work + (int64_t)a.n_rows * plan.chunks) + (int64_t)row * plan.segments;
+    uint32_t held[HELD];                                         // the first TOP_LIST segments' maxima; 0 for none, below all that can be
+    if (a.n_top > 0) {
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) held[k] = k * 64 + lane < plan.segments ? ordered(segments[k * 64 + lane]) : 0u;
+    }
     const By by = by_of(a, row);
-    // ---- the chunks' sums, in 64 bits
-    float top = LLMA_NEG_INF;
-    for (int i = threadIdx.x; i < plan.chunks; i += CHUNK_THREADS) top = fmaxf(top, parts[i].m);
-    butterfly<32>([&](auto o) { top = fmaxf(top, lane_xor<o.value>(top)); });
-    if (lane == 0) tops[wave] = top;
-    if (threadIdx.x == 0) n_keys = 0;
-    __syncthreads();
-    const float M = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
-    double s = 0., w = 0.;
+    const int token = a.tokens ? a.tokens[row] : -1;
+    const bool given = (unsigned)token < (unsigned)a.vocab;
+    const float xt = given ? logit_at<TYPE>(a, row, token) : LLMA_NEG_INF;
+    // ---- the chunks' sums, in 64 bits, relative to the largest R
+    double R = LLMA_NEG_INF, s = 0., w = 0.;
     int before = 0;
-    for (int i = threadIdx.x; i < plan.chunks; i += CHUNK_THREADS) {
+    for (int i = lane; i < plan.chunks; i += 64) R = fmax(R, parts[i].r);
+    butterfly<32>([&](auto o) { R = fmax(R, __longlong_as_double((long long)lane_xor<o.value>((unsigned long long)__double_as_longlong(R)))); });
+    for (int i = lane; i < plan.chunks; i += 64) {
         const LogprobPart p = parts[i];
-        const float d = p.m == M ? 0.f : p.m - M, f = p.m == LLMA_NEG_INF || d == LLMA_NEG_INF ? 0.f : power(d, by);
-        if (f > 0.f) {
-            s += (double)f * p.s;
-            w += (double)f * ((double)p.w + (double)d * p.s);
+        const double d = p.r == R ? 0. : p.r - R;
+        if (d > -1000.) {
+            // A term is 2^(x hi) for 2^(x by), hi the fp32 value of by: S lacks ln2 (by - hi) sum 2^t x, W that times the mean of t, and the sum itself (the spread of t, of the
+            // size of (by - hi) too, is left out: 2^-25 of it; |x hi| is below 2^12, so the squares are 2^-26).
+            // (Exponential and logarithm in fp32, of numbers near 1: off by 2^-23 of a part, which 64 bits would not notice in the result)
+            const double f = (double)__builtin_amdgcn_exp2f((float)d);
+            const double lack = p.tilt != 0.f ? (double)p.tilt * (p.w + p.r * p.s) : 0., mean = p.tilt != 0.f ? (double)(p.w / p.s) : 0.;
+            const double ps = p.s + 0.69314718055994530942 * lack, pw = p.w + lack * (1. + 0.69314718055994530942 * mean);
+            s += f * ps;
+            w += f * (pw + d * ps);
         }
         before += p.before;
     }
-    butterfly<32>([&](auto o) {
-        s += __longlong_as_double((long long)lane_xor<o.value>((unsigned long long)__double_as_longlong(s)));
-        w += __longlong_as_double((long long)lane_xor<o.value>((unsigned long long)__double_as_longlong(w)));
-        before += lane_xor<o.value>(before);
-    });
-    if (lane == 0) {
-        sums[wave][0] = s;
-        sums[wave][1] = w;
-        counts[wave] = before;
-    }
-    __syncthreads();
-    s = sums[0][0] + sums[1][0] + sums[2][0] + sums[3][0];
-    const double log_s = s > 0. ? log(s) : 0.;
-    const auto logprob_of = [&](float x) {
-        if (x == LLMA_NEG_INF) return LLMA_NEG_INF;
-        if (M == -LLMA_NEG_INF) return x == M ? (float)-log_s : LLMA_NEG_INF;
-        return (float)(((double)x - (double)M) / by.t - log_s);
+    add_over_wave(s);
+    add_over_wave(w);
+    add_over_wave(before);
+    const double log2_s = s > 0. ? (double)__builtin_amdgcn_logf((float)__builtin_amdgcn_frexp_mant(s)) + (double)__builtin_amdgcn_frexp_exp(s) : 0., ln2 = 0.69314718055994530942;
+    const bool infinite = R == -(double)LLMA_NEG_INF;
+    const auto minus_r = [&](double z) {
+#pragma clang fp contract(off)
+        return z - R;
     };
-    if (threadIdx.x == 0) {
-        const int token = a.tokens ? a.tokens[row] : -1;
-        const bool given = (unsigned)token < (unsigned)a.vocab;
-        if (a.logprob) a.logprob[row] = given ? logprob_of(logit_at<TYPE>(a, row, token)) : LLMA_NEG_INF;
-        if (a.rank) a.rank[row] = given ? counts[0] + counts[1] + counts[2] + counts[3] : -1;
-        if (a.entropy) a.entropy[row] = s > 0. ? (float)(log_s - (sums[0][1] + sums[1][1] + sums[2][1] + sums[3][1]) / s / by.t) : 0.f;
+    const auto logprob_of = [&](float v) {
+        if (v == LLMA_NEG_INF || (infinite && v != -LLMA_NEG_INF)) return LLMA_NEG_INF;
+        return (float)(ln2 * ((infinite ? 0. : minus_r(times_by(v, by))) - log2_s));
+    };
+    if (lane == 0) {
+        if (a.logprob) a.logprob[row] = logprob_of(xt);
+        if (a.rank) a.rank[row] = given ? before : -1;
+        if (a.entropy) a.entropy[row] = s > 0. ? (float)(ln2 * (log2_s - w / s)) : 0.f;
     }
     if (a.n_top < 1) return;
-    // ---- the n_top-th largest segment maximum: no alternative lies below it
-    const float *const segments = (const float *)((const LogprobPart *)a.work + (int64_t)a.n_rows * plan.chunks) + (int64_t)row * plan.segments;
-    if (wave == 0) {
-        uint32_t t = 0;
-        for (int bit = 31; bit >= 0; --bit) {
-            const uint32_t c = t | 1u << bit;
+    // ---- a bound that at least n_top segments' maxima reach, few more: no alternative lies below it.  Of few alternatives the lanes' own maxima will do: an eighth of the
+    // comparisons, and a fifth more segments that reach the bound (20 alternatives of 1002 segments: 24)
+    uint32_t reach = 0;
+    {
+        const bool few = a.n_top <= TOP_FEW;
+        uint32_t most = 0;
+#pragma unroll
+        for (int k = 0; k < HELD; ++k) most = held[k] > most ? held[k] : most;
+        if (plan.segments > TOP_LIST)
+            for (int i = TOP_LIST + lane; i < plan.segments; i += 64) {
+                const uint32_t c = ordered(segments[i]);
+                most = c > most ? c : most;
+            }
+        uint32_t above = most;                                   // (bits above the highest that the lanes' maxima do not share need no test)
+        if (few) {
+            uint32_t low = most;
+            butterfly<32>([&](auto o) {
+                const uint32_t m = (uint32_t)lane_xor<o.value>((int)above), l = (uint32_t)lane_xor<o.value>((int)low);
+                above = m > above ? m : above;
+                low = l < low ? l : low;
+            });
+            above ^= low;
+            reach = low;
+        } else above = ~0u;
+        const int bits = above == 0 ? 0 : 32 - __builtin_clz(above);
+        reach = bits == 32 ? 0u : reach >> bits << bits;
+        for (int bit = bits - 1; bit >= 0; --bit) {
+            const uint32_t c = reach | 1u << bit;
             int n = 0;
-            for (int i = lane; i < plan.segments; i += 64) n += ordered(segments[i]) >= c;
-            butterfly<32>([&](auto o) { n += lane_xor<o.value>(n); });
-            if (n >= a.n_top) t = c;
-            if (n == a.n_top) break;
+            if (few) n = __popcll(__ballot(most >= c));
+            else if (plan.segments <= TOP_LIST) {
+#pragma unroll
+                for (int k = 0; k < HELD; ++k) n += __popcll(__ballot(held[k] >= c));
+            } else {
+                for (int i = 0; i < plan.segments; i += 64) n += __popcll(__ballot(i + lane < plan.segments && ordered(segments[i + lane < plan.segments ? i + lane : 0]) >= c));
+            }
+            if (n >= a.n_top) reach = c;
+            if (n >= a.n_top && n <= a.n_top + (few ? 0 : 4)) break;
         }
-        if (lane == 0) least_segment = t;
     }
-    __syncthreads();
     const RowView view = row_view<TYPE>(a, row);
     const int pieces = (view.skip + a.vocab + EPB - 1) / EPB;
     const uint32_t nothing = ordered(LLMA_NEG_INF);
-    const uint32_t reach = least_segment > nothing ? least_segment : nothing + 1;
+    reach = reach > nothing ? reach : nothing + 1;
     unsigned long long least = (unsigned long long)reach << 32;  // keys: the logit's order, then the lower id
+    const int log_each = __builtin_ctz(plan.lanes);              // a segment's pieces, a power of two; segments lie as pieces do
+    int n_keys = 0;
     for (int g0 = 0; g0 < plan.segments; g0 += TOP_LIST) {
-        __syncthreads();
-        if (threadIdx.x == 0) n_list = 0;
-        __syncthreads();
-        for (int g = g0 + threadIdx.x; g < g0 + TOP_LIST && g < plan.segments; g += CHUNK_THREADS)
-            if (ordered(segments[g]) >= reach) list[atomicAdd(&n_list, 1)] = g;
-        __syncthreads();
-        const int all = n_list * 4 * plan.u;
-        for (int i0 = 0; i0 < all; i0 += CHUNK_THREADS) {
-            const int i = i0 + threadIdx.x;
-            if (i < all) {
-                const int g = list[i / (4 * plan.u)], u = i / 4 % plan.u;
-                const int p = (g / 64 * plan.u + u) * CHUNK_THREADS + g % 64 * 4 + i % 4;
-                float x[EPB];
-                piece_values<TYPE>(row_piece<TYPE>(view, p, pieces, a.vocab), x);
+        // the segments that reach it, in order
+        int n_list = 0;
 #pragma unroll
-                for (int e = 0; e < EPB; ++e) {
-                    const float v = fmaxf(x[e], LLMA_NEG_INF);
-                    const unsigned long long key = (unsigned long long)ordered(v) << 32 | (0xffffffffu - (uint32_t)(p * EPB - view.skip + e));
-                    if (key >= least) keys[atomicAdd(&n_keys, 1)] = key;
+        for (int k = 0; k < HELD; ++k) {
+            const int g = g0 + 64 * k + lane;
+            const bool in = g < plan.segments && (g0 == 0 ? held[k] : ordered(segments[g < plan.segments ? g : 0])) >= reach;
+            const unsigned long long all = __ballot(in);
+            if (in) list[n_list + __popcll(all & ((1ull << lane) - 1))] = g;
+            n_list += __popcll(all);
+        }
+        __syncthreads();
+        const int n_pieces = n_list << log_each;
+        for (int i0 = 0; i0 < n_pieces; i0 += TOP_AHEAD * 64) {
+            // (through LDS, for short code: a call of a few rows spends its time on fetching it)
+            u32x4 piece[TOP_AHEAD];
+            int at[TOP_AHEAD];
+#pragma unroll
+            for (int k = 0; k < TOP_AHEAD; ++k) {
+                const int i = i0 + 64 * k + lane, g = list[i < n_pieces ? i >> log_each : 0];
+                at[k] = (g << log_each) + (i & (plan.lanes - 1));
+                at[k] = i < n_pieces && at[k] < pieces ? at[k] : -1;
+                piece[k] = view.base[at[k] < 0 ? 0 : at[k]];
+            }
+            __syncthreads();
+#pragma unroll
+            for (int k = 0; k < TOP_AHEAD; ++k) {
+                ahead[k][lane] = piece[k];
+                ahead_at[k][lane] = at[k];
+            }
+#pragma unroll 1
+            for (int k = 0; k < TOP_AHEAD && i0 + 64 * k < n_pieces; ++k) {
+                const float floor = value_of((uint32_t)(least >> 32));
+                const int first = ahead_at[k][lane] * EPB - view.skip;
+                float x[EPB], top = LLMA_NEG_INF;
+                piece_values<TYPE>(ahead[k][lane], x);
+#pragma unroll
+                for (int e = 0; e < EPB; ++e) top = fmaxf(top, x[e]);
+                if (ahead_at[k][lane] < 0) top = LLMA_NEG_INF;
+                if (__ballot(top >= floor) == 0) continue;
+                // (a row's first and last piece hold what is not the row's)
+                uint32_t in = 0;
+#pragma unroll
+                for (int e = 0; e < EPB; ++e) in |= (top >= floor && x[e] >= floor && (unsigned)(first + e) < (unsigned)a.vocab ? 1u : 0u) << e;
+                while (__ballot(in != 0) != 0) {                 // (one a lane at a time: hardly any lane has two)
+                    const int e = in ? __builtin_ctz(in) : 0;
+                    float v;
+                    if constexpr (TYPE == ROWS_F32) v = ((const float *)&ahead[k][lane])[e];
+                    else if constexpr (TYPE == ROWS_F16) v = (float)((const _Float16 *)&ahead[k][lane])[e];
+                    else v = bf16_to_f32(((const bf16_t *)&ahead[k][lane])[e]);
+                    const unsigned long long key = (unsigned long long)ordered(v) << 32 | (0xffffffffu - (uint32_t)(first + e));
+                    const bool put = in != 0 && key >= least;
+                    const unsigned long long all = __ballot(put);
+                    if (put) keys[n_keys + __popcll(all & ((1ull << lane) - 1))] = key;
+                    n_keys += __popcll(all);
+                    in &= in - 1;
+                }
+                if (n_keys > TOP_KEPT) {                         // (many equal or rising logits) keep the n_top largest
+                    __syncthreads();
+                    least = nth_key(keys, n_keys, a.n_top);
+                    int n = 0;
+                    for (int i = 0; i < n_keys; i += 64) {       // (each round writes where it or one before it has read)
+                        const unsigned long long key = i + lane < n_keys ? keys[i + lane] : 0;
+                        const unsigned long long all = __ballot(key >= least);
+                        __syncthreads();
+                        if (key >= least) keys[n + __popcll(all & ((1ull << lane) - 1))] = key;
+                        __syncthreads();
+                        n += __popcll(all);
+                    }
+                    n_keys = n;
                 }
             }
-            __syncthreads();
-            if (n_keys > TOP_KEPT) {                             // (many equal or rising logits) keep the n_top largest
-                const int count = n_keys;
-                least = nth_key(keys, count, a.n_top, cut);
-                unsigned long long mine[(TOP_KEPT + 8 * CHUNK_THREADS) / CHUNK_THREADS];
-#pragma unroll
-                for (int k = 0; k < (TOP_KEPT + 8 * CHUNK_THREADS) / CHUNK_THREADS; ++k) mine[k] = k * CHUNK_THREADS + (int)threadIdx.x < count ? keys[k * CHUNK_THREADS + threadIdx.x] : 0;
-                __syncthreads();
-                if (threadIdx.x == 0) n_keys = 0;
-                __syncthreads();
-#pragma unroll
-                for (int k = 0; k < (TOP_KEPT + 8 * CHUNK_THREADS) / CHUNK_THREADS; ++k)
-                    if (mine[k] >= least) keys[atomicAdd(&n_keys, 1)] = mine[k];
-                __syncthreads();
-            }
-            __syncthreads();
         }
+        __syncthreads();
     }
-    __syncthreads();
     const int count = n_keys;
-    if (count > 4 * LOGPROB_MAX_TOP) least = nth_key(keys, count, a.n_top, cut);
+    if (count > 4 * LOGPROB_MAX_TOP) least = nth_key(keys, count, a.n_top);
     int *const tokens = a.top_tokens + (int64_t)row * a.n_top;
     float *const logprobs = a.top_logprobs + (int64_t)row * a.n_top;
-    for (int i = threadIdx.x; i < count; i += CHUNK_THREADS) {
+    for (int i = lane; i < count; i += 64) {
         const unsigned long long key = keys[i];
         if (key < least) continue;
         int place = 0;
+#pragma unroll 4
         for (int j = 0; j < count; ++j) place += keys[j] > key;
         if (place < a.n_top) {
             tokens[place] = (int)(0xffffffffu - (uint32_t)key);
             logprobs[place] = logprob_of(value_of((uint32_t)(key >> 32)));
         }
     }
-    for (int i = count + threadIdx.x; i < a.n_top; i += CHUNK_THREADS) {
+    for (int i = count + lane; i < a.n_top; i += 64) {
         tokens[i] = -1;
         logprobs[i] = LLMA_NEG_INF;
     }
@@ -342,12 +481,12 @@ void launch_token_logprobs(const LogprobArgs &a, hipStream_t st) {
     auto of = [&](auto type) {
         constexpr int TYPE = decltype(type)::value;
         const LogprobPlan p = logprob_plan(a.n_rows, a.vocab, sampled_epb<TYPE>);
-        const dim3 grid((unsigned)((int64_t)a.n_rows * p.chunks)), block(CHUNK_THREADS);
+        const dim3 grid((unsigned)(((int64_t)a.n_rows * p.chunks + 3) / 4)), block(256);
         if (p.u == 8) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 8>), grid, block, 0, st, a, p);
         else if (p.u == 4) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 4>), grid, block, 0, st, a, p);
         else if (p.u == 2) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 2>), grid, block, 0, st, a, p);
         else hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 1>), grid, block, 0, st, a, p);
-        hipLaunchKernelGGL((logprob_row_kernel<TYPE>), dim3(a.n_rows), block, 0, st, a, p);
+        hipLaunchKernelGGL((logprob_row_kernel<TYPE>), dim3(a.n_rows), dim3(64), 0, st, a, p);
     };
     if (a.type == ROWS_BF16) of(std::integral_constant<int, ROWS_BF16>{});
     else if (a.type == ROWS_F16) of(std::integral_constant<int, ROWS_F16>{});

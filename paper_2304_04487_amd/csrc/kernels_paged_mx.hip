@@ -13,6 +13,15 @@ template <int T> __device__ __forceinline__ uint32_t widen2(uint32_t c, float sc
 // eight neighbouring features: an operand
 __device__ __forceinline__ u32x4 widen8(uint32_t c, float scale) { return (u32x4){widen2<0>(c, scale), widen2<1>(c, scale), widen2<2>(c, scale), widen2<3>(c, scale)}; }
 __device__ __forceinline__ uint32_t nan_scales(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u; }      // 0x80 in the bytes that are 255
+// four words of four bytes, turned: word r gets byte r of each
+__device__ __forceinline__ void turn4(uint32_t *w) {
+    const uint32_t p = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), q = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
+    const uint32_t t = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), u = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
+    w[0] = __builtin_amdgcn_perm(q, p, 0x05040100u);
+    w[1] = __builtin_amdgcn_perm(q, p, 0x07060302u);
+    w[2] = __builtin_amdgcn_perm(u, t, 0x05040100u);
+    w[3] = __builtin_amdgcn_perm(u, t, 0x07060302u);
+}
 // exponent of the smallest power of two s from 2^-64 to 2^120 with amax / s <= 7: 6 is the largest code, and what lies up to 7 rounds to it by half a step as elsewhere
 // (7 costs less than 6: 19.0 dB of normal values' blocks kept, 18.75 with 6, 18.8 with 8)
 __device__ __forceinline__ int mx_exponent(float amax) {
@@ -79,13 +88,9 @@ __device__ __forceinline__ void append_mx_quad(const AppendMxArgs &a, int head, 
     } else {
         uint8_t *const to = a.c.v + (block * (DH / 2) + 4 * oct) * PAGE_POS + at;
         if (whole) {
-            // four rows' four bytes, turned
-            const uint32_t p = __builtin_amdgcn_perm(codes[1], codes[0], 0x05010400u), q = __builtin_amdgcn_perm(codes[3], codes[2], 0x05010400u);
-            const uint32_t t = __builtin_amdgcn_perm(codes[1], codes[0], 0x07030602u), u = __builtin_amdgcn_perm(codes[3], codes[2], 0x07030602u);
-            *(uint32_t *)to = __builtin_amdgcn_perm(q, p, 0x05040100u);
-            *(uint32_t *)(to + PAGE_POS) = __builtin_amdgcn_perm(q, p, 0x07060302u);
-            *(uint32_t *)(to + 2 * PAGE_POS) = __builtin_amdgcn_perm(u, t, 0x05040100u);
-            *(uint32_t *)(to + 3 * PAGE_POS) = __builtin_amdgcn_perm(u, t, 0x07060302u);
+            turn4(codes);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) *(uint32_t *)(to + j * PAGE_POS) = codes[j];
         } else {
 #pragma unroll
             for (int r = 0; r < 4; ++r)
@@ -145,121 +150,127 @@ void launch_append_paged_mx(const AppendMxArgs &a, hipStream_t st) {
 // ---------------------------------------------------------------------------------------------
 // rows out of the cache
 // ---------------------------------------------------------------------------------------------
-// Row j of sequence b is position first[b] + j.  A run = rows of one sequence inside one page; a workgroup takes one head of the runs that begin in its window of 64 rows (a long
-// sequence's: one).  K's rows lie as they leave.  V's lie across: a lane takes four positions of eight features, turns them in registers and has
-// eight neighbouring features of four rows.
-#define READ_WINDOW 64
-#define READ_KEPT 4097           // offsets in LDS: LLMA_PAGED_MAX_SEQS + 1
+// Row j of sequence b is position first[b] + j.  A run = rows of one sequence inside one page; a workgroup takes one head of the runs that begin in its window of
+// rows (64: a long sequence's one run).  A lane stores 16 bytes of a row, eight neighbouring lanes 128.  K's rows lie as they leave.  V's lie across: a lane takes four
+// positions of its features, turns them in registers and has its features of four rows.
 struct ReadRun { int row, n, page, at; };                        // page -1: none, the rows become 0
+template <int TYPE> constexpr int read_features = TYPE == ROWS_F32 ? 4 : 8;      // of 16 bytes
 template <int TYPE>
-__device__ __forceinline__ void store8(void *p, int64_t at, const float v[8]) {
-    if constexpr (TYPE == ROWS_F32) {
-        *(f32x4 *)((float *)p + at) = (f32x4){v[0], v[1], v[2], v[3]};
-        *(f32x4 *)((float *)p + at + 4) = (f32x4){v[4], v[5], v[6], v[7]};
-    } else if constexpr (TYPE == ROWS_F16) {
-        *(u32x4 *)((bf16_t *)p + at) = (u32x4){half_pair(v[0], v[1]), half_pair(v[2], v[3]), half_pair(v[4], v[5]), half_pair(v[6], v[7])};
-    } else {
-        *(u32x4 *)((bf16_t *)p + at) = (u32x4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
-    }
+__device__ __forceinline__ void store16(void *p, int64_t at, const float (&v)[read_features<TYPE>]) {
+    if constexpr (TYPE == ROWS_F32) *(f32x4 *)((float *)p + at) = (f32x4){v[0], v[1], v[2], v[3]};
+    else if constexpr (TYPE == ROWS_F16) *(u32x4 *)((bf16_t *)p + at) = (u32x4){half_pair(v[0], v[1]), half_pair(v[2], v[3]), half_pair(v[4], v[5]), half_pair(v[6], v[7])};
+    else *(u32x4 *)((bf16_t *)p + at) = (u32x4){bf16_pair(v[0], v[1]), bf16_pair(v[2], v[3]), bf16_pair(v[4], v[5]), bf16_pair(v[6], v[7])};
 }
+// four or eight neighbouring features' values
 typedef __attribute__((ext_vector_type(2))) float f32x2;
-template <int T> __device__ __forceinline__ f32x2 value2(uint32_t c, float scale) { return __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c, scale, T); }
-// eight features: 4-bit, one word
-__device__ __forceinline__ void values8(uint32_t c, float scale, float v[8]) {
-    const f32x2 p[4] = {value2<0>(c, scale), value2<1>(c, scale), value2<2>(c, scale), value2<3>(c, scale)};
+template <bool MX, int F>
+__device__ __forceinline__ void values_of(const uint32_t (&c)[2], float scale, float (&v)[F]) {
+    if constexpr (MX) {
+        const f32x2 a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], scale, 1);
+        v[0] = a[0]; v[1] = a[1]; v[2] = b[0]; v[3] = b[1];
+        if constexpr (F == 8) {
+            const f32x2 d = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], scale, 2), e = __builtin_amdgcn_cvt_scalef32_pk_f32_fp4(c[0], scale, 3);
+            v[4] = d[0]; v[5] = d[1]; v[6] = e[0]; v[7] = e[1];
+        }
+    } else {
 #pragma unroll
-    for (int e = 0; e < 8; ++e) v[e] = p[e / 2][e % 2];
-}
-// 8-bit, two words
-__device__ __forceinline__ void values8(u32x2 c, float scale, float v[8]) {
-#pragma unroll
-    for (int w = 0; w < 2; ++w) {
-        v[4 * w] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 0) * scale;
-        v[4 * w + 1] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 1) * scale;
-        v[4 * w + 2] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 2) * scale;
-        v[4 * w + 3] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 3) * scale;
+        for (int w = 0; w < F / 4; ++w) {
+            v[4 * w] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 0) * scale;
+            v[4 * w + 1] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 1) * scale;
+            v[4 * w + 2] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 2) * scale;
+            v[4 * w + 3] = __builtin_amdgcn_cvt_f32_fp8((int)c[w], 3) * scale;
+        }
     }
-}
-// four words of four bytes, turned: word r gets byte r of each
-__device__ __forceinline__ void turn4(uint32_t w[4]) {
-    const uint32_t p = __builtin_amdgcn_perm(w[1], w[0], 0x05010400u), q = __builtin_amdgcn_perm(w[3], w[2], 0x05010400u);
-    const uint32_t t = __builtin_amdgcn_perm(w[1], w[0], 0x07030602u), u = __builtin_amdgcn_perm(w[3], w[2], 0x07030602u);
-    w[0] = __builtin_amdgcn_perm(q, p, 0x05040100u);
-    w[1] = __builtin_amdgcn_perm(q, p, 0x07060302u);
-    w[2] = __builtin_amdgcn_perm(u, t, 0x05040100u);
-    w[3] = __builtin_amdgcn_perm(u, t, 0x07060302u);
 }
 template <typename C, int DH, int TYPE>
 __device__ __forceinline__ void read_run(const ReadArgs<C> &a, int head, const ReadRun &r) {
     constexpr bool MX = std::is_same_v<C, PagedMxCache>;
-    constexpr int OCTS = DH / 8, ROWS = 256 / OCTS, PASSES = PAGE_POS / ROWS;
+    constexpr int F = read_features<TYPE>, LANES = DH / F, ROWS = 256 / LANES, PASSES = PAGE_POS / ROWS;
+    constexpr int WORDS = MX ? F / 2 : F, VPASSES = (LANES * (PAGE_POS / 4) + 255) / 256;      // WORDS: of four positions each
     const size_t block = (size_t)(r.page < 0 ? 0 : r.page) * a.c.heads + head;
-    const bool none = r.page < 0;
-    {
-        const int oct = threadIdx.x % OCTS, j0 = threadIdx.x / OCTS;
-        std::conditional_t<MX, uint32_t, u32x2> c[PASSES];
-        float s[PASSES];
+    // ---- K's codes, then V's: all requested before the first is used
+    const int k_at = threadIdx.x % LANES, j0 = threadIdx.x / LANES;
+    uint32_t c[PASSES][2];
+    float ks[PASSES];
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int j = j0 + p * ROWS, at = r.at + (j < r.n ? j : 0);
-            if constexpr (MX) {
-                c[p] = ((const uint32_t *)(a.c.k + (block * PAGE_POS + at) * (DH / 2)))[oct];
-                s[p] = __uint_as_float((uint32_t)a.c.k_scale[(block * (DH / 32) + oct / 4) * PAGE_POS + at] << 23);
-            } else {
-                c[p] = ((const u32x2 *)(a.c.k + (block * PAGE_POS + at) * DH))[oct];
-                s[p] = a.c.k_scale[block];
+    for (int p = 0; p < PASSES; ++p) {
+        const int j = j0 + p * ROWS, pos = r.at + (j < r.n ? j : 0);
+        const uint8_t *const from = a.c.k + (block * PAGE_POS + pos) * (MX ? DH / 2 : DH) + k_at * (MX ? F / 2 : F);
+        c[p][1] = 0;
+        if constexpr (MX && F == 4) c[p][0] = *(const uint16_t *)from;
+        else if constexpr (MX || F == 4) c[p][0] = *(const uint32_t *)from;
+        else {
+            const u32x2 w = *(const u32x2 *)from;
+            c[p][0] = w[0];
+            c[p][1] = w[1];
+        }
+        if constexpr (MX) ks[p] = __uint_as_float((uint32_t)a.c.k_scale[(block * (DH / 32) + k_at * F / 32) * PAGE_POS + pos] << 23);
+        else ks[p] = a.c.k_scale[block];
+    }
+    uint32_t w[VPASSES][WORDS], sc[VPASSES];
+#pragma unroll
+    for (int p = 0; p < VPASSES; ++p) {
+        const int t = 256 * p + threadIdx.x, at = t % 8 + t / (8 * 16) * 8, quad = t / 8 % 16;
+        if (at >= LANES || 4 * quad + 3 < r.at || 4 * quad >= r.at + r.n) continue;
+#pragma unroll
+        for (int j = 0; j < WORDS; ++j) w[p][j] = *(const uint32_t *)(a.c.v + (block * (MX ? DH / 2 : DH) + WORDS * at + j) * PAGE_POS + 4 * quad);
+        if constexpr (MX) sc[p] = *(const uint32_t *)(a.c.v_scale + (block * (DH / 32) + at * F / 32) * PAGE_POS + 4 * quad);
+        else sc[p] = __float_as_uint(a.c.v_scale[block]);
+    }
+#pragma unroll
+    for (int p = 0; p < PASSES; ++p) {
+        const int j = j0 + p * ROWS;
+        if (j >= r.n) continue;
+        float v[F];
+        values_of<MX, F>(c[p], ks[p], v);
+#pragma unroll
+        for (int e = 0; e < F; ++e) v[e] = r.page < 0 ? 0.f : v[e];
+        store16<TYPE>(a.k, (r.row + j) * a.k_row + head * a.k_head + F * k_at, v);
+    }
+#pragma unroll
+    for (int p = 0; p < VPASSES; ++p) {
+        const int t = 256 * p + threadIdx.x, at = t % 8 + t / (8 * 16) * 8, quad = t / 8 % 16;
+        if (at >= LANES || 4 * quad + 3 < r.at || 4 * quad >= r.at + r.n) continue;
+        uint32_t row[4][2];                                      // the codes of a row's features
+        if constexpr (WORDS == 2) {
+            const uint32_t x = __builtin_amdgcn_perm(w[p][1], w[p][0], 0x05010400u), y = __builtin_amdgcn_perm(w[p][1], w[p][0], 0x07030602u);
+            row[0][0] = x;
+            row[1][0] = x >> 16;
+            row[2][0] = y;
+            row[3][0] = y >> 16;
+        } else {
+#pragma unroll
+            for (int g = 0; g < WORDS; g += 4) {
+                turn4(w[p] + g);
+#pragma unroll
+                for (int j = 0; j < 4; ++j) row[j][g / 4] = w[p][g + j];
             }
         }
 #pragma unroll
-        for (int p = 0; p < PASSES; ++p) {
-            const int j = j0 + p * ROWS;
-            if (j >= r.n) continue;
-            float v[8];
-            values8(c[p], s[p], v);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : v[e];
-            store8<TYPE>(a.k, (r.row + j) * a.k_row + head * a.k_head + 8 * oct, v);
-        }
-    }
-    // (lanes of a wave: neighbouring octets that fill 128 bytes of a row, times positions)
-    constexpr int NEAR = TYPE == ROWS_F32 ? 4 : 8, WORDS = MX ? 4 : 8;
-    for (int t = threadIdx.x; t < OCTS * (PAGE_POS / 4); t += 256) {
-        const int oct = t % NEAR + t / (NEAR * 16) * NEAR, quad = t / NEAR % 16;
-        if (4 * quad + 3 < r.at || 4 * quad >= r.at + r.n) continue;
-        uint32_t w[WORDS], sc = 0;
-        float s = 0.f;
-#pragma unroll
-        for (int j = 0; j < WORDS; ++j) w[j] = *(const uint32_t *)(a.c.v + (block * (MX ? DH / 2 : DH) + WORDS * oct + j) * PAGE_POS + 4 * quad);
-        if constexpr (MX) sc = *(const uint32_t *)(a.c.v_scale + (block * (DH / 32) + oct / 4) * PAGE_POS + 4 * quad);
-        else s = a.c.v_scale[block];
-        turn4(w);
-        if constexpr (!MX) turn4(w + 4);
-#pragma unroll
         for (int j = 0; j < 4; ++j) {
-            const int row = 4 * quad + j - r.at;
-            if (row < 0 || row >= r.n) continue;
-            float v[8];
-            if constexpr (MX) values8(w[j], __uint_as_float((sc >> 8 * j & 255u) << 23), v);
-            else values8((u32x2){w[j], w[j + 4]}, s, v);
+            const int i = 4 * quad + j - r.at;
+            if (i < 0 || i >= r.n) continue;
+            float v[F];
+            values_of<MX, F>(row[j], __uint_as_float(MX ? (sc[p] >> 8 * j & 255u) << 23 : sc[p]), v);
 #pragma unroll
-            for (int e = 0; e < 8; ++e) v[e] = none ? 0.f : v[e];
-            store8<TYPE>(a.v, (r.row + row) * a.v_row + head * a.v_head + 8 * oct, v);
+            for (int e = 0; e < F; ++e) v[e] = r.page < 0 ? 0.f : v[e];
+            store16<TYPE>(a.v, (r.row + i) * a.v_row + head * a.v_head + F * at, v);
         }
     }
 }
 template <typename C, int DH, int TYPE>
-__global__ __launch_bounds__(256) void read_paged_kernel(ReadArgs<C> a) {
-    __shared__ int offsets[READ_KEPT];
-    __shared__ ReadRun runs[READ_WINDOW];
+__global__ __launch_bounds__(256) void read_paged_kernel(ReadArgs<C> a, int window) {
+    extern __shared__ int offsets[];                             // [n_seqs + 1]
+    __shared__ ReadRun runs[64];
     __shared__ int n_runs;
-    const int head = blockIdx.x % a.c.heads, r0 = blockIdx.x / a.c.heads * READ_WINDOW;
+    const int head = blockIdx.x % a.c.heads, r0 = blockIdx.x / a.c.heads * window;
     for (int b = threadIdx.x; b <= a.n_seqs; b += 256) offsets[b] = a.row_offsets[b];
     __syncthreads();
     if (threadIdx.x < 64) {
         const int i = r0 + threadIdx.x;
         ReadRun run{i, 0, -1, 0};
         bool begins = false;
-        if (i < a.n_rows && i >= offsets[0] && i < offsets[a.n_seqs]) {
+        if ((int)threadIdx.x < window && i < a.n_rows && i >= offsets[0] && i < offsets[a.n_seqs]) {
             int b = count_le(offsets, a.n_seqs + 1, i) - 1;
             b = b < 0 ? 0 : b >= a.n_seqs ? a.n_seqs - 1 : b;
             const int64_t pos = (int64_t)(a.first ? a.first[b] : 0) + i - offsets[b];
@@ -285,12 +296,16 @@ __global__ __launch_bounds__(256) void read_paged_kernel(ReadArgs<C> a) {
 template <typename C>
 static void launch_read(const ReadArgs<C> &a, hipStream_t st) {
     if (a.n_seqs < 1 || a.n_rows < 1) return;
-    const unsigned blocks = (unsigned)((a.n_rows + READ_WINDOW - 1) / READ_WINDOW * a.c.heads);
+    // windows of a page's rows; where sequences have fewer, and there are too few windows for the chip, smaller ones: a workgroup takes its window's runs one after the other
+    int window = 64;
+    while (window > 4 && (int64_t)a.n_seqs * window > a.n_rows && (int64_t)((a.n_rows + window - 1) / window) * a.c.heads < 1024) window /= 2;
+    const unsigned blocks = (unsigned)((a.n_rows + window - 1) / window * a.c.heads);
+    const size_t bytes = (size_t)(a.n_seqs + 1) * 4;
     auto of = [&](auto dh) {
         constexpr int DH = decltype(dh)::value;
-        if (a.type == ROWS_BF16) hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_BF16>), dim3(blocks), dim3(256), 0, st, a);
-        else if (a.type == ROWS_F16) hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_F16>), dim3(blocks), dim3(256), 0, st, a);
-        else hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_F32>), dim3(blocks), dim3(256), 0, st, a);
+        if (a.type == ROWS_BF16) hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_BF16>), dim3(blocks), dim3(256), bytes, st, a, window);
+        else if (a.type == ROWS_F16) hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_F16>), dim3(blocks), dim3(256), bytes, st, a, window);
+        else hipLaunchKernelGGL((read_paged_kernel<C, DH, ROWS_F32>), dim3(blocks), dim3(256), bytes, st, a, window);
     };
     if (a.c.dh == 128) of(std::integral_constant<int, 128>{});
     else of(std::integral_constant<int, 64>{});

@@ -10,8 +10,10 @@ struct RowView { const u32x4 *base; int skip; };                // pieces from t
 template <int TYPE, typename A>
 __device__ __forceinline__ RowView row_view(const A &a, int64_t row) {
     constexpr int SIZE = TYPE == ROWS_F32 ? 4 : 2;
-    const uintptr_t at = (uintptr_t)a.logits + (uintptr_t)(row * a.row_stride) * SIZE;
-    return RowView{(const u32x4 *)(at & ~(uintptr_t)15), (int)(at & 15) / SIZE};
+    // (from the pointer, not from an integer: loads through that would be flat ones)
+    const char *const at = (const char *)a.logits + row * a.row_stride * SIZE;
+    const int skip = (int)((uintptr_t)at & 15);
+    return RowView{(const u32x4 *)(at - skip), skip / SIZE};
 }
 template <int TYPE>
 __device__ __forceinline__ void piece_values(u32x4 p, float v[sampled_epb<TYPE>]) {

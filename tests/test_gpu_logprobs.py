@@ -166,3 +166,22 @@ def test_sampled_tokens_and_their_logprobs_agree(llma):
     llma.llma_verify_sampled(x, i(B, 0), torch.empty((B, 0), device="cuda"), torch.zeros(B, device="cuda"), n_acc, nxt, emitted, temperature=torch.zeros(B, device="cuda"))
     got = check(llma, x[:, 0], nxt.cpu().numpy(), None, 1)
     assert (got["rank"] == 0).all() and np.array_equal(got["top_tokens"][:, 0], nxt.cpu().numpy())
+
+
+def test_signalling_nans_and_large_logits(llma):
+    """NaN of either kind in any place; rows far from zero, whose sums are taken with the fp32 value of log2(e) / T or in 64 bits"""
+    rng = np.random.default_rng(10)
+    x = 2 * rng.standard_normal((6, 5000))
+    x[1] += 900
+    x[2] -= 2500
+    x[3] += 4000
+    x[4] *= 300
+    for dtype, nans in (("fp32", [0x7f800001, 0xff800001 - (1 << 32), 0x7fc00000]), ("bf16", [0x7f81, 0xff81 - (1 << 16), 0x7fc0]), ("fp16", [0x7c01, 0xfc01 - (1 << 16), 0x7e00])):
+        t = torch.tensor(x, dtype=torch.float32).to(DT[dtype]).cuda()
+        bits = t.view(torch.int32 if dtype == "fp32" else torch.int16)
+        for k, nan in enumerate(nans):
+            bits[0, k::7] = nan
+            bits[5, [3 + k, 100 + k, 4990 + k]] = nan
+        assert t.isnan().sum() > 2000
+        check(llma, t, [6, 17, 18, 19, 20, 21], None, 9)
+        check(llma, t, [0, 17, 18, 19, 20, 3], [0.8, 0.9, 1.1, 1.0, 1.0, 1.3], 9)
