@@ -540,6 +540,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
 #pragma unroll
                     for (int e = 0; e < 16; ++e) x[e] = sc[n][e % 4][e / 4] * to_log2;
                     if (masked) {
+                        asm volatile("");                        // (a branch, not selections for every page)
                         const int left = (page < 0 ? -1 : limit[n]) - base - 16 * kb;
 #pragma unroll
                         for (int e = 0; e < 16; ++e) x[e] = e > left ? LLMA_NEG_INF : x[e];
@@ -652,6 +653,353 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
     }
 }
 
+#define ROWS_MIN 160
+// ---- many rows -----------------------------------------------------------------------------------
+// fp16 products keep the sums of each block of 32 features in units of a power of two, `now` its exponent plus 127, so that V fits: a code of 0.5 .. 6 times 2^-23 .. 2^12 is exact in fp16.
+// A page whose largest scale of the block lies outside 2^-8 .. 2^12 units makes that the unit, but none more than 2^60 below the largest before it (up to 2^62 units may have been
+// added up, and fp32 ends at 2^128).  So V loses bits below 2^-19 of the largest of the block in its page (and counts as zero from 2^-21 on), or 2^-80 of another page's.
+struct BlockUnit { int now, least; };
+__device__ __forceinline__ void unit_for(int most, BlockUnit &u) {               // most: 0 for none
+    const int near = most > u.least ? most : u.least;
+    const bool other = ((unsigned)(most - u.now + 8) > 20u) & (most > 0);
+    u.now = other ? near : u.now;
+    u.least = u.now - 60 > u.least ? u.now - 60 : u.least;
+}
+template <int T> __device__ __forceinline__ uint32_t widen2_half(uint32_t c, float scale) {
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, T));
+}
+// as widen_v, in fp16 and in units: by[t] for the word's four positions
+__device__ __forceinline__ void widen_word_half(uint32_t w, const float *by, uint32_t (&even)[2], uint32_t (&odd)[2]) {
+    const uint32_t p0 = widen2_half<0>(w, by[0]), p1 = widen2_half<1>(w, by[1]), p2 = widen2_half<2>(w, by[2]), p3 = widen2_half<3>(w, by[3]);
+    even[0] = __builtin_amdgcn_perm(p1, p0, 0x05040100u);
+    odd[0] = __builtin_amdgcn_perm(p1, p0, 0x07060302u);
+    even[1] = __builtin_amdgcn_perm(p3, p2, 0x05040100u);
+    odd[1] = __builtin_amdgcn_perm(p3, p2, 0x07060302u);
+}
+// Prompts: a workgroup takes 64 NT rows of a sequence's key head and all pages they see.  Each page is widened once, for all four waves, into LDS as the operands' images (16 KB of K,
+// 16 KB of V at head_dim 128): wave t has score tile t, and block t of V's features (of two blocks at head_dim 64: half of one's positions).  A page is requested two ahead, widened one
+// ahead, one barrier a page.  The rest is as with 8 bits: a wave holds its rows' queries and sums in registers, pages behind its rows are skipped, the longest row
+// blocks start first, and the reference of the exponentials moves only when a maximum passes it by 2^8.
+template <int DH> constexpr int rows_images = (4 * (DH / 32) + (DH / 16) * 2) * 64;          // 16-byte pieces of a page
+template <int DH, int NT, int TYPE>
+__global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, int blocks) {
+    constexpr bool HALF = TYPE == ROWS_BF16;
+    constexpr float BIAS = HALF ? 7.f : 0.f;
+    constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE, HALF>, STEPS = DH / 32, FB = DH / 32, DT = DH / 16;
+    constexpr int KI = 4 * STEPS, VI = DT * 2;                   // images of K, of V
+    constexpr int US = FB / 2;                                   // operand pairs of V a wave widens (positions 8 u .. of a lane's 16)
+    typedef std::conditional_t<DH == 128, u32x4, u32x2> KBytes;
+    extern __shared__ u32x4 lds[];                               // [2] pages
+    __shared__ int nan_seen[2][4];
+    __shared__ uint32_t units[2];                                // a byte a wave: of the page's images
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, b = rest % a.n_seqs, block = blocks - 1 - rest / a.n_seqs;
+    const int group = a.n_heads / a.c.heads, r0 = block * 64 * NT;
+    const AttendSeq s = uniform(attend_seq(a, b));
+    const int R = s.rows * group, seen = s.seen;
+    if (r0 >= R) return;
+    const int r1 = r0 + 64 * NT < R ? r0 + 64 * NT : R, furthest = seen + (r1 - 1) / group;        // the block's last position
+    const int pages = furthest < 0 ? 0 : furthest / PAGE_POS + 1;
+    const int kb = lane >> 4, col = lane & 15, w0 = r0 + wave * 16 * NT;
+    const int w1 = w0 + 16 * NT < R ? w0 + 16 * NT : R;
+    const int wave_first = w0 < R ? seen + w0 / group : -1, wave_last = w0 < R ? seen + (w1 - 1) / group : -1, block_first = seen + r0 / group;
+    const int vj = FB == 4 ? wave : wave / 2, u0 = FB == 4 ? 0 : wave % 2;       // the wave's block of V, its first operand pair
+    const uint32_t k_off = (4 * col + wave) * (DH / 2) + kb * (DH / 8), ks_off = (kb * FB / 4) * PAGE_POS + 4 * col + wave;
+    const uint32_t v_off = (16 * vj + col) * PAGE_POS + 16 * kb, vs_off = vj * PAGE_POS + 16 * kb;
+    // ---- the wave's queries.  A negative scale turns their signs, so that the largest score is the largest product
+    u32x4 q[NQ][NT][STEPS];
+    const uint32_t turn = a.scale < 0.f ? 0x80008000u : 0u;
+    int limit[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = w0 + 16 * n + col;
+        limit[n] = r < R ? seen + r / group : -1;
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) {
+            float v[8];
+#pragma unroll
+            for (int p = 0; p < NQ; ++p) q[p][n][t] = (u32x4){0, 0, 0, 0};
+            if (r < R) {
+                const int row = s.row0 + r / group, hq = head * group + r % group, d = (DH / 4) * kb + 8 * t;
+                row8<TYPE>(a.q, (int64_t)row * a.q_row + hq * a.q_head + d, v);
+#pragma unroll
+                for (int p = 0; p < NQ; ++p)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const uint32_t x = bf16_pair(v[2 * w], v[2 * w + 1]);
+                        q[p][n][t][w] = x ^ turn;
+                        v[2 * w] -= __uint_as_float(x << 16);
+                        v[2 * w + 1] -= __uint_as_float(x & 0xffff0000u);
+                    }
+            }
+        }
+    }
+    // ---- page numbers, 64 pages a lane at a time: the present 64 and the next
+    const auto pages_from = [&](int i0) {
+        const int i = i0 + lane;
+        int id = -1;
+        if (i < pages) id = a.table[(size_t)s.slot * a.max_blocks + i];
+        return (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
+    };
+    int now = pages_from(0), later = pages_from(64), now_at = 0;           // now_at: the first page of `now`
+    const auto id_of = [&](int i) { return i < now_at + 64 ? __builtin_amdgcn_readlane(now, i - now_at) : __builtin_amdgcn_readlane(later, i - now_at - 64); };
+    // a thread's share of a page
+    KBytes kc;
+    u32x4 vc, vs;
+    uint32_t ks;
+    const auto take = [&](int i) {
+        const int id = id_of(i);
+        const size_t at = (size_t)(id < 0 ? 0 : id) * a.c.heads + head;
+        kc = *(const KBytes *)(a.c.k + at * (PAGE_POS * DH / 2) + k_off);
+        ks = *(a.c.k_scale + at * (FB * PAGE_POS) + ks_off);
+        vc = *(const u32x4 *)(a.c.v + at * (PAGE_POS * DH / 2) + v_off);
+        vs = *(const u32x4 *)(a.c.v_scale + at * (FB * PAGE_POS) + vs_off);
+    };
+    BlockUnit unit{127, 67};                                     // of the wave's block, of the page that was widened last
+    const auto widen = [&](int i) {
+        u32x4 *const to = lds + (i & 1) * rows_images<DH> + lane;
+        const float k_by = __uint_as_float(ks << 23);
+#pragma unroll
+        for (int t = 0; t < STEPS; ++t) to[(wave * STEPS + t) * 64] = widen8(kc[t], k_by);
+        const bool masked = i * PAGE_POS + PAGE_POS - 1 > block_first || id_of(i) < 0;           // positions that some row does not see
+        uint32_t any = 0;
+        if (masked) {
+            const int there = id_of(i) < 0 ? 0 : s.len - i * PAGE_POS - 16 * kb;
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const uint32_t is = vs[w] & bytes_below(there - 4 * w), nan = nan_scales(is);
+                any |= nan;
+                vs[w] = is & ~(nan | (nan - (nan >> 7)));
+            }
+        }
+        any = __ballot(any != 0) != 0;
+        if (lane == 0) nan_seen[i & 1][wave] = (int)any;
+        bool plain = true;                                       // units of 1, and no scale that is not one of them: the scales as they lie
+        if constexpr (HALF) {
+            // (lanes of a group have the same 16 scales: each looks at four.  Bytes above 139; bytes of 119 and more)
+            const uint32_t x = col & 2 ? (col & 1 ? vs[3] : vs[2]) : (col & 1 ? vs[1] : vs[0]), low = x & 0x7f7f7f7fu;
+            plain = unit.now == 127 && __ballot((((low + 0x74747474u) & x) & 0x80808080u) != 0) == 0 && __ballot((((low + 0x09090909u) | x) & 0x80808080u) != 0) != 0;
+        }
+        float half_by[4 * 2 * US];                               // of fp16's positions
+        if constexpr (HALF) {
+            const auto byte_of = [&](int t) { const uint32_t x = FB == 4 ? vs[t / 4] : u0 ? vs[2 + t / 4] : vs[t / 4]; return x >> 8 * (t % 4) & 255u; };
+            if (plain) {
+#pragma unroll
+                for (int h = 0; h < 2 * US; ++h) {
+                    const uint32_t x = FB == 4 ? vs[h] : u0 ? vs[2 + h] : vs[h];
+                    half_by[4 * h] = scale_byte<0>(x);
+                    half_by[4 * h + 1] = scale_byte<1>(x);
+                    half_by[4 * h + 2] = scale_byte<2>(x);
+                    half_by[4 * h + 3] = scale_byte<3>(x);
+                }
+            } else {
+                uint32_t most = 0;
+#pragma unroll
+                for (int w = 0; w < 4; ++w)
+#pragma unroll
+                    for (int t = 0; t < 4; ++t) {
+                        const uint32_t e = vs[w] >> 8 * t & 255u;
+                        most = e > most && e != 255u ? e : most;
+                    }
+                most = max((int)most, lane_xor<16>((int)most));
+                most = max((int)most, lane_xor<32>((int)most));
+                unit_for(uniform((int)most), unit);
+#pragma unroll
+                for (int t = 0; t < 8 * US; ++t) {
+                    const int raw = (int)byte_of(t), e = raw - unit.now + 127;
+                    half_by[t] = __uint_as_float((uint32_t)(raw == 255 ? 255 : e > 0 ? e : 0) << 23);
+                }
+            }
+            if (lane == 0) ((uint8_t *)&units[i & 1])[wave] = (uint8_t)unit.now;
+        }
+#pragma unroll
+        for (int k = 0; k < US; ++k) {
+            const int u = u0 + k;
+            u32x4 even, odd;
+            if constexpr (HALF) {
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const uint32_t c = FB == 4 ? vc[2 * k + h] : u0 ? vc[2 + h] : vc[h];
+                    uint32_t e2[2], o2[2];
+                    widen_word_half(c, half_by + 4 * (2 * k + h), e2, o2);
+                    even[2 * h] = e2[0];
+                    even[2 * h + 1] = e2[1];
+                    odd[2 * h] = o2[0];
+                    odd[2 * h + 1] = o2[1];
+                }
+            } else if constexpr (FB == 4) widen_v(vc, vs, k, even, odd);
+            else {
+                const u32x4 c = u0 ? (u32x4){vc[2], vc[3], 0, 0} : (u32x4){vc[0], vc[1], 0, 0}, x = u0 ? (u32x4){vs[2], vs[3], 0, 0} : (u32x4){vs[0], vs[1], 0, 0};
+                widen_v(c, x, 0, even, odd);
+            }
+            to[(KI + 2 * (2 * vj) + u) * 64] = even;
+            to[(KI + 2 * (2 * vj + 1) + u) * 64] = odd;
+        }
+    };
+    f32x4 o[NT][DT];
+    float m[NT];
+    f32x4 l[NT];                                                 // the rows' sums, by products with ones
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        m[n] = LLMA_NEG_INF;
+        l[n] = (f32x4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int d = 0; d < DT; ++d) o[n][d] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    // (not 0: minus infinity has to stay that)
+    const float by = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1e-37f);
+    if (pages > 0) {
+        take(0);
+        widen(0);
+        if (pages > 1) take(1);
+    }
+    __syncthreads();
+    uint32_t o_units = 0x7f7f7f7fu;                              // that the wave's sums are in
+    for (int i = 0; i < pages; ++i) {
+        if (i + 1 < pages) widen(i + 1);
+        if (i + 2 < pages) take(i + 2);
+        const int base = i * PAGE_POS;
+        if (base <= wave_last) {                                 // (the wave's rows see some of it)
+            // operands come from LDS eight ahead of their products, V's first ones behind K's last
+            const u32x4 *const img = lds + (i & 1) * rows_images<DH> + lane;
+            u32x4 w[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = img[j * 64];
+            const int id = id_of(i);
+            const bool masked = id < 0 || base + PAGE_POS - 1 > wave_first;
+            u32x4 pb[NT][NP][2];
+            f32x4 sc[NT][4];
+            if constexpr (HALF) {
+                const uint32_t page_units = uniform((int)units[i & 1]);
+                if (page_units != o_units) {                     // (exact)
+#pragma unroll
+                    for (int j = 0; j < FB; ++j) {
+                        const int to = (int)(o_units >> 32 / FB * j & 255u) - (int)(page_units >> 32 / FB * j & 255u);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            o[n][2 * j] = times_pow2(o[n][2 * j], to);
+                            o[n][2 * j + 1] = times_pow2(o[n][2 * j + 1], to);
+                        }
+                    }
+                    o_units = page_units;
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n)
+#pragma unroll
+                for (int t = 0; t < 4; ++t) sc[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int j = 0; j < KI; ++j) {
+                const int t = j / STEPS, st = j % STEPS;
+#pragma unroll
+                for (int p = NQ - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) sc[n][t] = mfma16x16x32(w[j % 8], q[p][n][st], sc[n][t]);
+                w[j % 8] = img[(j + 8) * 64];
+                __builtin_amdgcn_sched_group_barrier(0x008, NT * NQ, 0);       // (products, then a load: as written)
+                __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            }
+            __builtin_amdgcn_s_setprio(0);
+            // position e of the lane's 16: tile e % 4, register e / 4
+            if (masked) {
+                asm volatile("");                                // (a branch: as selections this would cost every page 32 comparisons a tile)
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    const int left = (id < 0 ? -1 : limit[n]) - base - 16 * kb;
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) sc[n][e % 4][e / 4] = e > left ? LLMA_NEG_INF : sc[n][e % 4][e / 4];
+                }
+            }
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                float top = LLMA_NEG_INF;
+#pragma unroll
+                for (int t = 0; t < 4; ++t)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) top = fmaxf(top, sc[n][t][r]);
+                top = fmaxf(top, lane_xor<16>(top));
+                top = fmaxf(top, lane_xor<32>(top)) * by;
+                if (__ballot(top > m[n] + (8.f + BIAS)) != 0) {
+                    const float mn = fmaxf(m[n], top - BIAS), keep = __builtin_amdgcn_exp2f(m[n] - (mn == LLMA_NEG_INF ? 0.f : mn));
+                    m[n] = mn;
+                    l[n] *= keep;
+#pragma unroll
+                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+                }
+                const float ref = m[n] == LLMA_NEG_INF ? 0.f : m[n];
+#pragma unroll
+                for (int u = 0; u < 2; ++u)
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) {
+                        const int r = 2 * u + w / 2, t = 2 * (w & 1);
+                        float y = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][t][r], by, -ref)), z = __builtin_amdgcn_exp2f(__builtin_fmaf(sc[n][t + 1][r], by, -ref));
+#pragma unroll
+                        for (int p = 0; p < NP; ++p) {
+                            pb[n][p][u][w] = HALF ? half_pair(y, z) : bf16_pair(y, z);
+                            if (p + 1 < NP) { y -= __uint_as_float(pb[n][p][u][w] << 16); z -= __uint_as_float(pb[n][p][u][w] & 0xffff0000u); }
+                        }
+                    }
+            }
+            // (taken out of the image where the block's first row does not see all of the page: also for waves whose rows all do)
+            if (base + PAGE_POS - 1 > block_first && (nan_seen[i & 1][0] | nan_seen[i & 1][1] | nan_seen[i & 1][2] | nan_seen[i & 1][3])) {
+                u32x4 nans[FB];
+                const size_t at = (size_t)(id < 0 ? 0 : id) * a.c.heads + head;
+                const int there = id < 0 ? 0 : s.len - base - 16 * kb;
+#pragma unroll
+                for (int j = 0; j < FB; ++j) {
+                    nans[j] = *(const u32x4 *)(a.c.v_scale + (at * FB + j) * PAGE_POS + 16 * kb);
+#pragma unroll
+                    for (int w = 0; w < 4; ++w) nans[j][w] = nan_scales(nans[j][w] & bytes_below(there - 4 * w));
+                }
+                attend_mx_nans<DH, NT>(nans, base, limit, o);
+            }
+            __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n)
+                        l[n] = HALF ? mfma16x16x32_half((u32x4){0x3c003c00u, 0x3c003c00u, 0x3c003c00u, 0x3c003c00u}, pb[n][p][u], l[n])
+                                    : mfma16x16x32((u32x4){0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u}, pb[n][p][u], l[n]);
+#pragma unroll
+            for (int j = 0; j < VI; ++j) {
+                const int d = j / 2, u = j % 2;
+#pragma unroll
+                for (int p = NP - 1; p >= 0; --p)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) o[n][d] = HALF ? mfma16x16x32_half(w[(KI + j) % 8], pb[n][p][u], o[n][d]) : mfma16x16x32(w[(KI + j) % 8], pb[n][p][u], o[n][d]);
+                if (j + 8 < VI) {
+                    w[(KI + j) % 8] = img[(KI + j + 8) * 64];
+                    __builtin_amdgcn_sched_group_barrier(0x008, NT * NP, 0);
+                    __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+                }
+            }
+        }
+        __builtin_amdgcn_s_setprio(0);
+        if (i + 1 == now_at + 64) {
+            now = later;
+            now_at += 64;
+            later = pages_from(now_at + 64);
+        }
+        __syncthreads();
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const int r = w0 + 16 * n + col;
+        if (r >= R) continue;
+        const float inv = l[n][0] == 0.f ? 0.f : 1.f / l[n][0];
+#pragma unroll
+        for (int j = 0; j < FB; ++j)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const f32x4 v = (f32x4){o[n][2 * j][2 * h], o[n][2 * j + 1][2 * h], o[n][2 * j][2 * h + 1], o[n][2 * j + 1][2 * h + 1]} * inv;
+                attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 32 * j + 8 * kb + 4 * h, HALF ? times_pow2(v, (int)(o_units >> 32 / FB * j & 255u) - 127) : v);
+            }
+    }
+}
+
 template <int DH, int NT, int TYPE>
 static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStream_t st) {
     const size_t bytes = (size_t)attend_mx_lds<DH, NT, TYPE> + (size_t)(a.n_seqs + 1) * 4;
@@ -660,8 +1008,22 @@ static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStre
 static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
     return attend_plan(n_seqs, max_blocks, n_heads, kv_heads, dh / 2 + dh / 32, max_rows);
 }
+// row blocks of a call, at most: what blocks of 64 nt rows make of max_rows everywhere, or of all rows and a remainder per sequence
+static int64_t attend_row_blocks(const AttendMxArgs &a, int nt) {
+    const int64_t group = a.n_heads / a.c.heads, rows = 64 * nt;
+    const int64_t by_max = a.n_seqs * ((a.max_rows * group + rows - 1) / rows), by_all = a.n_rows * group / rows + a.n_seqs;
+    return (by_max < by_all ? by_max : by_all) * a.c.heads;
+}
+template <int DH, int NT, int TYPE>
+static void launch_attend_rows(const AttendMxArgs &a, hipStream_t st) {
+    const int group = a.n_heads / a.c.heads, blocks = (a.max_rows * group + 64 * NT - 1) / (64 * NT);
+    hipLaunchKernelGGL((attend_mx_rows_kernel<DH, NT, TYPE>), dim3((unsigned)blocks * a.n_seqs * a.c.heads), dim3(256), 2 * rows_images<DH> * 16, st, a, blocks);
+}
 template <int DH, int TYPE>
 static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
+    constexpr int ROWS_NT = TYPE == ROWS_F32 ? 1 : 2;            // (three planes of queries and probabilities leave room for one tile)
+    const int64_t group_rows = (int64_t)a.max_rows * (a.n_heads / a.c.heads), launched = (group_rows + 64 * ROWS_NT - 1) / (64 * ROWS_NT) * a.n_seqs * a.c.heads;
+    if (group_rows > 64 && attend_row_blocks(a, ROWS_NT) >= ROWS_MIN && launched < 1 << 23) return launch_attend_rows<DH, ROWS_NT, TYPE>(a, st);
     const AttendPlan p = attend_mx_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, DH, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
