@@ -406,7 +406,9 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
     const int64_t from = plan.whole ? 0 : (int64_t)share * per;
     if (from >= total) return;
     const int p0 = (int)from, p1 = p0 + per < total ? p0 + per : total;
-    const float to_log2 = a.scale * 1.44269504088896340736f;
+    // (not 0: minus infinity has to stay that.  A negative scale turns the queries' signs, so that the largest score is the largest product)
+    const float by = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1e-37f);
+    const uint32_t turn = a.scale < 0.f ? TYPE == ROWS_F32 ? 0x80000000u : 0x80008000u : 0u;
     const int kb = lane >> 4, col = lane & 15;
     const uint32_t k_off = 4 * col * (DH / 2) + kb * (DH / 8), ks_off = (kb * FB / 4) * PAGE_POS + 4 * col, v_off = col * PAGE_POS + 16 * kb;
 
@@ -461,6 +463,10 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
     }
     while (seg.last > 0) {
         const AttendSeq s = seg.s;
+#pragma unroll
+        for (int u = 0; u < (PIECES + 255) / 256; ++u)
+#pragma unroll
+            for (int h = 0; h < (TYPE == ROWS_F32 ? 2 : 1); ++h) qr.raw[u][h] ^= turn;
         __syncthreads();
         attend_put_q<DH, NT, NQ, TYPE>(qr, q);
         __syncthreads();
@@ -538,7 +544,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
                 for (int n = 0; n < NT; ++n) {
                     float x[16], top = LLMA_NEG_INF;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) x[e] = sc[n][e % 4][e / 4] * to_log2;
+                    for (int e = 0; e < 16; ++e) x[e] = sc[n][e % 4][e / 4];
                     if (masked) {
                         asm volatile("");                        // (a branch, not selections for every page)
                         const int left = (page < 0 ? -1 : limit[n]) - base - 16 * kb;
@@ -548,16 +554,19 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
 #pragma unroll
                     for (int e = 0; e < 16; ++e) top = fmaxf(top, x[e]);
                     top = fmaxf(top, lane_xor<16>(top));
-                    top = fmaxf(top, lane_xor<32>(top));
-                    const float mn = fmaxf(m[n], top), ref = mn == LLMA_NEG_INF ? 0.f : mn;
-                    const float keep = __builtin_amdgcn_exp2f(m[n] - ref);
-                    m[n] = mn;
-                    l[n] *= keep;
+                    top = fmaxf(top, lane_xor<32>(top)) * by;
+                    // the reference of the exponentials moves only when a maximum passes it by 2^8: once or twice a sequence instead of the sums' 32 products a page
+                    if (__ballot(top > m[n] + 8.f) != 0) {
+                        const float mn = fmaxf(m[n], top), keep = __builtin_amdgcn_exp2f(m[n] - (mn == LLMA_NEG_INF ? 0.f : mn));
+                        m[n] = mn;
+                        l[n] *= keep;
 #pragma unroll
-                    for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+                        for (int d = 0; d < DT; ++d) o[n][d] *= keep;
+                    }
+                    const float ref = m[n] == LLMA_NEG_INF ? 0.f : m[n];
 #pragma unroll
                     for (int e = 0; e < 16; ++e) {
-                        x[e] = __builtin_amdgcn_exp2f(x[e] - ref);
+                        x[e] = __builtin_amdgcn_exp2f(__builtin_fmaf(x[e], by, -ref));
                         l[n] += x[e];
                     }
 #pragma unroll
