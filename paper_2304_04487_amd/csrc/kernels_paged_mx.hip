@@ -527,6 +527,7 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
                 u32x4 nans[FB];
                 uint32_t any = 0;
                 if (masked) {
+                    asm volatile("");                            // (a branch, not 150 selections for every page)
                     const int there = page < 0 ? 0 : s.len - base - 16 * kb;       // of the lane's 16 positions of V
                     // what lies behind the last position may be anything, and a NaN that only later rows see must not reach the others through 0 * NaN
 #pragma unroll
@@ -662,7 +663,6 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
     }
 }
 
-#define ROWS_MIN 160
 // ---- many rows -----------------------------------------------------------------------------------
 // fp16 products keep the sums of each block of 32 features in units of a power of two, `now` its exponent plus 127, so that V fits: a code of 0.5 .. 6 times 2^-23 .. 2^12 is exact in fp16.
 // A page whose largest scale of the block lies outside 2^-8 .. 2^12 units makes that the unit, but none more than 2^60 below the largest before it (up to 2^62 units may have been
@@ -685,13 +685,31 @@ __device__ __forceinline__ void widen_word_half(uint32_t w, const float *by, uin
     even[1] = __builtin_amdgcn_perm(p3, p2, 0x05040100u);
     odd[1] = __builtin_amdgcn_perm(p3, p2, 0x07060302u);
 }
-// Prompts: a workgroup takes 64 NT rows of a sequence's key head and all pages they see.  Each page is widened once, for all four waves, into LDS as the operands' images (16 KB of K,
+// The blocks of 64 NT rows of all sequences, each with the pages that it sees, lie end to end as a list of pages, per key head; equal shares of the list go to two workgroups per
+// compute unit.  A block that lies in one share is finished there, the others' parts are joined by attend_mx_rows_join_kernel.  (Where there are many blocks a workgroup takes one,
+// the longest first.)
+struct RowsPlan { int blocks, shares; };                         // blocks: of the call's longest sequence; shares per key head, 0: a workgroup per block
+#define ROWS_LISTED 2048         // blocks of a list, of which every workgroup makes the sums
+#define ROWS_MIN_PAGES 8         // of a share
+static RowsPlan rows_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows, int rows) {
+    RowsPlan p;
+    p.blocks = (int)(((int64_t)max_rows * (n_heads / kv_heads) + rows - 1) / rows);
+    const int64_t listed = (int64_t)p.blocks * n_seqs, pages = listed * max_blocks, most = (pages + ROWS_MIN_PAGES - 1) / ROWS_MIN_PAGES;
+    int64_t shares = 2 * ATTEND_CUS / kv_heads;
+    shares = shares < 1 ? 1 : shares;
+    p.shares = listed > ROWS_LISTED ? 0 : (int)(shares < most ? shares : most);
+    return p;
+}
+// work: [pages before every block of the list, rounded up to 64 ints][parts' O][parts' m][parts' l]
+__host__ __device__ static inline int64_t rows_head(const RowsPlan &p, int n_seqs) { return ((int64_t)p.blocks * n_seqs + 1 + 63) / 64 * 64; }
+__host__ __device__ static inline int64_t rows_parts(const RowsPlan &p, int kv_heads) { return (int64_t)p.shares * 2 * kv_heads; }
+// Prompts: a workgroup takes 64 NT rows of a sequence's key head and pages that they see.  Each page is widened once, for all four waves, into LDS as the operands' images (16 KB of K,
 // 16 KB of V at head_dim 128): wave t has score tile t, and block t of V's features (of two blocks at head_dim 64: half of one's positions).  A page is requested two ahead, widened one
-// ahead, one barrier a page.  The rest is as with 8 bits: a wave holds its rows' queries and sums in registers, pages behind its rows are skipped, the longest row
-// blocks start first, and the reference of the exponentials moves only when a maximum passes it by 2^8.
+// ahead, one barrier a page.  The rest is as with 8 bits: a wave holds its rows' queries and sums in registers, pages behind its rows are skipped, and the
+// reference of the exponentials moves only when a maximum passes it by 2^8.
 template <int DH> constexpr int rows_images = (4 * (DH / 32) + (DH / 16) * 2) * 64;          // 16-byte pieces of a page
 template <int DH, int NT, int TYPE>
-__global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, int blocks) {
+__global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, RowsPlan plan) {
     constexpr bool HALF = TYPE == ROWS_BF16;
     constexpr float BIAS = HALF ? 7.f : 0.f;
     constexpr int NQ = attend_nq<TYPE>, NP = attend_np<TYPE, HALF>, STEPS = DH / 32, FB = DH / 32, DT = DH / 16;
@@ -702,13 +720,49 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
     __shared__ int nan_seen[2][4];
     __shared__ uint32_t units[2];                                // a byte a wave: of the page's images
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, b = rest % a.n_seqs, block = blocks - 1 - rest / a.n_seqs;
-    const int group = a.n_heads / a.c.heads, r0 = block * 64 * NT;
+    __shared__ int part[4];
+    int *const starts = (int *)(lds + 2 * rows_images<DH>);      // pages before every block of the list, and of all
+    const int head = blockIdx.x % a.c.heads, rest = blockIdx.x / a.c.heads, group = a.n_heads / a.c.heads;
+    const int listed = plan.shares > 0 ? plan.blocks * a.n_seqs : 1;
+    // pages that a block sees; one for a block that sees nothing (its rows become 0), none for one that is not there
+    const auto pages_of = [&](const AttendSeq &s, int r0) {
+        const int R = s.rows * group, r1 = r0 + 64 * NT < R ? r0 + 64 * NT : R, furthest = s.seen + (r1 - 1) / group;
+        return r0 >= R ? 0 : furthest < 0 ? 1 : furthest / PAGE_POS + 1;
+    };
+    int from = 0, to, g;                                         // pages of the list, the block that the first is in
+    if (plan.shares > 0) {
+        int total = 0;
+        for (int g0 = 0; g0 < listed; g0 += 256) {
+            const int i = g0 + threadIdx.x;
+            int sum, pages = 0;
+            if (i < listed) pages = pages_of(attend_seq(a, i / plan.blocks), i % plan.blocks * 64 * NT);
+            const int at = block_scan<4>(pages, part, &sum);
+            if (i < listed) starts[i] = total + at;
+            total += sum;
+        }
+        if (threadIdx.x == 0) starts[listed] = total;
+        __syncthreads();
+        if (blockIdx.x == 0)                                     // (for attend_mx_rows_join_kernel)
+            for (int i = threadIdx.x; i <= listed; i += 256) ((int *)a.work)[i] = starts[i];
+        total = uniform(total);
+        int per = (total + plan.shares - 1) / plan.shares;
+        per = per < ROWS_MIN_PAGES ? ROWS_MIN_PAGES : per;
+        if ((int64_t)rest * per >= total) return;
+        from = rest * per;
+        to = from + per < total ? from + per : total;
+        g = uniform(count_le(starts, listed + 1, from) - 1);
+    } else {
+        g = (plan.blocks - 1 - rest / a.n_seqs) + rest % a.n_seqs * plan.blocks;
+        to = pages_of(uniform(attend_seq(a, g / plan.blocks)), g % plan.blocks * 64 * NT);
+    }
+  for (; from < to; ++g) {
+    const int b = g / plan.blocks, r0 = g % plan.blocks * 64 * NT;
     const AttendSeq s = uniform(attend_seq(a, b));
     const int R = s.rows * group, seen = s.seen;
-    if (r0 >= R) return;
-    const int r1 = r0 + 64 * NT < R ? r0 + 64 * NT : R, furthest = seen + (r1 - 1) / group;        // the block's last position
-    const int pages = furthest < 0 ? 0 : furthest / PAGE_POS + 1;
+    const int begin = plan.shares > 0 ? uniform(starts[g]) : 0, all_pages = plan.shares > 0 ? uniform(starts[g + 1]) - begin : to;
+    const int p_first = from - begin, pages = to - begin < all_pages ? to - begin : all_pages;       // the block's pages here: p_first .. pages - 1
+    if (p_first >= pages) continue;
+    from = begin + pages;
     const int kb = lane >> 4, col = lane & 15, w0 = r0 + wave * 16 * NT;
     const int w1 = w0 + 16 * NT < R ? w0 + 16 * NT : R;
     const int wave_first = w0 < R ? seen + w0 / group : -1, wave_last = w0 < R ? seen + (w1 - 1) / group : -1, block_first = seen + r0 / group;
@@ -747,10 +801,10 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
     const auto pages_from = [&](int i0) {
         const int i = i0 + lane;
         int id = -1;
-        if (i < pages) id = a.table[(size_t)s.slot * a.max_blocks + i];
+        if (i < pages && i * PAGE_POS < s.len) id = a.table[(size_t)s.slot * a.max_blocks + i];      // (a sequence without positions may be one without a slot)
         return (unsigned)id < (unsigned)a.c.n_pages ? id : -1;
     };
-    int now = pages_from(0), later = pages_from(64), now_at = 0;           // now_at: the first page of `now`
+    int now = pages_from(p_first), later = pages_from(p_first + 64), now_at = p_first;           // now_at: the first page of `now`
     const auto id_of = [&](int i) { return i < now_at + 64 ? __builtin_amdgcn_readlane(now, i - now_at) : __builtin_amdgcn_readlane(later, i - now_at - 64); };
     // a thread's share of a page
     KBytes kc;
@@ -773,6 +827,7 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
         const bool masked = i * PAGE_POS + PAGE_POS - 1 > block_first || id_of(i) < 0;           // positions that some row does not see
         uint32_t any = 0;
         if (masked) {
+            asm volatile("");
             const int there = id_of(i) < 0 ? 0 : s.len - i * PAGE_POS - 16 * kb;
 #pragma unroll
             for (int w = 0; w < 4; ++w) {
@@ -857,14 +912,12 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
     }
     // (not 0: minus infinity has to stay that)
     const float by = fmaxf(fabsf(a.scale) * 1.44269504088896340736f, 1e-37f);
-    if (pages > 0) {
-        take(0);
-        widen(0);
-        if (pages > 1) take(1);
-    }
+    take(p_first);
+    widen(p_first);
+    if (p_first + 1 < pages) take(p_first + 1);
     __syncthreads();
     uint32_t o_units = 0x7f7f7f7fu;                              // that the wave's sums are in
-    for (int i = 0; i < pages; ++i) {
+    for (int i = p_first; i < pages; ++i) {
         if (i + 1 < pages) widen(i + 1);
         if (i + 2 < pages) take(i + 2);
         const int base = i * PAGE_POS;
@@ -994,18 +1047,73 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
         }
         __syncthreads();
     }
+    const bool whole = p_first == 0 && pages == all_pages;
+    // the part's place: a share has at most one block that began before it (0) and one that goes on behind it (1)
+    const int64_t at = (((int64_t)rest * 2 + (p_first == 0)) * a.c.heads + head) * (64 * NT) + wave * 16 * NT;
+    float *const po = (float *)a.work + rows_head(plan, a.n_seqs), *const pm = po + rows_parts(plan, a.c.heads) * 64 * NT * DH, *const pl = pm + rows_parts(plan, a.c.heads) * 64 * NT;
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
         const int r = w0 + 16 * n + col;
         if (r >= R) continue;
-        const float inv = l[n][0] == 0.f ? 0.f : 1.f / l[n][0];
+        const float inv = !whole ? 1.f : l[n][0] == 0.f ? 0.f : 1.f / l[n][0];
+        if (!whole && kb == 0) {
+            pm[at + 16 * n + col] = m[n];
+            pl[at + 16 * n + col] = l[n][0];
+        }
 #pragma unroll
         for (int j = 0; j < FB; ++j)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const f32x4 v = (f32x4){o[n][2 * j][2 * h], o[n][2 * j + 1][2 * h], o[n][2 * j][2 * h + 1], o[n][2 * j + 1][2 * h + 1]} * inv;
-                attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, 32 * j + 8 * kb + 4 * h, HALF ? times_pow2(v, (int)(o_units >> 32 / FB * j & 255u) - 127) : v);
+                f32x4 v = (f32x4){o[n][2 * j][2 * h], o[n][2 * j + 1][2 * h], o[n][2 * j][2 * h + 1], o[n][2 * j + 1][2 * h + 1]} * inv;
+                if constexpr (HALF) v = times_pow2(v, (int)(o_units >> 32 / FB * j & 255u) - 127);
+                const int d = 32 * j + 8 * kb + 4 * h;
+                if (whole) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, d, v);
+                else *(f32x4 *)(po + (at + 16 * n + col) * DH + d) = v;
             }
+    }
+  }
+}
+// rows of blocks that lie in several shares, 32 a workgroup; a thread has four features of several rows, whose parts are requested together
+#define JOIN_ROWS 32
+template <int DH, int TYPE>
+__global__ __launch_bounds__(256) void attend_mx_rows_join_kernel(AttendMxArgs a, RowsPlan plan, int rows) {
+    constexpr int LANES = DH / 4, EACH = JOIN_ROWS * LANES / 256;
+    const int group = a.n_heads / a.c.heads, b = blockIdx.z, head = blockIdx.y, r0 = blockIdx.x * JOIN_ROWS, block = r0 / rows;
+    const int *const starts = (const int *)a.work;
+    const int g = b * plan.blocks + block, total = starts[plan.blocks * a.n_seqs], p0 = starts[g], p1 = starts[g + 1];
+    int per = (total + plan.shares - 1) / plan.shares;
+    per = per < ROWS_MIN_PAGES ? ROWS_MIN_PAGES : per;
+    const int s0 = p0 / per, s1 = (p1 - 1) / per;
+    if (p0 >= p1 || s0 == s1) return;
+    const AttendSeq s = attend_seq(a, b);
+    const float *const po = (const float *)a.work + rows_head(plan, a.n_seqs), *const pm = po + rows_parts(plan, a.c.heads) * rows * DH, *const pl = pm + rows_parts(plan, a.c.heads) * rows;
+    const auto place = [&](int sh) { return (((int64_t)sh * 2 + (sh == s0)) * a.c.heads + head) * rows + r0 % rows; };
+    const int d = threadIdx.x % LANES * 4, at = threadIdx.x / LANES;
+    float m[EACH], l[EACH];
+    f32x4 o[EACH];
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        m[k] = LLMA_NEG_INF;
+        l[k] = 0.f;
+        o[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
+    }
+    // (rows behind the sequence's last have a place too: what lies there is read and not used)
+    for (int sh = s0; sh <= s1; ++sh)
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) m[k] = fmaxf(m[k], pm[place(sh) + at + k * (JOIN_ROWS / EACH)]);
+#pragma unroll 2
+    for (int sh = s0; sh <= s1; ++sh)
+#pragma unroll
+        for (int k = 0; k < EACH; ++k) {
+            const int64_t i = place(sh) + at + k * (JOIN_ROWS / EACH);
+            const float f = __builtin_amdgcn_exp2f(pm[i] - (m[k] == LLMA_NEG_INF ? 0.f : m[k]));
+            l[k] += pl[i] * f;
+            o[k] += *(const f32x4 *)(po + i * DH + d) * f;
+        }
+#pragma unroll
+    for (int k = 0; k < EACH; ++k) {
+        const int r = r0 + at + k * (JOIN_ROWS / EACH);
+        if (r < s.rows * group) attend_store<TYPE>(a, s.row0 + r / group, head * group + r % group, d, o[k] * (l[k] == 0.f ? 0.f : 1.f / l[k]));
     }
 }
 
@@ -1017,22 +1125,24 @@ static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStre
 static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
     return attend_plan(n_seqs, max_blocks, n_heads, kv_heads, dh / 2 + dh / 32, max_rows);
 }
-// row blocks of a call, at most: what blocks of 64 nt rows make of max_rows everywhere, or of all rows and a remainder per sequence
-static int64_t attend_row_blocks(const AttendMxArgs &a, int nt) {
-    const int64_t group = a.n_heads / a.c.heads, rows = 64 * nt;
-    const int64_t by_max = a.n_seqs * ((a.max_rows * group + rows - 1) / rows), by_all = a.n_rows * group / rows + a.n_seqs;
-    return (by_max < by_all ? by_max : by_all) * a.c.heads;
-}
 template <int DH, int NT, int TYPE>
 static void launch_attend_rows(const AttendMxArgs &a, hipStream_t st) {
-    const int group = a.n_heads / a.c.heads, blocks = (a.max_rows * group + 64 * NT - 1) / (64 * NT);
-    hipLaunchKernelGGL((attend_mx_rows_kernel<DH, NT, TYPE>), dim3((unsigned)blocks * a.n_seqs * a.c.heads), dim3(256), 2 * rows_images<DH> * 16, st, a, blocks);
+    const RowsPlan p = rows_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows, 64 * NT);
+    const unsigned grid = p.shares > 0 ? (unsigned)p.shares * a.c.heads : (unsigned)p.blocks * a.n_seqs * a.c.heads;
+    const size_t bytes = 2 * rows_images<DH> * 16 + (p.shares > 0 ? ((size_t)p.blocks * a.n_seqs + 1) * 4 : 0);
+    hipLaunchKernelGGL((attend_mx_rows_kernel<DH, NT, TYPE>), dim3(grid), dim3(256), bytes, st, a, p);
+    if (p.shares > 1)
+        hipLaunchKernelGGL((attend_mx_rows_join_kernel<DH, TYPE>), dim3((unsigned)p.blocks * (64 * NT / JOIN_ROWS), a.c.heads, a.n_seqs), dim3(256), 0, st, a, p, 64 * NT);
+}
+template <int TYPE> constexpr int rows_nt = TYPE == ROWS_F32 ? 1 : 2;             // (three planes of queries and probabilities leave room for one tile)
+// which calls take the many-rows form
+static bool takes_rows(int n_seqs, int n_heads, int kv_heads, int max_rows, int rows) {
+    const int64_t group_rows = (int64_t)max_rows * (n_heads / kv_heads);
+    return group_rows > 64 && (group_rows + rows - 1) / rows * n_seqs * kv_heads < 1 << 23;
 }
 template <int DH, int TYPE>
 static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
-    constexpr int ROWS_NT = TYPE == ROWS_F32 ? 1 : 2;            // (three planes of queries and probabilities leave room for one tile)
-    const int64_t group_rows = (int64_t)a.max_rows * (a.n_heads / a.c.heads), launched = (group_rows + 64 * ROWS_NT - 1) / (64 * ROWS_NT) * a.n_seqs * a.c.heads;
-    if (group_rows > 64 && attend_row_blocks(a, ROWS_NT) >= ROWS_MIN && launched < 1 << 23) return launch_attend_rows<DH, ROWS_NT, TYPE>(a, st);
+    if (takes_rows(a.n_seqs, a.n_heads, a.c.heads, a.max_rows, 64 * rows_nt<TYPE>)) return launch_attend_rows<DH, rows_nt<TYPE>, TYPE>(a, st);
     const AttendPlan p = attend_mx_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, DH, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
@@ -1042,7 +1152,14 @@ static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
         hipLaunchKernelGGL((attend_join_kernel<DH, TYPE, AttendMxArgs>), dim3((a.max_rows * (a.n_heads / a.c.heads) + 3) / 4, a.c.heads, a.n_seqs), dim3(256), 0, st, a, p);
 }
 int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
-    return attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, dh, max_rows), n_seqs, kv_heads, dh);
+    int64_t most = attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, dh, max_rows), n_seqs, kv_heads, dh);
+    for (int rows = 64; rows <= 128; rows += 64) {               // (fp32's row blocks, the others')
+        if (!takes_rows(n_seqs, n_heads, kv_heads, max_rows, rows)) continue;
+        const RowsPlan p = rows_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows, rows);
+        const int64_t bytes = p.shares > 0 ? (rows_head(p, n_seqs) + rows_parts(p, kv_heads) * rows * (dh + 2)) * 4 : 0;
+        most = bytes > most ? bytes : most;
+    }
+    return most;
 }
 void launch_attend_paged_mx(const AttendMxArgs &a, hipStream_t st) {
     if (a.n_seqs < 1 || a.n_rows < 1 || a.max_rows < 1) return;

@@ -492,3 +492,36 @@ def test_rows_read_go_into_a_context(llma):
         dumps.append(ctx.logits(4).copy())
         ctx.close()
     assert np.array_equal(dumps[0], dumps[1])
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("lens,rows,heads,kv,D", [
+    ([5000], [70], 2, 1, 64), ([3000, 1, 0, 900], [130, 1, 0, 300], 4, 2, 128), ([64 * 9 + 1], [200], 40, 40, 64), ([2000, 1999, 40], [129, 65, 90], 3, 1, 128)])
+def test_attend_blocks_of_rows_in_several_shares(llma, dtype, lens, rows, heads, kv, D):
+    """row blocks cut between workgroups: in the middle of a page list, over several of them, next to empty sequences and short ones"""
+    c, q, table, slots, off = attend_case(llma, lens, rows, heads, kv, D, dtype, 91, n_slots=len(lens) + 2, spare_rows=1)
+    check_attend(llma, c, q, table, slots, lens, off, max(rows), dtype)
+
+
+@pytest.mark.parametrize("rows", [3, 100])
+def test_attend_slots_that_do_not_exist(llma, rows):
+    """sequences whose slot is none see nothing: zeros; the others are as without them"""
+    c, q, table, slots, off = attend_case(llma, [200, 200, 200], [rows] * 3, 4, 2, 64, "bf16", 95)
+    args = (i32([200, 200, 200]), i32(off), rows, 0.125)
+    clean = llma.llma_attend_paged_mx(c, q, i32(table), *args, torch.empty_like(q), slots=i32(slots))
+    for bad in (-1, 3, 2 ** 31 - 1, -2 ** 31):
+        got = llma.llma_attend_paged_mx(c, q, i32(table), *args, torch.full_like(q, 7.0), slots=i32([slots[0], bad, slots[2]]))
+        assert not got[rows:2 * rows].any()
+        assert torch.equal(got[:rows], clean[:rows]) or (got[:rows].float() - clean[:rows].float()).abs().max() <= 2.0 ** -6 * clean.float().abs().max()      # (cut elsewhere)
+        assert (got[2 * rows:].float() - clean[2 * rows:].float()).abs().max() <= 2.0 ** -6 * clean.float().abs().max()
+
+
+def test_attend_more_blocks_of_rows_than_a_list_holds(llma):
+    """thousands of row blocks: a workgroup each"""
+    B = 700
+    rng = np.random.default_rng(97)
+    lens = [int(x) for x in rng.integers(1, 200, B)]
+    rows = [int(min(n, r)) for n, r in zip(lens, rng.integers(1, 140, B))]
+    rows[3], lens[3] = 390, 400
+    c, q, table, slots, off = attend_case(llma, lens, rows, 2, 2, 64, "bf16", 98)
+    check_attend(llma, c, q, table, slots, lens, off, max(rows), "bf16")
