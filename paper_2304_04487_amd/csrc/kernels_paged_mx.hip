@@ -690,14 +690,15 @@ __device__ __forceinline__ void widen_word_half(uint32_t w, const float *by, uin
 // the longest first.)
 struct RowsPlan { int blocks, shares; };                         // blocks: of the call's longest sequence; shares per key head, 0: a workgroup per block
 #define ROWS_LISTED 2048         // blocks of a list, of which every workgroup makes the sums
-#define ROWS_MIN_PAGES 8         // of a share
+#define ROWS_MIN_PAGES 4         // of a share
 static RowsPlan rows_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows, int rows) {
     RowsPlan p;
     p.blocks = (int)(((int64_t)max_rows * (n_heads / kv_heads) + rows - 1) / rows);
     const int64_t listed = (int64_t)p.blocks * n_seqs, pages = listed * max_blocks, most = (pages + ROWS_MIN_PAGES - 1) / ROWS_MIN_PAGES;
     int64_t shares = 2 * ATTEND_CUS / kv_heads;
     shares = shares < 1 ? 1 : shares;
-    p.shares = listed > ROWS_LISTED ? 0 : (int)(shares < most ? shares : most);
+    const bool small = max_blocks <= 8 && listed * kv_heads >= 128;      // (blocks enough, and so short that a share's several starts cost more than an uneven end)
+    p.shares = listed > ROWS_LISTED || small ? 0 : (int)(shares < most ? shares : most);
     return p;
 }
 // work: [pages before every block of the list, rounded up to 64 ints][parts' O][parts' m][parts' l]
@@ -1073,11 +1074,10 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
     }
   }
 }
-// rows of blocks that lie in several shares, 32 a workgroup; a thread has four features of several rows, whose parts are requested together
-#define JOIN_ROWS 32
-template <int DH, int TYPE>
+// rows of blocks that lie in several shares, JOIN_ROWS a workgroup; a thread has four features of several rows, whose parts are requested together, or of one row whose many parts are
+template <int DH, int TYPE, int JOIN_ROWS>
 __global__ __launch_bounds__(256) void attend_mx_rows_join_kernel(AttendMxArgs a, RowsPlan plan, int rows) {
-    constexpr int LANES = DH / 4, EACH = JOIN_ROWS * LANES / 256;
+    constexpr int LANES = DH / 4, EACH = JOIN_ROWS * LANES / 256, AHEAD = EACH == 1 ? 8 : 2;
     const int group = a.n_heads / a.c.heads, b = blockIdx.z, head = blockIdx.y, r0 = blockIdx.x * JOIN_ROWS, block = r0 / rows;
     const int *const starts = (const int *)a.work;
     const int g = b * plan.blocks + block, total = starts[plan.blocks * a.n_seqs], p0 = starts[g], p1 = starts[g + 1];
@@ -1098,10 +1098,11 @@ __global__ __launch_bounds__(256) void attend_mx_rows_join_kernel(AttendMxArgs a
         o[k] = (f32x4){0.f, 0.f, 0.f, 0.f};
     }
     // (rows behind the sequence's last have a place too: what lies there is read and not used)
+#pragma unroll AHEAD
     for (int sh = s0; sh <= s1; ++sh)
 #pragma unroll
         for (int k = 0; k < EACH; ++k) m[k] = fmaxf(m[k], pm[place(sh) + at + k * (JOIN_ROWS / EACH)]);
-#pragma unroll 2
+#pragma unroll AHEAD
     for (int sh = s0; sh <= s1; ++sh)
 #pragma unroll
         for (int k = 0; k < EACH; ++k) {
@@ -1122,8 +1123,10 @@ static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStre
     const size_t bytes = (size_t)attend_mx_lds<DH, NT, TYPE> + (size_t)(a.n_seqs + 1) * 4;
     hipLaunchKernelGGL((attend_paged_mx_kernel<DH, NT, TYPE>), dim3((p.whole ? a.n_seqs : p.shares) * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
 }
-static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
-    return attend_plan(n_seqs, max_blocks, n_heads, kv_heads, dh / 2 + dh / 32, max_rows);
+static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows) {
+    // (a page costs what 70 bytes a position would, for each tile of rows, whatever its head_dim)
+    const int64_t r = (int64_t)max_rows * (n_heads / kv_heads);
+    return attend_plan(n_seqs, max_blocks, n_heads, kv_heads, 70 * (r <= 16 ? 1 : r <= 32 ? 2 : r <= 48 ? 3 : 4), max_rows, 64);
 }
 template <int DH, int NT, int TYPE>
 static void launch_attend_rows(const AttendMxArgs &a, hipStream_t st) {
@@ -1131,19 +1134,26 @@ static void launch_attend_rows(const AttendMxArgs &a, hipStream_t st) {
     const unsigned grid = p.shares > 0 ? (unsigned)p.shares * a.c.heads : (unsigned)p.blocks * a.n_seqs * a.c.heads;
     const size_t bytes = 2 * rows_images<DH> * 16 + (p.shares > 0 ? ((size_t)p.blocks * a.n_seqs + 1) * 4 : 0);
     hipLaunchKernelGGL((attend_mx_rows_kernel<DH, NT, TYPE>), dim3(grid), dim3(256), bytes, st, a, p);
-    if (p.shares > 1)
-        hipLaunchKernelGGL((attend_mx_rows_join_kernel<DH, TYPE>), dim3((unsigned)p.blocks * (64 * NT / JOIN_ROWS), a.c.heads, a.n_seqs), dim3(256), 0, st, a, p, 64 * NT);
+    constexpr int ONE = 1024 / DH;                               // rows whose features fill a workgroup once
+    if (p.shares > 4 * p.blocks * a.n_seqs) hipLaunchKernelGGL((attend_mx_rows_join_kernel<DH, TYPE, ONE>), dim3((unsigned)p.blocks * (64 * NT / ONE), a.c.heads, a.n_seqs), dim3(256), 0, st, a, p, 64 * NT);
+    else if (p.shares > 1) hipLaunchKernelGGL((attend_mx_rows_join_kernel<DH, TYPE, 4 * ONE>), dim3((unsigned)p.blocks * (64 * NT / (4 * ONE)), a.c.heads, a.n_seqs), dim3(256), 0, st, a, p, 64 * NT);
 }
 template <int TYPE> constexpr int rows_nt = TYPE == ROWS_F32 ? 1 : 2;             // (three planes of queries and probabilities leave room for one tile)
-// which calls take the many-rows form
-static bool takes_rows(int n_seqs, int n_heads, int kv_heads, int max_rows, int rows) {
-    const int64_t group_rows = (int64_t)max_rows * (n_heads / kv_heads);
-    return group_rows > 64 && (group_rows + rows - 1) / rows * n_seqs * kv_heads < 1 << 23;
+// Which calls take the many-rows form: those with more rows a key head than the shares' kernel holds (64); at head_dim 64, whose pages are half as much work for the
+// same start and end, from 6144 rows in all blocks on.  us inside a captured graph, here and in shares of the steps' kernel (sequences x positions before, rows, query / key heads):
+//             head_dim 128                                                                                     head_dim 64
+//         1 x 1000, 70, 8/8   1 x 8000, 20, 32/8   1 x 20000, 130, 8/8   64 x 1000, 20, 32/8   4 x 200, 100, 32/32   8 x 2000, 40, 16/2   30 x 60, 70, 8/8   1 x 4000, 500, 8/8   1 x 20000, 70, 8/8
+//   bf16  21.9 26.7           31.0 35.4            47.8 57.8             54.5 130.3            18.7 28.3             25.8 29.0            12.6 18.9          36.3 27.3            44.0 25.6
+//   fp16  25.2 27.5           34.5 37.2            56.7 61.8             73.0 140.3            24.3 29.6             27.5 30.5            13.1 19.9          38.5 29.0            46.5 27.3
+//   fp32  23.2 29.9           33.5 43.3            60.8 73.6             87.0 167.3            17.3 36.0             31.1 34.0            11.9 21.9          36.4 32.8            37.0 31.3
+static bool takes_rows(int n_seqs, int n_heads, int kv_heads, int dh, int max_rows, int rows) {
+    const int64_t group_rows = (int64_t)max_rows * (n_heads / kv_heads), blocks = (group_rows + rows - 1) / rows * n_seqs * kv_heads;
+    return group_rows > 64 && (dh == 128 || blocks * rows >= 6144) && blocks < 1 << 23;
 }
 template <int DH, int TYPE>
 static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
-    if (takes_rows(a.n_seqs, a.n_heads, a.c.heads, a.max_rows, 64 * rows_nt<TYPE>)) return launch_attend_rows<DH, rows_nt<TYPE>, TYPE>(a, st);
-    const AttendPlan p = attend_mx_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, DH, a.max_rows);
+    if (takes_rows(a.n_seqs, a.n_heads, a.c.heads, DH, a.max_rows, 64 * rows_nt<TYPE>)) return launch_attend_rows<DH, rows_nt<TYPE>, TYPE>(a, st);
+    const AttendPlan p = attend_mx_plan(a.n_seqs, a.max_blocks, a.n_heads, a.c.heads, a.max_rows);
     if (p.nt == 1) launch_attend_nt<DH, 1, TYPE>(a, p, st);
     else if (p.nt == 2) launch_attend_nt<DH, 2, TYPE>(a, p, st);
     else if (p.nt == 3) launch_attend_nt<DH, 3, TYPE>(a, p, st);
@@ -1152,9 +1162,9 @@ static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
         hipLaunchKernelGGL((attend_join_kernel<DH, TYPE, AttendMxArgs>), dim3((a.max_rows * (a.n_heads / a.c.heads) + 3) / 4, a.c.heads, a.n_seqs), dim3(256), 0, st, a, p);
 }
 int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
-    int64_t most = attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, dh, max_rows), n_seqs, kv_heads, dh);
+    int64_t most = attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows), n_seqs, kv_heads, dh);
     for (int rows = 64; rows <= 128; rows += 64) {               // (fp32's row blocks, the others')
-        if (!takes_rows(n_seqs, n_heads, kv_heads, max_rows, rows)) continue;
+        if (!takes_rows(n_seqs, n_heads, kv_heads, dh, max_rows, rows)) continue;
         const RowsPlan p = rows_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows, rows);
         const int64_t bytes = p.shares > 0 ? (rows_head(p, n_seqs) + rows_parts(p, kv_heads) * rows * (dh + 2)) * 4 : 0;
         most = bytes > most ? bytes : most;

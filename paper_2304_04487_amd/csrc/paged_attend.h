@@ -83,8 +83,8 @@ __device__ __forceinline__ float pow2(int e) { return __uint_as_float((uint32_t)
 
 #define ATTEND_WHOLE_PAGES 40    // whole sequences: of a table's row, at most
 struct AttendPlan { int nt, tiles, shares; bool whole; };        // whole: sequences in place of shares
-// row: bytes of K, and of V, that a position has per head
-static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int row, int max_rows) {
+// row: bytes of K, and of V, that a position has per head; most_whole: pages of sequences that may stay whole
+static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int row, int max_rows, int most_whole = ATTEND_WHOLE_PAGES) {
     const int64_t r = (int64_t)max_rows * (n_heads / kv_heads);
     AttendPlan p;
     p.nt = r <= 64 ? (int)((r + 15) / 16) : 4;
@@ -97,7 +97,7 @@ static AttendPlan attend_plan(int n_seqs, int max_blocks, int n_heads, int kv_he
     // pages beyond an equal share, at 16 KB of K and V each: 512 KB, or where whole sequences leave half of the compute units without work 256 KB and, of a
     // single one (which costs the least when cut), 192 KB
     const int64_t beyond = (max_blocks - pages * columns / groups) * row;
-    p.whole = max_blocks <= ATTEND_WHOLE_PAGES && n_seqs * columns < 1 << 23 && beyond <= 128 * (n_seqs * columns >= ATTEND_CUS / 2 ? 32 : n_seqs > 1 ? 16 : 12);
+    p.whole = max_blocks <= most_whole && n_seqs * columns < 1 << 23 && beyond <= 128 * (n_seqs * columns >= ATTEND_CUS / 2 ? 32 : n_seqs > 1 ? 16 : 12);
     return p;
 }
 // work: [pages before every sequence, n_seqs + 1 ints, rounded up to 64][parts' O][parts' m][parts' l].  (Also where sequences stay whole: a workspace
