@@ -12,6 +12,10 @@ template <int T> __device__ __forceinline__ uint32_t widen2(uint32_t c, float sc
 }
 // eight neighbouring features: an operand
 __device__ __forceinline__ u32x4 widen8(uint32_t c, float scale) { return (u32x4){widen2<0>(c, scale), widen2<1>(c, scale), widen2<2>(c, scale), widen2<3>(c, scale)}; }
+template <int T> __device__ __forceinline__ uint32_t widen2_half(uint32_t c, float scale) {  // as fp16
+    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, T));
+}
+__device__ __forceinline__ u32x4 widen8_half(uint32_t c, float scale) { return (u32x4){widen2_half<0>(c, scale), widen2_half<1>(c, scale), widen2_half<2>(c, scale), widen2_half<3>(c, scale)}; }
 __device__ __forceinline__ uint32_t nan_scales(uint32_t w) { return ((w & 0x7f7f7f7fu) + 0x01010101u) & w & 0x80808080u; }      // 0x80 in the bytes that are 255
 // four words of four bytes, turned: word r gets byte r of each
 __device__ __forceinline__ void turn4(uint32_t *w) {
@@ -355,7 +359,14 @@ __device__ __forceinline__ void widen_v(const u32x4 &c, const u32x4 &s, int u, u
         odd[2 * h + 1] = __builtin_amdgcn_perm(p3, p2, 0x07060302u);
     }
 }
-template <int DH, int NT, int TYPE> constexpr int attend_mx_lds = 16 * (attend_nq<TYPE> * attend_pieces<DH, NT> > 4 * NT * (DH / 16) * 64 ? attend_nq<TYPE> * attend_pieces<DH, NT> : 4 * NT * (DH / 16) * 64);
+// planes of the queries in LDS: attend_nq of bf16, and fp16 rows as they are
+template <int TYPE> constexpr int attend_mx_planes = attend_nq<TYPE> + (TYPE == ROWS_F16);
+template <int DH, int NT, int TYPE> constexpr int attend_mx_lds = 16 * (attend_mx_planes<TYPE> * attend_pieces<DH, NT> > 4 * NT * (DH / 16) * 64 ? attend_mx_planes<TYPE> * attend_pieces<DH, NT> : 4 * NT * (DH / 16) * 64);
+// no byte outside 104 .. 139: a code times such a scale is exact in fp16
+__device__ __forceinline__ bool half_scales(uint32_t w) {
+    const uint32_t low = w & 0x7f7f7f7fu;
+    return (((low + 0x18181818u) | w) & ~((low + 0x74747474u) & w) & 0x80808080u) == 0x80808080u;
+}
 #define ATTEND_KEPT 256          // sequences whose lengths and rows the workgroup keeps in LDS
 
 template <int DH, int NT, int TYPE>
@@ -469,6 +480,10 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
             for (int h = 0; h < (TYPE == ROWS_F32 ? 2 : 1); ++h) qr.raw[u][h] ^= turn;
         __syncthreads();
         attend_put_q<DH, NT, NQ, TYPE>(qr, q);
+        if constexpr (TYPE == ROWS_F16)
+#pragma unroll
+            for (int u = 0; u < (PIECES + 255) / 256; ++u)
+                if (u * 256 + (int)threadIdx.x < PIECES) q[NQ * PIECES + u * 256 + threadIdx.x] = qr.raw[u][0];
         __syncthreads();
         const AttendSeg after = segment(seg.b + 1);
         int id_after = -1;
@@ -510,6 +525,17 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
 #pragma unroll
                     for (int t = 0; t < 4; ++t) sc[n][t] = (f32x4){0.f, 0.f, 0.f, 0.f};
                 const float k_by[4] = {scale_byte<0>(ks), scale_byte<1>(ks), scale_byte<2>(ks), scale_byte<3>(ks)};
+                // (fp16 rows: one product of fp16 where K's scales allow it, two of bf16 otherwise; both exact)
+                if (TYPE == ROWS_F16 && __ballot(!half_scales(ks)) == 0) {
+#pragma unroll
+                    for (int st = 0; st < STEPS; ++st)
+#pragma unroll
+                        for (int t = 0; t < 4; ++t) {
+                            const u32x4 w = widen8_half(kc[t][st], k_by[t]);
+#pragma unroll
+                            for (int n = 0; n < NT; ++n) sc[n][t] = mfma16x16x32_half(w, q[NQ * PIECES + (n * STEPS + st) * 64 + ql], sc[n][t]);
+                        }
+                } else
 #pragma unroll
                 for (int st = 0; st < STEPS; ++st)
 #pragma unroll
@@ -673,9 +699,6 @@ __device__ __forceinline__ void unit_for(int most, BlockUnit &u) {              
     const bool other = ((unsigned)(most - u.now + 8) > 20u) & (most > 0);
     u.now = other ? near : u.now;
     u.least = u.now - 60 > u.least ? u.now - 60 : u.least;
-}
-template <int T> __device__ __forceinline__ uint32_t widen2_half(uint32_t c, float scale) {
-    return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(c, scale, T));
 }
 // as widen_v, in fp16 and in units: by[t] for the word's four positions
 __device__ __forceinline__ void widen_word_half(uint32_t w, const float *by, uint32_t (&even)[2], uint32_t (&odd)[2]) {
