@@ -525,3 +525,24 @@ def test_attend_more_blocks_of_rows_than_a_list_holds(llma):
     rows[3], lens[3] = 390, 400
     c, q, table, slots, off = attend_case(llma, lens, rows, 2, 2, 64, "bf16", 98)
     check_attend(llma, c, q, table, slots, lens, off, max(rows), "bf16")
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("rows", [3, 30, 50, 130])
+@pytest.mark.parametrize("shift,spread", [(0, 34), (-40, 3), (30, 3), (-22, 6), (11, 2)])
+def test_attend_scales_far_from_one(llma, dtype, rows, shift, spread):
+    """caches whose scales fp16 does not hold, or not all of them: small and large values of K and V, with queries and outputs in their types' range"""
+    c, q, table, slots, off = attend_case(llma, [300], [rows], 4, 4, 64, dtype, 101, spread=0)
+    rng = np.random.default_rng(7)
+    for s in (c.k_scale, c.v_scale):
+        r = torch.tensor(rng.integers(-spread, 1, s.shape), device="cuda")
+        by = shift if s is c.k_scale or dtype != "fp16" else max(min(shift, 8), -16)        # (fp16 outputs end at 65504, and lose bits below 2^-14)
+        s.copy_(torch.where(s == 255, 255, s.int() + by + r).to(torch.uint8))
+    check_attend(llma, c, q, table, slots, [300], off, rows, dtype, scale=2.0 ** -(shift + 3))
+
+
+def test_attend_subnormal_queries(llma):
+    """fp16 queries below its normal range"""
+    for rows in (3, 30, 130):
+        c, q, table, slots, off = attend_case(llma, [300], [rows], 4, 2, 64, "fp16", 103, q_size=4e-6)
+        check_attend(llma, c, q, table, slots, [300], off, rows, "fp16", scale=3e4)
