@@ -17,7 +17,7 @@
 struct LogprobPlan { int u, lanes, chunks, segments; };          // pieces a lane; lanes of a segment; chunks and segments of a row
 static LogprobPlan logprob_plan(int n_rows, int vocab, int epb) {
     const int pieces = (vocab + epb - 1) / epb + 1;
-    LogprobPlan p{8, 16, 0, 0};
+    LogprobPlan p{4, 16, 0, 0};                                  // (2000 rows of 128256 bf16: eight 122 us, four 112, two 159)
     const auto chunks = [&] { return (pieces + CHUNK_PIECES(p.u) - 1) / CHUNK_PIECES(p.u); };
     while (p.u > 1 && (int64_t)n_rows * chunks() < 4096) p.u /= 2;
     p.chunks = chunks();
@@ -25,24 +25,20 @@ static LogprobPlan logprob_plan(int n_rows, int vocab, int epb) {
     p.segments = p.chunks * p.u * (64 / p.lanes);
     return p;
 }
-struct LogprobPart { double r; float s, w, tilt; int before, pad[2]; };      // tilt: (by - its fp32 value) by its fp32 value, where the sums were taken with that
+struct LogprobPart { double r; float s, w, hi; int before, pad[2]; };        // hi: what stood for by in fp32 (0: the sums were taken with by itself)
 static int64_t logprob_bytes(const LogprobPlan &p, int n_rows, int n_top) { return (int64_t)n_rows * (p.chunks * (int64_t)sizeof(LogprobPart) + (n_top > 0 ? p.segments * 4ll : 0)); }
 int64_t token_logprobs_bytes(int n_rows, int vocab, int n_top) {
     const int64_t narrow = logprob_bytes(logprob_plan(n_rows, vocab, 8), n_rows, n_top), wide = logprob_bytes(logprob_plan(n_rows, vocab, 4), n_rows, n_top);
     return (narrow > wide ? narrow : wide) + 16;
 }
 
-// log2(e) / T; the sums are taken with its fp32 value, whose own rounding would tilt all terms of a row alike, and put right when the parts are joined
-struct By { double by; float hi; };
-__device__ __forceinline__ By by_of(const LogprobArgs &a, int row) {
+// T as it counts, and by = log2(e) / T in 64 bits.  The chunks' sums are taken with an fp32 number near by, whose error tilts all terms of a row alike and is put right when the parts are joined
+__device__ __forceinline__ float temperature_of(const LogprobArgs &a, int row) {
     float t = a.temperature ? a.temperature[row] : 1.f;
     if (!(t > 0.f)) t = 1.f;                                     // (also NaN)
-    t = t > 3.402823466e38f ? 3.402823466e38f : t;
-    By b;
-    b.by = 1.4426950408889634074 / (double)t;
-    b.hi = (float)b.by;
-    return b;
+    return t > 3.402823466e38f ? 3.402823466e38f : t;
 }
+__device__ __forceinline__ double by_of(float t) { return 1.4426950408889634074 / (double)t; }
 template <int TYPE> __device__ __forceinline__ float logit_at(const LogprobArgs &a, int64_t row, int i) {
     const int64_t at = row * a.row_stride + i;
     float x;
@@ -70,9 +66,9 @@ __device__ __forceinline__ u32x4 row_piece(const RowView &v, int p, int pieces, 
     return w;
 }
 // x by, rounded: where logits are so large that this rounding shows, R has it too
-__device__ __forceinline__ double times_by(float x, const By &b) {
+__device__ __forceinline__ double times_by(float x, double by) {
 #pragma clang fp contract(off)
-    const double z = (double)x * b.by;
+    const double z = (double)x * by;
     return z;
 }
 // the smallest float above x (of plus infinity: NaN, which nothing reaches)
@@ -116,9 +112,10 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
     constexpr int EPB = sampled_epb<TYPE>, N = U * EPB;
     ieee_mode_off();
     const int lane = threadIdx.x & 63;
-    const int64_t id = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    if (id >= (int64_t)a.n_rows * plan.chunks) return;
-    const int row = (int)(id / plan.chunks), chunk = (int)(id % plan.chunks);
+    // (32 bits: a call's rows have at most 2^40 logits and a chunk of many rows 2^10.  A 64-bit division would be a sixth of a wave's instructions)
+    const uint32_t id = blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    if (id >= (uint32_t)a.n_rows * (uint32_t)plan.chunks) return;
+    const int row = (int)(id / (uint32_t)plan.chunks), chunk = (int)(id % (uint32_t)plan.chunks);
     const RowView view = row_view<TYPE>(a, row);
     const int pieces = (view.skip + a.vocab + EPB - 1) / EPB, p0 = chunk * CHUNK_PIECES(U);
     u32x4 w[U];
@@ -130,7 +127,7 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab);
     }
-    const By by = by_of(a, row);
+    const float T = temperature_of(a, row), hi = 1.4426950408889634f / T;
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool given = a.rank && (unsigned)token < (unsigned)a.vocab;
     const float xt = given ? logit_at<TYPE>(a, row, token) : 0.f;
@@ -175,18 +172,19 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
     butterfly<32>([&](auto o) { M = fmaxf(M, lane_xor<o.value>(M)); });
     // ---- sums
     double R = LLMA_NEG_INF;
-    float s = 0.f, sw = 0.f, tilt = 0.f;
-    const float r = M * by.hi;
-    if (fabsf(M) < 1e30f && by.hi > 1e-20f && fabsf(r) < 4096.f) {
+    float s = 0.f, sw = 0.f, taken = 0.f;
+    const float r = M * hi;
+    if (fabsf(M) < 1e30f && hi > 1e-20f && fabsf(r) < 4096.f) {
         R = (double)r;
-        tilt = (float)((by.by - (double)by.hi) / (double)by.hi);
+        taken = hi;
 #pragma unroll
         for (int i = 0; i < N; ++i) {
-            const float t = __builtin_fmaf(x[i], by.hi, -r), y = __builtin_amdgcn_exp2f(t);
+            const float t = __builtin_fmaf(x[i], hi, -r), y = __builtin_amdgcn_exp2f(t);
             s += y;
             sw = __builtin_fmaf(y, t, sw);
         }
     } else if (M != LLMA_NEG_INF) {                              // an infinite maximum (it counts 1, all else 0), large logits, cold or very hot rows: in 64 bits up to 2^t
+        const double by = by_of(T);
         R = times_by(M, by);
 #pragma unroll 1
         for (int u = 0; u < U; ++u) {
@@ -195,7 +193,7 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
 #pragma unroll
             for (int e = 0; e < EPB; ++e) {
                 const float z = fmaxf(v[e], LLMA_NEG_INF);
-                const double t = z == M ? 0. : ((double)z - (double)M) * by.by;
+                const double t = z == M ? 0. : ((double)z - (double)M) * by;
                 const float y = t < -1000. ? 0.f : __builtin_amdgcn_exp2f((float)t);
                 s += y;
                 sw += y > 0.f ? y * (float)t : 0.f;
@@ -245,7 +243,7 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
         t.r = R;
         t.s = s;
         t.w = sw;
-        t.tilt = tilt;
+        t.hi = taken;
         t.before = before;
         t.pad[0] = t.pad[1] = 0;
         ((LogprobPart *)a.work)[id] = t;
@@ -290,7 +288,7 @@ __global__ __launch_bounds__(64) void logprob_row_kernel(LogprobArgs a, LogprobP
 #pragma unroll
         for (int k = 0; k < HELD; ++k) held[k] = k * 64 + lane < plan.segments ? ordered(segments[k * 64 + lane]) : 0u;
     }
-    const By by = by_of(a, row);
+    const double by = by_of(temperature_of(a, row));
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool given = (unsigned)token < (unsigned)a.vocab;
     const float xt = given ? logit_at<TYPE>(a, row, token) : LLMA_NEG_INF;
@@ -303,11 +301,11 @@ __global__ __launch_bounds__(64) void logprob_row_kernel(LogprobArgs a, LogprobP
         const LogprobPart p = parts[i];
         const double d = p.r == R ? 0. : p.r - R;
         if (d > -1000.) {
-            // A term is 2^(x hi) for 2^(x by), hi the fp32 value of by: S lacks ln2 (by - hi) sum 2^t x, W that times the mean of t, and the sum itself (the spread of t, of the
-            // size of (by - hi) too, is left out: 2^-25 of it; |x hi| is below 2^12, so the squares are 2^-26).
+            // A term is 2^(x hi) for 2^(x by): S lacks ln2 (by - hi) sum 2^t x, W that times the mean of t, and the sum itself (the spread of t, of the
+            // size of (by - hi) too, is left out: 2^-24 of it; |x hi| is below 2^12, so the squares are 2^-24 at most, at logits of thousands).
             // (Exponential and logarithm in fp32, of numbers near 1: off by 2^-23 of a part, which 64 bits would not notice in the result)
             const double f = (double)__builtin_amdgcn_exp2f((float)d);
-            const double lack = p.tilt != 0.f ? (double)p.tilt * (p.w + p.r * p.s) : 0., mean = p.tilt != 0.f ? (double)(p.w / p.s) : 0.;
+            const double lack = p.hi != 0.f ? (by / (double)p.hi - 1.) * (p.w + p.r * p.s) : 0., mean = p.hi != 0.f ? (double)(p.w / p.s) : 0.;
             const double ps = p.s + 0.69314718055994530942 * lack, pw = p.w + lack * (1. + 0.69314718055994530942 * mean);
             s += f * ps;
             w += f * (pw + d * ps);
@@ -482,8 +480,7 @@ void launch_token_logprobs(const LogprobArgs &a, hipStream_t st) {
         constexpr int TYPE = decltype(type)::value;
         const LogprobPlan p = logprob_plan(a.n_rows, a.vocab, sampled_epb<TYPE>);
         const dim3 grid((unsigned)(((int64_t)a.n_rows * p.chunks + 3) / 4)), block(256);
-        if (p.u == 8) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 8>), grid, block, 0, st, a, p);
-        else if (p.u == 4) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 4>), grid, block, 0, st, a, p);
+        if (p.u == 4) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 4>), grid, block, 0, st, a, p);
         else if (p.u == 2) hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 2>), grid, block, 0, st, a, p);
         else hipLaunchKernelGGL((logprob_chunk_kernel<TYPE, 1>), grid, block, 0, st, a, p);
         hipLaunchKernelGGL((logprob_row_kernel<TYPE>), dim3(a.n_rows), dim3(64), 0, st, a, p);
