@@ -333,11 +333,14 @@ typedef struct {
 /* Writes rows into the 4-bit cache; arguments as llma_append_paged has them.  Every row has scales of its own: per 32 features the smallest power of
  * two (from 2^-64 to 2^120) s with max |x| / s <= 7 over the finite values; codes are x / s rounded to nearest even, +-6 beyond; +-inf become
  * +-6, a NaN makes its 32 features NaN.  So a write changes nothing but its rows' positions, and rows may come in any
- * order; a slot listed twice has either row's codes. */
+ * order; the position of a slot listed twice ends with some codes and scales of one row and some of the other. */
 int llma_append_paged_mx(const llma_paged_mx_cache *cache, const void *k, const void *v, int32_t dtype, int64_t k_row_stride,
                          int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot_map, int32_t n_rows,
                          void *hip_stream);
-/* llma_attend_paged and llma_read_paged over it. */
+/* llma_attend_paged and llma_read_paged over it.  Scores see exactly what codes and scales stand for; so does the product with V, except that with bf16 rows, where a key head
+ * has more than 64 of them, V loses bits where its scale is more than 2^15 below the largest of its page and 32 features (of positions that a row of the call sees), or more than 2^75 below 1
+ * or another page's, all of them 2^5 further down, and probabilities do so from 2^-21 of a row's largest on, all of them at 2^-31.  A scale that stands for NaN makes the 32 features
+ * of its position NaN for the rows that see it.  A workspace for some number of sequences does for fewer; beyond 64 rows a key head it has up to some 70 MB. */
 int64_t llma_attend_paged_mx_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);
 int llma_attend_paged_mx(const llma_paged_mx_cache *cache, const void *q, int32_t dtype, int32_t n_heads, int64_t q_row_stride,
                          int64_t q_head_stride, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,

@@ -41,6 +41,7 @@ __device__ __forceinline__ int mx_exponent(float amax) {
 // 16 (8) lanes share a row's 128 (64) features, eight each.  A lane has the rows of up to four neighbouring positions, a quad, so that a byte of the
 // transposed V leaves as one word for four positions, and so do the scales; a quad that is not whole leaves byte by byte.  A wave takes the quads that begin in its
 // window of rows, 4 (8) at once: a prompt's rows are quads from its second page position divisible by four on, wherever it begins.
+// Prompts are bound by memory: 4 of up to 2011 fp32 rows of 8 heads of 128, 58 MB, 13 us = 4.5 TB/s.  Steps by their chain of slots, rows and scale: 16 sequences of 9 rows of 32 heads 6.2 us.
 template <int DH, int TYPE, bool KEYS>
 __device__ __forceinline__ void append_mx_quad(const AppendMxArgs &a, int head, int row, int n, int slot, int oct) {
     constexpr int FB = DH / 32;
@@ -157,6 +158,9 @@ void launch_append_paged_mx(const AppendMxArgs &a, hipStream_t st) {
 // Row j of sequence b is position first[b] + j.  A run = rows of one sequence inside one page; a workgroup takes one head of the runs that begin in its window of
 // rows (64: a long sequence's one run).  A lane stores 16 bytes of a row, eight neighbouring lanes 128.  K's rows lie as they leave.  V's lie across: a lane takes four
 // positions of its features, turns them in registers and has its features of four rows.
+// Bound by memory, mostly by what is written: prefixes of five sequences of up to 4001 positions x 32 heads of 128 from 8 bits to bf16, 301 MB in 60 us = 5.0 TB/s; 37 of up to 1900 x 8 heads from 4 bits
+// to fp32, 400 MB, 90 us = 4.4 TB/s (118 with 32 bytes a lane in two halves, K and V one after the other).  Short ones by the chain of offsets, table and page: 1001 positions of 8 heads of 64 4.7 us,
+// 16 sequences of 9 rows of 32 heads 5.3 (18.7 in windows of 64 rows).
 struct ReadRun { int row, n, page, at; };                        // page -1: none, the rows become 0
 template <int TYPE> constexpr int read_features = TYPE == ROWS_F32 ? 4 : 8;      // of 16 bytes
 template <int TYPE>
@@ -327,6 +331,11 @@ void launch_read_paged(const ReadArgs<PagedMxCache> &a, hipStream_t st) { launch
 //   V: a byte is two features of a position.  Widened (with its position's scale) it is a pair across features; two positions' pairs, exchanged by halves, are
 //   pairs along the positions, of an even and of an odd feature: block jj of 32 features makes two operands, features 32 jj + 2 i and 32 jj + 2 i + 1.
 // Both products see exactly what codes and scales stand for.
+// Steps are bound by the read of the cache up to one tile of rows: 16 sequences of up to 4096 positions, 9 rows of 32 heads of 128, 192 MB in 36 us with the cache's bytes still in the last-level cache, 40 to
+// 47 without = 4.1 to 4.8 TB/s (a kernel of the same mapping that only loads: 31.5 with).  From two tiles on by the products and the vector instructions beside them, which take turns rather than
+// overlap: 61 of 5 rows, four query heads a key head, fp16, 358 MB in 95 us (load-only 74), a third of the cycles in matrix instructions, half in vector instructions.  Not faster: products in another order,
+// a page's scores a page ahead of its other product (39 and 115 us), one word of scales a lane exchanged between lanes; one fp16 plane of probabilities spills here (47 us).
+// Other matrix instructions would take the codes as they are, with their scales, beside queries in planes of 8 bits: their sums are off by 1e-5 of the largest product (rms).
 // rare: a page's V has scales that stand for NaN where not all rows see them.  The rows that see one get it in its 32 features.  seen: 0x80 in the bytes of the lane's 16 positions
 template <int DH, int NT>
 __device__ __forceinline__ void attend_mx_nans(const u32x4 (&nans)[DH / 32], int base, const int (&limit)[NT], f32x4 (&o)[NT][DH / 16]) {
@@ -692,7 +701,8 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
 // ---- many rows -----------------------------------------------------------------------------------
 // fp16 products keep the sums of each block of 32 features in units of a power of two, `now` its exponent plus 127, so that V fits: a code of 0.5 .. 6 times 2^-23 .. 2^12 is exact in fp16.
 // A page whose largest scale of the block lies outside 2^-8 .. 2^12 units makes that the unit, but none more than 2^60 below the largest before it (up to 2^62 units may have been
-// added up, and fp32 ends at 2^128).  So V loses bits below 2^-19 of the largest of the block in its page (and counts as zero from 2^-21 on), or 2^-80 of another page's.
+// added up, and fp32 ends at 2^128).  So V loses bits where its scale is more than 2^15 below the largest of the block in its page, or more than 2^75 below 1 or another page's (the last bit
+// 2^5 further down).
 struct BlockUnit { int now, least; };
 __device__ __forceinline__ void unit_for(int most, BlockUnit &u) {               // most: 0 for none
     const int near = most > u.least ? most : u.least;
@@ -721,7 +731,8 @@ static RowsPlan rows_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads,
     int64_t shares = 2 * ATTEND_CUS / kv_heads;
     shares = shares < 1 ? 1 : shares;
     const bool small = max_blocks <= 8 && listed * kv_heads >= 128;      // (blocks enough, and so short that a share's several starts cost more than an uneven end)
-    p.shares = listed > ROWS_LISTED || small ? 0 : (int)(shares < most ? shares : most);
+    // (pages of the list are counted in 32 bits)
+    p.shares = listed > ROWS_LISTED || pages > 0x7fffffff || small ? 0 : (int)(shares < most ? shares : most);
     return p;
 }
 // work: [pages before every block of the list, rounded up to 64 ints][parts' O][parts' m][parts' l]
@@ -731,6 +742,9 @@ __host__ __device__ static inline int64_t rows_parts(const RowsPlan &p, int kv_h
 // 16 KB of V at head_dim 128): wave t has score tile t, and block t of V's features (of two blocks at head_dim 64: half of one's positions).  A page is requested two ahead, widened one
 // ahead, one barrier a page.  The rest is as with 8 bits: a wave holds its rows' queries and sums in registers, pages behind its rows are skipped, and the
 // reference of the exponentials moves only when a maximum passes it by 2^8.
+// Bound by issue: two sequences of up to 2047 rows, 32 query and 8 key heads of 128, over up to 2900 positions before, bf16, 136 GFLOP in 258 us and 17 for the join = 0.49 PFLOP/s.  A workgroup per
+// block left the compute units empty for 30 % of the time (310 us); what is left is the products (a third of the cycles) and the vector instructions (half), which hardly overlap.  Wave
+// priorities, by phase or by wave, changed nothing.
 template <int DH> constexpr int rows_images = (4 * (DH / 32) + (DH / 16) * 2) * 64;          // 16-byte pieces of a page
 template <int DH, int NT, int TYPE>
 __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, RowsPlan plan) {
@@ -1147,7 +1161,11 @@ static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStre
     hipLaunchKernelGGL((attend_paged_mx_kernel<DH, NT, TYPE>), dim3((p.whole ? a.n_seqs : p.shares) * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
 }
 static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows) {
-    // (a page costs what 70 bytes a position would, for each tile of rows, whatever its head_dim)
+    // Which sequences stay whole: the 8-bit cache's rule, with a page at what 70 bytes a position would cost, for each tile of rows, whatever its head_dim, and tables of up to 64 pages.
+    // us inside a captured graph, cut and whole (32 heads of 128, 9 rows; 8 of 64; 32 / 8 of 128, 5 rows):
+    //          1 x 500    1 x 1001   1 x 1500   6 x 1001   6 x 3000   16 x 1001  64 x 1900 | 1 x 1001, 1 row  6 x 1300, 9  1 x 2000, 1  6 x 2400, 9 | 4 x 1001
+    //   bf16   11.9 9.5   12.3 11.7  12.8 13.8  20.2 12.8  28.3 22.8  20.7 18.3  117 110   | 10.7 9.7         13.8 11.3    11.0 12.7    15.7 14.5   | 14.3 15.6
+    //   fp32   12.5 10.5  12.8 13.7  13.6 17.0  21.9 14.9  32.1 28.9  24.3 21.7  129 128   | 11.0 10.9        14.7 13.2    11.4 15.0    16.7 17.6   | 16.4 19.7
     const int64_t r = (int64_t)max_rows * (n_heads / kv_heads);
     return attend_plan(n_seqs, max_blocks, n_heads, kv_heads, 70 * (r <= 16 ? 1 : r <= 32 ? 2 : r <= 48 ? 3 : 4), max_rows, 64);
 }
@@ -1188,8 +1206,12 @@ int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_he
     int64_t most = attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows), n_seqs, kv_heads, dh);
     for (int rows = 64; rows <= 128; rows += 64) {               // (fp32's row blocks, the others')
         if (!takes_rows(n_seqs, n_heads, kv_heads, dh, max_rows, rows)) continue;
-        const RowsPlan p = rows_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows, rows);
-        const int64_t bytes = p.shares > 0 ? (rows_head(p, n_seqs) + rows_parts(p, kv_heads) * rows * (dh + 2)) * 4 : 0;
+        // (as if cut, whether it is or not: a workspace for some number of sequences does for fewer, which may be cut where more are not)
+        RowsPlan p = rows_plan(1, max_blocks, n_heads, kv_heads, max_rows, rows);
+        if (p.blocks > ROWS_LISTED) continue;
+        const int listed = n_seqs < ROWS_LISTED / p.blocks ? n_seqs : ROWS_LISTED / p.blocks;
+        p.shares = 2 * ATTEND_CUS / kv_heads > 0 ? 2 * ATTEND_CUS / kv_heads : 1;
+        const int64_t bytes = (rows_head(p, listed) + rows_parts(p, kv_heads) * rows * (dh + 2)) * 4;
         most = bytes > most ? bytes : most;
     }
     return most;

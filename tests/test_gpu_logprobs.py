@@ -185,3 +185,14 @@ def test_signalling_nans_and_large_logits(llma):
         assert t.isnan().sum() > 2000
         check(llma, t, [6, 17, 18, 19, 20, 21], None, 9)
         check(llma, t, [0, 17, 18, 19, 20, 3], [0.8, 0.9, 1.1, 1.0, 1.0, 1.3], 9)
+
+
+@pytest.mark.parametrize("dtype,vocab", [("bf16", 1200007), ("fp32", 600011)])
+@pytest.mark.parametrize("n_top", [3, 40])
+def test_more_segments_than_a_row_keeps(llma, dtype, vocab, n_top):
+    """rows of more than a thousand segments: the rest of their maxima is read from memory; the best at both ends, in the middle, in one place"""
+    rng = np.random.default_rng(11)
+    x = torch.tensor(2 * rng.standard_normal((3, vocab)), dtype=torch.float32)
+    x[1, [0, vocab // 2, vocab - 1]] = 20.0
+    x[2, vocab - 50:] = torch.arange(50).float() + 15
+    check(llma, x.to(DT[dtype]).cuda(), [7, vocab - 1, vocab - 3], [0.7, 1.0, 1.9], n_top)

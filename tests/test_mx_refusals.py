@@ -116,3 +116,11 @@ def test_the_plain_encoding():
             assert np.allclose(err, abs(v[:, None] - s * mx.VALUES).min(-1), rtol=1e-12, atol=0)
     assert got[6, :10].tolist() == [6, -6, 4, 2, 4, 2, 1, 1, 0, 0]
     assert mx.encode(np.array([[np.nan] + [1.0] * 31 + [np.inf] + [2.0] * 31]))[1].tolist() == [[255, 126]]
+
+
+def test_a_workspace_for_many_sequences_does_for_fewer(lib):
+    for blocks in (3, 60, 4000):
+        for heads, kv, dh in ((32, 8, 128), (8, 8, 64), (64, 64, 128), (16, 1, 64)):
+            for rows in (1, 9, 65, 300, 2000):
+                sizes = [llma.llma_attend_paged_mx_workspace(n, blocks, heads, kv, dh, rows) for n in (1, 2, 3, 7, 30, 64, 200)]
+                assert sizes == sorted(sizes), (blocks, heads, kv, dh, rows, sizes)
