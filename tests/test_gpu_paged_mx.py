@@ -214,7 +214,7 @@ def attend_case(llma, lens, rows, heads, kv, D, dtype, seed, n_slots=None, spare
     return c, q, table, slots, off
 
 
-def check_attend(llma, c, q, table, slots, lens, off, max_rows, dtype, out=None, scale=None, **kw):
+def check_attend(llma, c, q, table, slots, lens, off, max_rows, dtype, out=None, scale=None, besides=None, **kw):
     D = q.shape[2]
     scale = scale if scale is not None else D ** -0.5
     kv, vv = cached(c)
@@ -231,6 +231,8 @@ def check_attend(llma, c, q, table, slots, lens, off, max_rows, dtype, out=None,
     tol = (1 + 2.0 ** -7) * size * (p_err + 2 * max(lens) * 2.0 ** -24)[..., None] + HALF[dtype] * np.abs(want) + 1e-30
     if dtype == "fp16":
         tol = tol + 2.0 ** -25                                          # (half a step below fp16's normal range)
+    if besides is not None:
+        tol[:n] += besides
     assert np.isfinite(got[:n]).all()
     worst = np.max((np.abs(got[:n] - want[:n]) / tol[:n])) if n else 0.0
     assert worst <= 1.0, worst
@@ -546,3 +548,68 @@ def test_attend_subnormal_queries(llma):
     for rows in (3, 30, 130):
         c, q, table, slots, off = attend_case(llma, [300], [rows], 4, 2, 64, "fp16", 103, q_size=4e-6)
         check_attend(llma, c, q, table, slots, [300], off, rows, "fp16", scale=3e4)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+def test_prompts_captured_and_replayed(llma, dtype):
+    """prompts in pieces: write, attention in the form for many rows, rows back, log probabilities of all rows; one graph, replayed with other lengths and tables between eager work"""
+    B, H, heads, D, m, blocks, V = 3, 2, 8, 128, 90, 9, 2600
+    P, n = B * blocks, B * m
+    rng = np.random.default_rng(91)
+    new = lambda *s, dt=DT[dtype]: torch.zeros(s, dtype=dt, device="cuda")
+    at = {"table": i32(np.zeros((B, blocks))), "lens": i32([m] * B), "first": i32([0] * B), "off": i32([0, m, 2 * m, 3 * m]), "slots": i32([-1] * n), "tokens": i32([0] * n),
+          "x": new(n, heads + 2 * H, D), "logits": new(n, V)}
+    ws = torch.empty(llma.llma_attend_paged_mx_workspace(B, blocks, heads, H, D, m), dtype=torch.uint8, device="cuda")
+
+    def state():
+        return {"c": random_cache(llma, P, H, D, 7, nans=False), "out": new(n, heads, D), "k": new(n, H, D), "v": new(n, H, D), "lp": new(n, dt=torch.float32), "rank": new(n, dt=torch.int32),
+                "top": new(n, 30, dt=torch.int32), "top_lp": new(n, 30, dt=torch.float32)}
+
+    def step(s, work):
+        llma.llma_append_paged_mx(s["c"], at["x"][:, heads:heads + H], at["x"][:, heads + H:], at["slots"])
+        llma.llma_attend_paged_mx(s["c"], at["x"][:, :heads], at["table"], at["lens"], at["off"], m, D ** -0.5, s["out"], workspace=work)
+        llma.llma_read_paged_mx(s["c"], at["table"], at["first"], at["off"], s["k"], s["v"])
+        llma.llma_token_logprobs(at["logits"], at["tokens"], s["lp"], rank=s["rank"], top_tokens=s["top"], top_logprobs=s["top_lp"])
+
+    eager, replayed = state(), state()
+    st, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    st.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.graph(graph, stream=st):
+        step(replayed, ws)
+    for it in range(6):
+        rows = rng.integers(0 if it else m, m + 1, B)
+        lens = rows + rng.integers(0, blocks * PAGE - m, B)
+        off = np.concatenate([[0], np.cumsum(rows)])
+        table = rng.permutation(P).reshape(B, blocks)
+        slots = np.full(n, -1)
+        for b in range(B):
+            pos = lens[b] - rows[b] + np.arange(rows[b])
+            slots[off[b]:off[b + 1]] = table[b, pos // PAGE] * PAGE + pos % PAGE
+        for name, value in (("table", table), ("lens", lens), ("first", lens - rows), ("off", off), ("slots", slots), ("tokens", rng.integers(0, V, n))):
+            at[name].copy_(i32(value))
+        for name in ("x", "logits"):
+            at[name].copy_(torch.tensor(rng.standard_normal(at[name].shape), dtype=torch.float32))
+        for o in (eager["out"], replayed["out"]):
+            o.fill_(7.0)
+        step(eager, None)
+        graph.replay()
+        torch.cuda.synchronize()
+        for name in eager:
+            if name != "c":
+                assert torch.equal(eager[name], replayed[name]), (it, name)
+        for a in ("k", "v", "k_scale", "v_scale"):
+            assert torch.equal(getattr(eager["c"], a), getattr(replayed["c"], a))
+        used = off[-1]
+        assert np.array_equal(eager["k"][:used].float().cpu().numpy(), mx.values(*mx.encode(at["x"][:used, heads:heads + H].double().cpu().numpy())).astype(np.float32))
+        keep = eager["out"].clone()
+        # These scores lie so far apart that the largest probability's V, where its code is 0, leaves features to probabilities of 1e-10.  bf16 rows' are held in fp16, the largest of a row and
+        # part of the pages as 2^7 or more: below fp16's normal range each is off by up to half a step, 2^-25, and so by up to 2^-32 of the largest, which is 1 at most.  2^-32 sum |v| in all
+        # (twice, for the rounding of the sum that divides is of that size too, times an output of at most the largest |v|).
+        _, vv = cached(eager["c"])
+        besides = np.zeros((used, heads, D))
+        for b in range(B):
+            pos = np.arange(lens[b])
+            v = np.abs(vv[table[b, pos // PAGE], :, pos % PAGE])
+            besides[off[b]:off[b + 1]] = 2.0 ** -32 * (v.sum(0) + lens[b] * v.max(0, initial=0)).repeat(heads // H, 0)
+        check_attend(llma, eager["c"], at["x"][:, :heads], table, range(B), lens, off, m, dtype, out=eager["out"], besides=besides if dtype == "bf16" else None)
+        assert torch.equal(keep, eager["out"])
