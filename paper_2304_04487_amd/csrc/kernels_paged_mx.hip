@@ -1211,7 +1211,7 @@ int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_he
         if (p.blocks > ROWS_LISTED) continue;
         const int listed = n_seqs < ROWS_LISTED / p.blocks ? n_seqs : ROWS_LISTED / p.blocks;
         p.shares = 2 * ATTEND_CUS / kv_heads > 0 ? 2 * ATTEND_CUS / kv_heads : 1;
-        const int64_t bytes = (rows_head(p, listed) + rows_parts(p, kv_heads) * rows * (dh + 2)) * 4;
+        const int64_t bytes = (rows_head(p, listed) + (p.shares > 1 ? rows_parts(p, kv_heads) * rows * (dh + 2) : 0)) * 4;       // (one share a key head cuts nothing)
         most = bytes > most ? bytes : most;
     }
     return most;

@@ -498,7 +498,8 @@ def test_rows_read_go_into_a_context(llma):
 
 @pytest.mark.parametrize("dtype", list(DT))
 @pytest.mark.parametrize("lens,rows,heads,kv,D", [
-    ([5000], [70], 2, 1, 64), ([3000, 1, 0, 900], [130, 1, 0, 300], 4, 2, 128), ([64 * 9 + 1], [200], 40, 40, 64), ([2000, 1999, 40], [129, 65, 90], 3, 1, 128)])
+    ([5000], [70], 2, 1, 64), ([3000, 1, 0, 900], [130, 1, 0, 300], 4, 2, 128), ([64 * 9 + 1], [200], 40, 40, 64), ([2000, 1999, 40], [129, 65, 90], 3, 1, 128),
+    ([150, 400], [70, 3], 300, 300, 64)])
 def test_attend_blocks_of_rows_in_several_shares(llma, dtype, lens, rows, heads, kv, D):
     """row blocks cut between workgroups: in the middle of a page list, over several of them, next to empty sequences and short ones"""
     c, q, table, slots, off = attend_case(llma, lens, rows, heads, kv, D, dtype, 91, n_slots=len(lens) + 2, spare_rows=1)

@@ -120,7 +120,8 @@ def test_the_plain_encoding():
 
 def test_a_workspace_for_many_sequences_does_for_fewer(lib):
     for blocks in (3, 60, 4000):
-        for heads, kv, dh in ((32, 8, 128), (8, 8, 64), (64, 64, 128), (16, 1, 64)):
+        for heads, kv, dh in ((32, 8, 128), (8, 8, 64), (64, 64, 128), (16, 1, 64), (600, 300, 128)):
             for rows in (1, 9, 65, 300, 2000):
                 sizes = [llma.llma_attend_paged_mx_workspace(n, blocks, heads, kv, dh, rows) for n in (1, 2, 3, 7, 30, 64, 200)]
                 assert sizes == sorted(sizes), (blocks, heads, kv, dh, rows, sizes)
+                assert sizes[-1] < 70 << 20, (blocks, heads, kv, dh, rows, sizes)
