@@ -338,7 +338,7 @@ int llma_append_paged_mx(const llma_paged_mx_cache *cache, const void *k, const 
                          int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot_map, int32_t n_rows,
                          void *hip_stream);
 /* llma_attend_paged and llma_read_paged over it.  Scores see exactly what codes and scales stand for; so does the product with V, except that with bf16 rows, where a key head
- * has more than 64 of them, V loses bits where its scale is more than 2^15 below the largest of its page and 32 features (of positions that a row of the call sees), or more than 2^75 below 1
+ * has more than 64 of them, V loses bits where its scale is more than 2^35 below the largest of its page and 32 features (of positions that a row of the call sees), or more than 2^75 below 1
  * or another page's, all of them 2^5 further down, and probabilities do so from 2^-21 of a row's largest on, all of them at 2^-32.  A scale that stands for NaN makes the 32 features
  * of its position NaN for the rows that see it.  A workspace for some number of sequences does for fewer; it has up to some 70 MB. */
 int64_t llma_attend_paged_mx_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);

@@ -701,13 +701,15 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
 // ---- many rows -----------------------------------------------------------------------------------
 // fp16 products keep the sums of each block of 32 features in units of a power of two, `now` its exponent plus 127, so that V fits: a code of 0.5 .. 6 times 2^-23 .. 2^12 is exact in fp16.
 // A page whose largest scale of the block lies outside 2^-8 .. 2^12 units makes that the unit, but none more than 2^60 below the largest before it (up to 2^62 units may have been
-// added up, and fp32 ends at 2^128).  So V loses bits where its scale is more than 2^15 below the largest of the block in its page, or more than 2^75 below 1 or another page's (the last bit
-// 2^5 further down).
+// added up, and fp32 ends at 2^128); and where a scale of the block lies below 2^-23 units, the unit goes down until the largest is 2^12.  So V loses bits where its scale is more than 2^35 below
+// the largest of the block in its page, or more than 2^75 below 1 or another page's (the last bit 2^5 further down).
 struct BlockUnit { int now, least; };
-__device__ __forceinline__ void unit_for(int most, BlockUnit &u) {               // most: 0 for none
-    const int near = most > u.least ? most : u.least;
+__device__ __forceinline__ void unit_for(int most, int fewest, BlockUnit &u) {   // the largest scale, 0 for none, and the smallest
     const bool other = ((unsigned)(most - u.now + 8) > 20u) & (most > 0);
-    u.now = other ? near : u.now;
+    u.now = other ? most : u.now;
+    const bool wide = (fewest - u.now < -23) & (most > 0);
+    u.now = wide ? most - 12 : u.now;
+    u.now = u.now > u.least ? u.now : u.least;
     u.least = u.now - 60 > u.least ? u.now - 60 : u.least;
 }
 // as widen_v, in fp16 and in units: by[t] for the word's four positions
@@ -878,9 +880,10 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
         if (lane == 0) nan_seen[i & 1][wave] = (int)any;
         bool plain = true;                                       // units of 1, and no scale that is not one of them: the scales as they lie
         if constexpr (HALF) {
-            // (lanes of a group have the same 16 scales: each looks at four.  Bytes above 139; bytes of 119 and more)
+            // (lanes of a group have the same 16 scales: each looks at four.  Bytes above 139, from 1 to 103; bytes of 119 and more)
             const uint32_t x = col & 2 ? (col & 1 ? vs[3] : vs[2]) : (col & 1 ? vs[1] : vs[0]), low = x & 0x7f7f7f7fu;
-            plain = unit.now == 127 && __ballot((((low + 0x74747474u) & x) & 0x80808080u) != 0) == 0 && __ballot((((low + 0x09090909u) | x) & 0x80808080u) != 0) != 0;
+            const uint32_t above = (low + 0x74747474u) & x, below = ((low + 0x7f7f7f7fu) | x) & ~((low + 0x18181818u) | x);
+            plain = unit.now == 127 && __ballot(((above | below) & 0x80808080u) != 0) == 0 && __ballot((((low + 0x09090909u) | x) & 0x80808080u) != 0) != 0;
         }
         float half_by[4 * 2 * US];                               // of fp16's positions
         if constexpr (HALF) {
@@ -895,17 +898,20 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
                     half_by[4 * h + 3] = scale_byte<3>(x);
                 }
             } else {
-                uint32_t most = 0;
+                uint32_t most = 0, fewest = 254;                 // (0: a position that is not there, or 2^-127)
 #pragma unroll
                 for (int w = 0; w < 4; ++w)
 #pragma unroll
                     for (int t = 0; t < 4; ++t) {
                         const uint32_t e = vs[w] >> 8 * t & 255u;
                         most = e > most && e != 255u ? e : most;
+                        fewest = e < fewest && e != 0u ? e : fewest;
                     }
                 most = max((int)most, lane_xor<16>((int)most));
                 most = max((int)most, lane_xor<32>((int)most));
-                unit_for(uniform((int)most), unit);
+                fewest = min((int)fewest, lane_xor<16>((int)fewest));
+                fewest = min((int)fewest, lane_xor<32>((int)fewest));
+                unit_for(uniform((int)most), uniform((int)fewest), unit);
 #pragma unroll
                 for (int t = 0; t < 8 * US; ++t) {
                     const int raw = (int)byte_of(t), e = raw - unit.now + 127;

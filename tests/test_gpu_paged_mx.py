@@ -614,3 +614,17 @@ def test_prompts_captured_and_replayed(llma, dtype):
             besides[off[b]:off[b + 1]] = 2.0 ** -32 * (v.sum(0) + lens[b] * v.max(0, initial=0)).repeat(heads // H, 0)
         check_attend(llma, eager["c"], at["x"][:, :heads], table, range(B), lens, off, m, dtype, out=eager["out"], besides=besides if dtype == "bf16" else None)
         assert torch.equal(keep, eager["out"])
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("lens,rows", [([130], [130]), ([300, 64], [70, 64])])
+@pytest.mark.parametrize("rising", [True, False])
+def test_attend_values_of_very_different_sizes_in_a_page(llma, dtype, lens, rows, rising):
+    """scales of V that rise or fall by 2^31 inside each page: rows that see only its small ones have them exactly"""
+    c, q, table, slots, off = attend_case(llma, lens, rows, 4, 2, 128, dtype, 111, q_size=0.2)
+    step = torch.arange(PAGE, device="cuda").int() // 2
+    by = (step if rising else 31 - step) - 20
+    c.v_scale.copy_(torch.where(c.v_scale == 255, 255, c.v_scale.int() + by).to(torch.uint8))
+    if dtype == "fp16":                                                 # (whose outputs end at 65504)
+        c.v_scale.copy_(torch.where(c.v_scale == 255, 255, (c.v_scale.int() - 4)).to(torch.uint8))
+    check_attend(llma, c, q, table, slots, lens, off, max(rows), dtype)
