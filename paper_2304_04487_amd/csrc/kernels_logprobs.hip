@@ -99,6 +99,29 @@ __device__ __forceinline__ float maxima16(const float (&m)[N]) {
     if constexpr (BIT > 1) return maxima16<(N > 1 ? N / 2 : 1), BIT / 2>(h);
     else return h[0];
 }
+// Over the wave, op of its two halves being the same either way: four steps inside 16 lanes (moves that the operation takes along), then 16 and 32 lanes swapped for a copy's.  (Steps by lane_xor
+// need three instructions more to pick each lane's of the two, and a maximum of floats quiets both arguments first: a third of what a wave spends besides its logits)
+template <typename F>
+__device__ __forceinline__ int over_wave(int v, F op) {
+    v = op(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true));         // (eight lanes on)
+    v = op(v, __builtin_amdgcn_mov_dpp(v, 0x141, 0xf, 0xf, true));         // (eight lanes mirrored)
+    v = op(v, __builtin_amdgcn_mov_dpp(v, 0x4e, 0xf, 0xf, true));          // (two lanes on, of four; one)
+    v = op(v, __builtin_amdgcn_mov_dpp(v, 0xb1, 0xf, 0xf, true));
+    const auto a = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+    v = op((int)a[0], (int)a[1]);
+    const auto b = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+    return op((int)b[0], (int)b[1]);
+}
+__device__ __forceinline__ float sum_of_wave(float x) {
+    return __int_as_float(over_wave(__float_as_int(x), [](int a, int b) { return __float_as_int(__int_as_float(a) + __int_as_float(b)); }));
+}
+// (of numbers that are no NaN, in the order of integers; the same in all lanes)
+__device__ __forceinline__ float max_of_wave(float x) {
+    int k = __float_as_int(x);
+    k = over_wave(k ^ (k >> 31 & 0x7fffffff), [](int a, int b) { return a > b ? a : b; });
+    k = __builtin_amdgcn_readfirstlane(k);
+    return __int_as_float(k ^ (k >> 31 & 0x7fffffff));
+}
 template <typename F>
 __device__ __forceinline__ void add_over_wave(F &v) {
     butterfly<32>([&](auto o) {
@@ -130,7 +153,8 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab);
     }
-    const float T = temperature_of(a, row), hi = 1.4426950408889634f / T;
+    // (hi: any number near by will do, the part names it; one step of Newton's takes it to a rounding.  Where that leaves fp32 it is no number or 0, and the sums are taken with by itself)
+    const float T = temperature_of(a, row), near = __builtin_amdgcn_rcpf(T), about = 1.4426950408889634f * near, hi = __builtin_fmaf(__builtin_fmaf(-T, about, 1.4426950408889634f), near, about);
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool given = a.rank && (unsigned)token < (unsigned)a.vocab;
     const float xt = given ? logit_at<TYPE>(a, row, token) : 0.f;
@@ -165,14 +189,14 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
         }
     }
     if (a.n_top > 0) {
-        float *const segments = (float *)((LogprobPart *)a.work + (int64_t)a.n_rows * plan.chunks) + (int64_t)row * plan.segments + chunk * U * (64 / plan.lanes);
+        const int log_lanes = __builtin_ctz(plan.lanes);
+        float *const segments = (float *)((LogprobPart *)a.work + (int64_t)a.n_rows * plan.chunks) + (int64_t)row * plan.segments + (chunk * U << (6 - log_lanes));
         float mine = maxima16<U>(m);
         if (plan.lanes >= 32) mine = fmaxf(mine, lane_xor<16>(mine));
         if (plan.lanes >= 64) mine = fmaxf(mine, lane_xor<32>(mine));
-        const int log_lanes = __builtin_ctz(plan.lanes);
         if ((lane & (16 / U - 1)) == 0 && (lane & (plan.lanes - 1)) < 16) segments[((lane & 15) / (16 / U) << (6 - log_lanes)) + (lane >> log_lanes)] = mine;
     }
-    butterfly<32>([&](auto o) { M = fmaxf(M, lane_xor<o.value>(M)); });
+    M = max_of_wave(M);
     // ---- sums
     double R = LLMA_NEG_INF;
     float s = 0.f, sw = 0.f, taken = 0.f;
@@ -239,8 +263,8 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
             }
         }
     }
-    add_over_wave(s);
-    add_over_wave(sw);
+    s = sum_of_wave(s);
+    sw = sum_of_wave(sw);
     if (lane == 0) {
         LogprobPart t;
         t.r = R;
