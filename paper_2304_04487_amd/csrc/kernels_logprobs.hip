@@ -4,7 +4,7 @@
 // Bound by one read of the logits: each wave takes a chunk of a row, all of it in registers, and leaves (R, S, W, the rank's count): sums of 2^t and 2^t t with t = x by - R,
 // by = log2(e) / T, R near the chunk's largest x by; and the maximum of every segment (16 or more pieces that lie together).  A second launch, a wave per row, joins them in 64 bits and in a fixed
 // order.  The n_top-th largest segment maximum bounds the alternatives from below, so it reads again only segments that reach it.
-// 2000 rows of 128256 bf16, 513 MB, 20 alternatives: 107 us = 4.8 TB/s and 23 us; the same reads alone take 82, the rest of the first launch is a dozen vector instructions a logit.  Its second half (row by
+// 2000 rows of 128256 bf16, 513 MB, 20 alternatives: 103 us = 5.0 TB/s and 23 us; the same reads alone take 82, the rest of the first launch is eleven vector instructions a logit.  Its second half (row by
 // row) is the chain of bound, segments and places, and 6 KB of scattered reads a row.  Nine rows of 32000 fp32, 5 alternatives: 3.6 and 9.8 us, of which an empty launch is 2 and half the
 // fetching of code.
 #include "../../include/llma.h"
