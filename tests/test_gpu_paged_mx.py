@@ -628,3 +628,30 @@ def test_attend_values_of_very_different_sizes_in_a_page(llma, dtype, lens, rows
     if dtype == "fp16":                                                 # (whose outputs end at 65504)
         c.v_scale.copy_(torch.where(c.v_scale == 255, 255, (c.v_scale.int() - 4)).to(torch.uint8))
     check_attend(llma, c, q, table, slots, lens, off, max(rows), dtype)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("rows", [[3, 5], [100, 41]])
+@pytest.mark.parametrize("scale", [0.0, -0.125, 1e-30])
+def test_attend_scales_of_the_scores(llma, dtype, rows, scale):
+    """all positions alike, the smallest product first"""
+    lens = [170, 64]
+    c, q, table, slots, off = attend_case(llma, lens, rows, 4, 2, 128, dtype, 121, q_size=1.0)
+    check_attend(llma, c, q, table, slots, lens, off, max(rows), dtype, scale=scale)
+
+
+def test_attend_infinite_queries_and_values(llma):
+    """infinite scores, whose differences are no numbers, and NaN stay in their row and head"""
+    for rows in ([4], [100]):
+        lens = [150]
+        c, q, table, slots, off = attend_case(llma, lens, rows, 2, 2, 128, "bf16", 131, q_size=1.0)
+        out, bad = torch.full_like(q, 7.0), torch.full_like(q, 7.0)
+        args = (i32(table), i32(lens), i32(off), max(rows), 128 ** -0.5)
+        llma.llma_attend_paged_mx(c, q, *args, out, slots=i32(slots))
+        q[1, 0, 5] = float("inf")
+        q[2, 1, 9] = float("nan")
+        llma.llma_attend_paged_mx(c, q, *args, bad, slots=i32(slots))
+        same = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+        same[1, 0] = same[2, 1] = False
+        assert torch.equal(out[same], bad[same])
+        assert bad[2, 1].isnan().all() and bad[1, 0].isnan().all()
