@@ -201,7 +201,8 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
     double R = LLMA_NEG_INF;
     float s = 0.f, sw = 0.f, taken = 0.f;
     const float r = M * hi;
-    if (fabsf(M) < 1e30f && hi > 1e-20f && fabsf(r) < 4096.f) {
+    // (hi has an upper end too: LOW times it has to stay finite, or 0 times minus infinity would make the second sum NaN)
+    if (fabsf(M) < 1e30f && hi > 1e-20f && hi < 1e8f && fabsf(r) < 4096.f) {
         R = (double)r;
         taken = hi;
 #pragma unroll
