@@ -35,11 +35,11 @@ int64_t token_logprobs_bytes(int n_rows, int vocab, int n_top) {
     return (narrow > wide ? narrow : wide) + 16;
 }
 
-// T as it counts, and by = log2(e) / T in 64 bits.  The chunks' sums are taken with an fp32 number near by, whose error tilts all terms of a row alike and is put right when the parts are joined
+// T as it counts (infinite: all tokens with a logit above minus infinity alike), and by = log2(e) / T in 64 bits.  The chunks' sums are taken with an fp32 number near by, whose error tilts all
+// terms of a row alike and is put right when the parts are joined
 __device__ __forceinline__ float temperature_of(const LogprobArgs &a, int row) {
-    float t = a.temperature ? a.temperature[row] : 1.f;
-    if (!(t > 0.f)) t = 1.f;                                     // (also NaN)
-    return t > 3.402823466e38f ? 3.402823466e38f : t;
+    const float t = a.temperature ? a.temperature[row] : 1.f;
+    return t > 0.f ? t : 1.f;                                    // (NaN too)
 }
 __device__ __forceinline__ double by_of(float t) { return 1.4426950408889634074 / (double)t; }
 template <int TYPE> __device__ __forceinline__ float logit_at(const LogprobArgs &a, int64_t row, int i) {
@@ -68,11 +68,11 @@ __device__ __forceinline__ u32x4 row_piece(const RowView &v, int p, int pieces, 
     }
     return w;
 }
-// x by, rounded: where logits are so large that this rounding shows, R has it too
-__device__ __forceinline__ double times_by(float x, double by) {
+// x by, rounded: where logits are so large that this rounding shows, R has it too.  (by is 0 at an infinite temperature, where an infinite x stays that)
+__device__ __forceinline__ double times_by(double x, double by) {
 #pragma clang fp contract(off)
-    const double z = (double)x * by;
-    return z;
+    const double z = x * by;
+    return fabs(x) < __builtin_huge_val() ? z : x;
 }
 // the smallest float above x (of plus infinity: NaN, which nothing reaches)
 __device__ __forceinline__ float next_above(float x) {
@@ -153,7 +153,7 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab);
     }
-    // (hi: any number near by will do, the part names it; one step of Newton's takes it to a rounding.  Where that leaves fp32 it is no number or 0, and the sums are taken with by itself)
+    // (hi: any number near by will do, the part names it; one step of Newton's takes it to a rounding.  Where that leaves fp32, or T is infinite, it is no number or 0, and the sums are taken with by itself)
     const float T = temperature_of(a, row), near = __builtin_amdgcn_rcpf(T), about = 1.4426950408889634f * near, hi = __builtin_fmaf(__builtin_fmaf(-T, about, 1.4426950408889634f), near, about);
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool given = a.rank && (unsigned)token < (unsigned)a.vocab;
@@ -221,7 +221,7 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
 #pragma unroll
             for (int e = 0; e < EPB; ++e) {
                 const float z = fmaxf(v[e], LLMA_NEG_INF);
-                const double t = z == M ? 0. : ((double)z - (double)M) * by;
+                const double t = z == M ? 0. : times_by((double)z - (double)M, by);
                 const float y = t < -1000. ? 0.f : __builtin_amdgcn_exp2f((float)t);
                 s += y;
                 sw += y > 0.f ? y * (float)t : 0.f;
