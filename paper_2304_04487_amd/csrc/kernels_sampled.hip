@@ -15,11 +15,13 @@ __device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
     const int n = a.n_draft ? a.n_draft[b] : a.k;
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
-// an infinite temperature counts as the largest there is: 0 times minus infinity, of a masked logit, would be no weight at all
-__device__ __forceinline__ float temperature_of(const SampledArgs &a, int b) {
-    const float t = a.temperature ? a.temperature[b] : 1.f;
-    return t > 3.402823466e38f ? 3.402823466e38f : t;
-}
+__device__ __forceinline__ float temperature_of(const SampledArgs &a, int b) { return a.temperature ? a.temperature[b] : 1.f; }
+// log2(e) / T, and twice that in fp32.  An infinite T takes all logits above minus infinity alike, the type's lowest among them, where a factor of 0 would make NaN of minus infinity, a masked
+// logit, in place of no weight at all: its factors leave nothing of differences up to 2^129 (2^-71; in fp32 2^-21, which takes 4e-7 of a weight).
+__device__ __forceinline__ double by64_of(float t) { return t > 3.402823466e38f ? 0x1p-200 : 1.4426950408889634074 / (double)t; }
+__device__ __forceinline__ float twice_by(float by, float t) { return t > 3.402823466e38f ? 0x1p-149f : 2.f * by; }
+// 2^((x - top) by), by halves: a difference of finite logits does not become infinite
+__device__ __forceinline__ float part_of(float x, float top, float by2) { return __builtin_amdgcn_exp2f(__builtin_fmaf(0.5f, x, -0.5f * top) * by2); }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? LLMA_NEG_INF : x; }           // NaN: a token that cannot be
 // A row's weights e^((x - top) / T) in 64 bits, as 2^((x - top) by), by = log2(e) / T.  2^f for |f| <= 1/2 by the polynomial of degree 10 that is 1 at 0 and meets it
 // at the ten Chebyshev points of the interval (off by 6e-16 of it); a whole number is split off by adding 1.5 2^52, whose low word it becomes.
@@ -44,7 +46,6 @@ __device__ __forceinline__ double weight64(float x, const Weigher &w) {
     p = __builtin_amdgcn_ldexp(p, (int)__double_as_longlong(t));
     return w.top == -LLMA_NEG_INF && x == w.top ? 1.0 : p;
 }
-__device__ __forceinline__ double log2_scale(const SampledArgs &a, int b) { return 1.4426950408889634074 / (double)temperature_of(a, b); }
 
 struct RowPart { float top, sum; int where; };                   // of a chunk: maximum, sum of 2^((x - top) log2(e) / T), first index of the maximum
 
@@ -129,13 +130,13 @@ __global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a
         }
         butterfly<32>([&](auto o) { const int w = lane_xor<o.value>(where); where = w < where ? w : where; });
     } else {
-        const float by = 1.44269504088896340736f / temp;
+        const float by2 = twice_by(1.44269504088896340736f / temp, temp);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             float f[EPB];
             values(i, f);
 #pragma unroll
-            for (int e = 0; e < EPB; ++e) sum += __builtin_amdgcn_exp2f((f[e] - top) * by);
+            for (int e = 0; e < EPB; ++e) sum += part_of(f[e], top, by2);
         }
         if (sum != sum) {                                        // a NaN among them, or an infinite top: token by token
             sum = 0.f;
@@ -148,7 +149,7 @@ __global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a
                 for (int e = 0; e < EPB; ++e) {
                     const int id = id0 + i * ROW_THREADS * EPB + e;
                     const float l = id >= 0 && id < a.vocab ? logit_of(f[e]) : LLMA_NEG_INF;
-                    const float w = l == top ? 1.f : __builtin_amdgcn_exp2f((l - top) * by);
+                    const float w = l == top ? 1.f : part_of(l, top, by2);
                     sum += l == LLMA_NEG_INF ? 0.f : w;
                 }
             }
@@ -245,8 +246,8 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
     }
     const int n_draft = drafts_of(a, b);
     const bool greedy = !(temp > 0.f);
-    const double by64 = greedy ? 0.0 : 1.4426950408889634074 / (double)temp;
-    const float by = (float)by64;
+    const double by64 = greedy ? 0.0 : by64_of(temp);
+    const float by2 = twice_by((float)by64, temp);
     const bool fits = tested && (unsigned)draft < (unsigned)a.vocab;
     const float logit = fits ? logit_at<TYPE>(a, row, draft) : 0.f;
     if (fits && a.probs) q = a.probs[((int64_t)b * a.k + lane) * a.vocab + draft];
@@ -260,7 +261,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
 #pragma unroll
         for (int c = 0; c < 8; ++c) here = fmaxf(here, x[c].top);
         // (a top that is infinite counts 1 by itself and leaves nothing to lower ones)
-        sum *= top == here ? 1.f : __builtin_amdgcn_exp2f((top - here) * by);
+        sum *= top == here ? 1.f : part_of(top, here, by2);
         if (top != here) where = 0x7fffffff;
         if (top == LLMA_NEG_INF) sum = 0.f;
         top = here;
@@ -268,7 +269,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
         for (int c = 0; c < 8; ++c) {
             if (c0 + c >= plan.chunks) continue;
             if (x[c].top == here && x[c].where < where) where = x[c].where;
-            if (x[c].top > LLMA_NEG_INF) sum += x[c].sum * (x[c].top == here ? 1.f : __builtin_amdgcn_exp2f((x[c].top - here) * by));
+            if (x[c].top > LLMA_NEG_INF) sum += x[c].sum * (x[c].top == here ? 1.f : part_of(x[c].top, here, by2));
         }
     }
     double left = 0.0, right = 0.0;                              // u q sum < e
@@ -369,7 +370,7 @@ __global__ __launch_bounds__(256) void sampled_pick_kernel(SampledArgs a, Sample
         }
     }
     if (c.greedy) return;
-    const Weigher weigh = weigher(c.top, log2_scale(a, b));
+    const Weigher weigh = weigher(c.top, by64_of(temperature_of(a, b)));
     const RowView v = row_view<TYPE>(a, c.row);
     const int blocks = (v.skip + a.vocab + EPB - 1) / EPB;
     const bool minus = PASS == 1 || (a.probs == nullptr && c.residual);
@@ -421,7 +422,7 @@ __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, Samp
     const Choice c = ((const Choice *)((const char *)a.work + plan.at_choice))[b];
     const double all0 = t < plan.picks ? base[t] : 0.0, left0 = a.probs && t < plan.picks ? base[plan.picks + t] : 0.0;
     const double u = (double)a.u_sample[b];
-    const Weigher weigh = weigher(c.top, log2_scale(a, b));
+    const Weigher weigh = weigher(c.top, by64_of(temperature_of(a, b)));
     const int draft = t < a.k ? a.drafts[(int64_t)b * a.draft_stride + t] : -1;
     int token = -1;
     if (c.greedy) {
