@@ -1193,9 +1193,11 @@ template <int TYPE> constexpr int rows_nt = TYPE == ROWS_F32 ? 1 : 2;           
 //   bf16  21.9 26.7           31.0 35.4            47.8 57.8             54.5 130.3            18.7 28.3             25.8 29.0            12.6 18.9          36.3 27.3            44.0 25.6
 //   fp16  25.2 27.5           34.5 37.2            56.7 61.8             73.0 140.3            24.3 29.6             27.5 30.5            13.1 19.9          38.5 29.0            46.5 27.3
 //   fp32  23.2 29.9           33.5 43.3            60.8 73.6             87.0 167.3            17.3 36.0             31.1 34.0            11.9 21.9          36.4 32.8            37.0 31.3
+#define ROWS_BLOCKS (1 << 23)    // of a launch: fewer
+static int64_t rows_blocks(int n_seqs, int n_heads, int kv_heads, int max_rows, int rows) { return ((int64_t)max_rows * (n_heads / kv_heads) + rows - 1) / rows * n_seqs * kv_heads; }
 static bool takes_rows(int n_seqs, int n_heads, int kv_heads, int dh, int max_rows, int rows) {
-    const int64_t group_rows = (int64_t)max_rows * (n_heads / kv_heads), blocks = (group_rows + rows - 1) / rows * n_seqs * kv_heads;
-    return group_rows > 64 && (dh == 128 || blocks * rows >= 6144) && blocks < 1 << 23;
+    const int64_t blocks = rows_blocks(n_seqs, n_heads, kv_heads, max_rows, rows);
+    return (int64_t)max_rows * (n_heads / kv_heads) > 64 && (dh == 128 || blocks * rows >= 6144) && blocks < ROWS_BLOCKS;
 }
 template <int DH, int TYPE>
 static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
@@ -1211,11 +1213,13 @@ static void launch_attend_type(const AttendMxArgs &a, hipStream_t st) {
 int64_t attend_paged_mx_bytes(int n_seqs, int max_blocks, int n_heads, int kv_heads, int dh, int max_rows) {
     int64_t most = attend_bytes(attend_mx_plan(n_seqs, max_blocks, n_heads, kv_heads, max_rows), n_seqs, kv_heads, dh);
     for (int rows = 64; rows <= 128; rows += 64) {               // (fp32's row blocks, the others')
-        if (!takes_rows(n_seqs, n_heads, kv_heads, dh, max_rows, rows)) continue;
-        // (as if cut, whether it is or not: a workspace for some number of sequences does for fewer, which may be cut where more are not)
+        // (a workspace for some number of sequences does for fewer: for the most that take this form, where more do not, and as if cut, where more are not)
+        const int64_t many = (ROWS_BLOCKS - 1) / rows_blocks(1, n_heads, kv_heads, max_rows, rows);
+        const int taken = many < n_seqs ? (int)many : n_seqs;
+        if (!takes_rows(taken, n_heads, kv_heads, dh, max_rows, rows)) continue;
         RowsPlan p = rows_plan(1, max_blocks, n_heads, kv_heads, max_rows, rows);
         if (p.blocks > ROWS_LISTED) continue;
-        const int listed = n_seqs < ROWS_LISTED / p.blocks ? n_seqs : ROWS_LISTED / p.blocks;
+        const int listed = taken < ROWS_LISTED / p.blocks ? taken : ROWS_LISTED / p.blocks;
         p.shares = 2 * ATTEND_CUS / kv_heads > 0 ? 2 * ATTEND_CUS / kv_heads : 1;
         const int64_t bytes = (rows_head(p, listed) + (p.shares > 1 ? rows_parts(p, kv_heads) * rows * (dh + 2) : 0)) * 4;       // (one share a key head cuts nothing)
         most = bytes > most ? bytes : most;
