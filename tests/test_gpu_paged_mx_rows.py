@@ -4,7 +4,7 @@ import numpy as np
 import pytest
 import torch
 
-from test_gpu_paged_mx import DT, PAGE, attend_case, check_attend, i32, llma  # noqa: F401
+from test_gpu_paged_mx import DT, HALF, PAGE, attend_case, cached, check_attend, i32, llma, random_cache  # noqa: F401
 
 pytestmark = pytest.mark.gpu
 
@@ -125,3 +125,68 @@ def test_blocks_of_rows_in_several_shares(llma, dtype, lens, rows, D, heads, kv)
     w = Work(llma, lens, rows, q, c, table, dtype)
     check_attend(llma, c, q, table, slots, lens, off, max(rows), dtype, workspace=w.ints)
     w.check()
+
+
+# ------------------------------------------------------------------------------------------------ long sequences in one share
+def long_case(llma, lens, rows, kv, D, dtype, seed):  # noqa: F811
+    """as many query as key heads; pages of all sequences in a random order, some of them none"""
+    rng = np.random.default_rng(seed)
+    need = [(n + PAGE - 1) // PAGE for n in lens]
+    P, blocks = sum(need), max(need)
+    c = random_cache(llma, P, kv, D, seed, nans=False)
+    perm, table = rng.permutation(P), np.full((len(lens), blocks), -1)
+    for b, n in enumerate(need):
+        table[b, :n] = perm[sum(need[:b]):sum(need[:b + 1])]
+    table[0, [3, need[0] // 2]] = -1, P
+    off = np.concatenate([[0], np.cumsum(rows)])
+    q = torch.tensor(0.02 * rng.standard_normal((off[-1], kv, D)), dtype=torch.float32).to(DT[dtype]).cuda()
+    return c, q, table, off
+
+
+def check_heads(got, c, q, table, lens, off, dtype, heads):
+    """some heads against 64 bits; tolerances as where all of a call is compared"""
+    part = type(c)(*(t[:, heads].contiguous() for t in (c.k, c.v, c.k_scale, c.v_scale)))
+    kv, vv = cached(part)
+    D = q.shape[2]
+    x, y = q[:, heads].double().cpu().numpy(), got[:, heads].double().cpu().numpy()
+    for b, n in enumerate(lens):
+        m = off[b + 1] - off[b]
+        pages = table[b, :(n + PAGE - 1) // PAGE]
+        have = ((pages >= 0) & (pages < len(kv))).repeat(PAGE)[:n]
+        idx = np.where((pages >= 0) & (pages < len(kv)), pages, 0)
+        sees = have[None] & (np.arange(n)[None] <= n - m + np.arange(m)[:, None])
+        for h in range(len(heads)):
+            K, V = (a[idx, h].reshape(-1, D)[:n] for a in (kv, vv))
+            Q = x[off[b]:off[b + 1], h]
+            s = np.where(sees, Q @ K.T * D ** -0.5, -np.inf)
+            p = np.exp(s - s.max(1, keepdims=True))
+            p /= p.sum(1, keepdims=True)
+            want, size = p @ V, p @ np.abs(V)
+            big = np.where(sees, np.abs(Q) @ np.abs(K).T, 0).max(1) * D ** -0.5
+            p_err = 2 * (D + 4) * 2.0 ** -24 * big + 2.0 ** -20 + {"bf16": 2.0 ** -11, "fp16": 2.0 ** -16, "fp32": 2.0 ** -24}[dtype]
+            tol = (1 + 2.0 ** -7) * size * (p_err + 2 * n * 2.0 ** -24)[:, None] + HALF[dtype] * np.abs(want) + (2.0 ** -25 if dtype == "fp16" else 1e-30)
+            worst = (np.abs(y[off[b]:off[b + 1], h] - want) / tol).max()
+            assert worst <= 1.0, (b, heads[h], worst)
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("kv,D,lens,rows", [(512, 64, [64 * 200 + 1], [140]), (256, 128, [64 * 300 + 5], [300]), (512, 64, [64 * 66, 64 * 131 + 9], [140, 131])])
+def test_blocks_of_many_rows_over_long_sequences(llma, dtype, kv, D, lens, rows):  # noqa: F811
+    """a share has more than 128 pages of a block, whose page numbers come 64 at a time: with one share a key head from the block's first page on, with two also from a page inside"""
+    c, q, table, off = long_case(llma, lens, rows, kv, D, dtype, 141)
+    w = Work(llma, lens, rows, q, c, table, dtype)
+    got = llma.llma_attend_paged_mx(c, q, i32(table), i32(lens), i32(off), max(rows), D ** -0.5, torch.full_like(q, 7.0), workspace=w.ints)
+    w.check()
+    assert (w.size < 1 << 16) == (kv == 512)                            # (parts only where a key head has two shares)
+    check_heads(got, c, q, table, lens, off, dtype, [0, kv // 2 + 1, kv - 1])
+
+
+@pytest.mark.parametrize("dtype", list(DT))
+@pytest.mark.parametrize("kv,D,lens,rows", [(512, 64, [64 * 601 + 9], [3]), (512, 64, [64 * 270 + 5, 64 * 300], [3, 2]), (512, 64, [64 * 520 + 1], [30]), (512, 64, [64 * 300 + 2], [50]), (512, 128, [64 * 270], [1])])
+def test_steps_over_long_sequences_in_one_share(llma, dtype, kv, D, lens, rows):  # noqa: F811
+    """the steps' form with more than 256 pages of a sequence in a share, whose page numbers come 64 a wave at a time"""
+    c, q, table, off = long_case(llma, lens, rows, kv, D, dtype, 143)
+    size = llma.llma_attend_paged_mx_workspace(len(lens), table.shape[1], kv, kv, D, max(rows))
+    assert size == 256                                                  # (no parts: a key head has one share)
+    got = llma.llma_attend_paged_mx(c, q, i32(table), i32(lens), i32(off), max(rows), D ** -0.5, torch.full_like(q, 7.0))
+    check_heads(got, c, q, table, lens, off, dtype, [0, kv // 2 + 1, kv - 1])
