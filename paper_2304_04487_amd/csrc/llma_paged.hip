@@ -169,6 +169,7 @@ static int attend_call(const C *cache, const void *q, int32_t dtype, int32_t n_h
     if (!aligned(q) || !aligned(out) || !stride_ok(q_row_stride, es) || !stride_ok(q_head_stride, es) || !stride_ok(out_row_stride, es) || !stride_ok(out_head_stride, es))
         return refuse(LLMA_E_INVAL, "%s: rows must be 16-byte aligned (pointers and strides)", who);
     if (out == q) return refuse(LLMA_E_INVAL, "%s: out is q", who);
+    if (scale != scale) return refuse(LLMA_E_INVAL, "%s: scale is NaN", who);
     // (rows of q may lie on top of each other, rows of out may not)
     if (!rows_apart(n_rows, n_heads, cache->head_dim, out_row_stride, out_head_stride)) return refuse(LLMA_E_INVAL, "%s: rows of out overlap", who);
     const int64_t need = bytes(n_seqs, max_blocks, n_heads, cache->n_kv_heads, cache->head_dim, max_rows);
