@@ -733,8 +733,8 @@ static RowsPlan rows_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads,
     int64_t shares = 2 * ATTEND_CUS / kv_heads;
     shares = shares < 1 ? 1 : shares;
     const bool small = max_blocks <= 8 && listed * kv_heads >= 128;      // (blocks enough, and so short that a share's several starts cost more than an uneven end)
-    // (pages of the list are counted in 32 bits)
-    p.shares = listed > ROWS_LISTED || pages > 0x7fffffff || small ? 0 : (int)(shares < most ? shares : most);
+    // (pages of the list, and those up to the last share's end, are counted in 32 bits)
+    p.shares = listed > ROWS_LISTED || pages > 0x7fffffff - 2 * ATTEND_CUS || small ? 0 : (int)(shares < most ? shares : most);
     return p;
 }
 // work: [pages before every block of the list, rounded up to 64 ints][parts' O][parts' m][parts' l]
