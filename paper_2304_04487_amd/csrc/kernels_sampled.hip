@@ -16,10 +16,11 @@ __device__ __forceinline__ int drafts_of(const SampledArgs &a, int b) {
     return n < 0 ? 0 : n > a.k ? a.k : n;
 }
 __device__ __forceinline__ float temperature_of(const SampledArgs &a, int b) { return a.temperature ? a.temperature[b] : 1.f; }
-// log2(e) / T, and twice that in fp32.  An infinite T takes all logits above minus infinity alike, the type's lowest among them, where a factor of 0 would make NaN of minus infinity, a masked
-// logit, in place of no weight at all: its factors leave nothing of differences up to 2^129 (2^-71; in fp32 2^-21, which takes 4e-7 of a weight).
-__device__ __forceinline__ double by64_of(float t) { return t > 3.402823466e38f ? 0x1p-200 : 1.4426950408889634074 / (double)t; }
-__device__ __forceinline__ float twice_by(float by, float t) { return t > 3.402823466e38f ? 0x1p-149f : 2.f * by; }
+// log2(e) / T, and twice that in fp32.  An infinite T takes all logits above minus infinity alike, the type's lowest among them, where a factor of 0 would make NaN of
+// minus infinity, a masked logit, in place of no weight at all: its factors leave nothing of differences up to 2^129 (2^-71; in fp32 2^-21, which takes 4e-7 of a
+// weight).
+__device__ __forceinline__ double by64_of(float t) { return fmax(1.4426950408889634074 / (double)t, 0x1p-200); }
+__device__ __forceinline__ float twice_by(float by) { return fmaxf(2.f * by, 0x1p-149f); }
 // 2^((x - top) by), by halves: a difference of finite logits does not become infinite
 __device__ __forceinline__ float part_of(float x, float top, float by2) { return __builtin_amdgcn_exp2f(__builtin_fmaf(0.5f, x, -0.5f * top) * by2); }
 __device__ __forceinline__ float logit_of(float x) { return x != x ? LLMA_NEG_INF : x; }           // NaN: a token that cannot be
@@ -130,7 +131,7 @@ __global__ __launch_bounds__(ROW_THREADS) void sampled_rows_kernel(SampledArgs a
         }
         butterfly<32>([&](auto o) { const int w = lane_xor<o.value>(where); where = w < where ? w : where; });
     } else {
-        const float by2 = twice_by(1.44269504088896340736f / temp, temp);
+        const float by2 = twice_by(1.44269504088896340736f / temp);
 #pragma unroll
         for (int i = 0; i < NB; ++i) {
             float f[EPB];
@@ -226,10 +227,10 @@ __device__ __forceinline__ float logit_at(const SampledArgs &a, int64_t row, int
     else return logit_of(bf16_to_f32(((const bf16_t *)a.logits)[at]));
 }
 
-// How many drafts of sequence b hold, and which row its token comes from.  All threads of a workgroup call it and get the same; lane j looks at
-// row j.  The sums of the rows' chunks are fp32: a test whose sides are nearer than 3e-5 of each other, and 2^-24 for each chunk, is decided
-// again with the row's sum in 64 bits.  (A chunk's sum is off by 5e-6 at most: 2e-7 of the exponent, which is up to 17 where weights still matter, 64 addends a thread, and its factor; each chunk
-// that is added rounds the sum by half of 2^-23.  A row has up to 4096.)
+// How many drafts of sequence b hold, and which row its token comes from.  All threads of a workgroup call it and get the same; lane j looks at row j.  The sums of the
+// rows' chunks are fp32: a test whose sides are nearer than 3e-5 of each other, and 2^-24 for each chunk, is decided again with the row's sum in 64 bits.  (A chunk's
+// sum is off by 5e-6 at most: 2e-7 of the exponent, which is up to 17 where weights still matter, 64 addends a thread, and its factor; each chunk that is added rounds
+// the sum by half of 2^-23.  A row has up to 4096.)
 template <int TYPE>
 __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, double *part) {
     const int lane = threadIdx.x & 63;
@@ -247,7 +248,7 @@ __device__ Choice decide(const SampledArgs &a, const SampledPlan &plan, int b, d
     const int n_draft = drafts_of(a, b);
     const bool greedy = !(temp > 0.f);
     const double by64 = greedy ? 0.0 : by64_of(temp);
-    const float by2 = twice_by((float)by64, temp);
+    const float by2 = twice_by((float)by64);
     const bool fits = tested && (unsigned)draft < (unsigned)a.vocab;
     const float logit = fits ? logit_at<TYPE>(a, row, draft) : 0.f;
     if (fits && a.probs) q = a.probs[((int64_t)b * a.k + lane) * a.vocab + draft];
@@ -410,7 +411,8 @@ __device__ __forceinline__ int first_of(bool hit, bool some, double at, int id, 
     return best < 0 ? 0 : is_hit ? 2 : 1;
 }
 // A workgroup per sequence: the range the random number falls into, then the token in it.  Bound by its chain: the choice and the ranges' sums, a scan, the range's
-// pieces (8 or 16 exponentials a thread), a scan.  With separate sums and scans, and atomics that look for the first hit, one sequence over 32000 tokens took 9.8 us where it takes 4.1.
+// pieces (8 or 16 exponentials a thread), a scan.  With separate sums and scans, and atomics that look for the first hit, one sequence over 32000 tokens took 9.8 us
+// where it takes 4.1.
 template <int TYPE>
 __global__ __launch_bounds__(256) void sampled_finish_kernel(SampledArgs a, SampledPlan plan) {
     constexpr int EPB = sampled_epb<TYPE>, PER = PICK_BLOCKS / 256;
