@@ -278,9 +278,10 @@ typedef struct {
  * Outputs: row_offsets[n_seqs+1] (sums of rows), lens_after[n_seqs] = lens + rows; for row i of sequence b, at row_offsets[b] + i:
  * row_pos = lens + i and slot_map = 64 * page + position in the page; entries behind the last row up to max_rows: 0 and -1.
  * With max_rows = 0 no row is mapped: slot_map and row_pos may be NULL, rows may be any, and all else is written as it is with a map.
- * *status: 0; the number of pages that were missing (2^31 - 1: as many or more); or a negative LLMA_E_* (INVAL: a negative length, a slot listed twice, counts that do not fit the table or the stack; RANGE: a slot outside [0, n_slots),
- * more than max_blocks pages, max_rows rows (unless that is 0) or 2^31 - 1).  Unless it is 0, table, owned and the stack stay as they were and
- * the call describes a step without rows.  lens_after may not be lens.  n_slots <= 65536. */
+ * *status: 0; the number of pages that were missing (2^31 - 1: as many or more); or a negative LLMA_E_* (INVAL: a negative length, a
+ * slot listed twice, counts that do not fit the table or the stack; RANGE: a slot outside [0, n_slots), more than max_blocks pages,
+ * max_rows rows (unless that is 0) or 2^31 - 1).  Unless it is 0, table, owned and the stack stay as they were and the call describes a
+ * step without rows.  lens_after may not be lens.  n_slots <= 65536. */
 int llma_map_pages(const int32_t *lens, const int32_t *rows, const int32_t *slots, int32_t n_seqs, int32_t n_slots,
                    int32_t *table, int32_t max_blocks, int32_t *owned, int32_t *free_pages, int32_t *n_free, int32_t n_pages,
                    int32_t *row_offsets, int32_t *lens_after, int32_t *slot_map, int32_t *row_pos, int32_t max_rows,
@@ -289,9 +290,9 @@ int llma_map_pages(const int32_t *lens, const int32_t *rows, const int32_t *slot
 /* Writes rows into the cache.  k, v: n_rows x n_kv_heads x head_dim values of dtype (LLMA_DTYPE_*), strides in elements
  * (features contiguous; pointers and strides multiples of 16 bytes); row i goes to slot_map[i], rows whose slot is negative or
  * no page's nowhere.  A run is a stretch of rows with consecutive slots inside one page; a call may have one run per page.  The
- * run's scale, per head, for K and for V: the smallest power of two (from 2^-64 to 2^120) s with max |x| / s <= 448 over its finite values; a run that
- * starts behind its page's first position keeps the page's scale where that is larger, and where s is larger the codes before
- * the run are rounded again to s.  Codes are x / s rounded to nearest even; +-inf become +-448, NaN stays NaN.  Codes
+ * run's scale, per head, for K and for V: the smallest power of two (from 2^-64 to 2^120) s with max |x| / s <= 448 over its finite
+ * values; a run that starts behind its page's first position keeps the page's scale where that is larger, and where s is larger the
+ * codes before the run are rounded again to s.  Codes are x / s rounded to nearest even; +-inf become +-448, NaN stays NaN.  Codes
  * behind the run stay as they are. */
 int llma_append_paged(const llma_paged_cache *cache, const void *k, const void *v, int32_t dtype, int64_t k_row_stride,
                       int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot_map, int32_t n_rows,
@@ -300,10 +301,12 @@ int llma_append_paged(const llma_paged_cache *cache, const void *k, const void *
 /* Causal attention of a step's rows over the cache.  Rows row_offsets[b] .. row_offsets[b+1]-1 of q are sequence b's; row j of
  * m sees positions 0 .. lens[b] - m + j of the pages table[slots[b]] (lens counts the step's own rows, which
  * llma_append_paged has written).  out = softmax(scale * q K^T) V per head; query head h reads key head h / (n_heads /
- * n_kv_heads).  q, out: n_rows x n_heads x head_dim of dtype, strides in elements, pointers and strides multiples of 16 bytes; rows of out may overlap neither each other nor q.
- * max_rows: at least the rows of every sequence (a sequence's further rows are not written); rows behind the last sequence's stay as they are.
- * A scale that is NaN is refused.  A row that sees nothing becomes 0.  Positions whose page number is outside [0, n_pages) are not seen.  Scales are taken as the powers of two that they
- * are; with bf16 rows, pages whose v_scale is more than 2^75 below another's of the sequence and head may count as zeros.
+ * n_kv_heads).  q, out: n_rows x n_heads x head_dim of dtype, strides in elements, pointers and strides multiples of 16 bytes; rows of
+ * out may overlap neither each other nor q.  A scale that is NaN is refused.  max_rows: at least the rows of every sequence (a sequence's
+ * further rows are not written); rows behind the last sequence's stay as they are.
+ * A row that sees nothing becomes 0.  Positions whose page number is outside [0, n_pages) are not seen.  The cache's scales are taken as
+ * the powers of two that they are; with bf16 rows, pages whose v_scale is more than 2^75 below another's of the sequence and head may
+ * count as zeros.
  * work: llma_attend_paged_workspace(...) bytes, 16-byte aligned. */
 int64_t llma_attend_paged_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);
 int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtype, int32_t n_heads, int64_t q_row_stride,
@@ -311,10 +314,10 @@ int llma_attend_paged(const llma_paged_cache *cache, const void *q, int32_t dtyp
                       const int32_t *lens, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, int32_t max_rows, float scale,
                       void *out, int64_t out_row_stride, int64_t out_head_stride, void *work, int64_t work_bytes, void *hip_stream);
 
-/* Rows out of the cache: row row_offsets[b] + j (below row_offsets[b+1]) of k and v becomes position first[b] + j (first NULL: 0) of the pages
- * table[slots[b]], all heads, in dtype (code * scale, rounded once).  For a cache in planes (llma_kv_import takes rows head by head: any strides will
- * do), for another program, for a look at what is cached.  k and v as llma_append_paged takes them, but not the same memory and without
- * rows on top of each other.  Positions outside the table, and those whose page number is outside [0, n_pages), read as 0; rows behind the
+/* Rows out of the cache: row row_offsets[b] + j (below row_offsets[b+1]) of k and v becomes position first[b] + j (first NULL: 0) of the
+ * pages table[slots[b]], all heads, in dtype (code * scale, rounded once).  For a cache in planes (llma_kv_import takes rows head by
+ * head: any strides will do), for another program, for a look at what is cached.  k and v as llma_append_paged takes them, but not the
+ * same memory and without rows on top of each other.  Positions outside the table, and those whose page number is outside [0, n_pages), read as 0; rows behind the
  * last sequence's stay as they are.  n_seqs <= LLMA_PAGED_MAX_SEQS, n_rows * n_kv_heads <= 2^28. */
 int llma_read_paged(const llma_paged_cache *cache, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,
                     const int32_t *first, const int32_t *row_offsets, int32_t n_seqs, int32_t n_rows, void *k, void *v, int32_t dtype,
@@ -330,17 +333,19 @@ typedef struct {
     int32_t n_pages, n_kv_heads, head_dim;
 } llma_paged_mx_cache;
 
-/* Writes rows into the 4-bit cache; arguments as llma_append_paged has them.  Every row has scales of its own: per 32 features the smallest power of
- * two (from 2^-64 to 2^120) s with max |x| / s <= 7 over the finite values; codes are x / s rounded to nearest even, +-6 beyond; +-inf become
- * +-6, a NaN makes its 32 features NaN.  So a write changes nothing but its rows' positions, and rows may come in any
+/* Writes rows into the 4-bit cache; arguments as llma_append_paged has them.  Every row has scales of its own: per 32 features the
+ * smallest power of two (from 2^-64 to 2^120) s with max |x| / s <= 7 over the finite values; codes are x / s rounded to nearest even,
+ * +-6 beyond; +-inf become +-6, a NaN makes its 32 features NaN.  So a write changes nothing but its rows' positions, and rows may come in any
  * order; the position of a slot listed twice ends with some codes and scales of one row and some of the other. */
 int llma_append_paged_mx(const llma_paged_mx_cache *cache, const void *k, const void *v, int32_t dtype, int64_t k_row_stride,
                          int64_t k_head_stride, int64_t v_row_stride, int64_t v_head_stride, const int32_t *slot_map, int32_t n_rows,
                          void *hip_stream);
-/* llma_attend_paged and llma_read_paged over it.  Scores see exactly what codes and scales stand for; so does the product with V, except that with bf16 rows, where a key head
- * has more than 64 of them, V loses bits where its scale is more than 2^35 below the largest of its page and 32 features (of positions that a row of the call sees), or more than 2^75 below 1
- * or another page's, all of them 2^5 further down, and probabilities do so from 2^-21 of a row's largest on, all of them at 2^-32.  A scale that stands for NaN makes the 32 features
- * of its position NaN for the rows that see it.  A workspace for some number of sequences does for fewer; it has up to some 70 MB. */
+/* llma_attend_paged and llma_read_paged over it.  Scores see exactly what codes and scales stand for; so does the product with V, except
+ * that with bf16 rows, where max_rows * n_heads / n_kv_heads is more than 64, probabilities have 11 bits (from 2^-21 of a row's largest
+ * on fewer, none at 2^-32) and V loses bits where its scale is more than 2^35 below the largest of its page and 32 features (of positions
+ * that a row of the call sees), or more than 2^75 below 1 or another page's, all of them 2^5 further down.  A scale that stands for NaN
+ * makes the 32 features of its position NaN for the rows that see it.  A workspace for some number of sequences does for fewer; it has up
+ * to some 70 MB. */
 int64_t llma_attend_paged_mx_workspace(int32_t n_seqs, int32_t max_blocks, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows);
 int llma_attend_paged_mx(const llma_paged_mx_cache *cache, const void *q, int32_t dtype, int32_t n_heads, int64_t q_row_stride,
                          int64_t q_head_stride, const int32_t *table, const int32_t *slots, int32_t n_slots, int32_t max_blocks,
@@ -358,7 +363,8 @@ int llma_read_paged_mx(const llma_paged_mx_cache *cache, const int32_t *table, c
  * the sum.  u in [0, 1).  temperature NULL: 1; not above 0: the arg max, lowest id on ties, as llma_verify_step has it;
  * infinite: all tokens with a logit above minus infinity alike.
  * NaN logits count as minus infinity; drafts outside [0, vocab) are rejected.  vocab <= 2^24, n_seqs * (k + 1) <= 2^22, else RANGE.
- * Outputs: n_accepted[b] = a, next_token[b] (-1: a row without a logit above minus infinity), emitted[b][0 .. k]: the accepted drafts, the next token, then -1. */
+ * Outputs: n_accepted[b] = a, next_token[b] (-1: a row without a logit above minus infinity), emitted[b][0 .. k]: the accepted drafts, the
+ * next token, then -1. */
 int64_t llma_verify_sampled_workspace(int32_t n_seqs, int32_t k, int32_t vocab);
 int llma_verify_sampled(const void *logits, int32_t dtype, int64_t row_stride, int32_t vocab, int32_t n_seqs, int32_t k,
                         const int32_t *drafts, const int32_t *n_draft, const float *draft_probs, const float *temperature,
@@ -370,10 +376,11 @@ int llma_verify_sampled(const void *logits, int32_t dtype, int64_t row_stride, i
  *   logprob[i]  log p of tokens[i] (minus infinity where p is 0, and for a token outside [0, vocab))
  *   rank[i]     tokens before it by falling logit, ties by rising id: 0 for the arg max; -1 for a token outside [0, vocab)
  *   entropy[i]  -sum p log p
- *   top_tokens, top_logprobs [i][0 .. n_top): the first n_top tokens of that order and their log p; -1 and minus infinity behind the last with a logit above it
+ *   top_tokens, top_logprobs [i][0 .. n_top): the first n_top tokens of that order and their log p; -1 and minus infinity behind the
+ *               last with a logit above it
  * (natural logarithms; logprob, rank, entropy may be NULL, tokens too without the first two; the alternatives are n_top > 0's, at most
- * LLMA_LOGPROBS_MAX_TOP).  NaN logits count as minus infinity, several plus infinities share the probability.  A row without a logit above minus infinity:
- * entropy 0, no alternatives.  vocab <= 2^24, n_rows <= 2^22, both together 2^40, else RANGE.
+ * LLMA_LOGPROBS_MAX_TOP).  NaN logits count as minus infinity, several plus infinities share the probability.  A row without a logit
+ * above minus infinity: entropy 0, no alternatives.  vocab <= 2^24, n_rows <= 2^22, both together 2^40, else RANGE.
  * work: llma_token_logprobs_workspace(...) bytes, 16-byte aligned. */
 int64_t llma_token_logprobs_workspace(int32_t n_rows, int32_t vocab, int32_t n_top);
 int llma_token_logprobs(const void *logits, int32_t dtype, int64_t row_stride, int32_t vocab, int32_t n_rows, const int32_t *tokens,

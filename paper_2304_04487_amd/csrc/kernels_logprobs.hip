@@ -1,12 +1,12 @@
 // Log probabilities of given tokens, with the distribution's entropy, the tokens' ranks and the likeliest alternatives.
 //   p = softmax(x / T);  log p(t) = (x_t - M) / T - ln S,  H = ln S - (W / S) / T  with M = max x, S = sum e^((x - M) / T), W = sum e^((x - M) / T) (x - M);
 //   rank = tokens before t in the order of falling logits, ties by rising id, whose first n_top are the alternatives.
-// Bound by one read of the logits: each wave takes a chunk of a row, all of it in registers, and leaves (R, S, W, the rank's count): sums of 2^t and 2^t t with t = x by - R,
-// by = log2(e) / T, R near the chunk's largest x by; and the maximum of every segment (16 or more pieces that lie together).  A second launch, a wave per row, joins them in 64 bits and in a fixed
-// order.  The n_top-th largest segment maximum bounds the alternatives from below, so it reads again only segments that reach it.
-// 2000 rows of 128256 bf16, 513 MB, 20 alternatives: 103 us = 5.0 TB/s and 23 us; the same reads alone take 82, the rest of the first launch is eleven vector instructions a logit.  Its second half (row by
-// row) is the chain of bound, segments and places, and 6 KB of scattered reads a row.  Nine rows of 32000 fp32, 5 alternatives: 3.6 and 9.8 us, of which an empty launch is 2 and half the
-// fetching of code.
+// Bound by one read of the logits: each wave takes a chunk of a row, all of it in registers, and leaves (R, S, W, the rank's count): sums of 2^t and 2^t t with t = x
+// by - R, by = log2(e) / T, R near the chunk's largest x by; and the maximum of every segment (16 or more pieces that lie together).  A second launch, a wave per row,
+// joins them in 64 bits and in a fixed order.  The n_top-th largest segment maximum bounds the alternatives from below, so it reads again only segments that reach it.
+// 2000 rows of 128256 bf16, 513 MB, 20 alternatives: 103 us = 5.0 TB/s and 23 us; the same reads alone take 82, the rest of the first launch is eleven vector
+// instructions a logit.  Its second half (row by row) is the chain of bound, segments and places, and 6 KB of scattered reads a row.  Nine rows of 32000 fp32, 5
+// alternatives: 3.6 and 9.8 us, of which an empty launch is 2 and half the fetching of code.
 #include "../../include/llma.h"
 #include "row_pieces.h"
 
@@ -15,12 +15,12 @@
 #define TOP_FEW 24               // alternatives
 #define TOP_AHEAD 4              // pieces a lane requests at once when it looks for them
 #define TOP_LIST 1024            // segments whose maxima a wave keeps in registers, and looks through at a time
-#define LOW (-1e30f)             // logits are raised to this where only sums and maxima are meant: it ends fewer sums in NaN than minus infinity, and NaN goes with it
+#define LOW (-1e30f)             // logits are raised to this where only sums and maxima are meant: its products stay finite where minus infinity would end sums in NaN, and NaN goes with it
 
 struct LogprobPlan { int u, lanes, chunks, segments; };          // pieces a lane; lanes of a segment; chunks and segments of a row
 static LogprobPlan logprob_plan(int n_rows, int vocab, int epb) {
     const int pieces = (vocab + epb - 1) / epb + 1;
-    LogprobPlan p{4, 16, 0, 0};                                  // (2000 rows of 128256 bf16: eight 122 us, four 112, two 159)
+    LogprobPlan p{4, 16, 0, 0};                                  // (2000 rows of 128256 bf16, both launches: eight 127 us, four 122, two 148)
     const auto chunks = [&] { return (pieces + CHUNK_PIECES(p.u) - 1) / CHUNK_PIECES(p.u); };
     while (p.u > 1 && (int64_t)n_rows * chunks() < 4096) p.u /= 2;
     p.chunks = chunks();
@@ -35,8 +35,8 @@ int64_t token_logprobs_bytes(int n_rows, int vocab, int n_top) {
     return (narrow > wide ? narrow : wide) + 16;
 }
 
-// T as it counts (infinite: all tokens with a logit above minus infinity alike), and by = log2(e) / T in 64 bits.  The chunks' sums are taken with an fp32 number near by, whose error tilts all
-// terms of a row alike and is put right when the parts are joined
+// T as it counts (infinite: all tokens with a logit above minus infinity alike), and by = log2(e) / T in 64 bits.  The chunks' sums are taken with an fp32 number near
+// by, whose error tilts all terms of a row alike and is put right when the parts are joined
 __device__ __forceinline__ float temperature_of(const LogprobArgs &a, int row) {
     const float t = a.temperature ? a.temperature[row] : 1.f;
     return t > 0.f ? t : 1.f;                                    // (NaN too)
@@ -99,8 +99,9 @@ __device__ __forceinline__ float maxima16(const float (&m)[N]) {
     if constexpr (BIT > 1) return maxima16<(N > 1 ? N / 2 : 1), BIT / 2>(h);
     else return h[0];
 }
-// Over the wave, op of its two halves being the same either way: four steps inside 16 lanes (moves that the operation takes along), then 16 and 32 lanes swapped for a copy's.  (Steps by lane_xor
-// need three instructions more to pick each lane's of the two, and a maximum of floats quiets both arguments first: a third of what a wave spends besides its logits)
+// Over the wave, op of its two halves being the same either way: four steps inside 16 lanes (moves that the operation takes along), then 16 and 32 lanes swapped for a
+// copy's.  (Steps by lane_xor need three instructions more to pick each lane's of the two, and a maximum of floats quiets both arguments first: a third of what a wave
+// spends besides its logits)
 template <typename F>
 __device__ __forceinline__ int over_wave(int v, F op) {
     v = op(v, __builtin_amdgcn_mov_dpp(v, 0x128, 0xf, 0xf, true));         // (eight lanes on)
@@ -153,7 +154,8 @@ __global__ __launch_bounds__(256) void logprob_chunk_kernel(LogprobArgs a, Logpr
 #pragma unroll
         for (int u = 0; u < U; ++u) w[u] = row_piece<TYPE>(view, p0 + 64 * u + lane, pieces, a.vocab);
     }
-    // (hi: any number near by will do, the part names it; one step of Newton's takes it to a rounding.  Where that leaves fp32, or T is infinite, it is no number or 0, and the sums are taken with by itself)
+    // (hi: any number near by will do, the part names it; one step of Newton's takes it to a rounding.  Where that leaves fp32, or T is infinite, it is no number or 0,
+    // and the sums are taken with by itself)
     const float T = temperature_of(a, row), near = __builtin_amdgcn_rcpf(T), about = 1.4426950408889634f * near, hi = __builtin_fmaf(__builtin_fmaf(-T, about, 1.4426950408889634f), near, about);
     const int token = a.tokens ? a.tokens[row] : -1;
     const bool given = a.rank && (unsigned)token < (unsigned)a.vocab;

@@ -41,7 +41,8 @@ __device__ __forceinline__ int mx_exponent(float amax) {
 // 16 (8) lanes share a row's 128 (64) features, eight each.  A lane has the rows of up to four neighbouring positions, a quad, so that a byte of the
 // transposed V leaves as one word for four positions, and so do the scales; a quad that is not whole leaves byte by byte.  A wave takes the quads that begin in its
 // window of rows, 4 (8) at once: a prompt's rows are quads from its second page position divisible by four on, wherever it begins.
-// Prompts are bound by memory: 4 of up to 2011 fp32 rows of 8 heads of 128, 58 MB, 13 us = 4.5 TB/s.  Steps by their chain of slots, rows and scale: 16 sequences of 9 rows of 32 heads 6.2 us.
+// Prompts are bound by memory: 4 of up to 2011 fp32 rows of 8 heads of 128, 58 MB, 13 us = 4.5 TB/s.  Steps by their chain of slots, rows and scale: 16 sequences of 9
+// rows of 32 heads 6.2 us.
 template <int DH, int TYPE, bool KEYS>
 __device__ __forceinline__ void append_mx_quad(const AppendMxArgs &a, int head, int row, int n, int slot, int oct) {
     constexpr int FB = DH / 32;
@@ -158,9 +159,9 @@ void launch_append_paged_mx(const AppendMxArgs &a, hipStream_t st) {
 // Row j of sequence b is position first[b] + j.  A run = rows of one sequence inside one page; a workgroup takes one head of the runs that begin in its window of
 // rows (64: a long sequence's one run).  A lane stores 16 bytes of a row, eight neighbouring lanes 128.  K's rows lie as they leave.  V's lie across: a lane takes four
 // positions of its features, turns them in registers and has its features of four rows.
-// Bound by memory, mostly by what is written: prefixes of five sequences of up to 4001 positions x 32 heads of 128 from 8 bits to bf16, 301 MB in 60 us = 5.0 TB/s; 37 of up to 1900 x 8 heads from 4 bits
-// to fp32, 400 MB, 90 us = 4.4 TB/s (118 with 32 bytes a lane in two halves, K and V one after the other).  Short ones by the chain of offsets, table and page: 1001 positions of 8 heads of 64 4.7 us,
-// 16 sequences of 9 rows of 32 heads 5.3 (18.7 in windows of 64 rows).
+// Bound by memory, mostly by what is written: prefixes of five sequences of up to 4001 positions x 32 heads of 128 from 8 bits to bf16, 301 MB in 60 us = 5.0 TB/s; 37
+// of up to 1900 x 8 heads from 4 bits to fp32, 400 MB, 90 us = 4.4 TB/s (118 with 32 bytes a lane in two halves, K and V one after the other).  Short ones by the chain
+// of offsets, table and page: 1001 positions of 8 heads of 64 4.7 us, 16 sequences of 9 rows of 32 heads 5.3 (18.7 in windows of 64 rows).
 struct ReadRun { int row, n, page, at; };                        // page -1: none, the rows become 0
 template <int TYPE> constexpr int read_features = TYPE == ROWS_F32 ? 4 : 8;      // of 16 bytes
 template <int TYPE>
@@ -331,10 +332,11 @@ void launch_read_paged(const ReadArgs<PagedMxCache> &a, hipStream_t st) { launch
 //   V: a byte is two features of a position.  Widened (with its position's scale) it is a pair across features; two positions' pairs, exchanged by halves, are
 //   pairs along the positions, of an even and of an odd feature: block jj of 32 features makes two operands, features 32 jj + 2 i and 32 jj + 2 i + 1.
 // Both products see exactly what codes and scales stand for.
-// Steps are bound by the read of the cache up to one tile of rows: 16 sequences of up to 4096 positions, 9 rows of 32 heads of 128, 192 MB in 36 us with the cache's bytes still in the last-level cache, 40 to
-// 47 without = 4.1 to 4.8 TB/s (a kernel of the same mapping that only loads: 31.5 with).  From two tiles on by the products and the vector instructions beside them, which take turns rather than
-// overlap: 61 of 5 rows, four query heads a key head, fp16, 358 MB in 95 us (load-only 74), a third of the cycles in matrix instructions, half in vector instructions.  Not faster: products in another order,
-// a page's scores a page ahead of its other product (39 and 115 us), one word of scales a lane exchanged between lanes; one fp16 plane of probabilities spills here (47 us).
+// Steps are bound by the read of the cache up to one tile of rows: 16 sequences of up to 4096 positions, 9 rows of 32 heads of 128, 192 MB in 36 us with the cache's
+// bytes still in the last-level cache, 40 to 47 without = 4.1 to 4.8 TB/s (a kernel of the same mapping that only loads: 31.5 with).  From two tiles on by the products
+// and the vector instructions beside them, which take turns rather than overlap: 61 of 5 rows, four query heads a key head, fp16, 358 MB in 95 us (load-only 74), a
+// third of the cycles in matrix instructions, half in vector instructions.  Not faster: products in another order, a page's scores a page ahead of its other product
+// (39 and 115 us), one word of scales a lane exchanged between lanes; one fp16 plane of probabilities spills here (47 us).
 // Other matrix instructions would take the codes as they are, with their scales, beside queries in planes of 8 bits: their sums are off by 1e-5 of the largest product (rms).
 // rare: a page's V has scales that stand for NaN where not all rows see them.  The rows that see one get it in its 32 features.  seen: 0x80 in the bytes of the lane's 16 positions
 template <int DH, int NT>
@@ -699,10 +701,11 @@ __global__ __launch_bounds__(256, NT <= 2 ? 2 : 1) void attend_paged_mx_kernel(A
 }
 
 // ---- many rows -----------------------------------------------------------------------------------
-// fp16 products keep the sums of each block of 32 features in units of a power of two, `now` its exponent plus 127, so that V fits: a code of 0.5 .. 6 times 2^-23 .. 2^12 is exact in fp16.
-// A page whose largest scale of the block lies outside 2^-8 .. 2^12 units makes that the unit, but none more than 2^60 below the largest before it (up to 2^62 units may have been
-// added up, and fp32 ends at 2^128); and where a scale of the block lies below 2^-23 units, the unit goes down until the largest is 2^12.  So V loses bits where its scale is more than 2^35 below
-// the largest of the block in its page, or more than 2^75 below 1 or another page's (the last bit 2^5 further down).
+// fp16 products keep the sums of each block of 32 features in units of a power of two, `now` its exponent plus 127, so that V fits: a code of 0.5 .. 6 times 2^-23 ..
+// 2^12 is exact in fp16.
+// A page whose largest scale of the block lies outside 2^-8 .. 2^12 units makes that the unit, but none more than 2^60 below the largest before it (up to 2^62 units
+// may have been added up, and fp32 ends at 2^128); and where a scale of the block lies below 2^-23 units, the unit goes down until the largest is 2^12.  So V loses
+// bits where its scale is more than 2^35 below the largest of the block in its page, or more than 2^75 below 1 or another page's (the last bit 2^5 further down).
 struct BlockUnit { int now, least; };
 __device__ __forceinline__ void unit_for(int most, int fewest, BlockUnit &u) {   // the largest scale, 0 for none, and the smallest
     const bool other = ((unsigned)(most - u.now + 8) > 20u) & (most > 0);
@@ -740,13 +743,16 @@ static RowsPlan rows_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads,
 // work: [pages before every block of the list, rounded up to 64 ints][parts' O][parts' m][parts' l]
 __host__ __device__ static inline int64_t rows_head(const RowsPlan &p, int n_seqs) { return ((int64_t)p.blocks * n_seqs + 1 + 63) / 64 * 64; }
 __host__ __device__ static inline int64_t rows_parts(const RowsPlan &p, int kv_heads) { return (int64_t)p.shares * 2 * kv_heads; }
-// Prompts: a workgroup takes 64 NT rows of a sequence's key head and pages that they see.  Each page is widened once, for all four waves, into LDS as the operands' images (16 KB of K,
-// 16 KB of V at head_dim 128): wave t has score tile t, and block t of V's features (of two blocks at head_dim 64: half of one's positions).  A page is requested two ahead, widened one
-// ahead, one barrier a page.  The rest is as with 8 bits: a wave holds its rows' queries and sums in registers, pages behind its rows are skipped, and the
-// reference of the exponentials moves only when a maximum passes it by 2^8.
-// Bound by issue: two sequences of up to 2047 rows, 32 query and 8 key heads of 128, over up to 2900 positions before, bf16, 136 GFLOP in 258 us and 17 for the join = 0.49 PFLOP/s.  A workgroup per
-// block left the compute units empty for 30 % of the time (310 us); what is left is the products (a third of the cycles) and the vector instructions (half), which hardly overlap.  Wave
-// priorities, by phase or by wave, changed nothing.
+// Prompts: a workgroup takes 64 NT rows of a sequence's key head and pages that they see.  Each page is widened once, for all four waves, into LDS as the operands'
+// images (16 KB of K, 16 KB of V at head_dim 128): wave t has score tile t, and block t of V's features (of two blocks at head_dim 64: half of one's positions).  A
+// page is requested two ahead, widened one ahead, one barrier a page.  The rest is as with 8 bits: a wave holds its rows' queries and sums in registers, pages behind
+// its rows are skipped, and the reference of the exponentials moves only when a maximum passes it by 2^8.
+// Bound by issue: two sequences of up to 2047 rows, 32 query and 8 key heads of 128, over up to 2900 positions before, bf16, 136 GFLOP in 258 us and 17 for the join =
+// 0.49 PFLOP/s.  A workgroup per block left the compute units empty for 30 % of the time (310 us); what is left is the products (a third of the cycles) and the vector
+// instructions (half), which hardly overlap.  Wave priorities, by phase or by wave, changed nothing.
+// bf16 rows' probabilities are one plane of fp16: with two of bf16, inside a captured graph, 284 us where both launches now take 247, and outputs 1.660e-3 (rms,
+// relative to 64 bits) off, which is their own rounding, where they are 1.670e-3.
+// (fp16 rows at head_dim 128: the second plane of queries costs 132 bytes of scratch a lane)
 template <int DH> constexpr int rows_images = (4 * (DH / 32) + (DH / 16) * 2) * 64;          // 16-byte pieces of a page
 template <int DH, int NT, int TYPE>
 __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, RowsPlan plan) {
@@ -1117,7 +1123,8 @@ __global__ __launch_bounds__(256, 2) void attend_mx_rows_kernel(AttendMxArgs a, 
     }
   }
 }
-// rows of blocks that lie in several shares, JOIN_ROWS a workgroup; a thread has four features of several rows, whose parts are requested together, or of one row whose many parts are
+// rows of blocks that lie in several shares, JOIN_ROWS a workgroup; a thread has four features of several rows, whose parts are requested together, or of one row whose
+// many parts are
 template <int DH, int TYPE, int JOIN_ROWS>
 __global__ __launch_bounds__(256) void attend_mx_rows_join_kernel(AttendMxArgs a, RowsPlan plan, int rows) {
     constexpr int LANES = DH / 4, EACH = JOIN_ROWS * LANES / 256, AHEAD = EACH == 1 ? 8 : 2;
@@ -1167,7 +1174,8 @@ static void launch_attend_nt(const AttendMxArgs &a, const AttendPlan &p, hipStre
     hipLaunchKernelGGL((attend_paged_mx_kernel<DH, NT, TYPE>), dim3((p.whole ? a.n_seqs : p.shares) * a.c.heads * p.tiles), dim3(256), bytes, st, a, p);
 }
 static AttendPlan attend_mx_plan(int n_seqs, int max_blocks, int n_heads, int kv_heads, int max_rows) {
-    // Which sequences stay whole: the 8-bit cache's rule, with a page at what 70 bytes a position would cost, for each tile of rows, whatever its head_dim, and tables of up to 64 pages.
+    // Which sequences stay whole: the 8-bit cache's rule, with a page at what 70 bytes a position would cost, for each tile of rows, whatever its head_dim, and tables
+    // of up to 64 pages.
     // us inside a captured graph, cut and whole (32 heads of 128, 9 rows; 8 of 64; 32 / 8 of 128, 5 rows):
     //          1 x 500    1 x 1001   1 x 1500   6 x 1001   6 x 3000   16 x 1001  64 x 1900 | 1 x 1001, 1 row  6 x 1300, 9  1 x 2000, 1  6 x 2400, 9 | 4 x 1001
     //   bf16   11.9 9.5   12.3 11.7  12.8 13.8  20.2 12.8  28.3 22.8  20.7 18.3  117 110   | 10.7 9.7         13.8 11.3    11.0 12.7    15.7 14.5   | 14.3 15.6
@@ -1187,12 +1195,23 @@ static void launch_attend_rows(const AttendMxArgs &a, hipStream_t st) {
 }
 template <int TYPE> constexpr int rows_nt = TYPE == ROWS_F32 ? 1 : 2;             // (three planes of queries and probabilities leave room for one tile)
 // Which calls take the many-rows form: those with more rows a key head than the shares' kernel holds (64); at head_dim 64, whose pages are half as much work for the
-// same start and end, from 6144 rows in all blocks on.  us inside a captured graph, here and in shares of the steps' kernel (sequences x positions before, rows, query / key heads):
+// same start and end, from 6144 rows in all blocks on.  us inside a captured graph, here and in shares of the steps' kernel (sequences x positions before, rows, query
+// / key heads):
 //             head_dim 128                                                                                     head_dim 64
 //         1 x 1000, 70, 8/8   1 x 8000, 20, 32/8   1 x 20000, 130, 8/8   64 x 1000, 20, 32/8   4 x 200, 100, 32/32   8 x 2000, 40, 16/2   30 x 60, 70, 8/8   1 x 4000, 500, 8/8   1 x 20000, 70, 8/8
 //   bf16  21.9 26.7           31.0 35.4            47.8 57.8             54.5 130.3            18.7 28.3             25.8 29.0            12.6 18.9          36.3 27.3            44.0 25.6
 //   fp16  25.2 27.5           34.5 37.2            56.7 61.8             73.0 140.3            24.3 29.6             27.5 30.5            13.1 19.9          38.5 29.0            46.5 27.3
 //   fp32  23.2 29.9           33.5 43.3            60.8 73.6             87.0 167.3            17.3 36.0             31.1 34.0            11.9 21.9          36.4 32.8            37.0 31.3
+// 49 .. 64 rows a key head stay with the steps' form, where bf16 rows' probabilities keep 16 bits and V its range.  Its fourth tile spills at head_dim 128 (296 / 460 /
+// 316 bytes a lane in bf16 / fp16 / fp32; two tiles 28 in fp16, 64 in fp32), and but for single long sequences this form would be the faster one (head_dim 128, lengths
+// up to what is named, here and there):
+//         1 x 20000, 8/8   1 x 4000, 32/8   16 x 4096, 32/32   61 x 1500, 32/8   4 x 300, 32/32
+//   48 rows  bf16  45.9 29.1        22.1 19.0        124 90             70.5 50.3         19.4 15.0
+//            fp16  52.2 30.1        25.4 19.6        165 96             89.5 54.3         25.2 16.1
+//            fp32  46.6 33.6        21.1 20.9        122 116            65.7 65.9         17.5 18.0
+//   56 rows  bf16  45.9 43.8        22.5 27.8        126 151            71.4 84.1         19.5 26.0
+//            fp16  53.3 51.4        26.0 31.8        167 192            91.0 107          25.3 30.6
+//            fp32  47.9 52.7        22.0 31.7        127 197            67.3 107          17.8 29.8
 #define ROWS_BLOCKS (1 << 23)    // of a launch: fewer
 static int64_t rows_blocks(int n_seqs, int n_heads, int kv_heads, int max_rows, int rows) { return ((int64_t)max_rows * (n_heads / kv_heads) + rows - 1) / rows * n_seqs * kv_heads; }
 static bool takes_rows(int n_seqs, int n_heads, int kv_heads, int dh, int max_rows, int rows) {

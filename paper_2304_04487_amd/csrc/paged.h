@@ -1,4 +1,5 @@
-// Argument structs and launchers of the paged caches (kernels_paged.hip: 8 bits, kernels_paged_mx.hip: 4), of sampled verification (kernels_sampled.hip) and of log probabilities (kernels_logprobs.hip).
+// Argument structs and launchers of the paged caches (kernels_paged.hip: 8 bits, kernels_paged_mx.hip: 4), of sampled verification (kernels_sampled.hip) and of log
+// probabilities (kernels_logprobs.hip).
 #pragma once
 #include "common.h"
 

@@ -197,18 +197,21 @@ __device__ __forceinline__ void attend_put_q(const AttendQ<DH, NT> &q, u32x4 *ld
             }
         }
     }
-}__device__ __forceinline__ f32x4 mfma16x16x32_half(u32x4 a, u32x4 b, f32x4 c) {
+}
+__device__ __forceinline__ f32x4 mfma16x16x32_half(u32x4 a, u32x4 b, f32x4 c) {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
 __device__ __forceinline__ uint32_t half_pair(float a, float b) {
     typedef __attribute__((ext_vector_type(2))) _Float16 f16x2;
     typedef __attribute__((ext_vector_type(2))) float f32x2;
     return __builtin_bit_cast(uint32_t, __builtin_convertvector((f32x2){a, b}, f16x2));
-}__device__ __forceinline__ f32x4 times_pow2(f32x4 v, int e) {
+}
+__device__ __forceinline__ f32x4 times_pow2(f32x4 v, int e) {
 #pragma unroll
     for (int r = 0; r < 4; ++r) v[r] = __builtin_amdgcn_ldexpf(v[r], e);
     return v;
-}// a word's first n bytes (all for n >= 4, none for n <= 0)
+}
+// a word's first n bytes (all for n >= 4, none for n <= 0)
 __device__ __forceinline__ uint32_t bytes_below(int n) { return n >= 4 ? ~0u : n <= 0 ? 0u : ~(~0u << (8 * n)); }
 
 template <int TYPE, typename A>
